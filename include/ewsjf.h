@@ -37,6 +37,16 @@
  *                    backfill from its neighbours, removal of queues that stay
  *                    empty (Section 3.2).
  *
+ * For the requests a step admits, beyond the paper's scheduler, it holds the
+ * two things that come next on the same card and stream:
+ *
+ *   ewsjf_cache_*    the pages of a key/value cache: taken for new tokens,
+ *                    forked from another slot, released, copied, compacted,
+ *                    and written (ewsjf_cache_append).
+ *   ewsjf_attention  attention over that cache, for sequences that share a long
+ *                    prefix (ewsjf_prefix_plan) or with a sliding window and a
+ *                    few first tokens that stay visible (ewsjf_window_plan).
+ *
  * Conventions shared by every entry point
  * ---------------------------------------
  *  * Array arguments are DEVICE pointers (hipMalloc'd or torch CUDA tensors)
@@ -451,6 +461,158 @@ ewsjf_status ewsjf_tactical_step(int32_t* len, const float* arrival, int64_t n, 
                                  int32_t* empty_cnt, double eps, int32_t flags, int32_t* ids, int32_t* n_sel,
                                  int32_t* q_prim, float* head_score, int32_t* removed, void* ws, size_t ws_bytes,
                                  hipStream_t stream);
+
+/* ---------------------------------------------------------------------------
+ * The paged key/value cache of the admitted requests.
+ *
+ * A slot holds one request's tokens.  Keys and values lie in pages of
+ * page_size tokens that any slot may hold; row `slot` of the table names the
+ * pages of its tokens [0, page_size), [page_size, 2 page_size), ...; -1 (any
+ * value outside [0, n_pages)) marks no page: its tokens are not visible to
+ * attention and are not written.  refs[p] counts the rows that hold page p; 0
+ * is a free page.  A page with room left belongs to one slot (a fork copies a
+ * partial page), so writing new tokens never changes what another slot reads.
+ *
+ * The struct is host memory; data, refs, table and length are device arrays
+ * of the caller.  Element (layer, x, page, head, token, d) of the data, x = 0
+ * for keys and 1 for values, is data[layer * layer_stride + x * kv_stride +
+ * page * page_stride + head * head_stride + token * token_stride + d] (strides
+ * in elements of 16 bits).  A page is one block of kv_heads * page_size *
+ * head_dim elements in either order of heads and tokens: (head_stride,
+ * token_stride) is (page_size * head_dim, head_dim) or (head_dim, kv_heads *
+ * head_dim).  data is 16-byte aligned, the outer strides are multiples of 8
+ * and blocks do not overlap.
+ *
+ * Requests of one call name distinct slots, and a child slot of a fork is not
+ * a parent in the same call.  Slots outside [0, n_slots) are refused.
+ * Requests are served in order: with need_i pages for request i, request i is
+ * granted as long as need_0 + .. + need_i does not exceed the free pages, and
+ * the free pages are taken in ascending order; so results do not depend on
+ * the order in which threads run. */
+enum {
+  EWSJF_MAX_CACHE_BATCH = 4096,    /* requests per cache call */
+  EWSJF_MAX_PAGES = 1 << 24,       /* pages of a cache */
+  EWSJF_MAX_PAGE_SIZE = 1024,      /* tokens per page (a power of two) */
+  EWSJF_MAX_HEAD_DIM = 256         /* of a cache; ewsjf_attention has 64 and 128 */
+};
+enum { EWSJF_BF16 = 0, EWSJF_F16 = 1 };
+
+typedef struct {
+  void* data;
+  int32_t* refs;   /* [n_pages] */
+  int32_t* table;  /* [n_slots][width] */
+  int32_t* length; /* [n_slots] tokens held, at most width * page_size */
+  int64_t layer_stride, kv_stride, page_stride, head_stride, token_stride;
+  int32_t layers, n_pages, page_size, kv_heads, head_dim, dtype;
+  int32_t n_slots, width;
+} ewsjf_cache;
+
+/* Workspace of ewsjf_cache_extend, _fork and _compact (0 for a cache that
+ * they refuse). */
+size_t ewsjf_cache_workspace_bytes(const ewsjf_cache* c);
+
+/* Room for tokens[i] >= 0 more tokens in slot[i]: its row gets ceil((length +
+ * tokens) / page_size) - ceil(length / page_size) pages and its length grows.
+ * granted[i] (device int32 [n]) = 1, or 0 for a request that does not fit the
+ * free pages or the row and leaves its slot as it is.  0 <= n <=
+ * EWSJF_MAX_CACHE_BATCH. */
+ewsjf_status ewsjf_cache_extend(const ewsjf_cache* c, const int32_t* slot, const int32_t* tokens, int32_t n,
+                                int32_t* granted, void* ws, size_t ws_bytes, hipStream_t stream);
+
+/* child[i] := the first tokens[i] tokens of parent[i]: whole pages are shared
+ * (refs + 1), a partial last page is copied, in every layer, to a page of its
+ * own.  Refused (granted[i] = 0): a child that holds tokens, tokens[i] < 0 or
+ * more than the parent holds, no free page. */
+ewsjf_status ewsjf_cache_fork(const ewsjf_cache* c, const int32_t* parent, const int32_t* child,
+                              const int32_t* tokens, int32_t n, int32_t* granted, void* ws, size_t ws_bytes,
+                              hipStream_t stream);
+
+/* begin == end == NULL: slot[i] is emptied (its pages' refs - 1, its row -1, its
+ * length 0).  Otherwise its full pages that lie wholly in tokens [begin[i],
+ * end[i]) are given up (refs - 1, entries -1) and the length stays: what a
+ * sliding window has left behind. */
+ewsjf_status ewsjf_cache_release(const ewsjf_cache* c, const int32_t* slot, const int32_t* begin,
+                                 const int32_t* end, int32_t n, hipStream_t stream);
+
+/* Page src[j] to page dst[j] in every layer (device int32 [n], 0 <= n <=
+ * n_pages); pairs outside the pool are skipped, no page is both read and
+ * written.  refs and rows stay as they are. */
+ewsjf_status ewsjf_cache_copy(const ewsjf_cache* c, const int32_t* src, const int32_t* dst, int32_t n,
+                              hipStream_t stream);
+
+/* Moves the used pages (refs > 0) to the front of the pool: with U used pages,
+ * the highest of those at or above U goes to the lowest free page below U,
+ * the next to the next.  out_table [n_slots][width] and out_refs [n_pages] get
+ * the new rows and counts, used (device int32 [1]) gets U.  They may be the
+ * cache's own arrays; other arrays leave the old rows valid for reading until
+ * a page is written again, since a moved page keeps its old copy. */
+ewsjf_status ewsjf_cache_compact(const ewsjf_cache* c, int32_t* out_table, int32_t* out_refs, int32_t* used, void* ws,
+                                 size_t ws_bytes, hipStream_t stream);
+
+/* Writes the keys and values of the newest tokens of one layer.  Sequence s
+ * (slot[s]) has the tokens [q_start[s], q_start[s + 1]) of k and v (device,
+ * 16-bit [total][kv_heads][head_dim] with strides in elements, multiples of
+ * 8, 16-byte aligned); with m of them, token i goes to position length - m +
+ * i.  q_start: device int32 [n_seqs + 1], ascending from 0 to total. */
+ewsjf_status ewsjf_cache_append(const ewsjf_cache* c, int32_t layer, const void* k, const void* v,
+                                int64_t k_token_stride, int64_t k_head_stride, int64_t v_token_stride,
+                                int64_t v_head_stride, const int32_t* slot, const int32_t* q_start, int32_t n_seqs,
+                                int64_t total, hipStream_t stream);
+
+/* ---------------------------------------------------------------------------
+ * Attention over the cache.
+ *
+ * Sequence s has the query tokens [q_start[s], q_start[s + 1]) and slot[s]'s
+ * keys; its query i of m is the token at position p = length - m + i and sees
+ * the keys j <= p, with a window also j > p - window or j < sinks.  Query head
+ * a reads key head a / (q_heads / kv_heads).
+ *   out = sum_j exp(scale q.k_j) v_j / sum_j exp(scale q.k_j)
+ *   lse = ln sum_j exp(scale q.k_j)
+ * over the visible keys; a query that sees none has out 0 and lse -inf.
+ * Products of 16-bit inputs are summed in binary32, so are the softmax's sum
+ * and the output, rounded once at the end; the weights are rounded to 16 bits
+ * for the product with the values.
+ *
+ * A plan holds what follows from the batch's lengths: made once a step, it
+ * serves every layer, until a length or a batch member changes. */
+typedef struct {
+  int32_t n_seqs;   /* 0 .. EWSJF_MAX_CACHE_BATCH */
+  int32_t n_groups; /* shared prefixes, 0 .. n_seqs */
+  int64_t total_q;  /* query tokens of the batch, below 2^24 */
+  int32_t max_q;    /* most query tokens of a sequence: chooses the kernels, >= 1 */
+  int32_t q_heads;  /* a multiple of kv_heads, at most 64 a key head */
+  int32_t window;   /* visible tokens before and with the query; 0: all */
+  int32_t sinks;    /* first tokens that stay visible (window > 0) */
+} ewsjf_batch;
+
+/* Device bytes of a plan, and of ewsjf_attention's workspace (0 for
+ * arguments that are refused). */
+size_t ewsjf_attention_plan_bytes(const ewsjf_cache* c, const ewsjf_batch* b);
+size_t ewsjf_attention_workspace_bytes(const ewsjf_cache* c, const ewsjf_batch* b);
+
+/* Plan of a batch whose sequences [group_start[g], group_start[g + 1]) share
+ * their first shared[g] tokens: the rows of their slots name the same pages
+ * there (as forks leave them) or pages with the same contents.  The shared
+ * keys are read once for the group, from the first member's row.  Of shared[g]
+ * counts at most the tokens before every member's first query.  n_groups = 0:
+ * nothing is shared.  window and sinks are 0.  slot, q_start, group_start,
+ * shared: device int32 [n_seqs], [n_seqs + 1], [n_groups + 1], [n_groups]. */
+ewsjf_status ewsjf_prefix_plan(const ewsjf_cache* c, const ewsjf_batch* b, const int32_t* slot,
+                               const int32_t* q_start, const int32_t* group_start, const int32_t* shared, void* plan,
+                               size_t plan_bytes, hipStream_t stream);
+
+/* Plan of a batch with a sliding window (window >= 1, sinks >= 0, n_groups = 0). */
+ewsjf_status ewsjf_window_plan(const ewsjf_cache* c, const ewsjf_batch* b, const int32_t* slot,
+                               const int32_t* q_start, void* plan, size_t plan_bytes, hipStream_t stream);
+
+/* Attention of one layer.  q: device, 16-bit [total_q][q_heads][head_dim] of
+ * the cache's type, strides in elements, multiples of 8, 16-byte aligned; out:
+ * [total_q][q_heads][head_dim], dense; lse: device float [total_q][q_heads] or
+ * NULL.  scale > 0.  head_dim 64 or 128.  The plan is one of this batch and
+ * cache. */
+ewsjf_status ewsjf_attention(const ewsjf_cache* c, const ewsjf_batch* b, int32_t layer, const void* q,
+                             int64_t q_token_stride, int64_t q_head_stride, float scale, const void* plan, void* out,
+                             float* lse, void* ws, size_t ws_bytes, hipStream_t stream);
 
 /* Human-readable name of a status code (static storage). */
 const char* ewsjf_status_string(ewsjf_status s);

@@ -24,8 +24,13 @@ EXPORTED = ("ewsjf_queue_table_bytes", "ewsjf_workspace_bytes", "ewsjf_table_upl
             "ewsjf_route", "ewsjf_score", "ewsjf_select", "ewsjf_step", "ewsjf_step_timed", "ewsjf_ring_insert",
             "ewsjf_tactical_step", "ewsjf_ring_step", "ewsjf_window_histogram", "ewsjf_window_advance",
             "ewsjf_partition_hist", "ewsjf_dispatch", "ewsjf_trial_step", "ewsjf_trial_finish",
-            "ewsjf_status_string", "ewsjf_version", "ewsjf_step_static")
+            "ewsjf_status_string", "ewsjf_version", "ewsjf_step_static",
+            "ewsjf_cache_workspace_bytes", "ewsjf_cache_extend", "ewsjf_cache_fork", "ewsjf_cache_release",
+            "ewsjf_cache_copy", "ewsjf_cache_compact", "ewsjf_cache_append", "ewsjf_attention_plan_bytes",
+            "ewsjf_attention_workspace_bytes", "ewsjf_prefix_plan", "ewsjf_window_plan", "ewsjf_attention")
 STATIC_SCRATCH_BYTES = 4 << 20
+MAX_CACHE_BATCH, MAX_PAGES, MAX_PAGE_SIZE, MAX_HEAD_DIM = 4096, 1 << 24, 1024, 256
+BF16, F16 = 0, 1
 
 
 class PartitionParams(C.Structure):
@@ -45,6 +50,19 @@ class QueueTable(C.Structure):
                 ("hi", C.c_int32 * MAX_QUEUES), ("count", C.c_int64 * MAX_QUEUES),
                 ("sum", C.c_int64 * MAX_QUEUES), ("mean", C.c_double * MAX_QUEUES),
                 ("lut", C.c_uint8 * (MAX_LEN + 16)), ("route", C.c_uint64 * ROUTE_WORDS)]
+
+
+class Cache(C.Structure):
+    _fields_ = [("data", C.c_void_p), ("refs", C.c_void_p), ("table", C.c_void_p), ("length", C.c_void_p),
+                ("layer_stride", C.c_int64), ("kv_stride", C.c_int64), ("page_stride", C.c_int64),
+                ("head_stride", C.c_int64), ("token_stride", C.c_int64), ("layers", C.c_int32),
+                ("n_pages", C.c_int32), ("page_size", C.c_int32), ("kv_heads", C.c_int32), ("head_dim", C.c_int32),
+                ("dtype", C.c_int32), ("n_slots", C.c_int32), ("width", C.c_int32)]
+
+
+class Batch(C.Structure):
+    _fields_ = [("n_seqs", C.c_int32), ("n_groups", C.c_int32), ("total_q", C.c_int64), ("max_q", C.c_int32),
+                ("q_heads", C.c_int32), ("window", C.c_int32), ("sinks", C.c_int32)]
 
 
 class EwsjfError(RuntimeError):
@@ -106,6 +124,31 @@ def lib():
         L.ewsjf_dispatch.restype = C.c_int
         L.ewsjf_partition_hist.argtypes = [vp, C.POINTER(PartitionParams), vp, vp, sz, vp]
         L.ewsjf_partition_hist.restype = C.c_int
+        # structs go by address (a plain integer), which keeps the host's part of a call short
+        L.ewsjf_cache_workspace_bytes.argtypes = [vp]
+        L.ewsjf_cache_workspace_bytes.restype = sz
+        L.ewsjf_cache_extend.argtypes = [vp, vp, vp, i32, vp, vp, sz, vp]
+        L.ewsjf_cache_extend.restype = C.c_int
+        L.ewsjf_cache_fork.argtypes = [vp, vp, vp, vp, i32, vp, vp, sz, vp]
+        L.ewsjf_cache_fork.restype = C.c_int
+        L.ewsjf_cache_release.argtypes = [vp, vp, vp, vp, i32, vp]
+        L.ewsjf_cache_release.restype = C.c_int
+        L.ewsjf_cache_copy.argtypes = [vp, vp, vp, i32, vp]
+        L.ewsjf_cache_copy.restype = C.c_int
+        L.ewsjf_cache_compact.argtypes = [vp, vp, vp, vp, vp, sz, vp]
+        L.ewsjf_cache_compact.restype = C.c_int
+        L.ewsjf_cache_append.argtypes = [vp, i32, vp, vp, i64, i64, i64, i64, vp, vp, i32, i64, vp]
+        L.ewsjf_cache_append.restype = C.c_int
+        L.ewsjf_attention_plan_bytes.argtypes = [vp, vp]
+        L.ewsjf_attention_plan_bytes.restype = sz
+        L.ewsjf_attention_workspace_bytes.argtypes = [vp, vp]
+        L.ewsjf_attention_workspace_bytes.restype = sz
+        L.ewsjf_prefix_plan.argtypes = [vp, vp, vp, vp, vp, vp, vp, sz, vp]
+        L.ewsjf_prefix_plan.restype = C.c_int
+        L.ewsjf_window_plan.argtypes = [vp, vp, vp, vp, vp, sz, vp]
+        L.ewsjf_window_plan.restype = C.c_int
+        L.ewsjf_attention.argtypes = [vp, vp, i32, vp, i64, i64, f32, vp, vp, vp, vp, sz, vp]
+        L.ewsjf_attention.restype = C.c_int
         L.ewsjf_status_string.argtypes = [C.c_int]
         L.ewsjf_status_string.restype = C.c_char_p
         L.ewsjf_version.argtypes = []

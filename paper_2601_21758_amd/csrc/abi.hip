@@ -12,6 +12,7 @@
 #include <mutex>
 
 #include "ewsjf.h"
+#include "ewsjf_cache.h"
 #include "ewsjf_launch.h"
 
 namespace {
@@ -70,6 +71,8 @@ constexpr int64_t kMaxN = 0x7fffffffLL;  // request ids are int32
 ewsjf_status launched(hipError_t e) { return e == hipSuccess ? EWSJF_OK : EWSJF_ERR_LAUNCH; }
 
 }  // namespace
+
+ewsjf_status ewsjf::device_ok() { return check_device(); }
 
 extern "C" {
 
