@@ -42,7 +42,7 @@ ewsjf_status cache_status(const ewsjf_cache* c) {
   if (c->head_dim < 8 || c->head_dim > EWSJF_MAX_HEAD_DIM || c->head_dim % 8) return EWSJF_ERR_ARG;
   if (c->dtype != EWSJF_BF16 && c->dtype != EWSJF_F16) return EWSJF_ERR_ARG;
   if (c->n_slots < 1 || c->n_slots > (1 << 24) || c->width < 1) return EWSJF_ERR_ARG;
-  if ((int64_t)c->width * c->page_size > 0x7fffffff) return EWSJF_ERR_ARG;
+  if ((int64_t)c->width * c->page_size > 0x7ffff000) return EWSJF_ERR_ARG;
   const int64_t D = c->head_dim, block = D * c->page_size * c->kv_heads;
   // a dim of size 1 may have any stride: it is never stepped over
   const bool head = c->kv_heads > 1, token = c->page_size > 1;

@@ -1,4 +1,26 @@
 // Attention over the paged key/value cache.
+//
+// A unit of work is one key head of a row tile: up to `rows` rows, a row being
+// a query token and one of the G = q_heads / kv_heads query heads that read
+// that key head, so the keys are read once for all of them.  The unit's keys
+// are cut into tiles.  All units' tiles lie on one line (key head, then row
+// tile, then key tile), and the line is cut into equal shares, one a worker: a
+// share may begin or end inside a unit, whose parts are joined afterwards
+// (running maximum, sum and output of a softmax join exactly, in any cut).
+// So one sequence of many tokens, many sequences of few, and anything ragged
+// between them all fill the chip evenly, and a worker writes at most two
+// partial results.
+//
+// A shared prefix is a phase of its own: the group's queries of all members
+// are the rows, the shared tokens the keys.
+//
+// Scores are computed transposed, S^T = K Q^T, with 32x32x16 matrix
+// instructions: a lane then holds scores of one row (its column), so the
+// softmax's maximum and sum are taken in the lane and joined once with the lane
+// 32 away, and the weights P^T are in the registers as the second product's
+// operand needs them, O^T = V^T P^T, when the keys are taken in the order
+// 4h, .., 4h + 3, 8 + 4h, .. in which the first product leaves them (h = lane /
+// 32).  V^T is read from LDS with the transposing read.
 #include <hip/hip_runtime.h>
 
 #include "ewsjf_cache.h"
@@ -6,107 +28,928 @@
 namespace ewsjf {
 namespace {
 
-// A query token's slot (-1: none) and position.
-struct Token {
-  int32_t slot, pos;
+constexpr int kRowTile = 32;     // rows of a unit of the wave kernel
+constexpr int kRowKeys = 32;     // its key tile
+constexpr int kBlockTile = 128;  // rows of a unit of the workgroup kernel (four waves of 32)
+constexpr int kBlockKeys = 64;
+constexpr int kWaves = 4;
+constexpr int kCUs = 256;
+constexpr int kBlocks = 2 * kCUs;  // both kernels: two workgroups a CU
+constexpr float kFloor = -3e38f;   // running maximum of a row that has seen no key
+constexpr float kLn2 = 0.6931471805599453f;
+constexpr float kLog2e = 1.4426950408889634f;
+
+// A row tile.  Row r is query token q0 + (row0 + r) / G and query head (row0 +
+// r) % G of the key head's; it sees keys up to pos0 + (row0 + r) / G.
+struct Entry {
+  int32_t slot;       // row of the table, -1: no keys
+  int32_t q0, row0, rows, pos0;
+  int32_t lo, end;    // keys of the main run
+  int32_t sink;       // keys [0, sink) come before it in tiles of their own
+  int32_t prefix;     // first row tile of the group's phase, -1: no shared keys
+  int32_t prefix_row; // row of this tile's row 0 in the group
+  int32_t tiles;
+  int32_t pad;
 };
 
-__global__ void plan_tokens(ewsjf_cache c, const int32_t* slot, const int32_t* q_start, int64_t total, Token* plan) {
-  const int s = blockIdx.x;
-  int64_t a = q_start[s], e = q_start[s + 1];
-  if (a < 0 || e < a || e > total) return;
-  const int r = slot[s];
-  const bool ok = r >= 0 && r < c.n_slots;
-  int64_t n = ok ? c.length[r] : 0;
-  const int64_t room = (int64_t)c.width * c.page_size;
-  n = n < 0 ? 0 : n > room ? room : n;
-  for (int64_t t = a + threadIdx.x; t < e; t += blockDim.x) plan[t] = Token{ok ? r : -1, (int32_t)(n - (e - t))};
+// A worker's first tile.
+struct Start {
+  int32_t entry, head, tile, pad;
+};
+
+// One phase of a plan.
+struct Phase {
+  int64_t total;    // key tiles of one key head
+  int64_t share;    // tiles per worker
+  int32_t entries;
+  int32_t workers;
+};
+
+struct Plan {
+  Phase* phase;      // [2]: shared prefixes, the sequences' own keys
+  Start* start[2];   // [workers]
+  Entry* entry[2];
+  int64_t* cum[2];   // tiles of one key head before a row tile
+  size_t bytes;
+};
+
+struct Shape {
+  int G;
+  int rows[2], keys[2], workers[2];
+  int64_t entries[2];  // most row tiles
+  bool block[2];       // the workgroup kernel
+};
+
+Shape shape_of(const ewsjf_cache& c, const ewsjf_batch& b) {
+  Shape s;
+  s.G = b.q_heads / c.kv_heads;
+  s.block[0] = b.n_groups > 0 && b.total_q * s.G > (int64_t)kRowTile * b.n_groups;
+  s.block[1] = (int64_t)b.max_q * s.G > kRowTile;
+  for (int p = 0; p < 2; ++p) {
+    s.rows[p] = s.block[p] ? kBlockTile : kRowTile;
+    s.keys[p] = s.block[p] ? kBlockKeys : kRowKeys;
+    s.workers[p] = s.block[p] ? kBlocks : kBlocks * kWaves;
+    s.entries[p] = b.total_q * s.G / s.rows[p] + (p ? b.n_seqs : b.n_groups);
+  }
+  if (b.n_groups == 0) s.entries[0] = 0;
+  return s;
 }
 
-__device__ float to_f32(__bf16 x) { return (float)x; }
-__device__ float to_f32(_Float16 x) { return (float)x; }
+struct Carve {
+  char* base;
+  size_t at = 0;
+  template <typename T>
+  T* take(size_t n) {
+    T* r = reinterpret_cast<T*>(base + at);
+    at += (n * sizeof(T) + 255) & ~size_t(255);
+    return r;
+  }
+};
 
-__device__ float wave_max(float v) {
-  for (int d = 32; d; d >>= 1) v = fmaxf(v, __shfl_xor(v, d));
-  return v;
-}
-__device__ float wave_sum(float v) {
-  for (int d = 32; d; d >>= 1) v += __shfl_xor(v, d);
-  return v;
+Plan plan_of(const Shape& s, void* base) {
+  Carve at{static_cast<char*>(base)};
+  Plan p;
+  p.phase = at.take<Phase>(2);
+  for (int i = 0; i < 2; ++i) {
+    p.start[i] = at.take<Start>(s.workers[i]);
+    p.entry[i] = at.take<Entry>(s.entries[i]);
+    p.cum[i] = at.take<int64_t>(s.entries[i] + 1);
+  }
+  p.bytes = at.at;
+  return p;
 }
 
-// One wave a query head of a token: 64 keys at a time, one key a lane, with the
-// running maximum m and sum l of the softmax; then the lanes share the dims.
-template <typename T, int D>
-__global__ __launch_bounds__(256) void attend_simple(ewsjf_cache c, ewsjf_batch b, const T* data, const T* q,
-                                                     int64_t q_token, int64_t q_head, float scale, const Token* plan,
-                                                     T* out, float* lse) {
-  __shared__ float query[4][D];
+// Partial results: outputs in binary32 before the division, and (maximum in
+// the exponent's units, sum) of each row.  Parts of a unit that is cut go to
+// the worker's slot 0 (its first unit) or 1 (its last), [worker][2][rows]; a
+// whole unit's rows that still have to be joined with the other phase go to
+// `whole`, [total_q][q_heads].
+struct Parts {
+  float* o;
+  float2* ml;
+  float* whole_o;
+  float2* whole_ml;
+};
+
+struct Work {
+  Parts part[2];
+  float* lse;       // [total_q][q_heads], where the caller gives none
+  int32_t* odd[2];  // of each wave: it met values that are not finite where some row does not look
+  size_t bytes;
+};
+
+Work work_of(const ewsjf_cache& c, const ewsjf_batch& b, const Shape& s, void* base) {
+  Carve at{static_cast<char*>(base)};
+  Work w;
+  for (int i = 0; i < 2; ++i) {
+    const bool used = i == 1 || b.n_groups > 0;
+    const size_t rows = used ? (size_t)s.workers[i] * 2 * s.rows[i] : 0;
+    const size_t whole = b.n_groups > 0 ? (size_t)b.total_q * b.q_heads : 0;
+    w.part[i].o = at.take<float>(rows * c.head_dim);
+    w.part[i].ml = at.take<float2>(rows);
+    w.part[i].whole_o = at.take<float>(whole * c.head_dim);
+    w.part[i].whole_ml = at.take<float2>(whole);
+    w.odd[i] = at.take<int32_t>((size_t)s.workers[i] * (s.block[i] ? kWaves : 1));
+  }
+  w.lse = at.take<float>((size_t)b.total_q * b.q_heads);
+  w.bytes = at.at;
+  return w;
+}
+
+// ---------------------------------------------------------------------------
+// The plan
+// ---------------------------------------------------------------------------
+constexpr int kPlanThreads = 1024;
+
+__device__ int64_t scan(int64_t v, int64_t* sums, int64_t& total) {  // exclusive over the workgroup
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int64_t t = blockIdx.x;
-  const int head = blockIdx.y * 4 + wave;
-  if (head >= b.q_heads) return;
-  for (int d = lane; d < D; d += 64) query[wave][d] = to_f32(q[t * q_token + head * q_head + d]);
-  __builtin_amdgcn_wave_barrier();
-  const Token me = plan[t];
-  const int h = head / (b.q_heads / c.kv_heads);
-  const int32_t* row = c.table + (int64_t)(me.slot < 0 ? 0 : me.slot) * c.width;
-  const int64_t last = me.slot < 0 ? -1 : me.pos;
-  float m = -3e38f, l = 0.f, o[D / 64] = {};
-  for (int64_t k0 = 0; k0 <= last; k0 += 64) {
-    if (b.window > 0 && k0 >= b.sinks && k0 + 63 <= last - b.window) continue;
-    const int64_t j = k0 + lane;
-    const bool seen = j <= last && (b.window == 0 || j > last - b.window || j < b.sinks);
-    int page = seen ? row[j / c.page_size] : -1;
-    if (page >= c.n_pages) page = -1;
-    const T* at = data + (page < 0 ? 0 : page) * c.page_stride + h * c.head_stride + (j % c.page_size) * c.token_stride;
-    float s = -INFINITY;
-    if (page >= 0) {
-      s = 0.f;
-      for (int d = 0; d < D; ++d) s = fmaf(query[wave][d], to_f32(at[d]), s);
-      s *= scale;
+  int64_t inc = v;
+  for (int d = 1; d < 64; d <<= 1) {
+    const int64_t o = __shfl_up(inc, d);
+    if (lane >= d) inc += o;
+  }
+  __syncthreads();
+  if (lane == 63) sums[wave] = inc;
+  __syncthreads();
+  int64_t base = 0, all = 0;
+  for (int i = 0; i < kPlanThreads / 64; ++i) {
+    if (i < wave) base += sums[i];
+    all += sums[i];
+  }
+  total = all;
+  return base + inc - v;
+}
+
+// The last i in [0, n) with key[i] <= v (0 if none).
+template <typename T>
+__device__ int last_at_most(const T* key, int n, int64_t v) {
+  int lo = 0, hi = n;
+  while (hi - lo > 1) {
+    const int mid = (lo + hi) / 2;
+    if (key[mid] <= v) lo = mid;
+    else hi = mid;
+  }
+  return lo;
+}
+
+struct PlanArgs {
+  const int32_t *slot, *q_start, *group_start, *shared;
+  int rows[2], keys[2], workers[2], G;
+};
+
+// One workgroup.  Everything read from the caller's arrays is bounded here, so
+// the other kernels follow the plan without checks of their own.
+__global__ __launch_bounds__(kPlanThreads) void make_plan(ewsjf_cache c, ewsjf_batch b, PlanArgs a, Plan plan) {
+  constexpr int kMost = EWSJF_MAX_CACHE_BATCH;
+  __shared__ int64_t sums[kPlanThreads / 64];
+  __shared__ int first[kMost + 1];  // first row tile of a sequence or group
+  __shared__ int common[kMost];     // a group's shared tokens that count
+  __shared__ int lead[kMost];       // its first member with queries
+  __shared__ int members[kMost];
+  const int n = b.n_seqs, groups = b.n_groups;
+  const int64_t room = (int64_t)c.width * c.page_size;
+  auto q_at = [&](int i) {
+    const int64_t v = a.q_start[i];
+    return v < 0 ? 0 : v > b.total_q ? b.total_q : v;
+  };
+  auto queries = [&](int i) {
+    const int64_t d = q_at(i + 1) - q_at(i);
+    return d < 0 ? 0 : d;
+  };
+  auto tokens = [&](int i) -> int64_t {
+    const int s = a.slot[i];
+    if (s < 0 || s >= c.n_slots) return 0;
+    const int64_t v = c.length[s];
+    return v < 0 ? 0 : v > room ? room : v;
+  };
+  auto group_at = [&](int g) {
+    const int v = a.group_start[g];
+    return v < 0 ? 0 : v > n ? n : v;
+  };
+  auto group_of = [&](int i) {  // -1: none
+    if (groups == 0) return -1;
+    const int g = last_at_most(a.group_start, groups, i);
+    return group_at(g) <= i && i < group_at(g + 1) ? g : -1;
+  };
+  for (int g = threadIdx.x; g < groups; g += kPlanThreads) {
+    const int v = a.shared[g];
+    common[g] = v < 0 ? 0 : v;
+    lead[g] = n;
+    members[g] = 0;
+  }
+  __syncthreads();
+  for (int i = threadIdx.x; i < n; i += kPlanThreads) {
+    const int g = group_of(i);
+    if (g < 0 || queries(i) == 0) continue;
+    const int64_t before = tokens(i) - queries(i);
+    atomicMin(&common[g], (int)(before < 0 ? 0 : before));
+    atomicMin(&lead[g], i);
+    atomicAdd(&members[g], 1);
+  }
+  __syncthreads();
+  for (int g = threadIdx.x; g < groups; g += kPlanThreads)
+    if (members[g] < 2) common[g] = 0;  // nobody to share with
+  __syncthreads();
+
+  for (int ph = 0; ph < 2; ++ph) {
+    const int R = a.rows[ph], TK = a.keys[ph], owners = ph ? n : groups;
+    Entry* entry = plan.entry[ph];
+    // row tiles of each sequence, or of each group with shared tokens
+    auto rows_of = [&](int i) -> int64_t {
+      if (ph) return queries(i) * a.G;
+      if (common[i] == 0) return 0;
+      const int64_t d = q_at(group_at(i + 1)) - q_at(group_at(i));
+      return d < 0 ? 0 : d * a.G;
+    };
+    int64_t run = 0;
+    // a group's first row tile is kept for phase 1, in `members`
+    for (int i0 = 0; i0 < owners; i0 += kPlanThreads) {
+      const int i = i0 + threadIdx.x;
+      const int64_t tiles = i < owners ? (rows_of(i) + R - 1) / R : 0;
+      int64_t total;
+      const int64_t before = scan(tiles, sums, total);
+      if (i < owners) first[i] = (int)(run + before);
+      if (i < owners && ph == 0) members[i] = (int)(run + before);
+      run += total;
     }
-    const float top = fmaxf(m, wave_max(s)), shrink = __expf(m - top);
-    const float p = page >= 0 ? __expf(s - top) : 0.f;
-    l = l * shrink + wave_sum(p);
-    m = top;
-    for (int d = 0; d < D / 64; ++d) o[d] *= shrink;
-    const uint64_t here = __ballot(page >= 0);
-    const uint64_t addr = reinterpret_cast<uint64_t>(at + c.kv_stride);
-    for (int i = 0; i < 64; ++i) {
-      if (!(here >> i & 1)) continue;
-      const float w = __shfl(p, i);
-      const T* v = reinterpret_cast<const T*>(__shfl(addr, i));
-      for (int d = 0; d < D / 64; ++d) o[d] = fmaf(w, to_f32(v[d * 64 + lane]), o[d]);
+    const int E = (int)run;
+    __syncthreads();
+    int64_t line = 0;
+    for (int e0 = 0; e0 < E; e0 += kPlanThreads) {
+      const int e = e0 + threadIdx.x;
+      Entry x = {};
+      if (e < E) {
+        // several owners without row tiles may begin where one with them does: the last one has them
+        const int i = last_at_most(first, owners, e);
+        const int64_t rows = rows_of(i);
+        x.row0 = (e - first[i]) * R;
+        x.rows = (int)(rows - x.row0 < R ? rows - x.row0 : R);
+        if (ph == 0) {
+          x.slot = a.slot[lead[i]];
+          x.q0 = (int)q_at(group_at(i));
+          x.pos0 = 1 << 30;
+          x.end = common[i];
+          x.prefix = -1;
+        } else {
+          const int g = group_of(i);
+          const int shared = g < 0 ? 0 : common[g];
+          const int s = a.slot[i];
+          const int64_t len = tokens(i);
+          x.slot = s < 0 || s >= c.n_slots ? -1 : s;
+          x.q0 = (int)q_at(i);
+          x.pos0 = (int)(len - queries(i));
+          const int p0 = x.pos0 + x.row0 / a.G, p1 = x.pos0 + (x.row0 + x.rows - 1) / a.G;
+          x.end = p1 + 1 > 0 ? p1 + 1 : 0;
+          x.lo = shared;
+          if (b.window > 0) {
+            const int64_t w = (int64_t)p0 - b.window + 1;
+            x.lo = w > 0 ? (int)w : 0;
+            x.sink = b.sinks < x.end ? b.sinks : x.end;
+            if (x.lo <= x.sink) x.lo = x.sink = 0;  // one run of keys
+          }
+          x.prefix = shared > 0 ? members[g] : -1;
+          x.prefix_row = shared > 0 ? (int)((q_at(i) - q_at(group_at(g))) * a.G + x.row0) : 0;
+        }
+        const int span = x.end > x.lo ? x.end - x.lo : 0;
+        x.tiles = (x.sink + TK - 1) / TK + (span + TK - 1) / TK;
+        if (x.tiles == 0) x.tiles = 1;  // a tile without keys, for the rows' zeros
+        entry[e] = x;
+      }
+      int64_t total;
+      const int64_t before = scan(x.tiles, sums, total);
+      if (e < E) plan.cum[ph][e] = line + before;
+      line += total;
+    }
+    const int64_t all = line * c.kv_heads;
+    const int64_t share = all > 0 ? (all + a.workers[ph] - 1) / a.workers[ph] : 1;
+    const int active = (int)((all + share - 1) / share);
+    if (threadIdx.x == 0) {
+      plan.cum[ph][E] = line;
+      plan.phase[ph] = Phase{line, share, E, active};
+    }
+    __syncthreads();  // entries and sums are read back by other threads
+    for (int w = threadIdx.x; w < active; w += kPlanThreads) {
+      const int64_t at = w * share, head = at / line, rest = at % line;
+      const int e = last_at_most(plan.cum[ph], E, rest);
+      plan.start[ph][w] = Start{e, (int)head, (int)(rest - plan.cum[ph][e]), 0};
+    }
+    __syncthreads();
+  }
+}
+
+// ---------------------------------------------------------------------------
+// Tiles
+// ---------------------------------------------------------------------------
+typedef __attribute__((ext_vector_type(4))) short short4v;
+typedef __attribute__((ext_vector_type(16))) float float16v;
+template <typename T>
+using vec8 = T __attribute__((ext_vector_type(8)));
+
+__device__ float16v mfma(vec8<__bf16> a, vec8<__bf16> b, float16v c) {
+  return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0);
+}
+__device__ float16v mfma(vec8<_Float16> a, vec8<_Float16> b, float16v c) {
+  return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0);
+}
+
+// The value of the lane 32 away joined with this lane's.
+__device__ float pair_max(float v) {
+  const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+__device__ float pair_sum(float v) {
+  const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+}
+
+// Places in LDS of a tile's keys (16-byte chunks) and values (64-byte blocks),
+// row by row, moved about within 256 bytes so that the 16 rows that one read of
+// the keys touches, and the four rows of a transposing read of the values, lie
+// in different banks.  Both moves are an exclusive or of the row with the
+// chunk, so a lane's places differ from its first one by a constant that the
+// loops apply (key_step, value_step).
+template <int D>
+__device__ int key_place(int key, int chunk) {
+  return D == 128 ? key * 256 + ((chunk ^ (key & 15)) << 4) : key * 128 + ((chunk ^ ((key >> 1) & 7)) << 4);
+}
+template <int D>
+__device__ int value_place(int key, int byte) {
+  const int block = byte >> 6, in = byte & 63;
+  return D == 128 ? key * 256 + ((block ^ (key & 3)) << 6) + in : key * 128 + ((block ^ ((key >> 1) & 1)) << 6) + in;
+}
+
+// Keeps what follows from x out of registers that live across the loop.
+__device__ int fresh(int x) {
+  asm volatile("" : "+v"(x));
+  return x;
+}
+
+__device__ uint32_t not_finite(uint32_t x, __bf16) { return ((x & 0x7f807f80u) + 0x00800080u) & 0x80008000u; }
+__device__ uint32_t not_finite(uint32_t x, _Float16) { return ((x & 0x7c007c00u) + 0x04000400u) & 0x80008000u; }
+
+// Where tile t of a row tile begins, and where its keys end.
+template <int TK>
+__device__ void tile_span(const Entry& x, int t, int& k0, int& kend) {
+  const int nst = (x.sink + TK - 1) / TK;
+  k0 = t < nst ? t * TK : x.lo + (t - nst) * TK;
+  kend = t < nst ? x.sink : x.end;
+}
+
+template <typename T>
+struct Args {
+  const T* data;  // the layer's keys
+  const T* q;
+  int64_t q_token, q_head;
+  const int32_t* table;
+  T* out;
+  float* lse;
+  int64_t kv_stride, page_stride, head_stride, token_stride;
+  int n_pages, page_shift, width, kv_heads, G, window, sinks;
+  float scale2;  // scale * log2(e)
+  bool join;     // a whole unit's rows still have to be joined with the other phase
+  Plan plan;
+  Work work;
+};
+
+// The softmax state and output of 32 rows, one a lane pair.
+template <typename T, int D>
+struct Rows {
+  vec8<T> q[D / 16];
+  float16v o[D / 32];
+  float top, sum;  // of the scaled scores in the exponent's units; the lane's own keys
+
+  __device__ void clear() {
+    top = kFloor;
+    sum = 0.f;
+#pragma unroll
+    for (int i = 0; i < D / 32; ++i)
+#pragma unroll
+      for (int j = 0; j < 16; ++j) o[i][j] = 0.f;
+  }
+
+  // S^T of the 32 keys at `keys`; first: key_place of the lane's row and half.
+  __device__ float16v scores(const char* keys, int first) const {
+    float16v s = {};
+#pragma unroll
+    for (int k = 0; k < D / 16; ++k) s = mfma(*reinterpret_cast<const vec8<T>*>(keys + (first ^ (k << 5))), q[k], s);
+    return s;
+  }
+
+  // The running maximum moves up only when a score passes it by 8 binary
+  // orders: until then the weights stay below 2^8, which loses nothing, and
+  // the output need not be scaled.
+  __device__ void raise(float most) {
+    if (__any(most > top + 8.f)) {
+      const float now = fmaxf(top, most), shrink = __builtin_amdgcn_exp2f(top - now);
+      top = now;
+      sum *= shrink;
+#pragma unroll
+      for (int i = 0; i < D / 32; ++i)
+#pragma unroll
+        for (int j = 0; j < 16; ++j) o[i][j] *= shrink;
     }
   }
-  for (int d = 0; d < D / 64; ++d)
-    out[(t * b.q_heads + head) * D + d * 64 + lane] = (T)(l > 0.f || l != l ? o[d] / l : 0.f);
-  if (lse != nullptr && lane == 0) lse[t * b.q_heads + head] = l > 0.f || l != l ? m + __logf(l) : -INFINITY;
+
+  // O^T += V^T P^T over the 16 keys of registers [8 half, 8 half + 8) of p;
+  // first: value_place of the lane's row and column.
+  __device__ void add(const char* values, int first, int half, const float16v& p) {
+    vec8<T> w;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) w[j] = (T)p[8 * half + j];
+    values += half * 16 * D * 2;
+#pragma unroll
+    for (int i = 0; i < D / 32; ++i) {
+      union {
+        short4v part[2];
+        vec8<T> all;
+      } v;
+      typedef __attribute__((address_space(3))) short4v* lds4;
+      const char* at = values + (first ^ (i << 6));
+      v.part[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4)at);
+      v.part[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4)(at + 8 * D * 2));
+      o[i] = mfma(v.all, w, o[i]);
+    }
+  }
+};
+
+// Where a lane's reads begin.
+template <int D>
+__device__ int first_key() {
+  const int lane = threadIdx.x & 63;
+  return key_place<D>(lane & 31, lane >> 5);
+}
+template <int D>
+__device__ int first_value() {
+  const int lane = threadIdx.x & 63, t = lane & 15;
+  return value_place<D>(4 * (lane >> 5) + (t >> 2), 32 * ((lane >> 4) & 1) + 8 * (t & 3));
+}
+
+// Bits of the keys [here, here + 64) that the row at position p sees.
+__device__ uint64_t bits_below(int n) { return n >= 64 ? ~0ull : n <= 0 ? 0ull : (1ull << n) - 1; }
+__device__ uint64_t seen_keys(uint64_t there, int here, int p, int window, int sinks) {
+  uint64_t m = there & bits_below(p - here + 1);
+  if (window > 0) m &= ~bits_below(p - window - here + 1) | bits_below(sinks - here);
+  return m;
+}
+
+// Scores of keys that a row does not see become -inf; seen: its keys from the
+// lane's first one on.
+__device__ void hide(float16v& s, uint32_t seen) {
+#pragma unroll
+  for (int r = 0; r < 16; ++r)
+    if (!(seen >> (8 * (r / 4) + r % 4) & 1)) s[r] = -INFINITY;
+}
+
+// Loads the queries of the rows of a lane, zeros past the last one.
+template <typename T, int D>
+__device__ void load_rows(const Args<T>& a, const Entry& x, int head, int row, vec8<T>* q) {
+  const int lane = threadIdx.x & 63;
+  const bool there = row < x.rows;
+  const int at = x.row0 + (there ? row : 0), token = at / a.G;
+  const T* p = a.q + (x.q0 + token) * a.q_token + (head * a.G + at - token * a.G) * a.q_head + 8 * (lane >> 5);
+#pragma unroll
+  for (int k = 0; k < D / 16; ++k) {
+    q[k] = *reinterpret_cast<const vec8<T>*>(p + 16 * k);
+    if (!there)
+#pragma unroll
+      for (int j = 0; j < 8; ++j) q[k][j] = (T)0.f;
+  }
+}
+
+// Writes a unit's rows of a wave: the result, or a part of it.
+template <typename T, int D>
+__device__ void store_rows(const Args<T>& a, int phase, const Entry& x, int head, int row, int tile_rows, bool whole,
+                           int64_t slot, Rows<T, D>& r) {
+  const int h = (threadIdx.x & 63) >> 5;
+  const float sum = pair_sum(r.sum);
+  if (row >= x.rows) return;
+  const int at = x.row0 + row, token = at / a.G;
+  const int64_t dense = (int64_t)(x.q0 + token) * (a.kv_heads * a.G) + head * a.G + at - token * a.G;
+  if (whole && !a.join) {
+    const float inv = sum > 0.f || sum != sum ? 1.f / sum : 0.f;
+    T* to = a.out + dense * D + 4 * h;
+#pragma unroll
+    for (int i = 0; i < D / 32; ++i)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        T v[4];
+#pragma unroll
+        for (int d = 0; d < 4; ++d) v[d] = (T)(sum == 0.f ? 0.f : r.o[i][4 * j + d] * inv);
+        *reinterpret_cast<uint2*>(to + 32 * i + 8 * j) = *reinterpret_cast<const uint2*>(v);
+      }
+    if (h == 0)
+      a.lse[dense] = sum == 0.f ? -INFINITY : kLn2 * (r.top + __builtin_amdgcn_logf(sum));
+    return;
+  }
+  const Parts& w = a.work.part[phase];
+  const int64_t at_row = whole ? dense : slot * tile_rows + row;
+  float* to = (whole ? w.whole_o : w.o) + at_row * D + 4 * h;
+#pragma unroll
+  for (int i = 0; i < D / 32; ++i)
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+      *reinterpret_cast<float4*>(to + 32 * i + 8 * j) =
+          make_float4(r.o[i][4 * j], r.o[i][4 * j + 1], r.o[i][4 * j + 2], r.o[i][4 * j + 3]);
+  if (h == 0) (whole ? w.whole_ml : w.ml)[at_row] = make_float2(r.top, sum);
+}
+
+// Key `key`'s page, -1 where no row of the tile sees it or there is none.
+template <typename T>
+__device__ int page_of(const Args<T>& a, const Entry& x, int key, int kend, int p_first) {
+  if (key >= kend || x.slot < 0) return -1;
+  if (a.window > 0 && key <= p_first - a.window && key >= a.sinks) return -1;
+  const int page = a.table[(int64_t)x.slot * a.width + (key >> a.page_shift)];
+  return page >= 0 && page < a.n_pages ? page : -1;
+}
+
+// Loads one row's 16 bytes of keys and values (page 0's where there is no page).
+template <typename T>
+__device__ void load_key(const Args<T>& a, int head, int page, int key, int chunk, uint4& k, uint4& v) {
+  const int in = key & ((1 << a.page_shift) - 1);
+  const T* p = a.data + (page < 0 ? 0 : page) * a.page_stride + head * a.head_stride + in * a.token_stride + chunk * 8;
+  k = *reinterpret_cast<const uint4*>(p);
+  v = *reinterpret_cast<const uint4*>(p + a.kv_stride);
+}
+
+// A tile's share of one wave, from registers to LDS: zeros for the keys that
+// are not there.  check: some row sees only a part of the tile; true is
+// returned where such a tile holds a value that is not finite.
+template <typename T, int D, int NI>
+__device__ bool put_keys(char* keys, char* values, int key0, uint64_t there, bool full, bool check,
+                         const uint4 (&k)[NI], const uint4 (&v)[NI]) {
+  constexpr int LPR = D / 8, KPI = 64 / LPR;
+  const int lane = threadIdx.x & 63, chunk = lane % LPR;
+  uint32_t bad = 0;
+#pragma unroll
+  for (int i = 0; i < NI; ++i) {
+    const int key = key0 + i * KPI + lane / LPR;
+    uint4 x = k[i], y = v[i];
+    if (!full) {
+      const uint32_t keep = there >> key & 1 ? ~0u : 0u;
+      x.x &= keep, x.y &= keep, x.z &= keep, x.w &= keep;
+      y.x &= keep, y.y &= keep, y.z &= keep, y.w &= keep;
+    }
+    *reinterpret_cast<uint4*>(keys + key_place<D>(key, chunk)) = x;
+    *reinterpret_cast<uint4*>(values + value_place<D>(key, chunk * 16)) = y;
+    if (check) bad |= not_finite(y.x, T()) | not_finite(y.y, T()) | not_finite(y.z, T()) | not_finite(y.w, T());
+  }
+  return bad != 0;
+}
+
+// ---------------------------------------------------------------------------
+// The workgroup kernel: 128 rows, 32 a wave; the four waves load a tile of 64
+// keys and values for all, one tile ahead of the one in use.
+// ---------------------------------------------------------------------------
+template <typename T, int D>
+__global__ __launch_bounds__(kWaves * 64, 2) void attend_block(Args<T> a, int phase) {
+  constexpr int TK = kBlockKeys, LPR = D / 8, KPI = 64 / LPR, NI = TK / kWaves / KPI;
+  __shared__ __align__(16) char keys[2][TK * D * 2];
+  __shared__ __align__(16) char values[2][TK * D * 2];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const Phase ph = a.plan.phase[phase];
+  // neighbouring shares of the line read the same keys: give them to one XCD
+  const int id = blockIdx.x % 8 * (gridDim.x / 8) + blockIdx.x / 8;
+  if (id >= ph.workers) return;
+  const int64_t all = ph.total * a.kv_heads;
+  const int64_t beg = id * ph.share, stop = beg + ph.share < all ? beg + ph.share : all;
+  const Start st = a.plan.start[phase][id];
+  int e = st.entry, head = st.head, t = st.tile;
+  int64_t left = stop - beg;
+  bool leading = true, odd = false;
+  Rows<T, D> rows;
+
+  while (left > 0) {
+    const Entry x = a.plan.entry[phase][e];
+    const int n = (int)(x.tiles - t < left ? x.tiles - t : left);
+    const bool whole = t == 0 && n == x.tiles;
+    const int row = wave * 32 + (lane & 31);
+    const bool busy = wave * 32 < x.rows;
+    load_rows<T, D>(a, x, head, row, rows.q);
+    rows.clear();
+    const int p_first = x.pos0 + x.row0 / a.G, p_last = x.pos0 + (x.row0 + x.rows - 1) / a.G;
+    const int w_last = wave * 32 + 31 < x.rows ? wave * 32 + 31 : x.rows - 1;
+    const int w_first = busy ? x.pos0 + (x.row0 + wave * 32) / a.G : p_first;
+    const int w_end = busy ? x.pos0 + (x.row0 + w_last) / a.G : p_first;
+    const int p = x.pos0 + (x.row0 + (row < x.rows ? row : x.rows - 1)) / a.G;
+
+    // every row of positions [first, last] sees every key of the tile that there is
+    auto even = [&](int k0, int kend, int first, int last) {
+      const int k1 = k0 + TK < kend ? k0 + TK : kend;
+      return k1 - 1 <= first && (a.window == 0 || k0 > last - a.window || k1 <= a.sinks);
+    };
+    uint4 kreg[NI], vreg[NI];
+    int k0, kend;
+    uint64_t there;
+    auto load = [&](int tile) {
+      tile_span<TK>(x, tile, k0, kend);
+      const int page = page_of(a, x, k0 + lane, kend, p_first);  // lane i: key i of the tile
+      there = __ballot(page >= 0);
+#pragma unroll
+      for (int i = 0; i < NI; ++i) {
+        const int key = wave * (TK / kWaves) + i * KPI + lane / LPR;
+        load_key(a, head, __shfl(page, key), k0 + key, lane % LPR, kreg[i], vreg[i]);
+      }
+    };
+    auto put = [&](int buf) {
+      odd |= put_keys<T, D, NI>(keys[buf], values[buf], wave * (TK / kWaves), there, there == ~0ull,
+                                !even(k0, kend, p_first, p_last), kreg, vreg);
+    };
+
+    load(t);
+    __syncthreads();  // the last unit's tiles are no longer read
+    put(0);
+    for (int i = 0; i < n; ++i) {
+      const int buf = i & 1, here = k0, here_end = kend;
+      const uint64_t held = there;
+      if (i + 1 < n) load(t + i + 1);
+      __syncthreads();
+      const bool any = here <= w_end && (a.window == 0 || here + TK - 1 > w_first - a.window || here < a.sinks);
+      if (busy && any && held != 0) {
+        float16v s[TK / 32];
+        const int kp = fresh(first_key<D>()), vp = fresh(first_value<D>());
+#pragma unroll
+        for (int j = 0; j < TK / 32; ++j) s[j] = rows.scores(keys[buf] + j * 32 * D * 2, kp);
+        if (held != ~0ull || !even(here, here_end, w_first, w_end)) {
+          const uint64_t seen = seen_keys(held, here, p, a.window, a.sinks) >> (4 * (lane >> 5));
+          hide(s[0], (uint32_t)seen);
+          hide(s[1], (uint32_t)(seen >> 32));
+        }
+        float most = s[0][0];
+#pragma unroll
+        for (int j = 0; j < TK / 32; ++j)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) most = fmaxf(most, s[j][r]);
+        rows.raise(pair_max(most) * a.scale2);
+#pragma unroll
+        for (int j = 0; j < TK / 32; ++j)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) {
+            s[j][r] = __builtin_amdgcn_exp2f(fmaf(s[j][r], a.scale2, -rows.top));
+            rows.sum += s[j][r];
+          }
+#pragma unroll
+        for (int j = 0; j < TK / 32; ++j)
+#pragma unroll
+          for (int half = 0; half < 2; ++half) rows.add(values[buf] + j * 32 * D * 2, vp, half, s[j]);
+      }
+      if (i + 1 < n) put(buf ^ 1);
+    }
+    store_rows<T, D>(a, phase, x, head, row, kBlockTile, whole, (int64_t)id * 2 + (leading ? 0 : 1), rows);
+    leading = false;
+    left -= n;
+    t = 0;
+    if (++e == ph.entries) {
+      e = 0;
+      ++head;
+    }
+  }
+  if (lane == 0) a.work.odd[phase][id * kWaves + wave] = 0;
+  if (odd) a.work.odd[phase][id * kWaves + wave] = 1;
+}
+
+// ---------------------------------------------------------------------------
+// The wave kernel: up to 32 rows (a few query tokens), the keys streamed by
+// waves that share nothing.
+// ---------------------------------------------------------------------------
+template <typename T, int D>
+__global__ __launch_bounds__(kWaves * 64, 2) void attend_wave(Args<T> a, int phase) {
+  constexpr int TK = kRowKeys, LPR = D / 8, KPI = 64 / LPR, NI = TK / KPI;
+  __shared__ __align__(16) char room[kWaves][2][TK * D * 2];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  char* keys = room[wave][0];
+  char* values = room[wave][1];
+  const Phase ph = a.plan.phase[phase];
+  const int id = (blockIdx.x % 8 * (gridDim.x / 8) + blockIdx.x / 8) * kWaves + wave;
+  if (id >= ph.workers) return;
+  const int64_t all = ph.total * a.kv_heads;
+  const int64_t beg = id * ph.share, stop = beg + ph.share < all ? beg + ph.share : all;
+  const Start st = a.plan.start[phase][id];
+  int e = st.entry, head = st.head, t = st.tile;
+  int64_t left = stop - beg;
+  bool leading = true;
+  bool odd = false;
+  Rows<T, D> rows;
+
+  while (left > 0) {
+    const Entry x = a.plan.entry[phase][e];
+    const int n = (int)(x.tiles - t < left ? x.tiles - t : left);
+    const bool whole = t == 0 && n == x.tiles;
+    const int row = lane & 31;
+    load_rows<T, D>(a, x, head, row, rows.q);
+    rows.clear();
+    const int p_first = x.pos0 + x.row0 / a.G, p_last = x.pos0 + (x.row0 + x.rows - 1) / a.G;
+    const int p = x.pos0 + (x.row0 + (row < x.rows ? row : x.rows - 1)) / a.G;
+    uint4 kreg[NI], vreg[NI];
+    int k0, kend;
+    uint32_t there;
+    auto load = [&](int tile) {
+      tile_span<TK>(x, tile, k0, kend);
+      const int page = page_of(a, x, k0 + (lane & 31), kend, p_first);
+      there = (uint32_t)__ballot(page >= 0);
+#pragma unroll
+      for (int i = 0; i < NI; ++i) {
+        const int key = i * KPI + lane / LPR;
+        load_key(a, head, __shfl(page, key), k0 + key, lane % LPR, kreg[i], vreg[i]);
+      }
+    };
+    load(t);
+    for (int i = 0; i < n; ++i) {
+      const int here = k0, k1 = k0 + TK < kend ? k0 + TK : kend;
+      const uint32_t held = there;
+      // a row sees only a part of the keys that are there (never with one position)
+      const bool uneven = p_first != p_last &&
+                          !(k1 - 1 <= p_first && (a.window == 0 || k0 > p_last - a.window || k1 <= a.sinks));
+      odd |= put_keys<T, D, NI>(keys, values, 0, held, held == ~0u, uneven, kreg, vreg);
+      if (i + 1 < n) load(t + i + 1);
+      __builtin_amdgcn_wave_barrier();
+      const int kp = fresh(first_key<D>()), vp = fresh(first_value<D>());
+      float16v s = rows.scores(keys, kp);
+      if (uneven || held != ~0u)
+        hide(s, (uint32_t)seen_keys(held, here, p, a.window, a.sinks) >> (4 * (lane >> 5)));
+      float most = s[0];
+#pragma unroll
+      for (int r = 1; r < 16; ++r) most = fmaxf(most, s[r]);
+      rows.raise(pair_max(most) * a.scale2);
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        s[r] = __builtin_amdgcn_exp2f(fmaf(s[r], a.scale2, -rows.top));
+        rows.sum += s[r];
+      }
+#pragma unroll
+      for (int half = 0; half < 2; ++half) rows.add(values, vp, half, s);
+      __builtin_amdgcn_wave_barrier();
+    }
+    store_rows<T, D>(a, phase, x, head, row, kRowTile, whole, (int64_t)id * 2 + (leading ? 0 : 1), rows);
+    leading = false;
+    left -= n;
+    t = 0;
+    if (++e == ph.entries) {
+      e = 0;
+      ++head;
+    }
+  }
+  if (lane == 0) a.work.odd[phase][id] = 0;
+  if (odd) a.work.odd[phase][id] = 1;
+}
+
+// ---------------------------------------------------------------------------
+// The join
+// ---------------------------------------------------------------------------
+
+// The parts of unit (entry, head) of a phase: workers [w0, w1], whole if one.
+struct Cut {
+  int64_t w0, w1, c0, share;
+};
+__device__ Cut cut_of(const Phase& ph, const int64_t* cum, int entry, int head) {
+  Cut u;
+  u.share = ph.share;
+  u.c0 = head * ph.total + cum[entry];
+  u.w0 = u.c0 / ph.share;
+  u.w1 = (head * ph.total + cum[entry + 1] - 1) / ph.share;
+  return u;
+}
+
+template <int D>
+struct Joined {
+  float top = kFloor, sum = 0.f, o[D / 64] = {};
+  __device__ void take(const float* part, float2 ml) {
+    const int lane = threadIdx.x & 63;
+    const float now = fmaxf(top, ml.x);
+    const float a = __builtin_amdgcn_exp2f(top - now), b = __builtin_amdgcn_exp2f(ml.x - now);
+    top = now;
+    sum = sum * a + ml.y * b;
+#pragma unroll
+    for (int i = 0; i < D / 64; ++i) o[i] = o[i] * a + part[lane * (D / 64) + i] * b;
+  }
+  __device__ void take(const Parts& p, const Cut& u, int tile_rows, int row, int64_t dense) {
+    if (u.w0 == u.w1) {
+      take(p.whole_o + dense * D, p.whole_ml[dense]);
+      return;
+    }
+    for (int64_t w = u.w0; w <= u.w1; ++w) {
+      const int64_t slot = 2 * w + (u.c0 <= w * u.share ? 0 : 1), at = slot * tile_rows + row;
+      take(p.o + at * D, p.ml[at]);
+    }
+  }
+};
+
+// A row's output again, key by key, without the keys that it does not see: the
+// products of whole tiles take a weight of 0 times a value, which is not 0
+// where the value is not finite.  lse2: the row's lse in the exponent's units.
+template <typename T, int D>
+__device__ void redo_row(const Args<T>& a, const Entry& x, int head, int row, float lse2) {
+  const int lane = threadIdx.x & 63;
+  const int at = x.row0 + row, token = at / a.G, member = at - token * a.G;
+  const int p = x.pos0 + token;
+  const T* q = a.q + (x.q0 + token) * a.q_token + (head * a.G + member) * a.q_head;
+  float o[D / 64] = {}, sum = 0.f;
+  for (int k0 = 0; k0 <= p && x.slot >= 0; k0 += 64) {
+    if (a.window > 0 && k0 >= a.sinks && k0 + 63 <= p - a.window) continue;
+    const int key = k0 + lane;
+    int page = -1;
+    if (key <= p && (a.window == 0 || key > p - a.window || key < a.sinks))
+      page = a.table[(int64_t)x.slot * a.width + (key >> a.page_shift)];
+    if (page >= a.n_pages) page = -1;
+    const int in = key & ((1 << a.page_shift) - 1);
+    const T* k = a.data + (page < 0 ? 0 : page) * a.page_stride + head * a.head_stride + in * a.token_stride;
+    float s = 0.f;
+    for (int d = 0; d < D; ++d) s = fmaf((float)q[d], (float)k[d], s);
+    const float w = __builtin_amdgcn_exp2f(fmaf(s, a.scale2, -lse2));
+    const uint64_t v_at = reinterpret_cast<uint64_t>(k + a.kv_stride);
+    for (uint64_t seen = __ballot(page >= 0); seen; seen &= seen - 1) {
+      const int i = __builtin_ctzll(seen);
+      const T* v = reinterpret_cast<const T*>(__shfl(v_at, i)) + lane * (D / 64);
+      const float wi = __shfl(w, i);
+      sum += wi;
+      for (int d = 0; d < D / 64; ++d) o[d] = fmaf(wi, (float)v[d], o[d]);
+    }
+  }
+  const int64_t dense = (int64_t)(x.q0 + token) * (a.kv_heads * a.G) + head * a.G + member;
+  for (int d = 0; d < D / 64; ++d) a.out[dense * D + lane * (D / 64) + d] = (T)(sum == 0.f ? 0.f : o[d] / sum);
+}
+
+// One workgroup a unit of the sequences' own keys, one wave a row.
+template <typename T, int D>
+__global__ __launch_bounds__(256) void join_parts(Args<T> a, int rows0, int rows1, int flags) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int e = blockIdx.x, head = blockIdx.y;
+  const Phase own = a.plan.phase[1];
+  if (e >= own.entries) return;
+  const Entry x = a.plan.entry[1][e];
+  const Cut u = cut_of(own, a.plan.cum[1], e, head);
+  int odd = 0;
+  for (int64_t w = u.w0 * flags + threadIdx.x; w < (u.w1 + 1) * flags; w += 256) odd |= a.work.odd[1][w];
+  odd = __syncthreads_or(odd);
+  if (u.w0 == u.w1 && !a.join && !odd) return;  // written by its worker
+  for (int row = wave; row < x.rows; row += 4) {
+    const int at = x.row0 + row, token = at / a.G;
+    const int64_t dense = (int64_t)(x.q0 + token) * (a.kv_heads * a.G) + head * a.G + at - token * a.G;
+    float lse2;
+    if (u.w0 == u.w1 && !a.join) {
+      lse2 = a.lse[dense] * kLog2e;
+    } else {
+      Joined<D> r;
+      if (x.prefix >= 0) {
+        const int e0 = x.prefix + (x.prefix_row + row) / rows0, row0 = (x.prefix_row + row) % rows0;
+        r.take(a.work.part[0], cut_of(a.plan.phase[0], a.plan.cum[0], e0, head), rows0, row0, dense);
+      }
+      r.take(a.work.part[1], u, rows1, row, dense);
+      const float inv = r.sum == 0.f ? 0.f : 1.f / r.sum;
+#pragma unroll
+      for (int i = 0; i < D / 64; ++i)
+        a.out[dense * D + lane * (D / 64) + i] = (T)(r.sum == 0.f ? 0.f : r.o[i] * inv);
+      lse2 = r.sum == 0.f ? -INFINITY : r.top + __builtin_amdgcn_logf(r.sum);
+      if (lane == 0) a.lse[dense] = kLn2 * lse2;
+    }
+    if (odd) redo_row<T, D>(a, x, head, row, lse2);
+  }
+}
+
+template <typename T, int D>
+hipError_t launch_typed(const ewsjf_cache& c, const ewsjf_batch& b, int32_t layer, const void* q, int64_t q_token,
+                        int64_t q_head, float scale, const void* plan, void* out, float* lse, void* ws,
+                        hipStream_t stream) {
+  const Shape s = shape_of(c, b);
+  Args<T> a;
+  a.data = static_cast<const T*>(c.data) + layer * c.layer_stride;
+  a.q = static_cast<const T*>(q);
+  a.q_token = q_token, a.q_head = q_head;
+  a.table = c.table;
+  a.out = static_cast<T*>(out);
+  a.kv_stride = c.kv_stride, a.page_stride = c.page_stride, a.head_stride = c.head_stride;
+  a.token_stride = c.token_stride;
+  a.n_pages = c.n_pages, a.page_shift = __builtin_ctz(c.page_size), a.width = c.width, a.kv_heads = c.kv_heads;
+  a.G = s.G, a.window = b.window, a.sinks = b.sinks;
+  a.scale2 = scale * kLog2e;
+  a.join = b.n_groups > 0;
+  a.plan = plan_of(s, const_cast<void*>(plan));
+  a.work = work_of(c, b, s, ws);
+  a.lse = lse != nullptr ? lse : a.work.lse;
+  for (int p = b.n_groups > 0 ? 0 : 1; p < 2; ++p) {
+    if (s.block[p]) attend_block<T, D><<<kBlocks, kWaves * 64, 0, stream>>>(a, p);
+    else attend_wave<T, D><<<kBlocks, kWaves * 64, 0, stream>>>(a, p);
+  }
+  join_parts<T, D><<<dim3((unsigned)s.entries[1], c.kv_heads), 256, 0, stream>>>(a, s.rows[0], s.rows[1],
+                                                                                s.block[1] ? kWaves : 1);
+  return hipGetLastError();
 }
 
 }  // namespace
 
 size_t attention_plan_bytes(const ewsjf_cache& c, const ewsjf_batch& b) {
-  return 256 + sizeof(Token) * (size_t)b.total_q;
+  return plan_of(shape_of(c, b), nullptr).bytes;
 }
-size_t attention_ws_bytes(const ewsjf_cache& c, const ewsjf_batch& b) { return 256; }
+size_t attention_ws_bytes(const ewsjf_cache& c, const ewsjf_batch& b) {
+  return work_of(c, b, shape_of(c, b), nullptr).bytes;
+}
 
 hipError_t launch_attention_plan(const ewsjf_cache& c, const ewsjf_batch& b, const int32_t* slot,
                                  const int32_t* q_start, const int32_t* group_start, const int32_t* shared,
                                  void* plan, hipStream_t stream) {
-  if (b.n_seqs == 0) return hipSuccess;
-  plan_tokens<<<b.n_seqs, 256, 0, stream>>>(c, slot, q_start, b.total_q, static_cast<Token*>(plan));
-  return hipGetLastError();
-}
-
-template <typename T, int D>
-hipError_t launch_typed(const ewsjf_cache& c, const ewsjf_batch& b, int32_t layer, const void* q, int64_t q_token,
-                        int64_t q_head, float scale, const void* plan, void* out, float* lse, hipStream_t stream) {
-  const T* data = static_cast<const T*>(c.data) + layer * c.layer_stride;
-  attend_simple<T, D><<<dim3((unsigned)b.total_q, (b.q_heads + 3) / 4), 256, 0, stream>>>(
-      c, b, data, static_cast<const T*>(q), q_token, q_head, scale, static_cast<const Token*>(plan),
-      static_cast<T*>(out), lse);
+  const Shape s = shape_of(c, b);
+  PlanArgs a{slot, q_start, group_start, shared, {s.rows[0], s.rows[1]}, {s.keys[0], s.keys[1]},
+             {s.workers[0], s.workers[1]}, s.G};
+  make_plan<<<1, kPlanThreads, 0, stream>>>(c, b, a, plan_of(s, plan));
   return hipGetLastError();
 }
 
@@ -114,7 +957,7 @@ hipError_t launch_attention(const ewsjf_cache& c, const ewsjf_batch& b, int32_t 
                             int64_t q_head, float scale, const void* plan, void* out, float* lse, void* ws,
                             hipStream_t stream) {
   if (b.total_q == 0 || b.n_seqs == 0) return hipSuccess;
-  auto go = [&](auto run) { return run(c, b, layer, q, q_token, q_head, scale, plan, out, lse, stream); };
+  auto go = [&](auto run) { return run(c, b, layer, q, q_token, q_head, scale, plan, out, lse, ws, stream); };
   if (c.dtype == EWSJF_BF16) return c.head_dim == 64 ? go(launch_typed<__bf16, 64>) : go(launch_typed<__bf16, 128>);
   return c.head_dim == 64 ? go(launch_typed<_Float16, 64>) : go(launch_typed<_Float16, 128>);
 }
