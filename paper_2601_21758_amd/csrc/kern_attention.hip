@@ -248,7 +248,7 @@ __global__ __launch_bounds__(kPlanThreads) void make_plan(ewsjf_cache c, ewsjf_b
   }
   __syncthreads();
   for (int g = threadIdx.x; g < groups; g += kPlanThreads)
-    if (members[g] < 2) common[g] = 0;  // nobody to share with
+    common[g] = members[g] < 2 ? 0 : common[g] & ~15;  // nobody to share with; tiles begin at multiples of 16
   __syncthreads();
 
   for (int ph = 0; ph < 2; ++ph) {
@@ -303,7 +303,7 @@ __global__ __launch_bounds__(kPlanThreads) void make_plan(ewsjf_cache c, ewsjf_b
           x.lo = shared;
           if (b.window > 0) {
             const int64_t w = (int64_t)p0 - b.window + 1;
-            x.lo = w > 0 ? (int)w : 0;
+            x.lo = w > 0 ? (int)w & ~15 : 0;
             x.sink = b.sinks < x.end ? b.sinks : x.end;
             if (x.lo <= x.sink) x.lo = x.sink = 0;  // one run of keys
           }
@@ -386,14 +386,6 @@ __device__ int fresh(int x) {
 
 __device__ uint32_t not_finite(uint32_t x, __bf16) { return ((x & 0x7f807f80u) + 0x00800080u) & 0x80008000u; }
 __device__ uint32_t not_finite(uint32_t x, _Float16) { return ((x & 0x7c007c00u) + 0x04000400u) & 0x80008000u; }
-
-// Where tile t of a row tile begins, and where its keys end.
-template <int TK>
-__device__ void tile_span(const Entry& x, int t, int& k0, int& kend) {
-  const int nst = (x.sink + TK - 1) / TK;
-  k0 = t < nst ? t * TK : x.lo + (t - nst) * TK;
-  kend = t < nst ? x.sink : x.end;
-}
 
 template <typename T>
 struct Args {
@@ -553,23 +545,79 @@ __device__ void store_rows(const Args<T>& a, int phase, const Entry& x, int head
   if (h == 0) (whole ? w.whole_ml : w.ml)[at_row] = make_float2(r.top, sum);
 }
 
-// Key `key`'s page, -1 where no row of the tile sees it or there is none.
-template <typename T>
-__device__ int page_of(const Args<T>& a, const Entry& x, int key, int kend, int p_first) {
-  if (key >= kend || x.slot < 0) return -1;
-  if (a.window > 0 && key <= p_first - a.window && key >= a.sinks) return -1;
-  const int page = a.table[(int64_t)x.slot * a.width + (key >> a.page_shift)];
-  return page >= 0 && page < a.n_pages ? page : -1;
-}
+// A tile of TK keys from k0 on, of which those below kend count, and the
+// pages that hold them.
+//
+// Sixteens: pages have at least 16 tokens.  Tiles begin at multiples of 16, so
+// 16 keys lie in one page: lane i holds the page of keys [16 i', 16 i' + 16),
+// i' = i mod TK / 16, and addresses are the wave's but for a constant of the
+// lane.  Otherwise lane i holds the page of key i.  -1: no page, or no row
+// looks there.
+template <typename T, int D, int TK, bool Sixteens>
+struct Tile {
+  static constexpr int LPR = D / 8, KPI = 64 / LPR;  // lanes a key, keys a load
+  int k0, kend, page;
 
-// Loads one row's 16 bytes of keys and values (page 0's where there is no page).
-template <typename T>
-__device__ void load_key(const Args<T>& a, int head, int page, int key, int chunk, uint4& k, uint4& v) {
-  const int in = key & ((1 << a.page_shift) - 1);
-  const T* p = a.data + (page < 0 ? 0 : page) * a.page_stride + head * a.head_stride + in * a.token_stride + chunk * 8;
-  k = *reinterpret_cast<const uint4*>(p);
-  v = *reinterpret_cast<const uint4*>(p + a.kv_stride);
-}
+  // The pages of tile t (a load in flight).
+  __device__ void find(const Args<T>& a, const Entry& x, int t) {
+    const int lane = threadIdx.x & 63;
+    const int nst = (x.sink + TK - 1) / TK;
+    k0 = t < nst ? t * TK : x.lo + (t - nst) * TK;
+    kend = t < nst ? x.sink : x.end;
+    const int key = k0 + (Sixteens ? 16 * (lane % (TK / 16)) : lane % TK);
+    const int in = key < kend ? key : kend > 0 ? kend - 1 : 0;
+    page = a.table[(int64_t)(x.slot < 0 ? 0 : x.slot) * a.width + (in >> a.page_shift)];
+    if (key >= kend || x.slot < 0 || page >= a.n_pages || page < 0) page = -1;
+  }
+
+  // Bits of the keys that are there and that some row may see.
+  __device__ uint64_t there(const Args<T>& a, int p_first) const {
+    uint64_t m;
+    if (Sixteens) {
+      m = 0;
+#pragma unroll
+      for (int j = 0; j < TK / 16; ++j)
+        if (__builtin_amdgcn_readlane(page, j) >= 0) m |= 0xffffull << (16 * j);
+    } else {
+      m = __ballot(page >= 0);
+      if (TK == 32) m = (uint32_t)m;
+    }
+    m &= bits_below(kend - k0);
+    if (a.window > 0) m &= ~bits_below(p_first - a.window - k0 + 1) | bits_below(a.sinks - k0);
+    return m;
+  }
+
+  // Loads keys [key0, key0 + NI KPI) of the tile: 16 bytes a lane (page 0's
+  // where there is no page).
+  template <int NI>
+  __device__ void load(const Args<T>& a, int head, int key0, uint4 (&k)[NI], uint4 (&v)[NI]) const {
+    const int lane = threadIdx.x & 63;
+    if (Sixteens) {
+      const uint32_t mine = (uint32_t)(lane / LPR * a.token_stride + lane % LPR * 8) * 2;
+#pragma unroll
+      for (int i = 0; i < NI; ++i) {
+        const int key = key0 + i * KPI;
+        const int held = __builtin_amdgcn_readlane(page, key / 16);
+        const int in = (k0 + key) & ((1 << a.page_shift) - 1);
+        const char* base = reinterpret_cast<const char*>(a.data + (held < 0 ? 0 : held) * a.page_stride +
+                                                         head * a.head_stride + in * a.token_stride);
+        k[i] = *reinterpret_cast<const uint4*>(base + mine);
+        v[i] = *reinterpret_cast<const uint4*>(base + a.kv_stride * 2 + mine);
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < NI; ++i) {
+        const int key = key0 + i * KPI + lane / LPR;
+        const int held = __shfl(page, key);
+        const int in = (k0 + key) & ((1 << a.page_shift) - 1);
+        const T* p = a.data + (held < 0 ? 0 : held) * a.page_stride + head * a.head_stride + in * a.token_stride +
+                     lane % LPR * 8;
+        k[i] = *reinterpret_cast<const uint4*>(p);
+        v[i] = *reinterpret_cast<const uint4*>(p + a.kv_stride);
+      }
+    }
+  }
+};
 
 // A tile's share of one wave, from registers to LDS: zeros for the keys that
 // are not there.  check: some row sees only a part of the tile; true is
@@ -579,30 +627,40 @@ __device__ bool put_keys(char* keys, char* values, int key0, uint64_t there, boo
                          const uint4 (&k)[NI], const uint4 (&v)[NI]) {
   constexpr int LPR = D / 8, KPI = 64 / LPR;
   const int lane = threadIdx.x & 63, chunk = lane % LPR;
+  const int kp = key_place<D>(key0 + lane / LPR, chunk), vp = value_place<D>(key0 + lane / LPR, chunk * 16);
+  if (full && !check) {
+#pragma unroll
+    for (int i = 0; i < NI; ++i) {
+      // KPI keys on, the place in the row moves with the key
+      const int step = i * KPI, kx = D == 128 ? (step & 15) << 4 : ((step >> 1) & 7) << 4;
+      *reinterpret_cast<uint4*>(keys + (kp ^ kx) + step * D * 2) = k[i];
+      *reinterpret_cast<uint4*>(values + vp + step * D * 2) = v[i];
+    }
+    return false;
+  }
   uint32_t bad = 0;
 #pragma unroll
   for (int i = 0; i < NI; ++i) {
     const int key = key0 + i * KPI + lane / LPR;
+    const uint32_t keep = there >> key & 1 ? ~0u : 0u;
     uint4 x = k[i], y = v[i];
-    if (!full) {
-      const uint32_t keep = there >> key & 1 ? ~0u : 0u;
-      x.x &= keep, x.y &= keep, x.z &= keep, x.w &= keep;
-      y.x &= keep, y.y &= keep, y.z &= keep, y.w &= keep;
-    }
+    x.x &= keep, x.y &= keep, x.z &= keep, x.w &= keep;
+    y.x &= keep, y.y &= keep, y.z &= keep, y.w &= keep;
     *reinterpret_cast<uint4*>(keys + key_place<D>(key, chunk)) = x;
     *reinterpret_cast<uint4*>(values + value_place<D>(key, chunk * 16)) = y;
-    if (check) bad |= not_finite(y.x, T()) | not_finite(y.y, T()) | not_finite(y.z, T()) | not_finite(y.w, T());
+    bad |= not_finite(y.x, T()) | not_finite(y.y, T()) | not_finite(y.z, T()) | not_finite(y.w, T());
   }
-  return bad != 0;
+  return check && bad != 0;
 }
 
 // ---------------------------------------------------------------------------
 // The workgroup kernel: 128 rows, 32 a wave; the four waves load a tile of 64
 // keys and values for all, one tile ahead of the one in use.
 // ---------------------------------------------------------------------------
-template <typename T, int D>
+template <typename T, int D, bool Sixteens>
 __global__ __launch_bounds__(kWaves * 64, 2) void attend_block(Args<T> a, int phase) {
-  constexpr int TK = kBlockKeys, LPR = D / 8, KPI = 64 / LPR, NI = TK / kWaves / KPI;
+  using Keys = Tile<T, D, kBlockKeys, Sixteens>;
+  constexpr int TK = kBlockKeys, NI = TK / kWaves / Keys::KPI;
   __shared__ __align__(16) char keys[2][TK * D * 2];
   __shared__ __align__(16) char values[2][TK * D * 2];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -638,30 +696,30 @@ __global__ __launch_bounds__(kWaves * 64, 2) void attend_block(Args<T> a, int ph
       return k1 - 1 <= first && (a.window == 0 || k0 > last - a.window || k1 <= a.sinks);
     };
     uint4 kreg[NI], vreg[NI];
-    int k0, kend;
+    Keys next, far;  // the tile in the registers, and the one whose pages are being looked up
     uint64_t there;
-    auto load = [&](int tile) {
-      tile_span<TK>(x, tile, k0, kend);
-      const int page = page_of(a, x, k0 + lane, kend, p_first);  // lane i: key i of the tile
-      there = __ballot(page >= 0);
-#pragma unroll
-      for (int i = 0; i < NI; ++i) {
-        const int key = wave * (TK / kWaves) + i * KPI + lane / LPR;
-        load_key(a, head, __shfl(page, key), k0 + key, lane % LPR, kreg[i], vreg[i]);
-      }
+    auto load = [&]() {
+      next = far;
+      there = next.there(a, p_first);
+      next.load(a, head, wave * (TK / kWaves), kreg, vreg);
     };
     auto put = [&](int buf) {
       odd |= put_keys<T, D, NI>(keys[buf], values[buf], wave * (TK / kWaves), there, there == ~0ull,
-                                !even(k0, kend, p_first, p_last), kreg, vreg);
+                                !even(next.k0, next.kend, p_first, p_last), kreg, vreg);
     };
 
-    load(t);
+    far.find(a, x, t);
+    load();
+    far.find(a, x, t + 1);
     __syncthreads();  // the last unit's tiles are no longer read
     put(0);
     for (int i = 0; i < n; ++i) {
-      const int buf = i & 1, here = k0, here_end = kend;
+      const int buf = i & 1, here = next.k0, here_end = next.kend;
       const uint64_t held = there;
-      if (i + 1 < n) load(t + i + 1);
+      if (i + 1 < n) {
+        load();
+        far.find(a, x, t + i + 2);
+      }
       __syncthreads();
       const bool any = here <= w_end && (a.window == 0 || here + TK - 1 > w_first - a.window || here < a.sinks);
       if (busy && any && held != 0) {
@@ -711,9 +769,10 @@ __global__ __launch_bounds__(kWaves * 64, 2) void attend_block(Args<T> a, int ph
 // The wave kernel: up to 32 rows (a few query tokens), the keys streamed by
 // waves that share nothing.
 // ---------------------------------------------------------------------------
-template <typename T, int D>
+template <typename T, int D, bool Sixteens>
 __global__ __launch_bounds__(kWaves * 64, 2) void attend_wave(Args<T> a, int phase) {
-  constexpr int TK = kRowKeys, LPR = D / 8, KPI = 64 / LPR, NI = TK / KPI;
+  using Keys = Tile<T, D, kRowKeys, Sixteens>;
+  constexpr int TK = kRowKeys, NI = TK / Keys::KPI;
   __shared__ __align__(16) char room[kWaves][2][TK * D * 2];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   char* keys = room[wave][0];
@@ -740,27 +799,27 @@ __global__ __launch_bounds__(kWaves * 64, 2) void attend_wave(Args<T> a, int pha
     const int p_first = x.pos0 + x.row0 / a.G, p_last = x.pos0 + (x.row0 + x.rows - 1) / a.G;
     const int p = x.pos0 + (x.row0 + (row < x.rows ? row : x.rows - 1)) / a.G;
     uint4 kreg[NI], vreg[NI];
-    int k0, kend;
+    Keys next, far;
     uint32_t there;
-    auto load = [&](int tile) {
-      tile_span<TK>(x, tile, k0, kend);
-      const int page = page_of(a, x, k0 + (lane & 31), kend, p_first);
-      there = (uint32_t)__ballot(page >= 0);
-#pragma unroll
-      for (int i = 0; i < NI; ++i) {
-        const int key = i * KPI + lane / LPR;
-        load_key(a, head, __shfl(page, key), k0 + key, lane % LPR, kreg[i], vreg[i]);
-      }
+    auto load = [&]() {
+      next = far;
+      there = (uint32_t)next.there(a, p_first);
+      next.load(a, head, 0, kreg, vreg);
     };
-    load(t);
+    far.find(a, x, t);
+    load();
+    far.find(a, x, t + 1);
     for (int i = 0; i < n; ++i) {
-      const int here = k0, k1 = k0 + TK < kend ? k0 + TK : kend;
+      const int here = next.k0, k1 = here + TK < next.kend ? here + TK : next.kend;
       const uint32_t held = there;
       // a row sees only a part of the keys that are there (never with one position)
       const bool uneven = p_first != p_last &&
-                          !(k1 - 1 <= p_first && (a.window == 0 || k0 > p_last - a.window || k1 <= a.sinks));
+                          !(k1 - 1 <= p_first && (a.window == 0 || here > p_last - a.window || k1 <= a.sinks));
       odd |= put_keys<T, D, NI>(keys, values, 0, held, held == ~0u, uneven, kreg, vreg);
-      if (i + 1 < n) load(t + i + 1);
+      if (i + 1 < n) {
+        load();
+        far.find(a, x, t + i + 2);
+      }
       __builtin_amdgcn_wave_barrier();
       const int kp = fresh(first_key<D>()), vp = fresh(first_value<D>());
       float16v s = rows.scores(keys, kp);
@@ -809,29 +868,72 @@ __device__ Cut cut_of(const Phase& ph, const int64_t* cum, int entry, int head) 
   return u;
 }
 
+// The parts of one row, joined by one wave.  Lane i first takes the maximum and
+// sum of part i, so that all parts' weights are known at once and their outputs
+// can be loaded without waiting for one another.
 template <int D>
 struct Joined {
-  float top = kFloor, sum = 0.f, o[D / 64] = {};
-  __device__ void take(const float* part, float2 ml) {
+  static constexpr int W = D / 64;
+  float top = kFloor, sum = 0.f, o[W] = {};
+
+  // from(i, o, ml): where part i's row lies.
+  template <typename From>
+  __device__ void take(int parts, From from) {
     const int lane = threadIdx.x & 63;
-    const float now = fmaxf(top, ml.x);
-    const float a = __builtin_amdgcn_exp2f(top - now), b = __builtin_amdgcn_exp2f(ml.x - now);
-    top = now;
-    sum = sum * a + ml.y * b;
+    for (int i0 = 0; i0 < parts; i0 += 64) {
+      const int n = parts - i0 < 64 ? parts - i0 : 64;
+      const float* at = nullptr;
+      float2 ml = make_float2(kFloor, 0.f);
+      if (lane < n) {
+        const float2* m;
+        from(i0 + lane, at, m);
+        ml = *m;
+      }
+      float now = fmaxf(top, ml.x);
+      for (int d = 32; d; d >>= 1) now = fmaxf(now, __shfl_xor(now, d));
+      const float w = __builtin_amdgcn_exp2f(ml.x - now), shrink = __builtin_amdgcn_exp2f(top - now);
+      float add = lane < n ? ml.y * w : 0.f;
+      for (int d = 32; d; d >>= 1) add += __shfl_xor(add, d);
+      sum = sum * shrink + add;
+      top = now;
 #pragma unroll
-    for (int i = 0; i < D / 64; ++i) o[i] = o[i] * a + part[lane * (D / 64) + i] * b;
-  }
-  __device__ void take(const Parts& p, const Cut& u, int tile_rows, int row, int64_t dense) {
-    if (u.w0 == u.w1) {
-      take(p.whole_o + dense * D, p.whole_ml[dense]);
-      return;
-    }
-    for (int64_t w = u.w0; w <= u.w1; ++w) {
-      const int64_t slot = 2 * w + (u.c0 <= w * u.share ? 0 : 1), at = slot * tile_rows + row;
-      take(p.o + at * D, p.ml[at]);
+      for (int d = 0; d < W; ++d) o[d] *= shrink;
+      const uint64_t addr = reinterpret_cast<uint64_t>(at);
+      constexpr int kBatch = 4;
+      for (int i = 0; i < n; i += kBatch) {
+        float v[kBatch][W], wi[kBatch];
+#pragma unroll
+        for (int j = 0; j < kBatch; ++j) {
+          const int k = i + j < n ? i + j : n - 1;
+          const uint32_t lo = __builtin_amdgcn_readlane((uint32_t)addr, k);
+          const uint32_t hi = __builtin_amdgcn_readlane((uint32_t)(addr >> 32), k);
+          const float* p = reinterpret_cast<const float*>((uint64_t)hi << 32 | lo);
+#pragma unroll
+          for (int d = 0; d < W; ++d) v[j][d] = p[lane * W + d];
+          wi[j] = i + j < n ? __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(w), k)) : 0.f;
+        }
+#pragma unroll
+        for (int j = 0; j < kBatch; ++j)
+          if (i + j < n)
+#pragma unroll
+            for (int d = 0; d < W; ++d) o[d] = fmaf(v[j][d], wi[j], o[d]);
+      }
     }
   }
 };
+
+// Part i of a cut unit's row.
+__device__ void part_at(const Parts& p, const Cut& u, int i, int tile_rows, int row, int64_t dense, int D,
+                        const float*& o, const float2*& ml) {
+  if (u.w0 == u.w1) {
+    o = p.whole_o + dense * D;
+    ml = p.whole_ml + dense;
+    return;
+  }
+  const int64_t w = u.w0 + i, at = (2 * w + (u.c0 <= w * u.share ? 0 : 1)) * tile_rows + row;
+  o = p.o + at * D;
+  ml = p.ml + at;
+}
 
 // A row's output again, key by key, without the keys that it does not see: the
 // products of whole tiles take a weight of 0 times a value, which is not 0
@@ -868,40 +970,92 @@ __device__ void redo_row(const Args<T>& a, const Entry& x, int head, int row, fl
   for (int d = 0; d < D / 64; ++d) a.out[dense * D + lane * (D / 64) + d] = (T)(sum == 0.f ? 0.f : o[d] / sum);
 }
 
-// One workgroup a unit of the sequences' own keys, one wave a row.
+// Joins the rows of a unit of the sequences' own keys that this wave has: every
+// `step`th from `row` on.
 template <typename T, int D>
-__global__ __launch_bounds__(256) void join_parts(Args<T> a, int rows0, int rows1, int flags) {
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int e = blockIdx.x, head = blockIdx.y;
+__device__ void join_rows(const Args<T>& a, const Entry& x, const Cut& u, int head, int row, int step, int rows0,
+                          int rows1, bool odd) {
+  const int lane = threadIdx.x & 63;
+  for (; row < x.rows; row += step) {
+    const int at = x.row0 + row, token = at / a.G;
+    const int64_t dense = (int64_t)(x.q0 + token) * (a.kv_heads * a.G) + head * a.G + at - token * a.G;
+    Cut u0 = {};
+    int before = 0, row0 = 0;
+    if (x.prefix >= 0) {
+      row0 = x.prefix_row + row;
+      u0 = cut_of(a.plan.phase[0], a.plan.cum[0], x.prefix + row0 / rows0, head);
+      row0 %= rows0;
+      before = (int)(u0.w1 - u0.w0) + 1;
+    }
+    Joined<D> r;
+    r.take(before + (int)(u.w1 - u.w0) + 1, [&](int i, const float*& o, const float2*& ml) {
+      if (i < before) part_at(a.work.part[0], u0, i, rows0, row0, dense, D, o, ml);
+      else part_at(a.work.part[1], u, i - before, rows1, row, dense, D, o, ml);
+    });
+    const float inv = r.sum == 0.f ? 0.f : 1.f / r.sum;
+    T v[D / 64];
+#pragma unroll
+    for (int i = 0; i < D / 64; ++i) v[i] = (T)(r.sum == 0.f ? 0.f : r.o[i] * inv);
+#pragma unroll
+    for (int i = 0; i < D / 64; ++i) a.out[dense * D + lane * (D / 64) + i] = v[i];
+    const float lse2 = r.sum == 0.f ? -INFINITY : r.top + __builtin_amdgcn_logf(r.sum);
+    if (lane == 0) a.lse[dense] = kLn2 * lse2;
+    if (odd) redo_row<T, D>(a, x, head, row, lse2);
+  }
+}
+
+// Whether a worker of the cut met values that are not finite (the workgroup
+// together).
+template <typename T>
+__device__ bool any_odd(const Args<T>& a, const Cut& u, int flags) {
+  int odd = 0;
+  for (int64_t w = u.w0 * flags + threadIdx.x; w < (u.w1 + 1) * flags; w += blockDim.x) odd |= a.work.odd[1][w];
+  return __syncthreads_or(odd);
+}
+
+// With a shared prefix every row is joined: a workgroup takes a unit, or a part
+// of its rows (blockIdx.z).
+template <typename T, int D>
+__global__ __launch_bounds__(256) void join_units(Args<T> a, int rows0, int rows1, int flags) {
+  const int e = blockIdx.x, head = blockIdx.y, wave = threadIdx.x >> 6;
   const Phase own = a.plan.phase[1];
   if (e >= own.entries) return;
   const Entry x = a.plan.entry[1][e];
   const Cut u = cut_of(own, a.plan.cum[1], e, head);
-  int odd = 0;
-  for (int64_t w = u.w0 * flags + threadIdx.x; w < (u.w1 + 1) * flags; w += 256) odd |= a.work.odd[1][w];
-  odd = __syncthreads_or(odd);
-  if (u.w0 == u.w1 && !a.join && !odd) return;  // written by its worker
-  for (int row = wave; row < x.rows; row += 4) {
-    const int at = x.row0 + row, token = at / a.G;
-    const int64_t dense = (int64_t)(x.q0 + token) * (a.kv_heads * a.G) + head * a.G + at - token * a.G;
-    float lse2;
-    if (u.w0 == u.w1 && !a.join) {
-      lse2 = a.lse[dense] * kLog2e;
-    } else {
-      Joined<D> r;
-      if (x.prefix >= 0) {
-        const int e0 = x.prefix + (x.prefix_row + row) / rows0, row0 = (x.prefix_row + row) % rows0;
-        r.take(a.work.part[0], cut_of(a.plan.phase[0], a.plan.cum[0], e0, head), rows0, row0, dense);
-      }
-      r.take(a.work.part[1], u, rows1, row, dense);
-      const float inv = r.sum == 0.f ? 0.f : 1.f / r.sum;
-#pragma unroll
-      for (int i = 0; i < D / 64; ++i)
-        a.out[dense * D + lane * (D / 64) + i] = (T)(r.sum == 0.f ? 0.f : r.o[i] * inv);
-      lse2 = r.sum == 0.f ? -INFINITY : r.top + __builtin_amdgcn_logf(r.sum);
-      if (lane == 0) a.lse[dense] = kLn2 * lse2;
+  join_rows<T, D>(a, x, u, head, blockIdx.z * 4 + wave, gridDim.z * 4, rows0, rows1, any_odd(a, u, flags));
+}
+
+// Otherwise only the units that are cut: the worker whose share begins inside a
+// unit, as the first one to, joins it.  A worker that met values that are not
+// finite also does its whole units' rows again.
+template <typename T, int D>
+__global__ __launch_bounds__(256) void join_cuts(Args<T> a, int rows1, int flags) {
+  const int w = blockIdx.x, row = blockIdx.z * 4 + (threadIdx.x >> 6), step = gridDim.z * 4;
+  const Phase own = a.plan.phase[1];
+  if (w >= own.workers) return;
+  const Start st = a.plan.start[1][w];
+  if (st.tile > 0 && st.tile <= own.share) {
+    const Entry x = a.plan.entry[1][st.entry];
+    const Cut u = cut_of(own, a.plan.cum[1], st.entry, st.head);
+    join_rows<T, D>(a, x, u, st.head, row, step, rows1, rows1, any_odd(a, u, flags));
+  }
+  if (!any_odd(a, Cut{w, w, 0, 0}, flags)) return;
+  const int64_t all = own.total * a.kv_heads, beg = w * own.share;
+  int e = st.entry, head = st.head, t = st.tile;
+  for (int64_t left = (beg + own.share < all ? beg + own.share : all) - beg; left > 0;) {
+    const Entry x = a.plan.entry[1][e];
+    const int n = (int)(x.tiles - t < left ? x.tiles - t : left);
+    for (int r = row; n == x.tiles && r < x.rows; r += step) {
+      const int at = x.row0 + r, token = at / a.G;
+      const int64_t dense = (int64_t)(x.q0 + token) * (a.kv_heads * a.G) + head * a.G + at - token * a.G;
+      redo_row<T, D>(a, x, head, r, a.lse[dense] * kLog2e);
     }
-    if (odd) redo_row<T, D>(a, x, head, row, lse2);
+    left -= n;
+    t = 0;
+    if (++e == own.entries) {
+      e = 0;
+      ++head;
+    }
   }
 }
 
@@ -925,12 +1079,20 @@ hipError_t launch_typed(const ewsjf_cache& c, const ewsjf_batch& b, int32_t laye
   a.plan = plan_of(s, const_cast<void*>(plan));
   a.work = work_of(c, b, s, ws);
   a.lse = lse != nullptr ? lse : a.work.lse;
+  const bool sixteens = c.page_size >= 16;
   for (int p = b.n_groups > 0 ? 0 : 1; p < 2; ++p) {
-    if (s.block[p]) attend_block<T, D><<<kBlocks, kWaves * 64, 0, stream>>>(a, p);
-    else attend_wave<T, D><<<kBlocks, kWaves * 64, 0, stream>>>(a, p);
+    auto kernel = s.block[p] ? (sixteens ? attend_block<T, D, true> : attend_block<T, D, false>)
+                             : (sixteens ? attend_wave<T, D, true> : attend_wave<T, D, false>);
+    kernel<<<kBlocks, kWaves * 64, 0, stream>>>(a, p);
   }
-  join_parts<T, D><<<dim3((unsigned)s.entries[1], c.kv_heads), 256, 0, stream>>>(a, s.rows[0], s.rows[1],
-                                                                                s.block[1] ? kWaves : 1);
+  // four rows a wave at most
+  const int64_t most = (int64_t)b.max_q * s.G < s.rows[1] ? (int64_t)b.max_q * s.G : s.rows[1];
+  const unsigned z = (unsigned)((most + 15) / 16);
+  const int flags = s.block[1] ? kWaves : 1;
+  if (a.join)
+    join_units<T, D><<<dim3((unsigned)s.entries[1], c.kv_heads, z), 256, 0, stream>>>(a, s.rows[0], s.rows[1], flags);
+  else
+    join_cuts<T, D><<<dim3(s.workers[1], 1, z), 256, 0, stream>>>(a, s.rows[1], flags);
   return hipGetLastError();
 }
 
