@@ -30,11 +30,9 @@ namespace {
 
 constexpr int kRowTile = 32;     // rows of a unit of the wave kernel
 constexpr int kRowKeys = 32;     // its key tile
-constexpr int kBlockTile = 128;  // rows of a unit of the workgroup kernel (four waves of 32)
-constexpr int kBlockKeys = 64;
-constexpr int kWaves = 4;
+constexpr int kBlockKeys = 64;   // key tile of the workgroup kernel (four or eight waves of 32 rows)
+constexpr int kWaves = 4;        // waves of a workgroup of the wave kernel
 constexpr int kCUs = 256;
-constexpr int kBlocks = 2 * kCUs;  // both kernels: two workgroups a CU
 constexpr float kFloor = -3e38f;   // running maximum of a row that has seen no key
 constexpr float kLn2 = 0.6931471805599453f;
 constexpr float kLog2e = 1.4426950408889634f;
@@ -75,20 +73,23 @@ struct Plan {
 
 struct Shape {
   int G;
-  int rows[2], keys[2], workers[2];
+  int waves[2];  // of a workgroup that shares a unit's keys; 0: the wave kernel
+  int rows[2], keys[2], workers[2], blocks[2];
   int64_t entries[2];  // most row tiles
-  bool block[2];       // the workgroup kernel
 };
 
 Shape shape_of(const ewsjf_cache& c, const ewsjf_batch& b) {
   Shape s;
   s.G = b.q_heads / c.kv_heads;
-  s.block[0] = b.n_groups > 0 && b.total_q * s.G > (int64_t)kRowTile * b.n_groups;
-  s.block[1] = (int64_t)b.max_q * s.G > kRowTile;
+  // rows that read the same keys: of a sequence, of a group on average
+  const int64_t most[2] = {b.n_groups > 0 ? b.total_q * s.G / b.n_groups : 0, (int64_t)b.max_q * s.G};
   for (int p = 0; p < 2; ++p) {
-    s.rows[p] = s.block[p] ? kBlockTile : kRowTile;
-    s.keys[p] = s.block[p] ? kBlockKeys : kRowKeys;
-    s.workers[p] = s.block[p] ? kBlocks : kBlocks * kWaves;
+    s.waves[p] = most[p] <= kRowTile ? 0 : most[p] <= 128 ? 4 : 8;
+    s.rows[p] = s.waves[p] ? 32 * s.waves[p] : kRowTile;
+    s.keys[p] = s.waves[p] ? kBlockKeys : kRowKeys;
+    // as many as fit the chip at once: eight waves of 256 registers a CU
+    s.blocks[p] = s.waves[p] == 8 ? kCUs : 2 * kCUs;
+    s.workers[p] = s.waves[p] ? s.blocks[p] : s.blocks[p] * kWaves;
     s.entries[p] = b.total_q * s.G / s.rows[p] + (p ? b.n_seqs : b.n_groups);
   }
   if (b.n_groups == 0) s.entries[0] = 0;
@@ -149,7 +150,7 @@ Work work_of(const ewsjf_cache& c, const ewsjf_batch& b, const Shape& s, void* b
     w.part[i].ml = at.take<float2>(rows);
     w.part[i].whole_o = at.take<float>(whole * c.head_dim);
     w.part[i].whole_ml = at.take<float2>(whole);
-    w.odd[i] = at.take<int32_t>((size_t)s.workers[i] * (s.block[i] ? kWaves : 1));
+    w.odd[i] = at.take<int32_t>((size_t)s.workers[i] * (s.waves[i] ? s.waves[i] : 1));
   }
   w.lse = at.take<float>((size_t)b.total_q * b.q_heads);
   w.bytes = at.at;
@@ -342,6 +343,10 @@ __global__ __launch_bounds__(kPlanThreads) void make_plan(ewsjf_cache c, ewsjf_b
 // ---------------------------------------------------------------------------
 typedef __attribute__((ext_vector_type(4))) short short4v;
 typedef __attribute__((ext_vector_type(16))) float float16v;
+template <int N>
+struct Const {
+  static constexpr int value = N;
+};
 template <typename T>
 using vec8 = T __attribute__((ext_vector_type(8)));
 
@@ -420,10 +425,14 @@ struct Rows {
   }
 
   // S^T of the 32 keys at `keys`; first: key_place of the lane's row and half.
-  __device__ float16v scores(const char* keys, int first) const {
+  __device__ void read_keys(const char* keys, int first, vec8<T> (&k)[D / 16]) const {
+#pragma unroll
+    for (int i = 0; i < D / 16; ++i) k[i] = *reinterpret_cast<const vec8<T>*>(keys + (first ^ (i << 5)));
+  }
+  __device__ float16v scores(const vec8<T> (&k)[D / 16]) const {
     float16v s = {};
 #pragma unroll
-    for (int k = 0; k < D / 16; ++k) s = mfma(*reinterpret_cast<const vec8<T>*>(keys + (first ^ (k << 5))), q[k], s);
+    for (int i = 0; i < D / 16; ++i) s = mfma(k[i], q[i], s);
     return s;
   }
 
@@ -442,24 +451,37 @@ struct Rows {
     }
   }
 
-  // O^T += V^T P^T over the 16 keys of registers [8 half, 8 half + 8) of p;
-  // first: value_place of the lane's row and column.
-  __device__ void add(const char* values, int first, int half, const float16v& p) {
+  // V^T of 16 keys and 32 dims, the first product's order of keys: chunk c of
+  // the keys, i of the dims, k = c D / 32 + i; first: value_place of the lane's
+  // row and column.
+  static __device__ vec8<T> read_values(const char* values, int first, int k) {
+    union {
+      short4v part[2];
+      vec8<T> all;
+    } v;
+    typedef __attribute__((address_space(3))) short4v* lds4;
+    const char* at = values + k / (D / 32) * 16 * D * 2 + (first ^ (k % (D / 32) << 6));
+    v.part[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4)at);
+    v.part[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4)(at + 8 * D * 2));
+    return v.all;
+  }
+
+  // O^T += V^T P^T over 32 N keys.  Reads run kAhead products ahead (the order
+  // is kept by the barriers: left alone, each product waits for its own read);
+  // v holds the first ones.
+  static constexpr int kAhead = 4;
+  template <int N>
+  __device__ void add(const char* values, int first, const float16v (&p)[N], vec8<T> (&v)[kAhead]) {
     vec8<T> w;
 #pragma unroll
-    for (int j = 0; j < 8; ++j) w[j] = (T)p[8 * half + j];
-    values += half * 16 * D * 2;
+    for (int k = 0; k < 2 * N * (D / 32); ++k) {
+      const int c = k / (D / 32), i = k % (D / 32);
+      if (i == 0)
 #pragma unroll
-    for (int i = 0; i < D / 32; ++i) {
-      union {
-        short4v part[2];
-        vec8<T> all;
-      } v;
-      typedef __attribute__((address_space(3))) short4v* lds4;
-      const char* at = values + (first ^ (i << 6));
-      v.part[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4)at);
-      v.part[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4)(at + 8 * D * 2));
-      o[i] = mfma(v.all, w, o[i]);
+        for (int j = 0; j < 8; ++j) w[j] = (T)p[c / 2][8 * (c % 2) + j];
+      o[i] = mfma(v[k % kAhead], w, o[i]);
+      if (k + kAhead < 2 * N * (D / 32)) v[k % kAhead] = read_values(values, first, k + kAhead);
+      __builtin_amdgcn_sched_barrier(0);
     }
   }
 };
@@ -545,125 +567,158 @@ __device__ void store_rows(const Args<T>& a, int phase, const Entry& x, int head
   if (h == 0) (whole ? w.whole_ml : w.ml)[at_row] = make_float2(r.top, sum);
 }
 
-// A tile of TK keys from k0 on, of which those below kend count, and the
-// pages that hold them.
+// The key tiles of a unit.  Tile t is keys [first(t), first(t) + TK), of which
+// those below end(t) count; the pages that hold them are looked up by find, one
+// register of the wave a tile.
 //
 // Sixteens: pages have at least 16 tokens.  Tiles begin at multiples of 16, so
-// 16 keys lie in one page: lane i holds the page of keys [16 i', 16 i' + 16),
-// i' = i mod TK / 16, and addresses are the wave's but for a constant of the
-// lane.  Otherwise lane i holds the page of key i.  -1: no page, or no row
-// looks there.
+// 16 keys lie in one page: lane i finds the page of keys [16 i', 16 i' + 16),
+// i' = i mod TK / 16, and a load's address is the wave's but for a constant of
+// the lane.  Otherwise lane i finds the page of key i.
 template <typename T, int D, int TK, bool Sixteens>
-struct Tile {
+struct Tiles {
   static constexpr int LPR = D / 8, KPI = 64 / LPR;  // lanes a key, keys a load
-  int k0, kend, page;
+  static constexpr int kGroup = 16 / KPI;            // loads of 16 keys
+  const int32_t* row;
+  const char* base;  // the key head's first key
+  int lo, hi, sink, nst, shift, pages;
+  int c0, c1;        // tiles [c0, c1): every row sees every key
+  int p_first, p_last, window, sinks;
+  bool there_is;
+  uint32_t step[kGroup];  // a lane's place in the loads of 16 keys
 
-  // The pages of tile t (a load in flight).
-  __device__ void find(const Args<T>& a, const Entry& x, int t) {
+  __device__ Tiles(const Args<T>& a, const Entry& x, int head) {
     const int lane = threadIdx.x & 63;
-    const int nst = (x.sink + TK - 1) / TK;
-    k0 = t < nst ? t * TK : x.lo + (t - nst) * TK;
-    kend = t < nst ? x.sink : x.end;
-    const int key = k0 + (Sixteens ? 16 * (lane % (TK / 16)) : lane % TK);
+    row = a.table + (int64_t)(x.slot < 0 ? 0 : x.slot) * a.width;
+    base = reinterpret_cast<const char*>(a.data + head * a.head_stride);
+    lo = x.lo, hi = x.end, sink = x.sink, nst = (x.sink + TK - 1) / TK;
+    shift = a.page_shift, pages = a.n_pages, window = a.window, sinks = a.sinks;
+    there_is = x.slot >= 0;
+    p_first = x.pos0 + x.row0 / a.G, p_last = x.pos0 + (x.row0 + x.rows - 1) / a.G;
+    const int below = p_first + 1 < hi ? p_first + 1 : hi;  // every row sees the keys before it,
+    const int above = window > 0 ? p_last - window + 1 : lo;  // and those from it on
+    c0 = nst + (above > lo ? (above - lo + TK - 1) / TK : 0);
+    c1 = there_is && below > lo ? nst + (below - lo) / TK : 0;
+#pragma unroll
+    for (int i = 0; i < kGroup; ++i)
+      step[i] = (uint32_t)((i * KPI + lane / LPR) * (int)a.token_stride + lane % LPR * 8) * 2;
+  }
+
+  __device__ int first(int t) const { return t < nst ? t * TK : lo + (t - nst) * TK; }
+  __device__ int end(int t) const { return t < nst ? sink : hi; }
+
+  __device__ int find(int t) const {
+    const int lane = threadIdx.x & 63, kend = end(t);
+    const int key = first(t) + (Sixteens ? 16 * (lane % (TK / 16)) : lane % TK);
     const int in = key < kend ? key : kend > 0 ? kend - 1 : 0;
-    page = a.table[(int64_t)(x.slot < 0 ? 0 : x.slot) * a.width + (in >> a.page_shift)];
-    if (key >= kend || x.slot < 0 || page >= a.n_pages || page < 0) page = -1;
+    return row[in >> shift];  // judged where it is used: nothing waits for it here
+  }
+
+  __device__ bool held(int page) const { return (unsigned)page < (unsigned)pages; }
+  // Every key is there, and every row sees it.
+  __device__ bool clean(int t, int page) const { return t >= c0 && t < c1 && __all(held(page)); }
+  // Every row of positions [from, to] sees every key of the tile that is there.
+  __device__ bool even(int t, int from, int to) const {
+    const int k0 = first(t), k1 = k0 + TK < end(t) ? k0 + TK : end(t);
+    return k1 - 1 <= from && (window == 0 || k0 > to - window || k1 <= sinks);
   }
 
   // Bits of the keys that are there and that some row may see.
-  __device__ uint64_t there(const Args<T>& a, int p_first) const {
-    uint64_t m;
+  __device__ uint64_t there(int t, int page) const {
+    uint64_t m = 0;
     if (Sixteens) {
-      m = 0;
 #pragma unroll
       for (int j = 0; j < TK / 16; ++j)
-        if (__builtin_amdgcn_readlane(page, j) >= 0) m |= 0xffffull << (16 * j);
+        if (held(__builtin_amdgcn_readlane(page, j))) m |= 0xffffull << (16 * j);
     } else {
-      m = __ballot(page >= 0);
+      m = __ballot(held(page));
       if (TK == 32) m = (uint32_t)m;
     }
-    m &= bits_below(kend - k0);
-    if (a.window > 0) m &= ~bits_below(p_first - a.window - k0 + 1) | bits_below(a.sinks - k0);
+    const int k0 = first(t);
+    m &= there_is ? bits_below(end(t) - k0) : 0;
+    if (window > 0) m &= ~bits_below(p_first - window - k0 + 1) | bits_below(sinks - k0);
     return m;
   }
 
   // Loads keys [key0, key0 + NI KPI) of the tile: 16 bytes a lane (page 0's
   // where there is no page).
   template <int NI>
-  __device__ void load(const Args<T>& a, int head, int key0, uint4 (&k)[NI], uint4 (&v)[NI]) const {
-    const int lane = threadIdx.x & 63;
+  __device__ void load(const Args<T>& a, int t, int page, int key0, uint4 (&k)[NI], uint4 (&v)[NI]) const {
+    const int lane = threadIdx.x & 63, mask = (1 << shift) - 1;
     if (Sixteens) {
-      const uint32_t mine = (uint32_t)(lane / LPR * a.token_stride + lane % LPR * 8) * 2;
+      constexpr int N = NI < kGroup ? NI : kGroup;
+      const int skip = key0 % 16 / KPI;  // a wave's first key lies inside 16 where it has fewer
 #pragma unroll
-      for (int i = 0; i < NI; ++i) {
-        const int key = key0 + i * KPI;
-        const int held = __builtin_amdgcn_readlane(page, key / 16);
-        const int in = (k0 + key) & ((1 << a.page_shift) - 1);
-        const char* base = reinterpret_cast<const char*>(a.data + (held < 0 ? 0 : held) * a.page_stride +
-                                                         head * a.head_stride + in * a.token_stride);
-        k[i] = *reinterpret_cast<const uint4*>(base + mine);
-        v[i] = *reinterpret_cast<const uint4*>(base + a.kv_stride * 2 + mine);
+      for (int g = 0; g < NI / N; ++g) {
+        const int key = key0 / 16 + g, at = __builtin_amdgcn_readlane(page, key);
+        const int in = (first(t) + 16 * key) & mask;
+        const char* p = base + 2 * ((held(at) ? at : 0) * a.page_stride + in * a.token_stride);
+        if (N < kGroup) p += 2 * (skip * KPI) * a.token_stride;
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+          k[g * N + i] = *reinterpret_cast<const uint4*>(p + step[i]);
+          v[g * N + i] = *reinterpret_cast<const uint4*>(p + 2 * a.kv_stride + step[i]);
+        }
       }
     } else {
 #pragma unroll
       for (int i = 0; i < NI; ++i) {
-        const int key = key0 + i * KPI + lane / LPR;
-        const int held = __shfl(page, key);
-        const int in = (k0 + key) & ((1 << a.page_shift) - 1);
-        const T* p = a.data + (held < 0 ? 0 : held) * a.page_stride + head * a.head_stride + in * a.token_stride +
-                     lane % LPR * 8;
+        const int key = key0 + i * KPI + lane / LPR, at = __shfl(page, key);
+        const int in = (first(t) + key) & mask;
+        const char* p =
+            base + 2 * ((held(at) ? at : 0) * a.page_stride + in * a.token_stride + lane % LPR * 8);
         k[i] = *reinterpret_cast<const uint4*>(p);
-        v[i] = *reinterpret_cast<const uint4*>(p + a.kv_stride);
+        v[i] = *reinterpret_cast<const uint4*>(p + 2 * a.kv_stride);
       }
     }
   }
 };
 
-// A tile's share of one wave, from registers to LDS: zeros for the keys that
-// are not there.  check: some row sees only a part of the tile; true is
-// returned where such a tile holds a value that is not finite.
+// A tile's share of one wave, from registers to LDS.
 template <typename T, int D, int NI>
-__device__ bool put_keys(char* keys, char* values, int key0, uint64_t there, bool full, bool check,
-                         const uint4 (&k)[NI], const uint4 (&v)[NI]) {
+__device__ void put_keys(char* keys, char* values, int key0, const uint4 (&k)[NI], const uint4 (&v)[NI]) {
   constexpr int LPR = D / 8, KPI = 64 / LPR;
   const int lane = threadIdx.x & 63, chunk = lane % LPR;
   const int kp = key_place<D>(key0 + lane / LPR, chunk), vp = value_place<D>(key0 + lane / LPR, chunk * 16);
-  if (full && !check) {
 #pragma unroll
-    for (int i = 0; i < NI; ++i) {
-      // KPI keys on, the place in the row moves with the key
-      const int step = i * KPI, kx = D == 128 ? (step & 15) << 4 : ((step >> 1) & 7) << 4;
-      *reinterpret_cast<uint4*>(keys + (kp ^ kx) + step * D * 2) = k[i];
-      *reinterpret_cast<uint4*>(values + vp + step * D * 2) = v[i];
-    }
-    return false;
+  for (int i = 0; i < NI; ++i) {
+    // KPI keys on, a chunk's place in its row moves with the key
+    const int step = i * KPI, move = D == 128 ? (step & 15) << 4 : ((step >> 1) & 7) << 4;
+    *reinterpret_cast<uint4*>(keys + (kp ^ move) + step * D * 2) = k[i];
+    *reinterpret_cast<uint4*>(values + vp + step * D * 2) = v[i];
   }
+}
+
+// Before that, zeros for the keys that are not there; true if a value is not
+// finite.
+template <typename T, int D, int NI>
+__device__ bool clear_keys(int key0, uint64_t there, uint4 (&k)[NI], uint4 (&v)[NI]) {
+  constexpr int LPR = D / 8, KPI = 64 / LPR;
+  const int lane = threadIdx.x & 63;
   uint32_t bad = 0;
 #pragma unroll
   for (int i = 0; i < NI; ++i) {
-    const int key = key0 + i * KPI + lane / LPR;
-    const uint32_t keep = there >> key & 1 ? ~0u : 0u;
-    uint4 x = k[i], y = v[i];
-    x.x &= keep, x.y &= keep, x.z &= keep, x.w &= keep;
-    y.x &= keep, y.y &= keep, y.z &= keep, y.w &= keep;
-    *reinterpret_cast<uint4*>(keys + key_place<D>(key, chunk)) = x;
-    *reinterpret_cast<uint4*>(values + value_place<D>(key, chunk * 16)) = y;
-    bad |= not_finite(y.x, T()) | not_finite(y.y, T()) | not_finite(y.z, T()) | not_finite(y.w, T());
+    const uint32_t keep = there >> (key0 + i * KPI + lane / LPR) & 1 ? ~0u : 0u;
+    k[i].x &= keep, k[i].y &= keep, k[i].z &= keep, k[i].w &= keep;
+    v[i].x &= keep, v[i].y &= keep, v[i].z &= keep, v[i].w &= keep;
+    bad |= not_finite(v[i].x, T()) | not_finite(v[i].y, T()) | not_finite(v[i].z, T()) | not_finite(v[i].w, T());
   }
-  return check && bad != 0;
+  return bad != 0;
 }
 
 // ---------------------------------------------------------------------------
-// The workgroup kernel: 128 rows, 32 a wave; the four waves load a tile of 64
-// keys and values for all, one tile ahead of the one in use.
+// The workgroup kernel: 32 rows a wave; the waves load a tile of 64 keys and
+// values for all, two tiles ahead of the one in use: one on its way to
+// registers, one from registers to the LDS that the tile before has left.
 // ---------------------------------------------------------------------------
-template <typename T, int D, bool Sixteens>
-__global__ __launch_bounds__(kWaves * 64, 2) void attend_block(Args<T> a, int phase) {
-  using Keys = Tile<T, D, kBlockKeys, Sixteens>;
-  constexpr int TK = kBlockKeys, NI = TK / kWaves / Keys::KPI;
+template <typename T, int D, int NW, bool Sixteens>
+__global__ __launch_bounds__(NW * 64, 2) void attend_block(Args<T> a, int phase) {
+  using Keys = Tiles<T, D, kBlockKeys, Sixteens>;
+  constexpr int TK = kBlockKeys, NI = TK / NW / Keys::KPI, S = NW / 4;
   __shared__ __align__(16) char keys[2][TK * D * 2];
   __shared__ __align__(16) char values[2][TK * D * 2];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int mine = wave * (TK / NW);  // the wave's first key of a tile
   const Phase ph = a.plan.phase[phase];
   // neighbouring shares of the line read the same keys: give them to one XCD
   const int id = blockIdx.x % 8 * (gridDim.x / 8) + blockIdx.x / 8;
@@ -671,64 +726,71 @@ __global__ __launch_bounds__(kWaves * 64, 2) void attend_block(Args<T> a, int ph
   const int64_t all = ph.total * a.kv_heads;
   const int64_t beg = id * ph.share, stop = beg + ph.share < all ? beg + ph.share : all;
   const Start st = a.plan.start[phase][id];
-  int e = st.entry, head = st.head, t = st.tile;
+  int e = st.entry, head = st.head, t0 = st.tile;
   int64_t left = stop - beg;
   bool leading = true, odd = false;
   Rows<T, D> rows;
 
   while (left > 0) {
     const Entry x = a.plan.entry[phase][e];
-    const int n = (int)(x.tiles - t < left ? x.tiles - t : left);
-    const bool whole = t == 0 && n == x.tiles;
+    const int n = (int)(x.tiles - t0 < left ? x.tiles - t0 : left);
+    const bool whole = t0 == 0 && n == x.tiles;
     const int row = wave * 32 + (lane & 31);
     const bool busy = wave * 32 < x.rows;
+    const Keys tiles(a, x, head);
     load_rows<T, D>(a, x, head, row, rows.q);
     rows.clear();
-    const int p_first = x.pos0 + x.row0 / a.G, p_last = x.pos0 + (x.row0 + x.rows - 1) / a.G;
     const int w_last = wave * 32 + 31 < x.rows ? wave * 32 + 31 : x.rows - 1;
-    const int w_first = busy ? x.pos0 + (x.row0 + wave * 32) / a.G : p_first;
-    const int w_end = busy ? x.pos0 + (x.row0 + w_last) / a.G : p_first;
+    const int w_first = busy ? x.pos0 + (x.row0 + wave * 32) / a.G : tiles.p_first;
+    const int w_end = busy ? x.pos0 + (x.row0 + w_last) / a.G : tiles.p_first;
     const int p = x.pos0 + (x.row0 + (row < x.rows ? row : x.rows - 1)) / a.G;
 
-    // every row of positions [first, last] sees every key of the tile that there is
-    auto even = [&](int k0, int kend, int first, int last) {
-      const int k1 = k0 + TK < kend ? k0 + TK : kend;
-      return k1 - 1 <= first && (a.window == 0 || k0 > last - a.window || k1 <= a.sinks);
+    uint4 kreg[S][NI], vreg[S][NI];
+    int page[S + 2];  // of tiles i (in use), i + 1, ..
+    auto put = [&](int buf, int t, int held, uint4(&k)[NI], uint4(&v)[NI]) {
+      if (!tiles.clean(t, held)) {
+        const bool bad = clear_keys<T, D, NI>(mine, tiles.there(t, held), k, v);
+        odd |= bad && !tiles.even(t, tiles.p_first, tiles.p_last);
+      }
+      put_keys<T, D, NI>(keys[buf], values[buf], mine, k, v);
     };
-    uint4 kreg[NI], vreg[NI];
-    Keys next, far;  // the tile in the registers, and the one whose pages are being looked up
-    uint64_t there;
-    auto load = [&]() {
-      next = far;
-      there = next.there(a, p_first);
-      next.load(a, head, wave * (TK / kWaves), kreg, vreg);
-    };
-    auto put = [&](int buf) {
-      odd |= put_keys<T, D, NI>(keys[buf], values[buf], wave * (TK / kWaves), there, there == ~0ull,
-                                !even(next.k0, next.kend, p_first, p_last), kreg, vreg);
-    };
-
-    far.find(a, x, t);
-    load();
-    far.find(a, x, t + 1);
-    __syncthreads();  // the last unit's tiles are no longer read
-    put(0);
-    for (int i = 0; i < n; ++i) {
-      const int buf = i & 1, here = next.k0, here_end = next.kend;
-      const uint64_t held = there;
-      if (i + 1 < n) {
-        load();
-        far.find(a, x, t + i + 2);
+    auto step = [&](int i, auto which) {
+      constexpr int buf = decltype(which)::value;
+      const int t = t0 + i;
+      if (i + S < n) {
+        tiles.load(a, t + S, page[S], mine, kreg[buf % S], vreg[buf % S]);
+        page[S + 1] = tiles.find(t + S + 1);
       }
       __syncthreads();
-      const bool any = here <= w_end && (a.window == 0 || here + TK - 1 > w_first - a.window || here < a.sinks);
-      if (busy && any && held != 0) {
+      bool go = busy, masked = false;
+      uint64_t held = 0;
+      if (!tiles.clean(t, page[0])) {
+        const int k0 = tiles.first(t);
+        held = tiles.there(t, page[0]);
+        go = busy && held != 0 && k0 <= w_end &&
+             (a.window == 0 || k0 + TK - 1 > w_first - a.window || k0 < a.sinks);
+        masked = held != ~0ull || !tiles.even(t, w_first, w_end);
+      }
+      if (go) {
         float16v s[TK / 32];
         const int kp = fresh(first_key<D>()), vp = fresh(first_value<D>());
+        vec8<T> k[TK / 32][D / 16];
 #pragma unroll
-        for (int j = 0; j < TK / 32; ++j) s[j] = rows.scores(keys[buf] + j * 32 * D * 2, kp);
-        if (held != ~0ull || !even(here, here_end, w_first, w_end)) {
-          const uint64_t seen = seen_keys(held, here, p, a.window, a.sinks) >> (4 * (lane >> 5));
+        for (int j = 0; j < TK / 32; ++j) rows.read_keys(keys[buf] + j * 32 * D * 2, kp, k[j]);
+#pragma unroll
+        for (int j = 0; j < TK / 32; ++j) s[j] = rows.scores(k[j]);
+        __builtin_amdgcn_sched_group_barrier(0x100, D / 16, 0);
+#pragma unroll
+        for (int j = 0; j < D / 16; ++j) {
+          __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+          __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+        }
+        __builtin_amdgcn_sched_group_barrier(0x008, D / 16, 0);
+        vec8<T> v[Rows<T, D>::kAhead];
+#pragma unroll
+        for (int j = 0; j < Rows<T, D>::kAhead; ++j) v[j] = rows.read_values(values[buf], vp, j);
+        if (masked) {
+          const uint64_t seen = seen_keys(held, tiles.first(t), p, a.window, a.sinks) >> (4 * (lane >> 5));
           hide(s[0], (uint32_t)seen);
           hide(s[1], (uint32_t)(seen >> 32));
         }
@@ -745,24 +807,34 @@ __global__ __launch_bounds__(kWaves * 64, 2) void attend_block(Args<T> a, int ph
             s[j][r] = __builtin_amdgcn_exp2f(fmaf(s[j][r], a.scale2, -rows.top));
             rows.sum += s[j][r];
           }
-#pragma unroll
-        for (int j = 0; j < TK / 32; ++j)
-#pragma unroll
-          for (int half = 0; half < 2; ++half) rows.add(values[buf] + j * 32 * D * 2, vp, half, s[j]);
+        rows.add(values[buf], vp, s, v);
       }
-      if (i + 1 < n) put(buf ^ 1);
+      if (i + 1 < n) put(buf ^ 1, t + 1, page[1], kreg[(buf + 1) % S], vreg[(buf + 1) % S]);
+#pragma unroll
+      for (int j = 0; j <= S; ++j) page[j] = page[j + 1];
+    };
+
+#pragma unroll
+    for (int i = 0; i <= S; ++i) page[i] = tiles.find(t0 + i);
+#pragma unroll
+    for (int i = 0; i < S; ++i) tiles.load(a, t0 + i, page[i], mine, kreg[i], vreg[i]);
+    __syncthreads();  // the last unit's tiles are no longer read
+    put(0, t0, page[0], kreg[0], vreg[0]);
+    for (int i = 0; i < n; i += 2) {
+      step(i, Const<0>());
+      if (i + 1 < n) step(i + 1, Const<1>());
     }
-    store_rows<T, D>(a, phase, x, head, row, kBlockTile, whole, (int64_t)id * 2 + (leading ? 0 : 1), rows);
+    store_rows<T, D>(a, phase, x, head, row, NW * 32, whole, (int64_t)id * 2 + (leading ? 0 : 1), rows);
     leading = false;
     left -= n;
-    t = 0;
+    t0 = 0;
     if (++e == ph.entries) {
       e = 0;
       ++head;
     }
   }
-  if (lane == 0) a.work.odd[phase][id * kWaves + wave] = 0;
-  if (odd) a.work.odd[phase][id * kWaves + wave] = 1;
+  if (lane == 0) a.work.odd[phase][id * NW + wave] = 0;
+  if (odd) a.work.odd[phase][id * NW + wave] = 1;
 }
 
 // ---------------------------------------------------------------------------
@@ -771,7 +843,7 @@ __global__ __launch_bounds__(kWaves * 64, 2) void attend_block(Args<T> a, int ph
 // ---------------------------------------------------------------------------
 template <typename T, int D, bool Sixteens>
 __global__ __launch_bounds__(kWaves * 64, 2) void attend_wave(Args<T> a, int phase) {
-  using Keys = Tile<T, D, kRowKeys, Sixteens>;
+  using Keys = Tiles<T, D, kRowKeys, Sixteens>;
   constexpr int TK = kRowKeys, NI = TK / Keys::KPI;
   __shared__ __align__(16) char room[kWaves][2][TK * D * 2];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -783,48 +855,49 @@ __global__ __launch_bounds__(kWaves * 64, 2) void attend_wave(Args<T> a, int pha
   const int64_t all = ph.total * a.kv_heads;
   const int64_t beg = id * ph.share, stop = beg + ph.share < all ? beg + ph.share : all;
   const Start st = a.plan.start[phase][id];
-  int e = st.entry, head = st.head, t = st.tile;
+  int e = st.entry, head = st.head, t0 = st.tile;
   int64_t left = stop - beg;
-  bool leading = true;
-  bool odd = false;
+  bool leading = true, odd = false;
   Rows<T, D> rows;
 
   while (left > 0) {
     const Entry x = a.plan.entry[phase][e];
-    const int n = (int)(x.tiles - t < left ? x.tiles - t : left);
-    const bool whole = t == 0 && n == x.tiles;
+    const int n = (int)(x.tiles - t0 < left ? x.tiles - t0 : left);
+    const bool whole = t0 == 0 && n == x.tiles;
     const int row = lane & 31;
+    const Keys tiles(a, x, head);
     load_rows<T, D>(a, x, head, row, rows.q);
     rows.clear();
-    const int p_first = x.pos0 + x.row0 / a.G, p_last = x.pos0 + (x.row0 + x.rows - 1) / a.G;
     const int p = x.pos0 + (x.row0 + (row < x.rows ? row : x.rows - 1)) / a.G;
     uint4 kreg[NI], vreg[NI];
-    Keys next, far;
-    uint32_t there;
-    auto load = [&]() {
-      next = far;
-      there = (uint32_t)next.there(a, p_first);
-      next.load(a, head, 0, kreg, vreg);
-    };
-    far.find(a, x, t);
-    load();
-    far.find(a, x, t + 1);
+    int page = tiles.find(t0);
+    tiles.load(a, t0, page, 0, kreg, vreg);
+    int page1 = tiles.find(t0 + 1);
     for (int i = 0; i < n; ++i) {
-      const int here = next.k0, k1 = here + TK < next.kend ? here + TK : next.kend;
-      const uint32_t held = there;
-      // a row sees only a part of the keys that are there (never with one position)
-      const bool uneven = p_first != p_last &&
-                          !(k1 - 1 <= p_first && (a.window == 0 || here > p_last - a.window || k1 <= a.sinks));
-      odd |= put_keys<T, D, NI>(keys, values, 0, held, held == ~0u, uneven, kreg, vreg);
+      const int t = t0 + i;
+      const bool clean = tiles.clean(t, page);
+      uint32_t held = ~0u;
+      if (!clean) {
+        held = (uint32_t)tiles.there(t, page);
+        const bool bad = clear_keys<T, D, NI>(0, held, kreg, vreg);
+        // with one position, what is there is seen by all rows
+        odd |= bad && tiles.p_first != tiles.p_last && !tiles.even(t, tiles.p_first, tiles.p_last);
+      }
+      put_keys<T, D, NI>(keys, values, 0, kreg, vreg);
+      page = page1;
       if (i + 1 < n) {
-        load();
-        far.find(a, x, t + i + 2);
+        tiles.load(a, t + 1, page, 0, kreg, vreg);
+        page1 = tiles.find(t + 2);
       }
       __builtin_amdgcn_wave_barrier();
       const int kp = fresh(first_key<D>()), vp = fresh(first_value<D>());
-      float16v s = rows.scores(keys, kp);
-      if (uneven || held != ~0u)
-        hide(s, (uint32_t)seen_keys(held, here, p, a.window, a.sinks) >> (4 * (lane >> 5)));
+      vec8<T> k[D / 16];
+      rows.read_keys(keys, kp, k);
+      float16v s = rows.scores(k);
+      vec8<T> v[Rows<T, D>::kAhead];
+#pragma unroll
+      for (int j = 0; j < Rows<T, D>::kAhead; ++j) v[j] = rows.read_values(values, vp, j);
+      if (!clean) hide(s, (uint32_t)seen_keys(held, tiles.first(t), p, a.window, a.sinks) >> (4 * (lane >> 5)));
       float most = s[0];
 #pragma unroll
       for (int r = 1; r < 16; ++r) most = fmaxf(most, s[r]);
@@ -834,14 +907,14 @@ __global__ __launch_bounds__(kWaves * 64, 2) void attend_wave(Args<T> a, int pha
         s[r] = __builtin_amdgcn_exp2f(fmaf(s[r], a.scale2, -rows.top));
         rows.sum += s[r];
       }
-#pragma unroll
-      for (int half = 0; half < 2; ++half) rows.add(values, vp, half, s);
+      const float16v w[1] = {s};
+      rows.add(values, vp, w, v);
       __builtin_amdgcn_wave_barrier();
     }
     store_rows<T, D>(a, phase, x, head, row, kRowTile, whole, (int64_t)id * 2 + (leading ? 0 : 1), rows);
     leading = false;
     left -= n;
-    t = 0;
+    t0 = 0;
     if (++e == ph.entries) {
       e = 0;
       ++head;
@@ -1081,14 +1154,15 @@ hipError_t launch_typed(const ewsjf_cache& c, const ewsjf_batch& b, int32_t laye
   a.lse = lse != nullptr ? lse : a.work.lse;
   const bool sixteens = c.page_size >= 16;
   for (int p = b.n_groups > 0 ? 0 : 1; p < 2; ++p) {
-    auto kernel = s.block[p] ? (sixteens ? attend_block<T, D, true> : attend_block<T, D, false>)
-                             : (sixteens ? attend_wave<T, D, true> : attend_wave<T, D, false>);
-    kernel<<<kBlocks, kWaves * 64, 0, stream>>>(a, p);
+    auto kernel = s.waves[p] == 8 ? (sixteens ? attend_block<T, D, 8, true> : attend_block<T, D, 8, false>)
+                  : s.waves[p]    ? (sixteens ? attend_block<T, D, 4, true> : attend_block<T, D, 4, false>)
+                                  : (sixteens ? attend_wave<T, D, true> : attend_wave<T, D, false>);
+    kernel<<<s.blocks[p], 64 * (s.waves[p] ? s.waves[p] : kWaves), 0, stream>>>(a, p);
   }
   // four rows a wave at most
   const int64_t most = (int64_t)b.max_q * s.G < s.rows[1] ? (int64_t)b.max_q * s.G : s.rows[1];
   const unsigned z = (unsigned)((most + 15) / 16);
-  const int flags = s.block[1] ? kWaves : 1;
+  const int flags = s.waves[1] ? s.waves[1] : 1;
   if (a.join)
     join_units<T, D><<<dim3((unsigned)s.entries[1], c.kv_heads, z), 256, 0, stream>>>(a, s.rows[0], s.rows[1], flags);
   else
