@@ -30,7 +30,9 @@ namespace {
 
 constexpr int kRowTile = 32;     // rows of a unit of the wave kernel
 constexpr int kRowKeys = 32;     // its key tile
-constexpr int kBlockKeys = 64;   // key tile of the workgroup kernel (four or eight waves of 32 rows)
+// Key tile of the workgroup kernel with four or eight waves of 32 rows: two
+// tiles fill the LDS that a workgroup can have with all waves resident.
+__host__ __device__ constexpr int block_keys(int waves) { return waves == 8 ? 128 : 64; }
 constexpr int kWaves = 4;        // waves of a workgroup of the wave kernel
 constexpr int kCUs = 256;
 constexpr float kFloor = -3e38f;   // running maximum of a row that has seen no key
@@ -50,10 +52,36 @@ struct Entry {
   int32_t pad;
 };
 
-// A worker's first tile.
+// A worker's first tile: its unit's place in the line, the unit, the tile.
 struct Start {
-  int32_t entry, head, tile, pad;
+  int32_t place, entry, head, tile;
 };
+
+// The unit at a place of the line.  By heads: the row tiles of a key head, then
+// the next head's.  In columns: each XCD's eighth of that list is dealt out to
+// `columns` workers in turn, a worker's units following one another on the
+// line; so at any time the workers of an XCD have neighbouring row tiles of one
+// head, which read much the same keys.
+__device__ int64_t unit_at(int64_t place, int64_t units, int columns) {
+  if (columns == 0) return place;
+  int64_t base = 0, size = units;
+  for (int x = 7; x >= 0; --x)
+    if (place >= units * x / 8) {
+      base = units * x / 8;
+      size = units * (x + 1) / 8 - base;
+      break;
+    }
+  int64_t k = place - base;
+  const int64_t rows = size / columns, longer = size % columns;  // the first `longer` columns have one row more
+  int64_t col, row;
+  if (k < longer * (rows + 1)) {
+    col = k / (rows + 1), row = k % (rows + 1);
+  } else {
+    k -= longer * (rows + 1);
+    col = longer + k / rows, row = k % rows;
+  }
+  return base + row * columns + col;
+}
 
 // One phase of a plan.
 struct Phase {
@@ -61,6 +89,8 @@ struct Phase {
   int64_t share;    // tiles per worker
   int32_t entries;
   int32_t workers;
+  int32_t columns;  // of unit_at
+  int32_t pad;
 };
 
 struct Plan {
@@ -68,6 +98,7 @@ struct Plan {
   Start* start[2];   // [workers]
   Entry* entry[2];
   int64_t* cum[2];   // tiles of one key head before a row tile
+  int64_t* line;     // tiles before a place of the line in columns
   size_t bytes;
 };
 
@@ -76,6 +107,8 @@ struct Shape {
   int waves[2];  // of a workgroup that shares a unit's keys; 0: the wave kernel
   int rows[2], keys[2], workers[2], blocks[2];
   int64_t entries[2];  // most row tiles
+  int kv_heads;
+  int columns;         // phase 1's line in columns of this many a XCD; 0: by heads
 };
 
 Shape shape_of(const ewsjf_cache& c, const ewsjf_batch& b) {
@@ -86,13 +119,16 @@ Shape shape_of(const ewsjf_cache& c, const ewsjf_batch& b) {
   for (int p = 0; p < 2; ++p) {
     s.waves[p] = most[p] <= kRowTile ? 0 : most[p] <= 128 ? 4 : 8;
     s.rows[p] = s.waves[p] ? 32 * s.waves[p] : kRowTile;
-    s.keys[p] = s.waves[p] ? kBlockKeys : kRowKeys;
+    s.keys[p] = s.waves[p] ? block_keys(s.waves[p]) : kRowKeys;
     // as many as fit the chip at once: eight waves of 256 registers a CU
     s.blocks[p] = s.waves[p] == 8 ? kCUs : 2 * kCUs;
     s.workers[p] = s.waves[p] ? s.blocks[p] : s.blocks[p] * kWaves;
     s.entries[p] = b.total_q * s.G / s.rows[p] + (p ? b.n_seqs : b.n_groups);
   }
   if (b.n_groups == 0) s.entries[0] = 0;
+  s.kv_heads = c.kv_heads;
+  // rows that read the same keys as the next tile's: many row tiles of long runs, and nothing to join them with
+  s.columns = s.waves[1] && b.n_groups == 0 ? s.workers[1] / 8 : 0;
   return s;
 }
 
@@ -116,6 +152,7 @@ Plan plan_of(const Shape& s, void* base) {
     p.entry[i] = at.take<Entry>(s.entries[i]);
     p.cum[i] = at.take<int64_t>(s.entries[i] + 1);
   }
+  p.line = at.take<int64_t>(s.columns ? s.entries[1] * s.kv_heads + 1 : 0);
   p.bytes = at.at;
   return p;
 }
@@ -195,7 +232,7 @@ __device__ int last_at_most(const T* key, int n, int64_t v) {
 
 struct PlanArgs {
   const int32_t *slot, *q_start, *group_start, *shared;
-  int rows[2], keys[2], workers[2], G;
+  int rows[2], keys[2], workers[2], G, columns;
 };
 
 // One workgroup.  Everything read from the caller's arrays is bounded here, so
@@ -304,7 +341,7 @@ __global__ __launch_bounds__(kPlanThreads) void make_plan(ewsjf_cache c, ewsjf_b
           x.lo = shared;
           if (b.window > 0) {
             const int64_t w = (int64_t)p0 - b.window + 1;
-            x.lo = w > 0 ? (int)w & ~15 : 0;
+            x.lo = w > 0 ? (int)w & ~(TK - 1) : 0;
             x.sink = b.sinks < x.end ? b.sinks : x.end;
             if (x.lo <= x.sink) x.lo = x.sink = 0;  // one run of keys
           }
@@ -326,13 +363,36 @@ __global__ __launch_bounds__(kPlanThreads) void make_plan(ewsjf_cache c, ewsjf_b
     const int active = (int)((all + share - 1) / share);
     if (threadIdx.x == 0) {
       plan.cum[ph][E] = line;
-      plan.phase[ph] = Phase{line, share, E, active};
+      plan.phase[ph] = Phase{line, share, E, active, ph ? a.columns : 0, 0};
     }
     __syncthreads();  // entries and sums are read back by other threads
+    const int64_t units = (int64_t)E * c.kv_heads;
+    if (ph && a.columns) {
+      int64_t before = 0;
+      for (int64_t k0 = 0; k0 < units; k0 += kPlanThreads) {
+        const int64_t k = k0 + threadIdx.x;
+        const int tiles = k < units ? entry[unit_at(k, units, a.columns) % E].tiles : 0;
+        int64_t total;
+        const int64_t mine = scan(tiles, sums, total);
+        if (k < units) plan.line[k] = before + mine;
+        before += total;
+      }
+      __syncthreads();
+    }
     for (int w = threadIdx.x; w < active; w += kPlanThreads) {
-      const int64_t at = w * share, head = at / line, rest = at % line;
-      const int e = last_at_most(plan.cum[ph], E, rest);
-      plan.start[ph][w] = Start{e, (int)head, (int)(rest - plan.cum[ph][e]), 0};
+      const int64_t at = w * share;
+      int64_t place, rest;
+      if (ph && a.columns) {
+        place = last_at_most(plan.line, (int)units, at);
+        rest = at - plan.line[place];
+      } else {
+        const int64_t head = at / line;
+        const int e = last_at_most(plan.cum[ph], E, at % line);
+        place = head * E + e;
+        rest = at % line - plan.cum[ph][e];
+      }
+      const int64_t unit = unit_at(place, units, ph ? a.columns : 0);
+      plan.start[ph][w] = Start{(int)place, (int)(unit % E), (int)(unit / E), (int)rest};
     }
     __syncthreads();
   }
@@ -391,6 +451,21 @@ __device__ int fresh(int x) {
 
 __device__ uint32_t not_finite(uint32_t x, __bf16) { return ((x & 0x7f807f80u) + 0x00800080u) & 0x80008000u; }
 __device__ uint32_t not_finite(uint32_t x, _Float16) { return ((x & 0x7c007c00u) + 0x04000400u) & 0x80008000u; }
+
+// The unit after a worker's present one.
+__device__ void next_unit(const Phase& ph, int units, int& place, int& e, int& head) {
+  ++place;
+  if (ph.columns == 0) {
+    if (++e == ph.entries) {
+      e = 0;
+      ++head;
+    }
+    return;
+  }
+  if (place >= units) return;
+  const int64_t u = unit_at(place, units, ph.columns);
+  e = (int)(u % ph.entries), head = (int)(u / ph.entries);
+}
 
 template <typename T>
 struct Args {
@@ -451,6 +526,38 @@ struct Rows {
     }
   }
 
+  // Weights of the scores s, rounded to 16 bits, their sum added to the row's.
+  // They are first taken with the maximum as it stands: a sum of at most 2^10
+  // says that none is too large, and a maximum that is a few orders too low
+  // loses nothing.  Else the maximum is raised and they are taken again.
+  template <int N>
+  __device__ void weigh(const float16v (&s)[N], float scale2, vec8<T> (&w)[2 * N]) {
+    float add = weights<N>(s, scale2, w);
+    if (__any(!(add <= 1024.f))) {
+      float most = s[0][0];
+#pragma unroll
+      for (int j = 0; j < N; ++j)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) most = fmaxf(most, s[j][r]);
+      raise(pair_max(most) * scale2);
+      add = weights<N>(s, scale2, w);
+    }
+    sum += add;
+  }
+  template <int N>
+  __device__ float weights(const float16v (&s)[N], float scale2, vec8<T> (&w)[2 * N]) const {
+    float add[2] = {0.f, 0.f};
+#pragma unroll
+    for (int j = 0; j < N; ++j)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        const float p = __builtin_amdgcn_exp2f(fmaf(s[j][r], scale2, -top));
+        add[r % 2] += p;
+        w[2 * j + r / 8][r % 8] = (T)p;
+      }
+    return add[0] + add[1];
+  }
+
   // V^T of 16 keys and 32 dims, the first product's order of keys: chunk c of
   // the keys, i of the dims, k = c D / 32 + i; first: value_place of the lane's
   // row and column.
@@ -471,15 +578,11 @@ struct Rows {
   // v holds the first ones.
   static constexpr int kAhead = 4;
   template <int N>
-  __device__ void add(const char* values, int first, const float16v (&p)[N], vec8<T> (&v)[kAhead]) {
-    vec8<T> w;
+  __device__ void add(const char* values, int first, const vec8<T> (&w)[2 * N], vec8<T> (&v)[kAhead]) {
 #pragma unroll
     for (int k = 0; k < 2 * N * (D / 32); ++k) {
-      const int c = k / (D / 32), i = k % (D / 32);
-      if (i == 0)
-#pragma unroll
-        for (int j = 0; j < 8; ++j) w[j] = (T)p[c / 2][8 * (c % 2) + j];
-      o[i] = mfma(v[k % kAhead], w, o[i]);
+      const int i = k % (D / 32);
+      o[i] = mfma(v[k % kAhead], w[k / (D / 32)], o[i]);
       if (k + kAhead < 2 * N * (D / 32)) v[k % kAhead] = read_values(values, first, k + kAhead);
       __builtin_amdgcn_sched_barrier(0);
     }
@@ -579,10 +682,12 @@ template <typename T, int D, int TK, bool Sixteens>
 struct Tiles {
   static constexpr int LPR = D / 8, KPI = 64 / LPR;  // lanes a key, keys a load
   static constexpr int kGroup = 16 / KPI;            // loads of 16 keys
+  static constexpr bool turned = TK >= 64;
   const int32_t* row;
   const char* base;  // the key head's first key
   int lo, hi, sink, nst, shift, pages;
-  int c0, c1;        // tiles [c0, c1): every row sees every key
+  int run, turn;     // tiles of the main run, and the one that it begins with
+  int c0, c1;        // every row sees every key of [c0, c1)
   int p_first, p_last, window, sinks;
   bool there_is;
   uint32_t step[kGroup];  // a lane's place in the loads of 16 keys
@@ -597,44 +702,62 @@ struct Tiles {
     p_first = x.pos0 + x.row0 / a.G, p_last = x.pos0 + (x.row0 + x.rows - 1) / a.G;
     const int below = p_first + 1 < hi ? p_first + 1 : hi;  // every row sees the keys before it,
     const int above = window > 0 ? p_last - window + 1 : lo;  // and those from it on
-    c0 = nst + (above > lo ? (above - lo + TK - 1) / TK : 0);
-    c1 = there_is && below > lo ? nst + (below - lo) / TK : 0;
+    c0 = above > lo ? above : lo;
+    c1 = there_is ? below : 0;
+    // Row tiles that are worked on side by side have windows that differ by a few tiles.  Each begins its run with the
+    // tile whose number the run's length divides: then all read the same keys at the same time, out of L2.
+    run = x.tiles - nst;
+    turn = turned && window > 0 && run > 1 ? (run - lo / TK % run) % run : 0;
 #pragma unroll
     for (int i = 0; i < kGroup; ++i)
       step[i] = (uint32_t)((i * KPI + lane / LPR) * (int)a.token_stride + lane % LPR * 8) * 2;
   }
 
-  __device__ int first(int t) const { return t < nst ? t * TK : lo + (t - nst) * TK; }
+  __device__ int first(int t) const {
+    if (t < nst) return t * TK;
+    int i = t - nst + turn;
+    if (turned && i >= run) i -= run;
+    return lo + i * TK;
+  }
   __device__ int end(int t) const { return t < nst ? sink : hi; }
 
   __device__ int find(int t) const {
-    const int lane = threadIdx.x & 63, kend = end(t);
-    const int key = first(t) + (Sixteens ? 16 * (lane % (TK / 16)) : lane % TK);
+    const int lane = threadIdx.x & 63;
+    return entry_of(t, first(t) + (Sixteens ? 16 * (lane % (TK / 16)) : lane % TK));
+  }
+  __device__ int find_key(int t, int from) const { return entry_of(t, first(t) + from + (threadIdx.x & 63)); }
+  __device__ int entry_of(int t, int key) const {
+    const int kend = end(t);
     const int in = key < kend ? key : kend > 0 ? kend - 1 : 0;
     return row[in >> shift];  // judged where it is used: nothing waits for it here
   }
 
   __device__ bool held(int page) const { return (unsigned)page < (unsigned)pages; }
   // Every key is there, and every row sees it.
-  __device__ bool clean(int t, int page) const { return t >= c0 && t < c1 && __all(held(page)); }
+  __device__ bool clean(int t, int page) const {
+    const int k0 = first(t);
+    if (!(t >= nst && k0 >= c0 && k0 + TK <= c1)) return false;
+    return __all(held(page)) && (Sixteens || TK <= 64 || __all(held(find_key(t, 64))));
+  }
   // Every row of positions [from, to] sees every key of the tile that is there.
   __device__ bool even(int t, int from, int to) const {
     const int k0 = first(t), k1 = k0 + TK < end(t) ? k0 + TK : end(t);
     return k1 - 1 <= from && (window == 0 || k0 > to - window || k1 <= sinks);
   }
 
-  // Bits of the keys that are there and that some row may see.
-  __device__ uint64_t there(int t, int page) const {
+  // Bits of the keys of chunk c (64 keys) that are there and that some row may
+  // see.
+  __device__ uint64_t there(int t, int page, int c = 0) const {
     uint64_t m = 0;
     if (Sixteens) {
 #pragma unroll
-      for (int j = 0; j < TK / 16; ++j)
-        if (held(__builtin_amdgcn_readlane(page, j))) m |= 0xffffull << (16 * j);
+      for (int j = 0; j < (TK < 64 ? TK : 64) / 16; ++j)
+        if (held(__builtin_amdgcn_readlane(page, 4 * c + j))) m |= 0xffffull << (16 * j);
     } else {
-      m = __ballot(held(page));
+      m = __ballot(held(TK > 64 ? find_key(t, 64 * c) : page));
       if (TK == 32) m = (uint32_t)m;
     }
-    const int k0 = first(t);
+    const int k0 = first(t) + 64 * c;
     m &= there_is ? bits_below(end(t) - k0) : 0;
     if (window > 0) m &= ~bits_below(p_first - window - k0 + 1) | bits_below(sinks - k0);
     return m;
@@ -656,14 +779,16 @@ struct Tiles {
         if (N < kGroup) p += 2 * (skip * KPI) * a.token_stride;
 #pragma unroll
         for (int i = 0; i < N; ++i) {
-          k[g * N + i] = *reinterpret_cast<const uint4*>(p + step[i]);
-          v[g * N + i] = *reinterpret_cast<const uint4*>(p + 2 * a.kv_stride + step[i]);
+          const uint32_t in_load = fresh(step[i]);  // the wave's address and the lane's place stay apart
+          k[g * N + i] = *reinterpret_cast<const uint4*>(p + in_load);
+          v[g * N + i] = *reinterpret_cast<const uint4*>(p + 2 * a.kv_stride + in_load);
         }
       }
     } else {
 #pragma unroll
       for (int i = 0; i < NI; ++i) {
-        const int key = key0 + i * KPI + lane / LPR, at = __shfl(page, key);
+        const int key = key0 + i * KPI + lane / LPR;
+        const int at = TK > 64 ? entry_of(t, first(t) + key) : __shfl(page, key);
         const int in = (first(t) + key) & mask;
         const char* p =
             base + 2 * ((held(at) ? at : 0) * a.page_stride + in * a.token_stride + lane % LPR * 8);
@@ -707,14 +832,16 @@ __device__ bool clear_keys(int key0, uint64_t there, uint4 (&k)[NI], uint4 (&v)[
 }
 
 // ---------------------------------------------------------------------------
-// The workgroup kernel: 32 rows a wave; the waves load a tile of 64 keys and
-// values for all, two tiles ahead of the one in use: one on its way to
-// registers, one from registers to the LDS that the tile before has left.
+// The workgroup kernel: 32 rows a wave; the waves load a tile of keys and
+// values for all, worked on in chunks of 64 keys.  While a tile is in use the
+// next one goes from registers to the other half of LDS and the one after
+// that is loaded; one barrier a tile.
 // ---------------------------------------------------------------------------
 template <typename T, int D, int NW, bool Sixteens>
 __global__ __launch_bounds__(NW * 64, 2) void attend_block(Args<T> a, int phase) {
-  using Keys = Tiles<T, D, kBlockKeys, Sixteens>;
-  constexpr int TK = kBlockKeys, NI = TK / NW / Keys::KPI, S = NW / 4;
+  constexpr int TK = block_keys(NW);
+  using Keys = Tiles<T, D, TK, Sixteens>;
+  constexpr int NI = TK / NW / Keys::KPI, kChunk = 64 * D * 2;
   __shared__ __align__(16) char keys[2][TK * D * 2];
   __shared__ __align__(16) char values[2][TK * D * 2];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -726,7 +853,7 @@ __global__ __launch_bounds__(NW * 64, 2) void attend_block(Args<T> a, int phase)
   const int64_t all = ph.total * a.kv_heads;
   const int64_t beg = id * ph.share, stop = beg + ph.share < all ? beg + ph.share : all;
   const Start st = a.plan.start[phase][id];
-  int e = st.entry, head = st.head, t0 = st.tile;
+  int place = st.place, e = st.entry, head = st.head, t0 = st.tile;
   int64_t left = stop - beg;
   bool leading = true, odd = false;
   Rows<T, D> rows;
@@ -740,98 +867,76 @@ __global__ __launch_bounds__(NW * 64, 2) void attend_block(Args<T> a, int phase)
     const Keys tiles(a, x, head);
     load_rows<T, D>(a, x, head, row, rows.q);
     rows.clear();
-    const int w_last = wave * 32 + 31 < x.rows ? wave * 32 + 31 : x.rows - 1;
-    const int w_first = busy ? x.pos0 + (x.row0 + wave * 32) / a.G : tiles.p_first;
-    const int w_end = busy ? x.pos0 + (x.row0 + w_last) / a.G : tiles.p_first;
     const int p = x.pos0 + (x.row0 + (row < x.rows ? row : x.rows - 1)) / a.G;
 
-    uint4 kreg[S][NI], vreg[S][NI];
-    int page[S + 2];  // of tiles i (in use), i + 1, ..
-    auto put = [&](int buf, int t, int held, uint4(&k)[NI], uint4(&v)[NI]) {
+    uint4 kreg[NI], vreg[NI];
+    int page[4];  // of tiles i (in use) .. i + 3
+    auto put = [&](int buf, int t, int held) {
       if (!tiles.clean(t, held)) {
-        const bool bad = clear_keys<T, D, NI>(mine, tiles.there(t, held), k, v);
+        const bool bad = clear_keys<T, D, NI>(mine % 64, tiles.there(t, held, mine / 64), kreg, vreg);
         odd |= bad && !tiles.even(t, tiles.p_first, tiles.p_last);
       }
-      put_keys<T, D, NI>(keys[buf], values[buf], mine, k, v);
+      put_keys<T, D, NI>(keys[buf], values[buf], mine, kreg, vreg);
     };
-    auto step = [&](int i, auto which) {
-      constexpr int buf = decltype(which)::value;
-      const int t = t0 + i;
-      if (i + S < n) {
-        tiles.load(a, t + S, page[S], mine, kreg[buf % S], vreg[buf % S]);
-        page[S + 1] = tiles.find(t + S + 1);
+    auto chunk = [&](int buf, int c, bool clean, int t) {
+      float16v s[2];
+      const int kp = fresh(first_key<D>()), vp = fresh(first_value<D>());
+      const char* kc = keys[buf] + c * kChunk;
+      const char* vc = values[buf] + c * kChunk;
+      vec8<T> k[2][D / 16], v[Rows<T, D>::kAhead], w[4];
+#pragma unroll
+      for (int j = 0; j < 2; ++j) rows.read_keys(kc + j * 32 * D * 2, kp, k[j]);
+#pragma unroll
+      for (int j = 0; j < 2; ++j) s[j] = rows.scores(k[j]);
+      __builtin_amdgcn_sched_group_barrier(0x100, D / 16, 0);
+#pragma unroll
+      for (int j = 0; j < D / 16; ++j) {
+        __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+        __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
       }
-      __syncthreads();
-      bool go = busy, masked = false;
-      uint64_t held = 0;
-      if (!tiles.clean(t, page[0])) {
-        const int k0 = tiles.first(t);
-        held = tiles.there(t, page[0]);
-        go = busy && held != 0 && k0 <= w_end &&
-             (a.window == 0 || k0 + TK - 1 > w_first - a.window || k0 < a.sinks);
-        masked = held != ~0ull || !tiles.even(t, w_first, w_end);
+      __builtin_amdgcn_sched_group_barrier(0x008, D / 16, 0);
+#pragma unroll
+      for (int j = 0; j < Rows<T, D>::kAhead; ++j) v[j] = rows.read_values(vc, vp, j);
+      if (!clean) {
+        const uint64_t seen = seen_keys(tiles.there(t, page[0], c), tiles.first(t) + 64 * c, p, a.window, a.sinks) >>
+                              (4 * (lane >> 5));
+        hide(s[0], (uint32_t)seen);
+        hide(s[1], (uint32_t)(seen >> 32));
       }
-      if (go) {
-        float16v s[TK / 32];
-        const int kp = fresh(first_key<D>()), vp = fresh(first_value<D>());
-        vec8<T> k[TK / 32][D / 16];
-#pragma unroll
-        for (int j = 0; j < TK / 32; ++j) rows.read_keys(keys[buf] + j * 32 * D * 2, kp, k[j]);
-#pragma unroll
-        for (int j = 0; j < TK / 32; ++j) s[j] = rows.scores(k[j]);
-        __builtin_amdgcn_sched_group_barrier(0x100, D / 16, 0);
-#pragma unroll
-        for (int j = 0; j < D / 16; ++j) {
-          __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
-          __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
-        }
-        __builtin_amdgcn_sched_group_barrier(0x008, D / 16, 0);
-        vec8<T> v[Rows<T, D>::kAhead];
-#pragma unroll
-        for (int j = 0; j < Rows<T, D>::kAhead; ++j) v[j] = rows.read_values(values[buf], vp, j);
-        if (masked) {
-          const uint64_t seen = seen_keys(held, tiles.first(t), p, a.window, a.sinks) >> (4 * (lane >> 5));
-          hide(s[0], (uint32_t)seen);
-          hide(s[1], (uint32_t)(seen >> 32));
-        }
-        float most = s[0][0];
-#pragma unroll
-        for (int j = 0; j < TK / 32; ++j)
-#pragma unroll
-          for (int r = 0; r < 16; ++r) most = fmaxf(most, s[j][r]);
-        rows.raise(pair_max(most) * a.scale2);
-#pragma unroll
-        for (int j = 0; j < TK / 32; ++j)
-#pragma unroll
-          for (int r = 0; r < 16; ++r) {
-            s[j][r] = __builtin_amdgcn_exp2f(fmaf(s[j][r], a.scale2, -rows.top));
-            rows.sum += s[j][r];
-          }
-        rows.add(values[buf], vp, s, v);
-      }
-      if (i + 1 < n) put(buf ^ 1, t + 1, page[1], kreg[(buf + 1) % S], vreg[(buf + 1) % S]);
-#pragma unroll
-      for (int j = 0; j <= S; ++j) page[j] = page[j + 1];
+      rows.template weigh<2>(s, a.scale2, w);
+      rows.template add<2>(vc, vp, w, v);
     };
 
 #pragma unroll
-    for (int i = 0; i <= S; ++i) page[i] = tiles.find(t0 + i);
-#pragma unroll
-    for (int i = 0; i < S; ++i) tiles.load(a, t0 + i, page[i], mine, kreg[i], vreg[i]);
+    for (int i = 0; i < 3; ++i) page[i] = tiles.find(t0 + i);
+    tiles.load(a, t0, page[0], mine, kreg, vreg);
     __syncthreads();  // the last unit's tiles are no longer read
-    put(0, t0, page[0], kreg[0], vreg[0]);
-    for (int i = 0; i < n; i += 2) {
-      step(i, Const<0>());
-      if (i + 1 < n) step(i + 1, Const<1>());
+    put(0, t0, page[0]);
+    tiles.load(a, t0 + 1, page[1], mine, kreg, vreg);
+    for (int i = 0; i < n; ++i) {
+      const int buf = i & 1, t = t0 + i;
+      __syncthreads();
+      const bool clean = tiles.clean(t, page[0]);
+#pragma unroll
+      for (int c = 0; c < TK / 64; ++c) {
+        const int k0 = tiles.first(t) + 64 * c;
+        if (busy && (clean || (k0 < tiles.end(t) && k0 <= tiles.p_last))) chunk(buf, c, clean, t);
+        if (c == 0 && i + 1 < n) {
+          put(buf ^ 1, t + 1, page[1]);
+          if (i + 2 < n) {
+            tiles.load(a, t + 2, page[2], mine, kreg, vreg);
+            page[3] = tiles.find(t + 3);
+          }
+        }
+      }
+#pragma unroll
+      for (int j = 0; j < 3; ++j) page[j] = page[j + 1];
     }
     store_rows<T, D>(a, phase, x, head, row, NW * 32, whole, (int64_t)id * 2 + (leading ? 0 : 1), rows);
     leading = false;
     left -= n;
     t0 = 0;
-    if (++e == ph.entries) {
-      e = 0;
-      ++head;
-    }
+    next_unit(ph, ph.entries * a.kv_heads, place, e, head);
   }
   if (lane == 0) a.work.odd[phase][id * NW + wave] = 0;
   if (odd) a.work.odd[phase][id * NW + wave] = 1;
@@ -855,7 +960,7 @@ __global__ __launch_bounds__(kWaves * 64, 2) void attend_wave(Args<T> a, int pha
   const int64_t all = ph.total * a.kv_heads;
   const int64_t beg = id * ph.share, stop = beg + ph.share < all ? beg + ph.share : all;
   const Start st = a.plan.start[phase][id];
-  int e = st.entry, head = st.head, t0 = st.tile;
+  int place = st.place, e = st.entry, head = st.head, t0 = st.tile;
   int64_t left = stop - beg;
   bool leading = true, odd = false;
   Rows<T, D> rows;
@@ -898,27 +1003,17 @@ __global__ __launch_bounds__(kWaves * 64, 2) void attend_wave(Args<T> a, int pha
 #pragma unroll
       for (int j = 0; j < Rows<T, D>::kAhead; ++j) v[j] = rows.read_values(values, vp, j);
       if (!clean) hide(s, (uint32_t)seen_keys(held, tiles.first(t), p, a.window, a.sinks) >> (4 * (lane >> 5)));
-      float most = s[0];
-#pragma unroll
-      for (int r = 1; r < 16; ++r) most = fmaxf(most, s[r]);
-      rows.raise(pair_max(most) * a.scale2);
-#pragma unroll
-      for (int r = 0; r < 16; ++r) {
-        s[r] = __builtin_amdgcn_exp2f(fmaf(s[r], a.scale2, -rows.top));
-        rows.sum += s[r];
-      }
-      const float16v w[1] = {s};
-      rows.add(values, vp, w, v);
+      const float16v one[1] = {s};
+      vec8<T> w[2];
+      rows.template weigh<1>(one, a.scale2, w);
+      rows.template add<1>(values, vp, w, v);
       __builtin_amdgcn_wave_barrier();
     }
     store_rows<T, D>(a, phase, x, head, row, kRowTile, whole, (int64_t)id * 2 + (leading ? 0 : 1), rows);
     leading = false;
     left -= n;
     t0 = 0;
-    if (++e == ph.entries) {
-      e = 0;
-      ++head;
-    }
+    next_unit(ph, ph.entries * a.kv_heads, place, e, head);
   }
   if (lane == 0) a.work.odd[phase][id] = 0;
   if (odd) a.work.odd[phase][id] = 1;
@@ -1109,12 +1204,16 @@ __global__ __launch_bounds__(256) void join_cuts(Args<T> a, int rows1, int flags
   const Start st = a.plan.start[1][w];
   if (st.tile > 0 && st.tile <= own.share) {
     const Entry x = a.plan.entry[1][st.entry];
-    const Cut u = cut_of(own, a.plan.cum[1], st.entry, st.head);
+    Cut u;
+    u.share = own.share;
+    u.c0 = w * own.share - st.tile;
+    u.w0 = u.c0 / u.share;
+    u.w1 = (u.c0 + x.tiles - 1) / u.share;
     join_rows<T, D>(a, x, u, st.head, row, step, rows1, rows1, any_odd(a, u, flags));
   }
   if (!any_odd(a, Cut{w, w, 0, 0}, flags)) return;
   const int64_t all = own.total * a.kv_heads, beg = w * own.share;
-  int e = st.entry, head = st.head, t = st.tile;
+  int place = st.place, e = st.entry, head = st.head, t = st.tile;
   for (int64_t left = (beg + own.share < all ? beg + own.share : all) - beg; left > 0;) {
     const Entry x = a.plan.entry[1][e];
     const int n = (int)(x.tiles - t < left ? x.tiles - t : left);
@@ -1125,10 +1224,7 @@ __global__ __launch_bounds__(256) void join_cuts(Args<T> a, int rows1, int flags
     }
     left -= n;
     t = 0;
-    if (++e == own.entries) {
-      e = 0;
-      ++head;
-    }
+    next_unit(own, own.entries * a.kv_heads, place, e, head);
   }
 }
 
@@ -1184,7 +1280,7 @@ hipError_t launch_attention_plan(const ewsjf_cache& c, const ewsjf_batch& b, con
                                  void* plan, hipStream_t stream) {
   const Shape s = shape_of(c, b);
   PlanArgs a{slot, q_start, group_start, shared, {s.rows[0], s.rows[1]}, {s.keys[0], s.keys[1]},
-             {s.workers[0], s.workers[1]}, s.G};
+             {s.workers[0], s.workers[1]}, s.G, s.columns};
   make_plan<<<1, kPlanThreads, 0, stream>>>(c, b, a, plan_of(s, plan));
   return hipGetLastError();
 }
