@@ -452,6 +452,29 @@ __device__ int fresh(int x) {
 __device__ uint32_t not_finite(uint32_t x, __bf16) { return ((x & 0x7f807f80u) + 0x00800080u) & 0x80008000u; }
 __device__ uint32_t not_finite(uint32_t x, _Float16) { return ((x & 0x7c007c00u) + 0x04000400u) & 0x80008000u; }
 
+// Global memory: a pointer read from memory does not say so by itself, and a
+// load that may be from LDS waits for LDS too.
+template <typename T>
+using Global = __attribute__((address_space(1))) T*;
+template <typename T>
+__device__ Global<T> global(T* p) {
+  return (Global<T>)p;
+}
+
+// What no kernel of the call writes: read by scalar loads where the index is the
+// wave's.
+template <typename T>
+__device__ T constant(const T* p) {
+  union {
+    T all;
+    uint32_t part[sizeof(T) / 4];
+  } r;
+  const auto* from = (const __attribute__((address_space(4))) uint32_t*)p;
+#pragma unroll
+  for (size_t i = 0; i < sizeof(T) / 4; ++i) r.part[i] = from[i];
+  return r.all;
+}
+
 // The unit after a worker's present one.
 __device__ void next_unit(const Phase& ph, int units, int& place, int& e, int& head) {
   ++place;
@@ -483,6 +506,15 @@ struct Args {
   Work work;
 };
 
+// The kernel's arguments, read again where they are used: kept in registers from
+// the start they would push the loops' own scalars out.
+template <typename T>
+__device__ const Args<T>& arguments() {
+  auto p = __builtin_amdgcn_kernarg_segment_ptr();
+  asm volatile("" : "+s"(p));
+  return *(const Args<T>*)p;
+}
+
 // The softmax state and output of 32 rows, one a lane pair.
 template <typename T, int D>
 struct Rows {
@@ -499,31 +531,38 @@ struct Rows {
       for (int j = 0; j < 16; ++j) o[i][j] = 0.f;
   }
 
-  // S^T of the 32 keys at `keys`; first: key_place of the lane's row and half.
-  __device__ void read_keys(const char* keys, int first, vec8<T> (&k)[D / 16]) const {
-#pragma unroll
-    for (int i = 0; i < D / 16; ++i) k[i] = *reinterpret_cast<const vec8<T>*>(keys + (first ^ (i << 5)));
+  // Keys of product k (32 keys k / (D / 16), dims k % (D / 16)) of a chunk;
+  // first: key_place of the lane's row and half.
+  static __device__ vec8<T> read_keys(const char* keys, int first, int k) {
+    return *reinterpret_cast<const vec8<T>*>(keys + k / (D / 16) * 32 * D * 2 + (first ^ (k % (D / 16) << 5)));
   }
-  __device__ float16v scores(const vec8<T> (&k)[D / 16]) const {
-    float16v s = {};
+  // S^T of 32 N keys.  Reads run kAhead products ahead (the order is kept by the
+  // barriers: left alone, each product waits for its own read).
+  static constexpr int kAhead = 4;
+  template <int N>
+  __device__ void scores(const char* keys, int first, float16v (&s)[N]) const {
+    vec8<T> k[kAhead];
 #pragma unroll
-    for (int i = 0; i < D / 16; ++i) s = mfma(k[i], q[i], s);
-    return s;
+    for (int j = 0; j < kAhead; ++j) k[j] = read_keys(keys, first, j);
+#pragma unroll
+    for (int j = 0; j < N; ++j) s[j] = float16v{};
+#pragma unroll
+    for (int j = 0; j < N * (D / 16); ++j) {
+      s[j / (D / 16)] = mfma(k[j % kAhead], q[j % (D / 16)], s[j / (D / 16)]);
+      if (j + kAhead < N * (D / 16)) k[j % kAhead] = read_keys(keys, first, j + kAhead);
+      __builtin_amdgcn_sched_barrier(0);
+    }
   }
 
-  // The running maximum moves up only when a score passes it by 8 binary
-  // orders: until then the weights stay below 2^8, which loses nothing, and
-  // the output need not be scaled.
+  // Raises the running maximum.
   __device__ void raise(float most) {
-    if (__any(most > top + 8.f)) {
-      const float now = fmaxf(top, most), shrink = __builtin_amdgcn_exp2f(top - now);
-      top = now;
-      sum *= shrink;
+    const float now = fmaxf(top, most), shrink = __builtin_amdgcn_exp2f(top - now);
+    top = now;
+    sum *= shrink;
 #pragma unroll
-      for (int i = 0; i < D / 32; ++i)
+    for (int i = 0; i < D / 32; ++i)
 #pragma unroll
-        for (int j = 0; j < 16; ++j) o[i][j] *= shrink;
-    }
+      for (int j = 0; j < 16; ++j) o[i][j] *= shrink;
   }
 
   // Weights of the scores s, rounded to 16 bits, their sum added to the row's.
@@ -573,10 +612,7 @@ struct Rows {
     return v.all;
   }
 
-  // O^T += V^T P^T over 32 N keys.  Reads run kAhead products ahead (the order
-  // is kept by the barriers: left alone, each product waits for its own read);
-  // v holds the first ones.
-  static constexpr int kAhead = 4;
+  // O^T += V^T P^T over 32 N keys; v holds the values of the first products.
   template <int N>
   __device__ void add(const char* values, int first, const vec8<T> (&w)[2 * N], vec8<T> (&v)[kAhead]) {
 #pragma unroll
@@ -623,10 +659,11 @@ __device__ void load_rows(const Args<T>& a, const Entry& x, int head, int row, v
   const int lane = threadIdx.x & 63;
   const bool there = row < x.rows;
   const int at = x.row0 + (there ? row : 0), token = at / a.G;
-  const T* p = a.q + (x.q0 + token) * a.q_token + (head * a.G + at - token * a.G) * a.q_head + 8 * (lane >> 5);
+  const Global<const T> p =
+      global(a.q) + (x.q0 + token) * a.q_token + (head * a.G + at - token * a.G) * a.q_head + 8 * (lane >> 5);
 #pragma unroll
   for (int k = 0; k < D / 16; ++k) {
-    q[k] = *reinterpret_cast<const vec8<T>*>(p + 16 * k);
+    q[k] = *(Global<const vec8<T>>)(p + 16 * k);
     if (!there)
 #pragma unroll
       for (int j = 0; j < 8; ++j) q[k][j] = (T)0.f;
@@ -644,7 +681,7 @@ __device__ void store_rows(const Args<T>& a, int phase, const Entry& x, int head
   const int64_t dense = (int64_t)(x.q0 + token) * (a.kv_heads * a.G) + head * a.G + at - token * a.G;
   if (whole && !a.join) {
     const float inv = sum > 0.f || sum != sum ? 1.f / sum : 0.f;
-    T* to = a.out + dense * D + 4 * h;
+    const Global<T> to = global(a.out) + dense * D + 4 * h;
 #pragma unroll
     for (int i = 0; i < D / 32; ++i)
 #pragma unroll
@@ -652,148 +689,205 @@ __device__ void store_rows(const Args<T>& a, int phase, const Entry& x, int head
         T v[4];
 #pragma unroll
         for (int d = 0; d < 4; ++d) v[d] = (T)(sum == 0.f ? 0.f : r.o[i][4 * j + d] * inv);
-        *reinterpret_cast<uint2*>(to + 32 * i + 8 * j) = *reinterpret_cast<const uint2*>(v);
+        *(Global<uint64_t>)(to + 32 * i + 8 * j) = *reinterpret_cast<const uint64_t*>(v);
       }
     if (h == 0)
-      a.lse[dense] = sum == 0.f ? -INFINITY : kLn2 * (r.top + __builtin_amdgcn_logf(sum));
+      global(a.lse)[dense] = sum == 0.f ? -INFINITY : kLn2 * (r.top + __builtin_amdgcn_logf(sum));
     return;
   }
   const Parts& w = a.work.part[phase];
   const int64_t at_row = whole ? dense : slot * tile_rows + row;
-  float* to = (whole ? w.whole_o : w.o) + at_row * D + 4 * h;
+  const Global<float> to = global(whole ? w.whole_o : w.o) + at_row * D + 4 * h;
+  typedef __attribute__((ext_vector_type(4))) float f4;
+  typedef __attribute__((ext_vector_type(2))) float f2;
 #pragma unroll
   for (int i = 0; i < D / 32; ++i)
 #pragma unroll
     for (int j = 0; j < 4; ++j)
-      *reinterpret_cast<float4*>(to + 32 * i + 8 * j) =
-          make_float4(r.o[i][4 * j], r.o[i][4 * j + 1], r.o[i][4 * j + 2], r.o[i][4 * j + 3]);
-  if (h == 0) (whole ? w.whole_ml : w.ml)[at_row] = make_float2(r.top, sum);
+      *(Global<f4>)(to + 32 * i + 8 * j) =
+          f4{r.o[i][4 * j], r.o[i][4 * j + 1], r.o[i][4 * j + 2], r.o[i][4 * j + 3]};
+  if (h == 0) *((Global<f2>)(whole ? w.whole_ml : w.ml) + at_row) = f2{r.top, sum};
+}
+
+// Keeps an address of the wave apart from the lane's places that are added to
+// it, so that loads take both as they are.
+__device__ Global<const char> apart(Global<const char> p) {
+  asm volatile("" : "+s"(p));
+  return p;
+}
+__device__ uint4 load_uint4(Global<const char> p) {
+  typedef __attribute__((ext_vector_type(4))) uint32_t u4;
+  const u4 x = *(Global<const u4>)p;
+  return make_uint4(x.x, x.y, x.z, x.w);
 }
 
 // The key tiles of a unit.  Tile t is keys [first(t), first(t) + TK), of which
-// those below end(t) count; the pages that hold them are looked up by find, one
-// register of the wave a tile.
+// those below end(t) count.
 //
 // Sixteens: pages have at least 16 tokens.  Tiles begin at multiples of 16, so
-// 16 keys lie in one page: lane i finds the page of keys [16 i', 16 i' + 16),
-// i' = i mod TK / 16, and a load's address is the wave's but for a constant of
-// the lane.  Otherwise lane i finds the page of key i.
+// each 16 keys lie in one page and are loaded from one address of the wave.
+// The pages of kBatch tiles are looked up at once, one lane a page: those of
+// the batch that the present tile is in and of the next one are held, even
+// batches' in one register and odd ones' in the other.
+// Otherwise every lane looks its key's page up before it loads.
 template <typename T, int D, int TK, bool Sixteens>
 struct Tiles {
   static constexpr int LPR = D / 8, KPI = 64 / LPR;  // lanes a key, keys a load
-  static constexpr int kGroup = 16 / KPI;            // loads of 16 keys
-  static constexpr bool turned = TK >= 64;
-  const int32_t* row;
-  const char* base;  // the key head's first key
+  static constexpr int kLoads = 16 / KPI;            // loads of 16 keys
+  static constexpr int kGroups = TK / 16, kBatch = 64 / kGroups;
+  Global<const int32_t> row;
+  Global<const char> base;  // the key head's first key
   int lo, hi, sink, nst, shift, pages;
-  int run, turn;     // tiles of the main run, and the one that it begins with
-  int c0, c1;        // every row sees every key of [c0, c1)
+  int c0, c1;        // in tiles [c0, c1) every row sees every key
   int p_first, p_last, window, sinks;
-  bool there_is;
-  uint32_t step[kGroup];  // a lane's place in the loads of 16 keys
+  uint32_t page_bytes, page_bytes_hi, token_bytes;
+  int64_t to_values;
+  uint32_t step;  // a lane's place in a load, and how far on the next load of 16 keys is
+  uint32_t stride;
+  int batch, evens, odds;
 
   __device__ Tiles(const Args<T>& a, const Entry& x, int head) {
     const int lane = threadIdx.x & 63;
-    row = a.table + (int64_t)(x.slot < 0 ? 0 : x.slot) * a.width;
-    base = reinterpret_cast<const char*>(a.data + head * a.head_stride);
-    lo = x.lo, hi = x.end, sink = x.sink, nst = (x.sink + TK - 1) / TK;
+    const bool there_is = x.slot >= 0;
+    row = global(a.table + (int64_t)(there_is ? x.slot : 0) * a.width);
+    base = global(reinterpret_cast<const char*>(a.data + head * a.head_stride));
+    lo = x.lo, hi = there_is ? x.end : 0, sink = there_is ? x.sink : 0;
+    nst = (x.sink + TK - 1) / TK;
     shift = a.page_shift, pages = a.n_pages, window = a.window, sinks = a.sinks;
-    there_is = x.slot >= 0;
     p_first = x.pos0 + x.row0 / a.G, p_last = x.pos0 + (x.row0 + x.rows - 1) / a.G;
-    const int below = p_first + 1 < hi ? p_first + 1 : hi;  // every row sees the keys before it,
+    const int below = p_first + 1 < hi ? p_first + 1 : hi;    // every row sees the keys before it,
     const int above = window > 0 ? p_last - window + 1 : lo;  // and those from it on
-    c0 = above > lo ? above : lo;
-    c1 = there_is ? below : 0;
-    // Row tiles that are worked on side by side have windows that differ by a few tiles.  Each begins its run with the
-    // tile whose number the run's length divides: then all read the same keys at the same time, out of L2.
-    run = x.tiles - nst;
-    turn = turned && window > 0 && run > 1 ? (run - lo / TK % run) % run : 0;
-#pragma unroll
-    for (int i = 0; i < kGroup; ++i)
-      step[i] = (uint32_t)((i * KPI + lane / LPR) * (int)a.token_stride + lane % LPR * 8) * 2;
+    c0 = nst + (above > lo ? (above - lo + TK - 1) / TK : 0);
+    c1 = nst + (below > lo ? (below - lo) / TK : 0);
+    const uint64_t bytes = 2 * a.page_stride;
+    page_bytes = (uint32_t)bytes, page_bytes_hi = (uint32_t)(bytes >> 32);
+    token_bytes = 2 * (uint32_t)a.token_stride;
+    to_values = 2 * a.kv_stride;
+    step = lane / LPR * token_bytes + lane % LPR * 16;
+    stride = KPI * token_bytes;
   }
 
-  __device__ int first(int t) const {
-    if (t < nst) return t * TK;
-    int i = t - nst + turn;
-    if (turned && i >= run) i -= run;
-    return lo + i * TK;
-  }
+  __device__ int first(int t) const { return t < nst ? t * TK : lo + (t - nst) * TK; }
   __device__ int end(int t) const { return t < nst ? sink : hi; }
-
-  __device__ int find(int t) const {
-    const int lane = threadIdx.x & 63;
-    return entry_of(t, first(t) + (Sixteens ? 16 * (lane % (TK / 16)) : lane % TK));
-  }
-  __device__ int find_key(int t, int from) const { return entry_of(t, first(t) + from + (threadIdx.x & 63)); }
+  __device__ bool held(int page) const { return (unsigned)page < (unsigned)pages; }
+  // The table's entry for a key of tile t (some entry, past the tile's end).
   __device__ int entry_of(int t, int key) const {
     const int kend = end(t);
-    const int in = key < kend ? key : kend > 0 ? kend - 1 : 0;
-    return row[in >> shift];  // judged where it is used: nothing waits for it here
+    return row[(key < kend ? key : kend > 0 ? kend - 1 : 0) >> shift];
   }
 
-  __device__ bool held(int page) const { return (unsigned)page < (unsigned)pages; }
-  // Every key is there, and every row sees it.
-  __device__ bool clean(int t, int page) const {
-    const int k0 = first(t);
-    if (!(t >= nst && k0 >= c0 && k0 + TK <= c1)) return false;
-    return __all(held(page)) && (Sixteens || TK <= 64 || __all(held(find_key(t, 64))));
+  __device__ int find(int b) const {
+    const int lane = threadIdx.x & 63, t = b * kBatch + lane / kGroups;
+    return entry_of(t, first(t) + 16 * (lane % kGroups));
   }
-  // Every row of positions [from, to] sees every key of the tile that is there.
-  __device__ bool even(int t, int from, int to) const {
+  __device__ void begin(int t) {
+    if (!Sixteens) return;
+    batch = t / kBatch;
+    evens = find(batch + batch % 2);
+    odds = find(batch + 1 - batch % 2);
+  }
+  __device__ void advance(int t) {
+    if (!Sixteens || t / kBatch == batch) return;
+    ++batch;
+    if (batch % 2) evens = find(batch + 1);
+    else odds = find(batch + 1);
+  }
+  // The lookup that tile t is in.  Branches, so that nothing waits for the next
+  // batch that does not need it: loads return in order, and the wait would be
+  // for all loads before it.
+  __device__ int lookup(int t) const {
+    int r;
+    if (t / kBatch % 2) {
+      r = odds;
+      asm volatile("" : "+v"(r));
+    } else {
+      r = evens;
+      asm volatile("" : "+v"(r));
+    }
+    return r;
+  }
+  __device__ int page_at(int t, int group) const {
+    return __builtin_amdgcn_readlane(lookup(t), t % kBatch * kGroups + group);
+  }
+
+  // Every key is there, and every row sees it.
+  __device__ bool clean(int t) const {
+    if (t < c0 || t >= c1) return false;
+    if (Sixteens) {
+      const uint64_t ok = __ballot(held(lookup(t)));
+      const uint32_t mask = (1u << kGroups) - 1;
+      return ((uint32_t)(ok >> (t % kBatch * kGroups)) & mask) == mask;
+    }
+    bool all = true;
+#pragma unroll
+    for (int c = 0; c < TK; c += 64) all = all && __all(held(entry_of(t, first(t) + c + (threadIdx.x & (TK < 64 ? 31 : 63)))));
+    return all;
+  }
+  // Every row sees every key of the tile that is there.
+  __device__ bool even(int t) const {
     const int k0 = first(t), k1 = k0 + TK < end(t) ? k0 + TK : end(t);
-    return k1 - 1 <= from && (window == 0 || k0 > to - window || k1 <= sinks);
+    return k1 - 1 <= p_first && (window == 0 || k0 > p_last - window || k1 <= sinks);
   }
 
   // Bits of the keys of chunk c (64 keys) that are there and that some row may
   // see.
-  __device__ uint64_t there(int t, int page, int c = 0) const {
+  __device__ uint64_t there(int t, int c = 0) const {
+    const int k0 = first(t) + 64 * c;
     uint64_t m = 0;
     if (Sixteens) {
 #pragma unroll
       for (int j = 0; j < (TK < 64 ? TK : 64) / 16; ++j)
-        if (held(__builtin_amdgcn_readlane(page, 4 * c + j))) m |= 0xffffull << (16 * j);
+        if (held(page_at(t, 4 * c + j))) m |= 0xffffull << (16 * j);
     } else {
-      m = __ballot(held(TK > 64 ? find_key(t, 64 * c) : page));
+      m = __ballot(held(entry_of(t, k0 + (threadIdx.x & 63))));
       if (TK == 32) m = (uint32_t)m;
     }
-    const int k0 = first(t) + 64 * c;
-    m &= there_is ? bits_below(end(t) - k0) : 0;
+    m &= bits_below(end(t) - k0);
     if (window > 0) m &= ~bits_below(p_first - window - k0 + 1) | bits_below(sinks - k0);
     return m;
   }
 
-  // Loads keys [key0, key0 + NI KPI) of the tile: 16 bytes a lane (page 0's
-  // where there is no page).
+  // Where 16 keys of a tile lie (page 0's where there is no page).
+  struct At {
+    Global<const char> k, v;
+  };
+  __device__ At address(int t, int key) const {
+    const int at = page_at(t, key / 16);
+    const uint32_t page = held(at) ? at : 0, in = (first(t) + key) & ((1 << shift) - 1);
+    const uint64_t off = (uint64_t)page * page_bytes + ((uint64_t)(page * page_bytes_hi) << 32) + in * token_bytes;
+    At r;
+    r.k = apart(base + off);
+    r.v = apart(r.k + to_values);
+    return r;
+  }
+
+  __device__ uint4 load16(Global<const char> p, int i) const {  // load i of 16 keys
+    return load_uint4(apart(p + i * stride) + step);
+  }
+
+  // Loads keys [key0, key0 + NI KPI) of the tile, key0 a multiple of 16: 16
+  // bytes a lane.
   template <int NI>
-  __device__ void load(const Args<T>& a, int t, int page, int key0, uint4 (&k)[NI], uint4 (&v)[NI]) const {
+  __device__ void load(int t, int key0, uint4 (&k)[NI], uint4 (&v)[NI]) const {
     const int lane = threadIdx.x & 63, mask = (1 << shift) - 1;
     if (Sixteens) {
-      constexpr int N = NI < kGroup ? NI : kGroup;
-      const int skip = key0 % 16 / KPI;  // a wave's first key lies inside 16 where it has fewer
 #pragma unroll
-      for (int g = 0; g < NI / N; ++g) {
-        const int key = key0 / 16 + g, at = __builtin_amdgcn_readlane(page, key);
-        const int in = (first(t) + 16 * key) & mask;
-        const char* p = base + 2 * ((held(at) ? at : 0) * a.page_stride + in * a.token_stride);
-        if (N < kGroup) p += 2 * (skip * KPI) * a.token_stride;
+      for (int g = 0; g < NI / kLoads; ++g) {
+        const At at = address(t, key0 + 16 * g);
 #pragma unroll
-        for (int i = 0; i < N; ++i) {
-          const uint32_t in_load = fresh(step[i]);  // the wave's address and the lane's place stay apart
-          k[g * N + i] = *reinterpret_cast<const uint4*>(p + in_load);
-          v[g * N + i] = *reinterpret_cast<const uint4*>(p + 2 * a.kv_stride + in_load);
+        for (int i = 0; i < kLoads; ++i) {
+          k[g * kLoads + i] = load16(at.k, i);
+          v[g * kLoads + i] = load16(at.v, i);
         }
       }
     } else {
 #pragma unroll
       for (int i = 0; i < NI; ++i) {
-        const int key = key0 + i * KPI + lane / LPR;
-        const int at = TK > 64 ? entry_of(t, first(t) + key) : __shfl(page, key);
-        const int in = (first(t) + key) & mask;
-        const char* p =
-            base + 2 * ((held(at) ? at : 0) * a.page_stride + in * a.token_stride + lane % LPR * 8);
-        k[i] = *reinterpret_cast<const uint4*>(p);
-        v[i] = *reinterpret_cast<const uint4*>(p + 2 * a.kv_stride);
+        const int key = first(t) + key0 + i * KPI + lane / LPR, at = entry_of(t, key);
+        const Global<const char> p = base + (held(at) ? at : 0) * (int64_t)((uint64_t)page_bytes_hi << 32 | page_bytes) +
+                                     (key & mask) * token_bytes + lane % LPR * 16;
+        k[i] = load_uint4(p);
+        v[i] = load_uint4(p + to_values);
       }
     }
   }
@@ -804,7 +898,8 @@ template <typename T, int D, int NI>
 __device__ void put_keys(char* keys, char* values, int key0, const uint4 (&k)[NI], const uint4 (&v)[NI]) {
   constexpr int LPR = D / 8, KPI = 64 / LPR;
   const int lane = threadIdx.x & 63, chunk = lane % LPR;
-  const int kp = key_place<D>(key0 + lane / LPR, chunk), vp = value_place<D>(key0 + lane / LPR, chunk * 16);
+  const int kp = fresh(key_place<D>(key0 + lane / LPR, chunk));
+  const int vp = fresh(value_place<D>(key0 + lane / LPR, chunk * 16));
 #pragma unroll
   for (int i = 0; i < NI; ++i) {
     // KPI keys on, a chunk's place in its row moves with the key
@@ -838,7 +933,7 @@ __device__ bool clear_keys(int key0, uint64_t there, uint4 (&k)[NI], uint4 (&v)[
 // that is loaded; one barrier a tile.
 // ---------------------------------------------------------------------------
 template <typename T, int D, int NW, bool Sixteens>
-__global__ __launch_bounds__(NW * 64, 2) void attend_block(Args<T> a, int phase) {
+__global__ __launch_bounds__(NW * 64, 2) void attend_block(Args<T>, int phase) {
   constexpr int TK = block_keys(NW);
   using Keys = Tiles<T, D, TK, Sixteens>;
   constexpr int NI = TK / NW / Keys::KPI, kChunk = 64 * D * 2;
@@ -846,100 +941,100 @@ __global__ __launch_bounds__(NW * 64, 2) void attend_block(Args<T> a, int phase)
   __shared__ __align__(16) char values[2][TK * D * 2];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int mine = wave * (TK / NW);  // the wave's first key of a tile
-  const Phase ph = a.plan.phase[phase];
-  // neighbouring shares of the line read the same keys: give them to one XCD
   const int id = blockIdx.x % 8 * (gridDim.x / 8) + blockIdx.x / 8;
-  if (id >= ph.workers) return;
-  const int64_t all = ph.total * a.kv_heads;
-  const int64_t beg = id * ph.share, stop = beg + ph.share < all ? beg + ph.share : all;
-  const Start st = a.plan.start[phase][id];
-  int place = st.place, e = st.entry, head = st.head, t0 = st.tile;
-  int64_t left = stop - beg;
+  int place, e, head, t0;
+  int64_t left;
+  {
+    const Args<T>& a = arguments<T>();
+    const Phase ph = constant(a.plan.phase + phase);
+    if (id >= ph.workers) return;
+    const int64_t all = ph.total * a.kv_heads, beg = id * ph.share;
+    left = (beg + ph.share < all ? beg + ph.share : all) - beg;
+    const Start st = constant(a.plan.start[phase] + id);
+    place = st.place, e = st.entry, head = st.head, t0 = st.tile;
+  }
+  const float scale2 = arguments<T>().scale2;
   bool leading = true, odd = false;
   Rows<T, D> rows;
 
   while (left > 0) {
-    const Entry x = a.plan.entry[phase][e];
+    const Args<T>& a = arguments<T>();
+    const Entry x = constant(a.plan.entry[phase] + e);
     const int n = (int)(x.tiles - t0 < left ? x.tiles - t0 : left);
-    const bool whole = t0 == 0 && n == x.tiles;
     const int row = wave * 32 + (lane & 31);
-    const bool busy = wave * 32 < x.rows;
-    const Keys tiles(a, x, head);
+    Keys tiles(a, x, head);
+    tiles.begin(t0);
     load_rows<T, D>(a, x, head, row, rows.q);
     rows.clear();
     const int p = x.pos0 + (x.row0 + (row < x.rows ? row : x.rows - 1)) / a.G;
 
+    const bool busy = wave * 32 < x.rows;  // the wave's rows are at positions w_first .. w_end
+    const int w_last = wave * 32 + 31 < x.rows ? wave * 32 + 31 : x.rows - 1;
+    const int w_first = x.pos0 + (x.row0 + wave * 32) / a.G, w_end = x.pos0 + (x.row0 + w_last) / a.G;
+
     uint4 kreg[NI], vreg[NI];
-    int page[4];  // of tiles i (in use) .. i + 3
-    auto put = [&](int buf, int t, int held) {
-      if (!tiles.clean(t, held)) {
-        const bool bad = clear_keys<T, D, NI>(mine % 64, tiles.there(t, held, mine / 64), kreg, vreg);
-        odd |= bad && !tiles.even(t, tiles.p_first, tiles.p_last);
-      }
-      put_keys<T, D, NI>(keys[buf], values[buf], mine, kreg, vreg);
+    auto clear = [&](int t) {
+      const bool bad = clear_keys<T, D, NI>(mine % 64, tiles.there(t, mine / 64), kreg, vreg);
+      odd |= bad && !tiles.even(t);
     };
     auto chunk = [&](int buf, int c, bool clean, int t) {
       float16v s[2];
       const int kp = fresh(first_key<D>()), vp = fresh(first_value<D>());
       const char* kc = keys[buf] + c * kChunk;
       const char* vc = values[buf] + c * kChunk;
-      vec8<T> k[2][D / 16], v[Rows<T, D>::kAhead], w[4];
-#pragma unroll
-      for (int j = 0; j < 2; ++j) rows.read_keys(kc + j * 32 * D * 2, kp, k[j]);
-#pragma unroll
-      for (int j = 0; j < 2; ++j) s[j] = rows.scores(k[j]);
-      __builtin_amdgcn_sched_group_barrier(0x100, D / 16, 0);
-#pragma unroll
-      for (int j = 0; j < D / 16; ++j) {
-        __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
-        __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
-      }
-      __builtin_amdgcn_sched_group_barrier(0x008, D / 16, 0);
+      vec8<T> v[Rows<T, D>::kAhead], w[4];
+      rows.template scores<2>(kc, kp, s);
 #pragma unroll
       for (int j = 0; j < Rows<T, D>::kAhead; ++j) v[j] = rows.read_values(vc, vp, j);
       if (!clean) {
-        const uint64_t seen = seen_keys(tiles.there(t, page[0], c), tiles.first(t) + 64 * c, p, a.window, a.sinks) >>
+        const uint64_t seen = seen_keys(tiles.there(t, c), tiles.first(t) + 64 * c, p, tiles.window, tiles.sinks) >>
                               (4 * (lane >> 5));
         hide(s[0], (uint32_t)seen);
         hide(s[1], (uint32_t)(seen >> 32));
       }
-      rows.template weigh<2>(s, a.scale2, w);
+      rows.template weigh<2>(s, scale2, w);
       rows.template add<2>(vc, vp, w, v);
     };
 
-#pragma unroll
-    for (int i = 0; i < 3; ++i) page[i] = tiles.find(t0 + i);
-    tiles.load(a, t0, page[0], mine, kreg, vreg);
+    bool clean = tiles.clean(t0), next = tiles.clean(t0 + 1);
+    tiles.load(t0, mine, kreg, vreg);
     __syncthreads();  // the last unit's tiles are no longer read
-    put(0, t0, page[0]);
-    tiles.load(a, t0 + 1, page[1], mine, kreg, vreg);
+    if (!clean) clear(t0);
+    put_keys<T, D, NI>(keys[0], values[0], mine, kreg, vreg);
+    tiles.load(t0 + 1, mine, kreg, vreg);
     for (int i = 0; i < n; ++i) {
-      const int buf = i & 1, t = t0 + i;
+      const int buf = i & 1, t = t0 + i, t2 = i + 2 < n ? t + 2 : t0 + n - 1;  // the last loads are of no use
+      // The pages are looked up before the tile's loads: what waits for a lookup then does not wait for them.
+      tiles.advance(t);
+      const bool third = tiles.clean(t + 2);
       __syncthreads();
-      const bool clean = tiles.clean(t, page[0]);
 #pragma unroll
       for (int c = 0; c < TK / 64; ++c) {
         const int k0 = tiles.first(t) + 64 * c;
-        if (busy && (clean || (k0 < tiles.end(t) && k0 <= tiles.p_last))) chunk(buf, c, clean, t);
-        if (c == 0 && i + 1 < n) {
-          put(buf ^ 1, t + 1, page[1]);
-          if (i + 2 < n) {
-            tiles.load(a, t + 2, page[2], mine, kreg, vreg);
-            page[3] = tiles.find(t + 3);
-          }
+        if (busy && (clean || (k0 < tiles.end(t) && k0 <= w_end &&
+                               (tiles.window == 0 || k0 + 63 > w_first - tiles.window || k0 < tiles.sinks))))
+          chunk(buf, c, clean, t);
+        if (c == 0) {
+          // no load in a branch: where the ways meet, the registers would be copied, and the copies would wait
+          if (!next) clear(t + 1);
+          put_keys<T, D, NI>(keys[buf ^ 1], values[buf ^ 1], mine, kreg, vreg);
+          tiles.load(t2, mine, kreg, vreg);
         }
       }
-#pragma unroll
-      for (int j = 0; j < 3; ++j) page[j] = page[j + 1];
+      clean = next, next = third;
     }
-    store_rows<T, D>(a, phase, x, head, row, NW * 32, whole, (int64_t)id * 2 + (leading ? 0 : 1), rows);
+    const Args<T>& z = arguments<T>();
+    const Entry y = constant(z.plan.entry[phase] + e);
+    store_rows<T, D>(z, phase, y, head, row, NW * 32, t0 == 0 && n == y.tiles, (int64_t)id * 2 + (leading ? 0 : 1), rows);
     leading = false;
     left -= n;
     t0 = 0;
-    next_unit(ph, ph.entries * a.kv_heads, place, e, head);
+    const Phase ph = constant(z.plan.phase + phase);
+    next_unit(ph, ph.entries * z.kv_heads, place, e, head);
   }
-  if (lane == 0) a.work.odd[phase][id * NW + wave] = 0;
-  if (odd) a.work.odd[phase][id * NW + wave] = 1;
+  const Global<int32_t> flags = global(arguments<T>().work.odd[phase]);
+  if (lane == 0) flags[id * NW + wave] = 0;
+  if (odd) flags[id * NW + wave] = 1;
 }
 
 // ---------------------------------------------------------------------------
@@ -947,76 +1042,79 @@ __global__ __launch_bounds__(NW * 64, 2) void attend_block(Args<T> a, int phase)
 // waves that share nothing.
 // ---------------------------------------------------------------------------
 template <typename T, int D, bool Sixteens>
-__global__ __launch_bounds__(kWaves * 64, 2) void attend_wave(Args<T> a, int phase) {
+__global__ __launch_bounds__(kWaves * 64, 2) void attend_wave(Args<T>, int phase) {
   using Keys = Tiles<T, D, kRowKeys, Sixteens>;
   constexpr int TK = kRowKeys, NI = TK / Keys::KPI;
   __shared__ __align__(16) char room[kWaves][2][TK * D * 2];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   char* keys = room[wave][0];
   char* values = room[wave][1];
-  const Phase ph = a.plan.phase[phase];
   const int id = (blockIdx.x % 8 * (gridDim.x / 8) + blockIdx.x / 8) * kWaves + wave;
-  if (id >= ph.workers) return;
-  const int64_t all = ph.total * a.kv_heads;
-  const int64_t beg = id * ph.share, stop = beg + ph.share < all ? beg + ph.share : all;
-  const Start st = a.plan.start[phase][id];
-  int place = st.place, e = st.entry, head = st.head, t0 = st.tile;
-  int64_t left = stop - beg;
+  int place, e, head, t0;
+  int64_t left;
+  {
+    const Args<T>& a = arguments<T>();
+    const Phase ph = constant(a.plan.phase + phase);
+    if (id >= ph.workers) return;
+    const int64_t all = ph.total * a.kv_heads, beg = id * ph.share;
+    left = (beg + ph.share < all ? beg + ph.share : all) - beg;
+    const Start st = constant(a.plan.start[phase] + id);
+    place = st.place, e = st.entry, head = st.head, t0 = st.tile;
+  }
+  const float scale2 = arguments<T>().scale2;
   bool leading = true, odd = false;
   Rows<T, D> rows;
 
   while (left > 0) {
-    const Entry x = a.plan.entry[phase][e];
+    const Args<T>& a = arguments<T>();
+    const Entry x = constant(a.plan.entry[phase] + e);
     const int n = (int)(x.tiles - t0 < left ? x.tiles - t0 : left);
-    const bool whole = t0 == 0 && n == x.tiles;
     const int row = lane & 31;
-    const Keys tiles(a, x, head);
+    Keys tiles(a, x, head);
+    tiles.begin(t0);
     load_rows<T, D>(a, x, head, row, rows.q);
     rows.clear();
     const int p = x.pos0 + (x.row0 + (row < x.rows ? row : x.rows - 1)) / a.G;
     uint4 kreg[NI], vreg[NI];
-    int page = tiles.find(t0);
-    tiles.load(a, t0, page, 0, kreg, vreg);
-    int page1 = tiles.find(t0 + 1);
+    tiles.load(t0, 0, kreg, vreg);
     for (int i = 0; i < n; ++i) {
       const int t = t0 + i;
-      const bool clean = tiles.clean(t, page);
+      const bool clean = tiles.clean(t);
       uint32_t held = ~0u;
       if (!clean) {
-        held = (uint32_t)tiles.there(t, page);
+        held = (uint32_t)tiles.there(t);
         const bool bad = clear_keys<T, D, NI>(0, held, kreg, vreg);
         // with one position, what is there is seen by all rows
-        odd |= bad && tiles.p_first != tiles.p_last && !tiles.even(t, tiles.p_first, tiles.p_last);
+        odd |= bad && tiles.p_first != tiles.p_last && !tiles.even(t);
       }
       put_keys<T, D, NI>(keys, values, 0, kreg, vreg);
-      page = page1;
-      if (i + 1 < n) {
-        tiles.load(a, t + 1, page, 0, kreg, vreg);
-        page1 = tiles.find(t + 2);
-      }
+      tiles.advance(t + 1);
+      if (i + 1 < n) tiles.load(t + 1, 0, kreg, vreg);
       __builtin_amdgcn_wave_barrier();
       const int kp = fresh(first_key<D>()), vp = fresh(first_value<D>());
-      vec8<T> k[D / 16];
-      rows.read_keys(keys, kp, k);
-      float16v s = rows.scores(k);
+      float16v s[1];
+      rows.template scores<1>(keys, kp, s);
       vec8<T> v[Rows<T, D>::kAhead];
 #pragma unroll
       for (int j = 0; j < Rows<T, D>::kAhead; ++j) v[j] = rows.read_values(values, vp, j);
-      if (!clean) hide(s, (uint32_t)seen_keys(held, tiles.first(t), p, a.window, a.sinks) >> (4 * (lane >> 5)));
-      const float16v one[1] = {s};
+      if (!clean) hide(s[0], (uint32_t)seen_keys(held, tiles.first(t), p, tiles.window, tiles.sinks) >> (4 * (lane >> 5)));
       vec8<T> w[2];
-      rows.template weigh<1>(one, a.scale2, w);
+      rows.template weigh<1>(s, scale2, w);
       rows.template add<1>(values, vp, w, v);
       __builtin_amdgcn_wave_barrier();
     }
-    store_rows<T, D>(a, phase, x, head, row, kRowTile, whole, (int64_t)id * 2 + (leading ? 0 : 1), rows);
+    const Args<T>& z = arguments<T>();
+    const Entry y = constant(z.plan.entry[phase] + e);
+    store_rows<T, D>(z, phase, y, head, row, kRowTile, t0 == 0 && n == y.tiles, (int64_t)id * 2 + (leading ? 0 : 1), rows);
     leading = false;
     left -= n;
     t0 = 0;
-    next_unit(ph, ph.entries * a.kv_heads, place, e, head);
+    const Phase ph = constant(z.plan.phase + phase);
+    next_unit(ph, ph.entries * z.kv_heads, place, e, head);
   }
-  if (lane == 0) a.work.odd[phase][id] = 0;
-  if (odd) a.work.odd[phase][id] = 1;
+  const Global<int32_t> flags = global(arguments<T>().work.odd[phase]);
+  if (lane == 0) flags[id] = 0;
+  if (odd) flags[id] = 1;
 }
 
 // ---------------------------------------------------------------------------
