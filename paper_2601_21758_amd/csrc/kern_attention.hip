@@ -103,6 +103,8 @@ struct Plan {
 };
 
 struct Shape {
+  bool groups;  // a shared prefix is a phase of its own
+  bool whole;   // a worker a unit: nothing is cut, nothing joined
   int G;
   int waves[2];  // of a workgroup that shares a unit's keys; 0: the wave kernel
   int rows[2], keys[2], workers[2], blocks[2];
@@ -114,8 +116,12 @@ struct Shape {
 Shape shape_of(const ewsjf_cache& c, const ewsjf_batch& b) {
   Shape s;
   s.G = b.q_heads / c.kv_heads;
+  const int64_t most_keys = (int64_t)c.width * c.page_size;  // of a sequence
+  // Below 16 MiB of keys and values in all, each sequence's read for itself, what sharing them saves is less than what
+  // its kernels cost (four sequences behind 288 tokens: one kernel of 7 us against three, 17 us).
+  s.groups = b.n_groups > 0 && 4 * most_keys * b.n_seqs * c.kv_heads * c.head_dim > (16 << 20);
   // rows that read the same keys: of a sequence, of a group on average
-  const int64_t most[2] = {b.n_groups > 0 ? b.total_q * s.G / b.n_groups : 0, (int64_t)b.max_q * s.G};
+  const int64_t most[2] = {s.groups ? b.total_q * s.G / b.n_groups : 0, (int64_t)b.max_q * s.G};
   for (int p = 0; p < 2; ++p) {
     s.waves[p] = most[p] <= kRowTile ? 0 : most[p] <= 128 ? 4 : 8;
     s.rows[p] = s.waves[p] ? 32 * s.waves[p] : kRowTile;
@@ -125,10 +131,19 @@ Shape shape_of(const ewsjf_cache& c, const ewsjf_batch& b) {
     s.workers[p] = s.waves[p] ? s.blocks[p] : s.blocks[p] * kWaves;
     s.entries[p] = b.total_q * s.G / s.rows[p] + (p ? b.n_seqs : b.n_groups);
   }
-  if (b.n_groups == 0) s.entries[0] = 0;
+  if (!s.groups) s.entries[0] = 0;
   s.kv_heads = c.kv_heads;
-  // rows that read the same keys as the next tile's: many row tiles of long runs, and nothing to join them with
-  s.columns = s.waves[1] && b.n_groups == 0 ? s.workers[1] / 8 : 0;
+  // One token a sequence, few keys: a wave takes a whole unit sooner than a join of its parts takes (16 tiles: 8 us).
+  // With one token, no row sees less of a unit than another, so no row is done again either.
+  const int64_t keys = b.window > 0 && (int64_t)b.window + b.sinks < most_keys ? (int64_t)b.window + b.sinks : most_keys;
+  s.whole = !s.groups && s.waves[1] == 0 && b.max_q == 1 && keys <= 16 * kRowKeys;
+  if (s.whole) {
+    const int64_t units = s.entries[1] * c.kv_heads;
+    s.blocks[1] = (int)((units + kWaves * 8 - 1) / (kWaves * 8) * 8);
+    s.workers[1] = s.blocks[1] * kWaves;
+  }
+  // many row tiles of long runs, and nothing to join them with
+  s.columns = s.waves[1] && !s.groups ? s.workers[1] / 8 : 0;
   return s;
 }
 
@@ -180,9 +195,9 @@ Work work_of(const ewsjf_cache& c, const ewsjf_batch& b, const Shape& s, void* b
   Carve at{static_cast<char*>(base)};
   Work w;
   for (int i = 0; i < 2; ++i) {
-    const bool used = i == 1 || b.n_groups > 0;
+    const bool used = i == 1 ? !s.whole : s.groups;
     const size_t rows = used ? (size_t)s.workers[i] * 2 * s.rows[i] : 0;
-    const size_t whole = b.n_groups > 0 ? (size_t)b.total_q * b.q_heads : 0;
+    const size_t whole = s.groups ? (size_t)b.total_q * b.q_heads : 0;
     w.part[i].o = at.take<float>(rows * c.head_dim);
     w.part[i].ml = at.take<float2>(rows);
     w.part[i].whole_o = at.take<float>(whole * c.head_dim);
@@ -198,6 +213,7 @@ Work work_of(const ewsjf_cache& c, const ewsjf_batch& b, const Shape& s, void* b
 // The plan
 // ---------------------------------------------------------------------------
 constexpr int kPlanThreads = 1024;
+constexpr int kLeast = 4;  // tiles a share has at least
 
 __device__ int64_t scan(int64_t v, int64_t* sums, int64_t& total) {  // exclusive over the workgroup
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
@@ -233,6 +249,7 @@ __device__ int last_at_most(const T* key, int n, int64_t v) {
 struct PlanArgs {
   const int32_t *slot, *q_start, *group_start, *shared;
   int rows[2], keys[2], workers[2], G, columns;
+  bool whole;
 };
 
 // One workgroup.  Everything read from the caller's arrays is bounded here, so
@@ -359,8 +376,10 @@ __global__ __launch_bounds__(kPlanThreads) void make_plan(ewsjf_cache c, ewsjf_b
       line += total;
     }
     const int64_t all = line * c.kv_heads;
-    const int64_t share = all > 0 ? (all + a.workers[ph] - 1) / a.workers[ph] : 1;
-    const int active = (int)((all + share - 1) / share);
+    // Shares below a few tiles are not worth the parts that they leave to join.  0: a worker a unit.
+    const int64_t even = (all + a.workers[ph] - 1) / a.workers[ph];
+    const int64_t share = ph && a.whole ? 0 : even < kLeast ? kLeast : even;
+    const int active = share ? (int)((all + share - 1) / share) : E * c.kv_heads;
     if (threadIdx.x == 0) {
       plan.cum[ph][E] = line;
       plan.phase[ph] = Phase{line, share, E, active, ph ? a.columns : 0, 0};
@@ -382,7 +401,9 @@ __global__ __launch_bounds__(kPlanThreads) void make_plan(ewsjf_cache c, ewsjf_b
     for (int w = threadIdx.x; w < active; w += kPlanThreads) {
       const int64_t at = w * share;
       int64_t place, rest;
-      if (ph && a.columns) {
+      if (share == 0) {
+        place = w, rest = 0;
+      } else if (ph && a.columns) {
         place = last_at_most(plan.line, (int)units, at);
         rest = at - plan.line[place];
       } else {
@@ -952,6 +973,7 @@ __global__ __launch_bounds__(NW * 64, 2) void attend_block(Args<T>, int phase) {
     left = (beg + ph.share < all ? beg + ph.share : all) - beg;
     const Start st = constant(a.plan.start[phase] + id);
     place = st.place, e = st.entry, head = st.head, t0 = st.tile;
+    if (ph.share == 0) left = constant(a.plan.entry[phase] + e).tiles;
   }
   const float scale2 = arguments<T>().scale2;
   bool leading = true, odd = false;
@@ -1060,6 +1082,7 @@ __global__ __launch_bounds__(kWaves * 64, 2) void attend_wave(Args<T>, int phase
     left = (beg + ph.share < all ? beg + ph.share : all) - beg;
     const Start st = constant(a.plan.start[phase] + id);
     place = st.place, e = st.entry, head = st.head, t0 = st.tile;
+    if (ph.share == 0) left = constant(a.plan.entry[phase] + e).tiles;
   }
   const float scale2 = arguments<T>().scale2;
   bool leading = true, odd = false;
@@ -1134,55 +1157,60 @@ __device__ Cut cut_of(const Phase& ph, const int64_t* cum, int entry, int head) 
   return u;
 }
 
-// The parts of one row, joined by one wave.  Lane i first takes the maximum and
-// sum of part i, so that all parts' weights are known at once and their outputs
-// can be loaded without waiting for one another.
+// The parts of a row, joined by 16 lanes, four rows a wave.  Lane i of them
+// first takes the maximum and sum of part i, so that all parts' weights are
+// known at once and their outputs are loaded without waiting for one another.
 template <int D>
 struct Joined {
-  static constexpr int W = D / 64;
+  static constexpr int W = D / 16;  // a lane's dims
   float top = kFloor, sum = 0.f, o[W] = {};
 
-  // from(i, o, ml): where part i's row lies.
+  // from(i, o, ml): where part i's row lies; 0 parts where there is no row.
   template <typename From>
   __device__ void take(int parts, From from) {
-    const int lane = threadIdx.x & 63;
-    for (int i0 = 0; i0 < parts; i0 += 64) {
-      const int n = parts - i0 < 64 ? parts - i0 : 64;
+    const int i16 = threadIdx.x & 15;
+    for (int i0 = 0; __any(i0 < parts); i0 += 16) {
+      const int n = parts - i0 < 16 ? parts - i0 : 16;
       const float* at = nullptr;
       float2 ml = make_float2(kFloor, 0.f);
-      if (lane < n) {
+      if (i16 < n) {
         const float2* m;
-        from(i0 + lane, at, m);
+        from(i0 + i16, at, m);
         ml = *m;
       }
       float now = fmaxf(top, ml.x);
-      for (int d = 32; d; d >>= 1) now = fmaxf(now, __shfl_xor(now, d));
+#pragma unroll
+      for (int d = 8; d; d >>= 1) now = fmaxf(now, __shfl_xor(now, d, 16));
       const float w = __builtin_amdgcn_exp2f(ml.x - now), shrink = __builtin_amdgcn_exp2f(top - now);
-      float add = lane < n ? ml.y * w : 0.f;
-      for (int d = 32; d; d >>= 1) add += __shfl_xor(add, d);
+      float add = i16 < n ? ml.y * w : 0.f;
+#pragma unroll
+      for (int d = 8; d; d >>= 1) add += __shfl_xor(add, d, 16);
       sum = sum * shrink + add;
       top = now;
 #pragma unroll
       for (int d = 0; d < W; ++d) o[d] *= shrink;
       const uint64_t addr = reinterpret_cast<uint64_t>(at);
       constexpr int kBatch = 4;
-      for (int i = 0; i < n; i += kBatch) {
-        float v[kBatch][W], wi[kBatch];
+      for (int i = 0; __any(i < n); i += kBatch) {
+        float4 v[kBatch][W / 4];
 #pragma unroll
         for (int j = 0; j < kBatch; ++j) {
-          const int k = i + j < n ? i + j : n - 1;
-          const uint32_t lo = __builtin_amdgcn_readlane((uint32_t)addr, k);
-          const uint32_t hi = __builtin_amdgcn_readlane((uint32_t)(addr >> 32), k);
-          const float* p = reinterpret_cast<const float*>((uint64_t)hi << 32 | lo);
+          const float4* p = reinterpret_cast<const float4*>(__shfl(addr, i + j, 16)) + i16 * (W / 4);
 #pragma unroll
-          for (int d = 0; d < W; ++d) v[j][d] = p[lane * W + d];
-          wi[j] = i + j < n ? __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(w), k)) : 0.f;
+          for (int d = 0; d < W / 4; ++d) v[j][d] = i + j < n ? p[d] : make_float4(0.f, 0.f, 0.f, 0.f);
         }
 #pragma unroll
-        for (int j = 0; j < kBatch; ++j)
+        for (int j = 0; j < kBatch; ++j) {
+          const float wi = __shfl(w, i + j, 16);
           if (i + j < n)
 #pragma unroll
-            for (int d = 0; d < W; ++d) o[d] = fmaf(v[j][d], wi[j], o[d]);
+            for (int d = 0; d < W / 4; ++d) {
+              o[4 * d] = fmaf(v[j][d].x, wi, o[4 * d]);
+              o[4 * d + 1] = fmaf(v[j][d].y, wi, o[4 * d + 1]);
+              o[4 * d + 2] = fmaf(v[j][d].z, wi, o[4 * d + 2]);
+              o[4 * d + 3] = fmaf(v[j][d].w, wi, o[4 * d + 3]);
+            }
+        }
       }
     }
   }
@@ -1236,37 +1264,44 @@ __device__ void redo_row(const Args<T>& a, const Entry& x, int head, int row, fl
   for (int d = 0; d < D / 64; ++d) a.out[dense * D + lane * (D / 64) + d] = (T)(sum == 0.f ? 0.f : o[d] / sum);
 }
 
-// Joins the rows of a unit of the sequences' own keys that this wave has: every
-// `step`th from `row` on.
+// Joins the rows of a unit of the sequences' own keys that this wave has: four
+// from `row` on, then `step` on.
 template <typename T, int D>
 __device__ void join_rows(const Args<T>& a, const Entry& x, const Cut& u, int head, int row, int step, int rows0,
                           int rows1, bool odd) {
-  const int lane = threadIdx.x & 63;
+  const int lane = threadIdx.x & 63, i16 = lane & 15;
+  constexpr int W = Joined<D>::W;
   for (; row < x.rows; row += step) {
-    const int at = x.row0 + row, token = at / a.G;
+    const int mine = row + lane / 16;
+    const bool there = mine < x.rows;
+    const int at = x.row0 + (there ? mine : row), token = at / a.G;
     const int64_t dense = (int64_t)(x.q0 + token) * (a.kv_heads * a.G) + head * a.G + at - token * a.G;
     Cut u0 = {};
     int before = 0, row0 = 0;
     if (x.prefix >= 0) {
-      row0 = x.prefix_row + row;
+      row0 = x.prefix_row + (there ? mine : row);
       u0 = cut_of(a.plan.phase[0], a.plan.cum[0], x.prefix + row0 / rows0, head);
       row0 %= rows0;
       before = (int)(u0.w1 - u0.w0) + 1;
     }
     Joined<D> r;
-    r.take(before + (int)(u.w1 - u.w0) + 1, [&](int i, const float*& o, const float2*& ml) {
+    r.take(there ? before + (int)(u.w1 - u.w0) + 1 : 0, [&](int i, const float*& o, const float2*& ml) {
       if (i < before) part_at(a.work.part[0], u0, i, rows0, row0, dense, D, o, ml);
-      else part_at(a.work.part[1], u, i - before, rows1, row, dense, D, o, ml);
+      else part_at(a.work.part[1], u, i - before, rows1, mine, dense, D, o, ml);
     });
     const float inv = r.sum == 0.f ? 0.f : 1.f / r.sum;
-    T v[D / 64];
-#pragma unroll
-    for (int i = 0; i < D / 64; ++i) v[i] = (T)(r.sum == 0.f ? 0.f : r.o[i] * inv);
-#pragma unroll
-    for (int i = 0; i < D / 64; ++i) a.out[dense * D + lane * (D / 64) + i] = v[i];
     const float lse2 = r.sum == 0.f ? -INFINITY : r.top + __builtin_amdgcn_logf(r.sum);
-    if (lane == 0) a.lse[dense] = kLn2 * lse2;
-    if (odd) redo_row<T, D>(a, x, head, row, lse2);
+    if (there) {
+      vec8<T> v = {};
+#pragma unroll
+      for (int i = 0; i < W; ++i) v[i] = (T)(r.sum == 0.f ? 0.f : r.o[i] * inv);
+      T* to = a.out + dense * D + i16 * W;
+      if (W == 8) *reinterpret_cast<uint4*>(to) = *reinterpret_cast<const uint4*>(&v);
+      else *reinterpret_cast<uint2*>(to) = *reinterpret_cast<const uint2*>(&v);
+      if (i16 == 0) a.lse[dense] = kLn2 * lse2;
+    }
+    for (int i = 0; odd && i < 4 && row + i < x.rows; ++i)
+      redo_row<T, D>(a, x, head, row + i, __shfl(lse2, 16 * i));
   }
 }
 
@@ -1288,7 +1323,7 @@ __global__ __launch_bounds__(256) void join_units(Args<T> a, int rows0, int rows
   if (e >= own.entries) return;
   const Entry x = a.plan.entry[1][e];
   const Cut u = cut_of(own, a.plan.cum[1], e, head);
-  join_rows<T, D>(a, x, u, head, blockIdx.z * 4 + wave, gridDim.z * 4, rows0, rows1, any_odd(a, u, flags));
+  join_rows<T, D>(a, x, u, head, (blockIdx.z * 4 + wave) * 4, gridDim.z * 16, rows0, rows1, any_odd(a, u, flags));
 }
 
 // Otherwise only the units that are cut: the worker whose share begins inside a
@@ -1296,7 +1331,7 @@ __global__ __launch_bounds__(256) void join_units(Args<T> a, int rows0, int rows
 // finite also does its whole units' rows again.
 template <typename T, int D>
 __global__ __launch_bounds__(256) void join_cuts(Args<T> a, int rows1, int flags) {
-  const int w = blockIdx.x, row = blockIdx.z * 4 + (threadIdx.x >> 6), step = gridDim.z * 4;
+  const int w = blockIdx.x, row = (blockIdx.z * 4 + (threadIdx.x >> 6)) * 4, step = gridDim.z * 16;
   const Phase own = a.plan.phase[1];
   if (w >= own.workers) return;
   const Start st = a.plan.start[1][w];
@@ -1315,7 +1350,7 @@ __global__ __launch_bounds__(256) void join_cuts(Args<T> a, int rows1, int flags
   for (int64_t left = (beg + own.share < all ? beg + own.share : all) - beg; left > 0;) {
     const Entry x = a.plan.entry[1][e];
     const int n = (int)(x.tiles - t < left ? x.tiles - t : left);
-    for (int r = row; n == x.tiles && r < x.rows; r += step) {
+    for (int r = row / 4; n == x.tiles && r < x.rows; r += step / 4) {
       const int at = x.row0 + r, token = at / a.G;
       const int64_t dense = (int64_t)(x.q0 + token) * (a.kv_heads * a.G) + head * a.G + at - token * a.G;
       redo_row<T, D>(a, x, head, r, a.lse[dense] * kLog2e);
@@ -1342,18 +1377,19 @@ hipError_t launch_typed(const ewsjf_cache& c, const ewsjf_batch& b, int32_t laye
   a.n_pages = c.n_pages, a.page_shift = __builtin_ctz(c.page_size), a.width = c.width, a.kv_heads = c.kv_heads;
   a.G = s.G, a.window = b.window, a.sinks = b.sinks;
   a.scale2 = scale * kLog2e;
-  a.join = b.n_groups > 0;
+  a.join = s.groups;
   a.plan = plan_of(s, const_cast<void*>(plan));
   a.work = work_of(c, b, s, ws);
   a.lse = lse != nullptr ? lse : a.work.lse;
   const bool sixteens = c.page_size >= 16;
-  for (int p = b.n_groups > 0 ? 0 : 1; p < 2; ++p) {
+  for (int p = s.groups ? 0 : 1; p < 2; ++p) {
     auto kernel = s.waves[p] == 8 ? (sixteens ? attend_block<T, D, 8, true> : attend_block<T, D, 8, false>)
                   : s.waves[p]    ? (sixteens ? attend_block<T, D, 4, true> : attend_block<T, D, 4, false>)
                                   : (sixteens ? attend_wave<T, D, true> : attend_wave<T, D, false>);
     kernel<<<s.blocks[p], 64 * (s.waves[p] ? s.waves[p] : kWaves), 0, stream>>>(a, p);
   }
-  // four rows a wave at most
+  if (s.whole) return hipGetLastError();
+  // four rows a wave, at once
   const int64_t most = (int64_t)b.max_q * s.G < s.rows[1] ? (int64_t)b.max_q * s.G : s.rows[1];
   const unsigned z = (unsigned)((most + 15) / 16);
   const int flags = s.waves[1] ? s.waves[1] : 1;
@@ -1378,8 +1414,10 @@ hipError_t launch_attention_plan(const ewsjf_cache& c, const ewsjf_batch& b, con
                                  void* plan, hipStream_t stream) {
   const Shape s = shape_of(c, b);
   PlanArgs a{slot, q_start, group_start, shared, {s.rows[0], s.rows[1]}, {s.keys[0], s.keys[1]},
-             {s.workers[0], s.workers[1]}, s.G, s.columns};
-  make_plan<<<1, kPlanThreads, 0, stream>>>(c, b, a, plan_of(s, plan));
+             {s.workers[0], s.workers[1]}, s.G, s.columns, s.whole};
+  ewsjf_batch batch = b;
+  if (!s.groups) batch.n_groups = 0;
+  make_plan<<<1, kPlanThreads, 0, stream>>>(c, batch, a, plan_of(s, plan));
   return hipGetLastError();
 }
 

@@ -12,6 +12,11 @@ namespace {
 constexpr int kThreads = 256;
 constexpr int kChunk = 4096;  // pages ranked by one workgroup
 constexpr int kMaxReq = EWSJF_MAX_CACHE_BATCH;
+// One workgroup ranks the pages of a pool up to this size in less time than a
+// second launch takes (65,536 pages: 256 KiB of counts).
+constexpr int kSmallPool = 65536;
+constexpr int kSmallThreads = 1024;
+constexpr int kFewRequests = 64;  // and writes the rows of so many requests itself
 
 // Workspace: counts of the chunks, the requests' running needs, the pages
 // picked for them; for a compaction the two ends of each move and, per moved
@@ -58,6 +63,7 @@ __device__ int wave_scan(int v) {  // inclusive over the 64 lanes
 }
 
 // Exclusive prefix sum over the workgroup; total gets the sum.
+template <int kThreads = ewsjf::kThreads>
 __device__ int block_scan(int v, int* sums, int& total) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int inc = wave_scan(v);
@@ -82,24 +88,12 @@ __device__ int held(const ewsjf_cache& c, int slot) {
   return n < 0 ? 0 : n;
 }
 
-// Workgroups 0 .. chunks - 1 count their chunk's free (or used) pages; the
-// last one checks the requests and sums what they need.
-__global__ __launch_bounds__(kThreads) void count_pages(ewsjf_cache c, CacheWs w, int chunks, bool used,
-                                                        const int32_t* parent, const int32_t* slot,
-                                                        const int32_t* tokens, int n) {
-  __shared__ int sums[kThreads / 64];
-  if ((int)blockIdx.x < chunks) {
-    int mine = 0;
-    const int64_t base = (int64_t)blockIdx.x * kChunk;
-    for (int i = threadIdx.x; i < kChunk; i += kThreads)
-      if (base + i < c.n_pages) mine += (c.refs[base + i] != 0) == used;
-    int total;
-    block_scan(mine, sums, total);
-    if (threadIdx.x == 0) w.counts[blockIdx.x] = total;
-    return;
-  }
+// Checks the requests and sums what they need; the sum of all is returned.
+template <int N>
+__device__ int sum_needs(const ewsjf_cache& c, const CacheWs& w, int* sums, const int32_t* parent,
+                         const int32_t* slot, const int32_t* tokens, int n) {
   int run = 0;
-  for (int i0 = 0; i0 < n; i0 += kThreads) {
+  for (int i0 = 0; i0 < n; i0 += N) {
     const int i = i0 + threadIdx.x;
     int need = 0, ok = 0;
     if (i < n) {
@@ -124,13 +118,33 @@ __global__ __launch_bounds__(kThreads) void count_pages(ewsjf_cache c, CacheWs w
       }
     }
     int total;
-    const int before = block_scan(need, sums, total);
+    const int before = block_scan<N>(need, sums, total);
     if (i < n) {
       w.cum[i] = run + before + need;
       w.fine[i] = ok;
     }
     run += total;
   }
+  return run;
+}
+
+// Workgroups 0 .. chunks - 1 count their chunk's free (or used) pages; the
+// last one checks the requests and sums what they need.
+__global__ __launch_bounds__(kThreads) void count_pages(ewsjf_cache c, CacheWs w, int chunks, bool used,
+                                                        const int32_t* parent, const int32_t* slot,
+                                                        const int32_t* tokens, int n) {
+  __shared__ int sums[kThreads / 64];
+  if ((int)blockIdx.x < chunks) {
+    int mine = 0;
+    const int64_t base = (int64_t)blockIdx.x * kChunk;
+    for (int i = threadIdx.x; i < kChunk; i += kThreads)
+      if (base + i < c.n_pages) mine += (c.refs[base + i] != 0) == used;
+    int total;
+    block_scan(mine, sums, total);
+    if (threadIdx.x == 0) w.counts[blockIdx.x] = total;
+    return;
+  }
+  sum_needs<kThreads>(c, w, sums, parent, slot, tokens, n);
 }
 
 // Chunk sums before this workgroup's and in all.
@@ -173,46 +187,98 @@ __global__ __launch_bounds__(kThreads) void pick_pages(ewsjf_cache c, CacheWs w,
   }
 }
 
+// Writes request i's grant and row, and a fork's length, with threads `at`, `at`
+// + step, ..; true if it is granted.  For new tokens the caller writes the
+// length (grown), once all threads have read it.
+__device__ bool write_row(const ewsjf_cache& c, const CacheWs& w, int free, const int32_t* parent, const int32_t* slot,
+                          const int32_t* tokens, int32_t* granted, int i, int at, int step) {
+  const int after = w.cum[i], first = i ? w.cum[i - 1] : 0;
+  const bool ok = w.fine[i] && after <= free;
+  if (at == 0) granted[i] = ok;
+  if (!ok) return false;
+  const int s = slot[i], t = tokens[i];
+  int32_t* row = c.table + (int64_t)s * c.width;
+  if (parent == nullptr) {
+    const int64_t have = held(c, s);
+    const int from = pages_of(c, have);
+    for (int j = at; j < after - first && from + j < c.width; j += step) row[from + j] = w.picked[first + j];
+    return true;
+  }
+  const int32_t* from = c.table + (int64_t)parent[i] * c.width;
+  const int full = t / c.page_size;
+  for (int j = at; j < full; j += step) {
+    const int p = from[j];
+    row[j] = p;
+    if (in_pool(c, p)) atomicAdd(&c.refs[p], 1);
+  }
+  if (at == 0) {
+    if (t % c.page_size) row[full] = after > first ? w.picked[first] : -1;
+    c.length[s] = t;
+  }
+  return true;
+}
+
+__device__ void grown(const ewsjf_cache& c, int slot, int tokens) { c.length[slot] = held(c, slot) + tokens; }
+
 // Request blockIdx.x: plane 0's workgroup writes its row, length and grant; for
 // a fork each plane's (layer and keys or values) copies the partial page.
 __global__ __launch_bounds__(kThreads) void apply_growth(ewsjf_cache c, CacheWs w, const int32_t* parent,
                                                          const int32_t* slot, const int32_t* tokens,
                                                          int32_t* granted) {
-  const int i = blockIdx.x, plane = blockIdx.y;
-  const int after = w.cum[i], first = i ? w.cum[i - 1] : 0;
-  const bool ok = w.fine[i] && after <= w.head[0];
-  if (plane == 0 && threadIdx.x == 0) granted[i] = ok;
-  if (!ok) return;
-  const int s = slot[i], t = tokens[i];
-  int32_t* row = c.table + (int64_t)s * c.width;
+  const int i = blockIdx.x, plane = blockIdx.y, free = w.head[0];
+  if (plane == 0 && !write_row(c, w, free, parent, slot, tokens, granted, i, threadIdx.x, kThreads)) return;
   if (parent == nullptr) {
-    const int64_t have = held(c, s);
-    const int at = pages_of(c, have);
-    for (int j = threadIdx.x; j < after - first && at + j < c.width; j += kThreads) row[at + j] = w.picked[first + j];
     __syncthreads();
-    if (threadIdx.x == 0) c.length[s] = (int)(have + t);
+    if (threadIdx.x == 0) grown(c, slot[i], tokens[i]);
     return;
   }
-  const int32_t* from = c.table + (int64_t)parent[i] * c.width;
-  const int full = t / c.page_size;
-  if (plane == 0) {
-    for (int j = threadIdx.x; j < full; j += kThreads) {
-      const int p = from[j];
-      row[j] = p;
-      if (in_pool(c, p)) atomicAdd(&c.refs[p], 1);
+  const int after = w.cum[i], first = i ? w.cum[i - 1] : 0;
+  if (!w.fine[i] || after > free || after == first) return;
+  const int src = c.table[(int64_t)parent[i] * c.width + tokens[i] / c.page_size];
+  if (!in_pool(c, src)) return;
+  uint16_t* data = static_cast<uint16_t*>(c.data) + plane / 2 * c.layer_stride + plane % 2 * c.kv_stride;
+  const uint4* a = reinterpret_cast<const uint4*>(data + src * c.page_stride);
+  uint4* b = reinterpret_cast<uint4*>(data + w.picked[first] * c.page_stride);
+  const int vecs = c.kv_heads * c.page_size * c.head_dim / 8;
+  for (int j = threadIdx.x; j < vecs; j += kThreads) b[j] = a[j];
+}
+
+// count_pages and pick_pages of a small pool; for few requests of new tokens
+// their rows too.
+__global__ __launch_bounds__(kSmallThreads) void grow_small(ewsjf_cache c, CacheWs w, const int32_t* parent,
+                                                            const int32_t* slot, const int32_t* tokens, int n,
+                                                            int32_t* granted, bool rows) {
+  __shared__ int sums[kSmallThreads / 64];
+  __shared__ int top;
+  sum_needs<kSmallThreads>(c, w, sums, parent, slot, tokens, n);
+  // a thread's pages lie together: one scan ranks them all
+  const int each = (c.n_pages + kSmallThreads - 1) / kSmallThreads;
+  const int64_t from = (int64_t)threadIdx.x * each, end = from + each < c.n_pages ? from + each : c.n_pages;
+  int mine = 0;
+  for (int64_t p = from; p < end; ++p) mine += c.refs[p] == 0;
+  int free;
+  int rank = block_scan<kSmallThreads>(mine, sums, free);
+  if (threadIdx.x == 0) top = 0;
+  __syncthreads();
+  int most = 0;
+  for (int i = threadIdx.x; i < n; i += kSmallThreads)
+    if (w.cum[i] <= free) most = w.cum[i] > most ? w.cum[i] : most;
+  atomicMax(&top, most);
+  __syncthreads();
+  for (int64_t p = from; p < end && rank < top; ++p)
+    if (c.refs[p] == 0) {
+      w.picked[rank++] = (int)p;
+      c.refs[p] = 1;
     }
-    if (threadIdx.x == 0) {
-      if (t % c.page_size) row[full] = after > first ? w.picked[first] : -1;
-      c.length[s] = t;
+  if (threadIdx.x == 0) w.head[0] = free;
+  if (!rows) return;
+  __syncthreads();
+  for (int i0 = 0; i0 < n; i0 += kSmallThreads / 64) {  // a wave a request
+    const int i = i0 + threadIdx.x / 64, lane = threadIdx.x & 63;
+    if (i < n && write_row(c, w, free, parent, slot, tokens, granted, i, lane, 64)) {
+      __builtin_amdgcn_wave_barrier();
+      if (lane == 0) grown(c, slot[i], tokens[i]);
     }
-  }
-  if (after > first && in_pool(c, from[full])) {
-    const int64_t off = plane / 2 * c.layer_stride + plane % 2 * c.kv_stride;
-    const uint16_t* data = static_cast<const uint16_t*>(c.data) + off;
-    const uint4* a = reinterpret_cast<const uint4*>(data + from[full] * c.page_stride);
-    uint4* b = reinterpret_cast<uint4*>(const_cast<uint16_t*>(data) + w.picked[first] * c.page_stride);
-    const int vecs = c.kv_heads * c.page_size * c.head_dim / 8;
-    for (int j = threadIdx.x; j < vecs; j += kThreads) b[j] = a[j];
   }
 }
 
@@ -347,8 +413,14 @@ hipError_t launch_cache_grow(const ewsjf_cache& c, const int32_t* parent, const 
   if (n == 0) return hipSuccess;
   const CacheWs w = cache_ws(c, ws);
   const int chunks = (c.n_pages + kChunk - 1) / kChunk;
-  count_pages<<<chunks + 1, kThreads, 0, stream>>>(c, w, chunks, false, parent, slot, tokens, n);
-  pick_pages<<<chunks, kThreads, 0, stream>>>(c, w, chunks, n);
+  if (c.n_pages <= kSmallPool) {
+    const bool rows = parent == nullptr && n <= kFewRequests;
+    grow_small<<<1, kSmallThreads, 0, stream>>>(c, w, parent, slot, tokens, n, granted, rows);
+    if (rows) return hipGetLastError();
+  } else {
+    count_pages<<<chunks + 1, kThreads, 0, stream>>>(c, w, chunks, false, parent, slot, tokens, n);
+    pick_pages<<<chunks, kThreads, 0, stream>>>(c, w, chunks, n);
+  }
   apply_growth<<<dim3(n, parent ? 2 * c.layers : 1), kThreads, 0, stream>>>(c, w, parent, slot, tokens, granted);
   return hipGetLastError();
 }
