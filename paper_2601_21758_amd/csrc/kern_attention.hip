@@ -35,6 +35,8 @@ constexpr int kRowKeys = 32;     // its key tile
 __host__ __device__ constexpr int block_keys(int waves) { return waves == 8 ? 128 : 64; }
 constexpr int kWaves = 4;        // waves of a workgroup of the wave kernel
 constexpr int kCUs = 256;
+constexpr int kWholeKeys = 1024;   // of a unit that one workgroup takes whole,
+constexpr int kWholeUnits = 2048;  // in a batch of so many
 constexpr float kFloor = -3e38f;   // running maximum of a row that has seen no key
 constexpr float kLn2 = 0.6931471805599453f;
 constexpr float kLog2e = 1.4426950408889634f;
@@ -133,15 +135,12 @@ Shape shape_of(const ewsjf_cache& c, const ewsjf_batch& b) {
   }
   if (!s.groups) s.entries[0] = 0;
   s.kv_heads = c.kv_heads;
-  // One token a sequence, few keys: a wave takes a whole unit sooner than a join of its parts takes (16 tiles: 8 us).
-  // With one token, no row sees less of a unit than another, so no row is done again either.
+  // One token a sequence and few keys: a workgroup takes a unit sooner than a second kernel joins its parts.  With one
+  // token, no row sees less of a unit than another, so no row is done again either.
   const int64_t keys = b.window > 0 && (int64_t)b.window + b.sinks < most_keys ? (int64_t)b.window + b.sinks : most_keys;
-  s.whole = !s.groups && s.waves[1] == 0 && b.max_q == 1 && keys <= 16 * kRowKeys;
-  if (s.whole) {
-    const int64_t units = s.entries[1] * c.kv_heads;
-    s.blocks[1] = (int)((units + kWaves * 8 - 1) / (kWaves * 8) * 8);
-    s.workers[1] = s.blocks[1] * kWaves;
-  }
+  const int64_t units = s.entries[1] * c.kv_heads;
+  s.whole = !s.groups && s.waves[1] == 0 && b.max_q == 1 && keys <= kWholeKeys && units <= kWholeUnits;
+  if (s.whole) s.workers[1] = s.blocks[1] = (int)((units + 7) / 8 * 8);
   // many row tiles of long runs, and nothing to join them with
   s.columns = s.waves[1] && !s.groups ? s.workers[1] / 8 : 0;
   return s;
@@ -1062,8 +1061,11 @@ __global__ __launch_bounds__(NW * 64, 2) void attend_block(Args<T>, int phase) {
 // ---------------------------------------------------------------------------
 // The wave kernel: up to 32 rows (a few query tokens), the keys streamed by
 // waves that share nothing.
+//
+// Split: a workgroup takes one unit, a quarter of its tiles a wave, and joins
+// the four parts itself.
 // ---------------------------------------------------------------------------
-template <typename T, int D, bool Sixteens>
+template <typename T, int D, bool Sixteens, bool Split>
 __global__ __launch_bounds__(kWaves * 64, 2) void attend_wave(Args<T>, int phase) {
   using Keys = Tiles<T, D, kRowKeys, Sixteens>;
   constexpr int TK = kRowKeys, NI = TK / Keys::KPI;
@@ -1071,7 +1073,7 @@ __global__ __launch_bounds__(kWaves * 64, 2) void attend_wave(Args<T>, int phase
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   char* keys = room[wave][0];
   char* values = room[wave][1];
-  const int id = (blockIdx.x % 8 * (gridDim.x / 8) + blockIdx.x / 8) * kWaves + wave;
+  const int block = blockIdx.x % 8 * (gridDim.x / 8) + blockIdx.x / 8, id = Split ? block : block * kWaves + wave;
   int place, e, head, t0;
   int64_t left;
   {
@@ -1082,12 +1084,18 @@ __global__ __launch_bounds__(kWaves * 64, 2) void attend_wave(Args<T>, int phase
     left = (beg + ph.share < all ? beg + ph.share : all) - beg;
     const Start st = constant(a.plan.start[phase] + id);
     place = st.place, e = st.entry, head = st.head, t0 = st.tile;
-    if (ph.share == 0) left = constant(a.plan.entry[phase] + e).tiles;
+    if (Split) {
+      const int tiles = constant(a.plan.entry[phase] + e).tiles, part = (tiles + kWaves - 1) / kWaves;
+      t0 = wave * part;
+      left = tiles - t0 < part ? tiles - t0 : part;
+      if (left < 0) left = 0;
+    }
   }
   const float scale2 = arguments<T>().scale2;
   bool leading = true, odd = false;
   Rows<T, D> rows;
 
+  if (Split) rows.clear();
   while (left > 0) {
     const Args<T>& a = arguments<T>();
     const Entry x = constant(a.plan.entry[phase] + e);
@@ -1126,6 +1134,7 @@ __global__ __launch_bounds__(kWaves * 64, 2) void attend_wave(Args<T>, int phase
       rows.template add<1>(values, vp, w, v);
       __builtin_amdgcn_wave_barrier();
     }
+    if (Split) break;
     const Args<T>& z = arguments<T>();
     const Entry y = constant(z.plan.entry[phase] + e);
     store_rows<T, D>(z, phase, y, head, row, kRowTile, t0 == 0 && n == y.tiles, (int64_t)id * 2 + (leading ? 0 : 1), rows);
@@ -1135,9 +1144,53 @@ __global__ __launch_bounds__(kWaves * 64, 2) void attend_wave(Args<T>, int phase
     const Phase ph = constant(z.plan.phase + phase);
     next_unit(ph, ph.entries * z.kv_heads, place, e, head);
   }
-  const Global<int32_t> flags = global(arguments<T>().work.odd[phase]);
-  if (lane == 0) flags[id] = 0;
-  if (odd) flags[id] = 1;
+  if (!Split) {
+    const Global<int32_t> flags = global(arguments<T>().work.odd[phase]);
+    if (lane == 0) flags[id] = 0;
+    if (odd) flags[id] = 1;
+    return;
+  }
+  __shared__ float2 ml[kWaves][kRowTile];
+  const Args<T>& a = arguments<T>();
+  const Entry x = constant(a.plan.entry[phase] + e);
+  const int row = lane & 31, h = lane >> 5;
+  const float sum = pair_sum(rows.sum);
+  if (row < x.rows) {
+    float* to = reinterpret_cast<float*>(room[wave]) + row * D + 4 * h;  // the tiles have been read
+#pragma unroll
+    for (int i = 0; i < D / 32; ++i)
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+        *reinterpret_cast<float4*>(to + 32 * i + 8 * j) = make_float4(
+            rows.o[i][4 * j], rows.o[i][4 * j + 1], rows.o[i][4 * j + 2], rows.o[i][4 * j + 3]);
+    if (h == 0) ml[wave][row] = make_float2(rows.top, sum);
+  }
+  __syncthreads();
+  constexpr int W = D / 16;
+  const int i16 = threadIdx.x & 15;
+  for (int r = threadIdx.x / 16; r < x.rows; r += kWaves * 4) {
+    float top = kFloor, all = 0.f, o[W] = {};
+#pragma unroll
+    for (int i = 0; i < kWaves; ++i) top = fmaxf(top, ml[i][r].x);
+#pragma unroll
+    for (int i = 0; i < kWaves; ++i) {
+      const float w = __builtin_amdgcn_exp2f(ml[i][r].x - top);
+      all = fmaf(ml[i][r].y, w, all);
+      const float* from = reinterpret_cast<const float*>(room[i]) + r * D + i16 * W;
+#pragma unroll
+      for (int d = 0; d < W; ++d) o[d] = fmaf(from[d], w, o[d]);
+    }
+    const int at = x.row0 + r, token = at / a.G;
+    const int64_t dense = (int64_t)(x.q0 + token) * (a.kv_heads * a.G) + head * a.G + at - token * a.G;
+    const float inv = all == 0.f ? 0.f : 1.f / all;
+    vec8<T> v = {};
+#pragma unroll
+    for (int d = 0; d < W; ++d) v[d] = (T)(all == 0.f ? 0.f : o[d] * inv);
+    const Global<T> to = global(a.out) + dense * D + i16 * W;
+    if (W == 8) *(Global<vec8<T>>)to = v;
+    else *(Global<uint64_t>)to = *reinterpret_cast<const uint64_t*>(&v);
+    if (i16 == 0) global(a.lse)[dense] = all == 0.f ? -INFINITY : kLn2 * (top + __builtin_amdgcn_logf(all));
+  }
 }
 
 // ---------------------------------------------------------------------------
@@ -1385,7 +1438,8 @@ hipError_t launch_typed(const ewsjf_cache& c, const ewsjf_batch& b, int32_t laye
   for (int p = s.groups ? 0 : 1; p < 2; ++p) {
     auto kernel = s.waves[p] == 8 ? (sixteens ? attend_block<T, D, 8, true> : attend_block<T, D, 8, false>)
                   : s.waves[p]    ? (sixteens ? attend_block<T, D, 4, true> : attend_block<T, D, 4, false>)
-                                  : (sixteens ? attend_wave<T, D, true> : attend_wave<T, D, false>);
+                  : s.whole && p  ? (sixteens ? attend_wave<T, D, true, true> : attend_wave<T, D, false, true>)
+                                  : (sixteens ? attend_wave<T, D, true, false> : attend_wave<T, D, false, false>);
     kernel<<<s.blocks[p], 64 * (s.waves[p] ? s.waves[p] : kWaves), 0, stream>>>(a, p);
   }
   if (s.whole) return hipGetLastError();
