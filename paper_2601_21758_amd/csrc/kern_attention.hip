@@ -35,6 +35,7 @@ constexpr int kRowKeys = 32;     // its key tile
 __host__ __device__ constexpr int block_keys(int waves) { return waves == 8 ? 128 : 64; }
 constexpr int kWaves = 4;        // waves of a workgroup of the wave kernel
 constexpr int kCUs = 256;
+constexpr int64_t kMostJoins = 1 << 24;  // waves of a grid's row: a launch has below 2^32 threads in one
 constexpr int kWholeKeys = 1024;   // of a unit that one workgroup takes whole,
 constexpr int kWholeUnits = 2048;  // in a batch of so many
 constexpr float kFloor = -3e38f;   // running maximum of a row that has seen no key
@@ -107,6 +108,7 @@ struct Plan {
 struct Shape {
   bool groups;  // a shared prefix is a phase of its own
   bool whole;   // a worker a unit: nothing is cut, nothing joined
+  bool both;    // both phases in one kernel
   int G;
   int waves[2];  // of a workgroup that shares a unit's keys; 0: the wave kernel
   int rows[2], keys[2], workers[2], blocks[2];
@@ -124,12 +126,18 @@ Shape shape_of(const ewsjf_cache& c, const ewsjf_batch& b) {
   s.groups = b.n_groups > 0 && 4 * most_keys * b.n_seqs * c.kv_heads * c.head_dim > (16 << 20);
   // rows that read the same keys: of a sequence, of a group on average
   const int64_t most[2] = {s.groups ? b.total_q * s.G / b.n_groups : 0, (int64_t)b.max_q * s.G};
+  // One kernel for both phases, half of each CU to either, up to 100 GFLOP against shared keys: 64 sequences behind 2048
+  // tokens took 59 us, as two kernels 71; 512 behind 4096, 109 against 143, behind 8192 (69 GFLOP) 158 against 174.
+  // Beyond, a kernel with all of each CU and tiles of 256 rows makes up for the second one: 512 behind 16,123
+  // (135 GFLOP) took 263 us, in one kernel 270.
+  const double flops = 4. * b.total_q * b.q_heads * c.head_dim * most_keys;
+  s.both = most[0] > kRowTile && most[1] <= kRowTile && flops < 100e9;
   for (int p = 0; p < 2; ++p) {
-    s.waves[p] = most[p] <= kRowTile ? 0 : most[p] <= 128 ? 4 : 8;
+    s.waves[p] = most[p] <= kRowTile ? 0 : most[p] <= 128 || s.both ? 4 : 8;
     s.rows[p] = s.waves[p] ? 32 * s.waves[p] : kRowTile;
     s.keys[p] = s.waves[p] ? block_keys(s.waves[p]) : kRowKeys;
     // as many as fit the chip at once: eight waves of 256 registers a CU
-    s.blocks[p] = s.waves[p] == 8 ? kCUs : 2 * kCUs;
+    s.blocks[p] = s.waves[p] == 8 || s.both ? kCUs : 2 * kCUs;
     s.workers[p] = s.waves[p] ? s.blocks[p] : s.blocks[p] * kWaves;
     s.entries[p] = b.total_q * s.G / s.rows[p] + (p ? b.n_seqs : b.n_groups);
   }
@@ -212,7 +220,6 @@ Work work_of(const ewsjf_cache& c, const ewsjf_batch& b, const Shape& s, void* b
 // The plan
 // ---------------------------------------------------------------------------
 constexpr int kPlanThreads = 1024;
-constexpr int kLeast = 4;  // tiles a share has at least
 
 __device__ int64_t scan(int64_t v, int64_t* sums, int64_t& total) {  // exclusive over the workgroup
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
@@ -375,9 +382,8 @@ __global__ __launch_bounds__(kPlanThreads) void make_plan(ewsjf_cache c, ewsjf_b
       line += total;
     }
     const int64_t all = line * c.kv_heads;
-    // Shares below a few tiles are not worth the parts that they leave to join.  0: a worker a unit.
-    const int64_t even = (all + a.workers[ph] - 1) / a.workers[ph];
-    const int64_t share = ph && a.whole ? 0 : even < kLeast ? kLeast : even;
+    // 0: a worker a unit
+    const int64_t share = ph && a.whole ? 0 : all > 0 ? (all + a.workers[ph] - 1) / a.workers[ph] : 1;
     const int active = share ? (int)((all + share - 1) / share) : E * c.kv_heads;
     if (threadIdx.x == 0) {
       plan.cum[ph][E] = line;
@@ -952,16 +958,19 @@ __device__ bool clear_keys(int key0, uint64_t there, uint4 (&k)[NI], uint4 (&v)[
 // next one goes from registers to the other half of LDS and the one after
 // that is loaded; one barrier a tile.
 // ---------------------------------------------------------------------------
+template <int D, int NW>
+constexpr int kBlockRoom = 2 * 2 * block_keys(NW) * D * 2;  // LDS: two tiles' keys and values
+
 template <typename T, int D, int NW, bool Sixteens>
-__global__ __launch_bounds__(NW * 64, 2) void attend_block(Args<T>, int phase) {
+__device__ __forceinline__ void block_units(char* room, int phase, int block, int blocks) {
   constexpr int TK = block_keys(NW);
   using Keys = Tiles<T, D, TK, Sixteens>;
-  constexpr int NI = TK / NW / Keys::KPI, kChunk = 64 * D * 2;
-  __shared__ __align__(16) char keys[2][TK * D * 2];
-  __shared__ __align__(16) char values[2][TK * D * 2];
+  constexpr int NI = TK / NW / Keys::KPI, kChunk = 64 * D * 2, kTile = TK * D * 2;
+  char* const keys = room;
+  char* const values = room + 2 * kTile;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int mine = wave * (TK / NW);  // the wave's first key of a tile
-  const int id = blockIdx.x % 8 * (gridDim.x / 8) + blockIdx.x / 8;
+  const int id = block % 8 * (blocks / 8) + block / 8;
   int place, e, head, t0;
   int64_t left;
   {
@@ -1001,8 +1010,8 @@ __global__ __launch_bounds__(NW * 64, 2) void attend_block(Args<T>, int phase) {
     auto chunk = [&](int buf, int c, bool clean, int t) {
       float16v s[2];
       const int kp = fresh(first_key<D>()), vp = fresh(first_value<D>());
-      const char* kc = keys[buf] + c * kChunk;
-      const char* vc = values[buf] + c * kChunk;
+      const char* kc = keys + buf * kTile + c * kChunk;
+      const char* vc = values + buf * kTile + c * kChunk;
       vec8<T> v[Rows<T, D>::kAhead], w[4];
       rows.template scores<2>(kc, kp, s);
 #pragma unroll
@@ -1021,7 +1030,7 @@ __global__ __launch_bounds__(NW * 64, 2) void attend_block(Args<T>, int phase) {
     tiles.load(t0, mine, kreg, vreg);
     __syncthreads();  // the last unit's tiles are no longer read
     if (!clean) clear(t0);
-    put_keys<T, D, NI>(keys[0], values[0], mine, kreg, vreg);
+    put_keys<T, D, NI>(keys, values, mine, kreg, vreg);
     tiles.load(t0 + 1, mine, kreg, vreg);
     for (int i = 0; i < n; ++i) {
       const int buf = i & 1, t = t0 + i, t2 = i + 2 < n ? t + 2 : t0 + n - 1;  // the last loads are of no use
@@ -1038,7 +1047,7 @@ __global__ __launch_bounds__(NW * 64, 2) void attend_block(Args<T>, int phase) {
         if (c == 0) {
           // no load in a branch: where the ways meet, the registers would be copied, and the copies would wait
           if (!next) clear(t + 1);
-          put_keys<T, D, NI>(keys[buf ^ 1], values[buf ^ 1], mine, kreg, vreg);
+          put_keys<T, D, NI>(keys + (buf ^ 1) * kTile, values + (buf ^ 1) * kTile, mine, kreg, vreg);
           tiles.load(t2, mine, kreg, vreg);
         }
       }
@@ -1058,6 +1067,12 @@ __global__ __launch_bounds__(NW * 64, 2) void attend_block(Args<T>, int phase) {
   if (odd) flags[id * NW + wave] = 1;
 }
 
+template <typename T, int D, int NW, bool Sixteens>
+__global__ __launch_bounds__(NW * 64, 2) void attend_block(Args<T>, int phase) {
+  __shared__ __align__(16) char room[kBlockRoom<D, NW>];
+  block_units<T, D, NW, Sixteens>(room, phase, blockIdx.x, gridDim.x);
+}
+
 // ---------------------------------------------------------------------------
 // The wave kernel: up to 32 rows (a few query tokens), the keys streamed by
 // waves that share nothing.
@@ -1065,15 +1080,17 @@ __global__ __launch_bounds__(NW * 64, 2) void attend_block(Args<T>, int phase) {
 // Split: a workgroup takes one unit, a quarter of its tiles a wave, and joins
 // the four parts itself.
 // ---------------------------------------------------------------------------
+template <int D>
+constexpr int kWaveRoom = 2 * kRowKeys * D * 2;  // LDS of a wave: a tile's keys and values
+
 template <typename T, int D, bool Sixteens, bool Split>
-__global__ __launch_bounds__(kWaves * 64, 2) void attend_wave(Args<T>, int phase) {
+__device__ __forceinline__ void wave_units(char* room, int phase, int block, int blocks) {
   using Keys = Tiles<T, D, kRowKeys, Sixteens>;
   constexpr int TK = kRowKeys, NI = TK / Keys::KPI;
-  __shared__ __align__(16) char room[kWaves][2][TK * D * 2];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  char* keys = room[wave][0];
-  char* values = room[wave][1];
-  const int block = blockIdx.x % 8 * (gridDim.x / 8) + blockIdx.x / 8, id = Split ? block : block * kWaves + wave;
+  char* const keys = room + wave * kWaveRoom<D>;
+  char* const values = keys + TK * D * 2;
+  const int at_line = block % 8 * (blocks / 8) + block / 8, id = Split ? at_line : at_line * kWaves + wave;
   int place, e, head, t0;
   int64_t left;
   {
@@ -1156,7 +1173,7 @@ __global__ __launch_bounds__(kWaves * 64, 2) void attend_wave(Args<T>, int phase
   const int row = lane & 31, h = lane >> 5;
   const float sum = pair_sum(rows.sum);
   if (row < x.rows) {
-    float* to = reinterpret_cast<float*>(room[wave]) + row * D + 4 * h;  // the tiles have been read
+    float* to = reinterpret_cast<float*>(keys) + row * D + 4 * h;  // the tiles have been read
 #pragma unroll
     for (int i = 0; i < D / 32; ++i)
 #pragma unroll
@@ -1176,7 +1193,7 @@ __global__ __launch_bounds__(kWaves * 64, 2) void attend_wave(Args<T>, int phase
     for (int i = 0; i < kWaves; ++i) {
       const float w = __builtin_amdgcn_exp2f(ml[i][r].x - top);
       all = fmaf(ml[i][r].y, w, all);
-      const float* from = reinterpret_cast<const float*>(room[i]) + r * D + i16 * W;
+      const float* from = reinterpret_cast<const float*>(room + i * kWaveRoom<D>) + r * D + i16 * W;
 #pragma unroll
       for (int d = 0; d < W; ++d) o[d] = fmaf(from[d], w, o[d]);
     }
@@ -1191,6 +1208,26 @@ __global__ __launch_bounds__(kWaves * 64, 2) void attend_wave(Args<T>, int phase
     else *(Global<uint64_t>)to = *reinterpret_cast<const uint64_t*>(&v);
     if (i16 == 0) global(a.lse)[dense] = all == 0.f ? -INFINITY : kLn2 * (top + __builtin_amdgcn_logf(all));
   }
+}
+
+template <typename T, int D, bool Sixteens, bool Split>
+__global__ __launch_bounds__(kWaves * 64, 2) void attend_wave(Args<T>, int phase) {
+  __shared__ __align__(16) char room[kWaves * kWaveRoom<D>];
+  wave_units<T, D, Sixteens, Split>(room, phase, blockIdx.x, gridDim.x);
+}
+
+// Both phases of a batch behind shared prefixes at once: on each CU one
+// workgroup has the shared keys, where the matrix unit is the limit, and one
+// streams sequences' own keys, where memory is.
+template <typename T, int D, bool Sixteens>
+__global__ __launch_bounds__(kWaves * 64, 2) void attend_both(Args<T>) {
+  static_assert(kBlockRoom<D, 4> == kWaves * kWaveRoom<D>, "one room serves either");
+  __shared__ __align__(16) char room[kBlockRoom<D, 4>];
+  // Eight by eight, so that each XCD has both, and the other way round from the XCD's 33rd on, which join its first 32
+  // on their CUs.
+  const int block = blockIdx.x / 16 * 8 + blockIdx.x % 8;
+  if ((blockIdx.x / 8 + blockIdx.x / 256) % 2 == 0) block_units<T, D, 4, Sixteens>(room, 0, block, gridDim.x / 2);
+  else wave_units<T, D, Sixteens, false>(room, 1, block, gridDim.x / 2);
 }
 
 // ---------------------------------------------------------------------------
@@ -1358,33 +1395,35 @@ __device__ void join_rows(const Args<T>& a, const Entry& x, const Cut& u, int he
   }
 }
 
-// Whether a worker of the cut met values that are not finite (the workgroup
-// together).
+// Whether a worker of the cut met values that are not finite.
 template <typename T>
 __device__ bool any_odd(const Args<T>& a, const Cut& u, int flags) {
   int odd = 0;
-  for (int64_t w = u.w0 * flags + threadIdx.x; w < (u.w1 + 1) * flags; w += blockDim.x) odd |= a.work.odd[1][w];
-  return __syncthreads_or(odd);
+  for (int64_t w = u.w0 * flags + (threadIdx.x & 63); w < (u.w1 + 1) * flags; w += 64) odd |= a.work.odd[1][w];
+  return __any(odd);
 }
 
-// With a shared prefix every row is joined: a workgroup takes a unit, or a part
-// of its rows (blockIdx.z).
+// With a shared prefix every row is joined: `fours` waves take a unit of key
+// head blockIdx.y, four rows each.
 template <typename T, int D>
-__global__ __launch_bounds__(256) void join_units(Args<T> a, int rows0, int rows1, int flags) {
-  const int e = blockIdx.x, head = blockIdx.y, wave = threadIdx.x >> 6;
+__global__ __launch_bounds__(256) void join_units(Args<T> a, int rows0, int rows1, int flags, int fours) {
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), head = blockIdx.y;
   const Phase own = a.plan.phase[1];
-  if (e >= own.entries) return;
-  const Entry x = a.plan.entry[1][e];
-  const Cut u = cut_of(own, a.plan.cum[1], e, head);
-  join_rows<T, D>(a, x, u, head, (blockIdx.z * 4 + wave) * 4, gridDim.z * 16, rows0, rows1, any_odd(a, u, flags));
+  for (int id = blockIdx.x * 4 + wave; id < own.entries * fours; id += gridDim.x * 4) {
+    const int e = id / fours;
+    const Entry x = a.plan.entry[1][e];
+    const Cut u = cut_of(own, a.plan.cum[1], e, head);
+    join_rows<T, D>(a, x, u, head, (id - e * fours) * 4, fours * 4, rows0, rows1, any_odd(a, u, flags));
+  }
 }
 
 // Otherwise only the units that are cut: the worker whose share begins inside a
 // unit, as the first one to, joins it.  A worker that met values that are not
 // finite also does its whole units' rows again.
 template <typename T, int D>
-__global__ __launch_bounds__(256) void join_cuts(Args<T> a, int rows1, int flags) {
-  const int w = blockIdx.x, row = (blockIdx.z * 4 + (threadIdx.x >> 6)) * 4, step = gridDim.z * 16;
+__global__ __launch_bounds__(256) void join_cuts(Args<T> a, int rows1, int flags, int fours) {
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), id = blockIdx.x * 4 + wave, w = id / fours;
+  const int row = (id - w * fours) * 4, step = fours * 4;
   const Phase own = a.plan.phase[1];
   if (w >= own.workers) return;
   const Start st = a.plan.start[1][w];
@@ -1435,7 +1474,11 @@ hipError_t launch_typed(const ewsjf_cache& c, const ewsjf_batch& b, int32_t laye
   a.work = work_of(c, b, s, ws);
   a.lse = lse != nullptr ? lse : a.work.lse;
   const bool sixteens = c.page_size >= 16;
-  for (int p = s.groups ? 0 : 1; p < 2; ++p) {
+  if (s.both) {
+    auto kernel = sixteens ? attend_both<T, D, true> : attend_both<T, D, false>;
+    kernel<<<s.blocks[0] + s.blocks[1], kWaves * 64, 0, stream>>>(a);
+  }
+  for (int p = s.groups ? 0 : 1; p < 2 && !s.both; ++p) {
     auto kernel = s.waves[p] == 8 ? (sixteens ? attend_block<T, D, 8, true> : attend_block<T, D, 8, false>)
                   : s.waves[p]    ? (sixteens ? attend_block<T, D, 4, true> : attend_block<T, D, 4, false>)
                   : s.whole && p  ? (sixteens ? attend_wave<T, D, true, true> : attend_wave<T, D, false, true>)
@@ -1443,14 +1486,12 @@ hipError_t launch_typed(const ewsjf_cache& c, const ewsjf_batch& b, int32_t laye
     kernel<<<s.blocks[p], 64 * (s.waves[p] ? s.waves[p] : kWaves), 0, stream>>>(a, p);
   }
   if (s.whole) return hipGetLastError();
-  // four rows a wave, at once
   const int64_t most = (int64_t)b.max_q * s.G < s.rows[1] ? (int64_t)b.max_q * s.G : s.rows[1];
-  const unsigned z = (unsigned)((most + 15) / 16);
-  const int flags = s.waves[1] ? s.waves[1] : 1;
-  if (a.join)
-    join_units<T, D><<<dim3((unsigned)s.entries[1], c.kv_heads, z), 256, 0, stream>>>(a, s.rows[0], s.rows[1], flags);
-  else
-    join_cuts<T, D><<<dim3(s.workers[1], 1, z), 256, 0, stream>>>(a, s.rows[1], flags);
+  const int fours = (int)((most + 3) / 4), flags = s.waves[1] ? s.waves[1] : 1;
+  const int64_t waves = (a.join ? s.entries[1] : s.workers[1]) * fours;
+  const unsigned grid = (unsigned)(waves < kMostJoins ? (waves + 3) / 4 : kMostJoins / 4);
+  if (a.join) join_units<T, D><<<dim3(grid, c.kv_heads), 256, 0, stream>>>(a, s.rows[0], s.rows[1], flags, fours);
+  else join_cuts<T, D><<<grid, 256, 0, stream>>>(a, s.rows[1], flags, fours);
   return hipGetLastError();
 }
 

@@ -30,9 +30,9 @@ def _addr(struct) -> int:
     return C.addressof(struct)
 
 
-def _strides(t: torch.Tensor) -> list[int]:
-    """Strides in elements, 0 for a dim of size 1 (torch leaves any value there)."""
-    return [s if n > 1 else 0 for n, s in zip(t.shape, t.stride())]
+def _stride(t: torch.Tensor, dim: int) -> int:
+    """Stride in elements, 0 for a dim of size 1 (torch leaves any value there)."""
+    return t.stride(dim) if t.shape[dim] > 1 else 0
 
 
 def _new(stream, *args, dtype: torch.dtype, device) -> torch.Tensor:
@@ -73,8 +73,8 @@ class PagedCache:
         if any(t.device != data.device for t in (refs, table, length)):
             raise ValueError("data, refs, table and length are on one device")
         self.data, self.refs, self.table, self.length = data, refs, table, length
-        self.page_size, self.device = page_size, data.device
-        self.c = L.Cache(data.data_ptr(), refs.data_ptr(), table.data_ptr(), length.data_ptr(), *_strides(data)[:5],
+        self.page_size, self.device, self.dtype = page_size, data.device, data.dtype
+        self.c = L.Cache(data.data_ptr(), refs.data_ptr(), table.data_ptr(), length.data_ptr(), *[_stride(data, d) for d in range(5)],
                          layers, n_pages, page_size, kv_heads, head_dim, _DTYPES[data.dtype], *table.shape)
         self._c = _addr(self.c)
         self._ws_bytes = int(L.lib().ewsjf_cache_workspace_bytes(self._c))
@@ -97,8 +97,7 @@ class PagedCache:
                    torch.zeros(n_slots, dtype=torch.int32, device=dev))
 
     def _ids(self, t: torch.Tensor, name: str, n: int | None = None) -> int:
-        _need(t, torch.int32, name)
-        if t.device != self.device:
+        if _need(t, torch.int32, name).device != self.device:
             raise ValueError(f"{name} is on another device than the cache")
         if n is not None and t.numel() != n:
             raise ValueError(f"{name} needs {n} entries")
@@ -171,11 +170,11 @@ class PagedCache:
         newest tokens (ewsjf_cache_append)."""
         n, want = slot.numel(), (self.c.kv_heads, self.c.head_dim)
         for t, name in ((k, "k"), (v, "v")):
-            if not isinstance(t, torch.Tensor) or t.dtype != self.data.dtype or t.device != self.device \
+            if not isinstance(t, torch.Tensor) or t.dtype != self.dtype or t.device != self.device \
                     or t.dim() != 3 or tuple(t.shape[1:]) != want or t.stride(2) != 1 or t.shape != k.shape:
                 raise TypeError(f"{name} must be a CUDA tensor [total][kv_heads][head_dim] of the cache's type")
-        L.check(L.lib().ewsjf_cache_append(self._c, int(layer), k.data_ptr(), v.data_ptr(), *_strides(k)[:2],
-                                           *_strides(v)[:2], self._ids(slot, "slot"),
+        L.check(L.lib().ewsjf_cache_append(self._c, int(layer), k.data_ptr(), v.data_ptr(), _stride(k, 0),
+                                           _stride(k, 1), _stride(v, 0), _stride(v, 1), self._ids(slot, "slot"),
                                            self._ids(q_start, "q_start", n + 1), n, k.shape[0], _stream(stream)),
                 "ewsjf_cache_append")
 
@@ -186,6 +185,7 @@ class AttentionPlan:
 
     def __init__(self, cache: PagedCache, batch: L.Batch, stream=None):
         self.b = batch
+        self.q_shape = (batch.total_q, batch.q_heads, cache.c.head_dim)
         self._b = _addr(batch)
         lib = L.lib()
         nbytes = int(lib.ewsjf_attention_plan_bytes(cache._c, self._b))
@@ -231,9 +231,9 @@ def attention(q: torch.Tensor, cache: PagedCache, layer: int, plan: AttentionPla
     strides free) over one layer: (out, lse), lse float32
     [total_q][q_heads] the ln of the softmax's sum (ewsjf_attention).  scale
     defaults to head_dim ** -0.5."""
-    b, shape = plan.b, (plan.b.total_q, plan.b.q_heads, cache.c.head_dim)
-    if not isinstance(q, torch.Tensor) or q.dtype != cache.data.dtype or q.device != cache.device \
-            or tuple(q.shape) != shape or q.stride(2) != 1:
+    shape = plan.q_shape
+    if not isinstance(q, torch.Tensor) or q.dtype != cache.dtype or q.device != cache.device or q.shape != shape \
+            or q.stride(2) != 1:
         raise TypeError(f"q must be a CUDA tensor {shape} of the cache's type with contiguous dims")
     if out is None:
         out = _new(stream, shape, dtype=q.dtype, device=q.device)
@@ -244,7 +244,7 @@ def attention(q: torch.Tensor, cache: PagedCache, layer: int, plan: AttentionPla
     elif _need(lse, torch.float32, "lse").shape != q.shape[:2]:
         raise ValueError("lse is [total_q][q_heads]")
     buf = _scratch(ws, plan.ws_bytes, cache.device, stream)
-    L.check(L.lib().ewsjf_attention(cache._c, plan._b, int(layer), q.data_ptr(), *_strides(q)[:2],
+    L.check(L.lib().ewsjf_attention(cache._c, plan._b, int(layer), q.data_ptr(), _stride(q, 0), _stride(q, 1),
                                     shape[2] ** -0.5 if scale is None else float(scale), plan.buf.data_ptr(),
                                     out.data_ptr(), lse.data_ptr(), buf.data_ptr(), buf.numel(), _stream(stream)),
             "ewsjf_attention")
