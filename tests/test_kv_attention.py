@@ -191,6 +191,67 @@ def test_many_members_share(K):
     b.check(K)
     b.check(K, groups=False)
 
+def widen(b, heavy=False):
+    """A table so wide that shared prefixes count; heavy: that their phase takes kernels of its own."""
+    keys = (16 << 20) // (4 * len(b.slot) * b.Hk * b.D) + 1
+    if heavy:
+        keys = max(keys, int(100e9 / (4 * b.total * b.Hq * b.D)) + 1)
+    b.table = np.pad(b.table, ((0, 0), (0, -(-keys // b.page))), constant_values=-1)
+    return b
+
+
+@pytest.mark.parametrize("heavy", [False, True])
+@pytest.mark.parametrize("dtype,D,group", [("bf16", 128, 4), ("f16", 64, 5), ("f16", 128, 1), ("bf16", 64, 16)])
+@pytest.mark.parametrize("shared", [16, 47, 64, 130, 300])
+@pytest.mark.parametrize("q", ["one", "few", "many"])
+def test_shared_phase(K, heavy, dtype, D, group, shared, q):
+    """The shared keys as a phase of their own: tiles of 32, 128 and 256 rows there and in the sequences' own keys, the
+    phases in one kernel and in two."""
+    n = {"one": [1] * 9, "few": [1, 1, 3, 2, 1, 7, 1, 4, 0], "many": [1, 60, 3, 200, 1, 5, 1, 40, 130]}[q]
+    own = [x + (7 * i) % 90 for i, x in enumerate(n)]
+    lengths = [shared + x for x in own[:5]] + [33 + x for x in own[5:]]
+    widen(Batch(31, dtype, D, 2, group, 16, lengths, n, shared=[(5, shared), (4, 33)]), heavy).check(K)
+
+
+@pytest.mark.parametrize("heavy", [False, True])
+@pytest.mark.parametrize("page", [1, 8, 64])
+def test_shared_phase_pages(K, heavy, page):
+    own = [1 + (11 * i) % 70 for i in range(40)]
+    b = Batch(32, "bf16", 128, 2, 4, page, [210 + x for x in own], [1] * 40, shared=[(17, 192), (23, 210)], order="token")
+    widen(b, heavy).check(K)
+    b.table[b.table == b.table[b.slot[20], 1]] = -1  # a page that a group shared
+    b.check(K)
+
+
+@pytest.mark.parametrize("value", [float("nan"), float("inf")])
+@pytest.mark.parametrize("heavy", [False, True])
+def test_shared_phase_hidden_values(K, value, heavy):
+    """Keys and values that are not finite behind each sequence's end, and in values that only the later of a sequence's
+    query tokens sees."""
+    n = [1, 2, 1, 40]
+    lengths = [140 + x + (13 * i) % 50 for i, x in enumerate(n)]
+    b = widen(Batch(33, "f16", 64, 2, 4, 16, lengths, n, shared=[(4, 140)]), heavy)
+    for s, x in zip(b.slot, lengths):
+        if x % 16:
+            b.data[:, :, b.table[s, x // 16], :, x % 16:] = value
+    b.check(K)
+    s, x = b.slot[1], lengths[1]
+    b.data[:, 1, b.table[s, (x - 1) // 16], :, (x - 1) % 16] = value
+    out, lse = b.run(K)
+    last = int(b.q_start[2]) - 1
+    ref = b.reference(b.D ** -0.5)
+    keep = [i for i in range(b.total) if i != last]
+    assert not torch.isfinite(out[last]).any()
+    b.compare(out[keep], lse[keep], [r[keep] for r in ref])
+
+
+def test_shared_phase_same_bits(K):
+    b = widen(Batch(34, "bf16", 128, 2, 4, 16, [3000, 1200, 1140, 1130], [1, 5, 40, 1], shared=[(4, 1100)]))
+    first = b.run(K)
+    for _ in range(3):
+        for x, y in zip(first, b.run(K)):
+            assert torch.equal(x, y)
+
 
 @pytest.mark.parametrize("scale", [1e-6, 0.5, 3.0])
 def test_scale(K, scale):
