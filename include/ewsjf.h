@@ -592,11 +592,15 @@ size_t ewsjf_attention_workspace_bytes(const ewsjf_cache* c, const ewsjf_batch* 
 
 /* Plan of a batch whose sequences [group_start[g], group_start[g + 1]) share
  * their first shared[g] tokens: the rows of their slots name the same pages
- * there (as forks leave them) or pages with the same contents.  The shared
- * keys are read once for the group, from the first member's row.  Of shared[g]
- * counts at most the tokens before every member's first query.  n_groups = 0:
- * nothing is shared.  window and sinks are 0.  slot, q_start, group_start,
- * shared: device int32 [n_seqs], [n_seqs + 1], [n_groups + 1], [n_groups]. */
+ * there (as forks leave them) or pages with the same contents.  Shared keys
+ * are read once for the group, from the row of its first member that has
+ * queries; a small batch, a group with fewer than two such members, and the
+ * tokens after the last multiple of 16 are read member by member.  Of
+ * shared[g] counts at most the tokens before every member's first query.
+ * n_groups = 0: nothing is shared.  window and sinks are 0.  slot, q_start,
+ * group_start, shared: device int32 [n_seqs], [n_seqs + 1], [n_groups + 1],
+ * [n_groups]; starts ascend, to total_q and n_seqs (one that falls back or
+ * leaves that range counts as the largest before it, within the range). */
 ewsjf_status ewsjf_prefix_plan(const ewsjf_cache* c, const ewsjf_batch* b, const int32_t* slot,
                                const int32_t* q_start, const int32_t* group_start, const int32_t* shared, void* plan,
                                size_t plan_bytes, hipStream_t stream);

@@ -252,6 +252,34 @@ __device__ int last_at_most(const T* key, int n, int64_t v) {
   return lo;
 }
 
+// Starts brought into [0, most], and into order: each at least as large as those
+// before it.  So the row tiles of a batch are never more than its sizes allow.
+__device__ void climb(const int32_t* from, int n, int most, int* to, int64_t* sums) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  int64_t run = 0;
+  for (int i0 = 0; i0 < n; i0 += kPlanThreads) {
+    const int i = i0 + threadIdx.x;
+    int64_t v = i < n ? from[i] : 0;
+    v = v < 0 ? 0 : v > most ? most : v;
+    for (int d = 1; d < 64; d <<= 1) {
+      const int64_t o = __shfl_up(v, d);
+      if (lane >= d && o > v) v = o;
+    }
+    __syncthreads();
+    if (lane == 63) sums[wave] = v;
+    __syncthreads();
+    int64_t all = run;
+    for (int k = 0; k < kPlanThreads / 64; ++k) {
+      if (k == wave) {
+        if (all > v) v = all;
+        if (i < n) to[i] = (int)v;
+      }
+      if (sums[k] > all) all = sums[k];
+    }
+    run = all;
+  }
+}
+
 struct PlanArgs {
   const int32_t *slot, *q_start, *group_start, *shared;
   int rows[2], keys[2], workers[2], G, columns;
@@ -267,29 +295,25 @@ __global__ __launch_bounds__(kPlanThreads) void make_plan(ewsjf_cache c, ewsjf_b
   __shared__ int common[kMost];     // a group's shared tokens that count
   __shared__ int lead[kMost];       // its first member with queries
   __shared__ int members[kMost];
+  __shared__ int q_from[kMost + 1];
+  __shared__ int g_from[kMost + 1];
   const int n = b.n_seqs, groups = b.n_groups;
   const int64_t room = (int64_t)c.width * c.page_size;
-  auto q_at = [&](int i) {
-    const int64_t v = a.q_start[i];
-    return v < 0 ? 0 : v > b.total_q ? b.total_q : v;
-  };
-  auto queries = [&](int i) {
-    const int64_t d = q_at(i + 1) - q_at(i);
-    return d < 0 ? 0 : d;
-  };
+  climb(a.q_start, n + 1, (int)b.total_q, q_from, sums);
+  if (groups > 0) climb(a.group_start, groups + 1, n, g_from, sums);
+  __syncthreads();
+  auto q_at = [&](int i) -> int64_t { return q_from[i]; };
+  auto queries = [&](int i) { return q_at(i + 1) - q_at(i); };
   auto tokens = [&](int i) -> int64_t {
     const int s = a.slot[i];
     if (s < 0 || s >= c.n_slots) return 0;
     const int64_t v = c.length[s];
     return v < 0 ? 0 : v > room ? room : v;
   };
-  auto group_at = [&](int g) {
-    const int v = a.group_start[g];
-    return v < 0 ? 0 : v > n ? n : v;
-  };
+  auto group_at = [&](int g) { return g_from[g]; };
   auto group_of = [&](int i) {  // -1: none
     if (groups == 0) return -1;
-    const int g = last_at_most(a.group_start, groups, i);
+    const int g = last_at_most(g_from, groups, i);
     return group_at(g) <= i && i < group_at(g + 1) ? g : -1;
   };
   for (int g = threadIdx.x; g < groups; g += kPlanThreads) {
@@ -319,8 +343,7 @@ __global__ __launch_bounds__(kPlanThreads) void make_plan(ewsjf_cache c, ewsjf_b
     auto rows_of = [&](int i) -> int64_t {
       if (ph) return queries(i) * a.G;
       if (common[i] == 0) return 0;
-      const int64_t d = q_at(group_at(i + 1)) - q_at(group_at(i));
-      return d < 0 ? 0 : d * a.G;
+      return (q_at(group_at(i + 1)) - q_at(group_at(i))) * a.G;
     };
     int64_t run = 0;
     // a group's first row tile is kept for phase 1, in `members`
@@ -981,7 +1004,6 @@ __device__ __forceinline__ void block_units(char* room, int phase, int block, in
     left = (beg + ph.share < all ? beg + ph.share : all) - beg;
     const Start st = constant(a.plan.start[phase] + id);
     place = st.place, e = st.entry, head = st.head, t0 = st.tile;
-    if (ph.share == 0) left = constant(a.plan.entry[phase] + e).tiles;
   }
   const float scale2 = arguments<T>().scale2;
   bool leading = true, odd = false;

@@ -16,6 +16,7 @@ constexpr int kMaxReq = EWSJF_MAX_CACHE_BATCH;
 // second launch takes (65,536 pages: 256 KiB of counts).
 constexpr int kSmallPool = 65536;
 constexpr int kSmallThreads = 1024;
+constexpr int kMostGrid = 65536;  // workgroups that copy pages of one plane: a launch has below 2^32 threads
 constexpr int kFewRequests = 64;  // and writes the rows of so many requests itself
 
 // Workspace: counts of the chunks, the requests' running needs, the pages
@@ -62,15 +63,16 @@ __device__ int wave_scan(int v) {  // inclusive over the 64 lanes
   return v;
 }
 
-// Exclusive prefix sum over the workgroup; total gets the sum.
-template <int kThreads = ewsjf::kThreads>
-__device__ int block_scan(int v, int* sums, int& total) {
+// Exclusive prefix sum over the workgroup; total gets the sum.  A wave's sum
+// has to fit 32 bits.
+template <int kThreads = ewsjf::kThreads, typename N>
+__device__ N block_scan(int v, N* sums, N& total) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int inc = wave_scan(v);
   __syncthreads();
   if (lane == 63) sums[wave] = inc;
   __syncthreads();
-  int base = 0, all = 0;
+  N base = 0, all = 0;
   for (int i = 0; i < kThreads / 64; ++i) {
     if (i < wave) base += sums[i];
     all += sums[i];
@@ -88,11 +90,12 @@ __device__ int held(const ewsjf_cache& c, int slot) {
   return n < 0 ? 0 : n;
 }
 
-// Checks the requests and sums what they need; the sum of all is returned.
+// Checks the requests and sums what they need, in 64 bits: requests of up to
+// 2^24 pages each pass 32 bits together.
 template <int N>
-__device__ int sum_needs(const ewsjf_cache& c, const CacheWs& w, int* sums, const int32_t* parent,
-                         const int32_t* slot, const int32_t* tokens, int n) {
-  int run = 0;
+__device__ void sum_needs(const ewsjf_cache& c, const CacheWs& w, int64_t* sums, const int32_t* parent,
+                          const int32_t* slot, const int32_t* tokens, int n) {
+  int64_t run = 0;
   for (int i0 = 0; i0 < n; i0 += N) {
     const int i = i0 + threadIdx.x;
     int need = 0, ok = 0;
@@ -117,15 +120,15 @@ __device__ int sum_needs(const ewsjf_cache& c, const CacheWs& w, int* sums, cons
         }
       }
     }
-    int total;
-    const int before = block_scan<N>(need, sums, total);
+    if (need > c.n_pages) need = c.n_pages + 1;
+    int64_t total;
+    const int64_t after = run + block_scan<N>(need, sums, total) + need;
     if (i < n) {
-      w.cum[i] = run + before + need;
+      w.cum[i] = after <= c.n_pages ? (int)after : c.n_pages + 1;  // more than are free
       w.fine[i] = ok;
     }
     run += total;
   }
-  return run;
 }
 
 // Workgroups 0 .. chunks - 1 count their chunk's free (or used) pages; the
@@ -133,15 +136,15 @@ __device__ int sum_needs(const ewsjf_cache& c, const CacheWs& w, int* sums, cons
 __global__ __launch_bounds__(kThreads) void count_pages(ewsjf_cache c, CacheWs w, int chunks, bool used,
                                                         const int32_t* parent, const int32_t* slot,
                                                         const int32_t* tokens, int n) {
-  __shared__ int sums[kThreads / 64];
+  __shared__ int64_t sums[kThreads / 64];
   if ((int)blockIdx.x < chunks) {
     int mine = 0;
     const int64_t base = (int64_t)blockIdx.x * kChunk;
     for (int i = threadIdx.x; i < kChunk; i += kThreads)
       if (base + i < c.n_pages) mine += (c.refs[base + i] != 0) == used;
-    int total;
+    int64_t total;
     block_scan(mine, sums, total);
-    if (threadIdx.x == 0) w.counts[blockIdx.x] = total;
+    if (threadIdx.x == 0) w.counts[blockIdx.x] = (int)total;
     return;
   }
   sum_needs<kThreads>(c, w, sums, parent, slot, tokens, n);
@@ -248,9 +251,10 @@ __global__ __launch_bounds__(kThreads) void apply_growth(ewsjf_cache c, CacheWs 
 __global__ __launch_bounds__(kSmallThreads) void grow_small(ewsjf_cache c, CacheWs w, const int32_t* parent,
                                                             const int32_t* slot, const int32_t* tokens, int n,
                                                             int32_t* granted, bool rows) {
+  __shared__ int64_t needs[kSmallThreads / 64];
   __shared__ int sums[kSmallThreads / 64];
   __shared__ int top;
-  sum_needs<kSmallThreads>(c, w, sums, parent, slot, tokens, n);
+  sum_needs<kSmallThreads>(c, w, needs, parent, slot, tokens, n);
   // a thread's pages lie together: one scan ranks them all
   const int each = (c.n_pages + kSmallThreads - 1) / kSmallThreads;
   const int64_t from = (int64_t)threadIdx.x * each, end = from + each < c.n_pages ? from + each : c.n_pages;
@@ -305,14 +309,17 @@ __global__ __launch_bounds__(kThreads) void release_rows(ewsjf_cache c, const in
   if (begin == nullptr && threadIdx.x == 0) c.length[s] = 0;
 }
 
-__global__ __launch_bounds__(kThreads) void copy_pages(ewsjf_cache c, const int32_t* src, const int32_t* dst) {
-  const int a = src[blockIdx.x], b = dst[blockIdx.x], plane = blockIdx.y;
-  if (!in_pool(c, a) || !in_pool(c, b)) return;
+__global__ __launch_bounds__(kThreads) void copy_pages(ewsjf_cache c, const int32_t* src, const int32_t* dst, int n) {
+  const int plane = blockIdx.y;
   uint16_t* data = static_cast<uint16_t*>(c.data) + plane / 2 * c.layer_stride + plane % 2 * c.kv_stride;
-  const uint4* from = reinterpret_cast<const uint4*>(data + a * c.page_stride);
-  uint4* to = reinterpret_cast<uint4*>(data + b * c.page_stride);
   const int vecs = c.kv_heads * c.page_size * c.head_dim / 8;
-  for (int j = threadIdx.x; j < vecs; j += kThreads) to[j] = from[j];
+  for (int i = blockIdx.x; i < n; i += gridDim.x) {
+    const int a = src[i], b = dst[i];
+    if (!in_pool(c, a) || !in_pool(c, b)) continue;
+    const uint4* from = reinterpret_cast<const uint4*>(data + a * c.page_stride);
+    uint4* to = reinterpret_cast<uint4*>(data + b * c.page_stride);
+    for (int j = threadIdx.x; j < vecs; j += kThreads) to[j] = from[j];
+  }
 }
 
 // The moves of a compaction.  With U used pages and before(p) used pages below
@@ -435,7 +442,7 @@ hipError_t launch_cache_release(const ewsjf_cache& c, const int32_t* slot, const
 hipError_t launch_cache_copy(const ewsjf_cache& c, const int32_t* src, const int32_t* dst, int32_t n,
                              hipStream_t stream) {
   if (n == 0) return hipSuccess;
-  copy_pages<<<dim3(n, 2 * c.layers), kThreads, 0, stream>>>(c, src, dst);
+  copy_pages<<<dim3(n < kMostGrid ? n : kMostGrid, 2 * c.layers), kThreads, 0, stream>>>(c, src, dst, n);
   return hipGetLastError();
 }
 

@@ -456,3 +456,23 @@ def test_empty_batches(K):
     plan = K.window_plan(c, ints(np.zeros(0)), ints([0]), 5, 1, total_q=0, max_q=1, q_heads=8)
     out, lse = K.attention(b.q, c, 0, plan)
     assert out.numel() == 0
+
+
+def test_starts_out_of_order(K):
+    """Starts that fall back or leave the batch count as the largest before them, within the batch."""
+    b = widen(Batch(35, "bf16", 64, 2, 4, 16, [60 + 3 * i for i in range(12)], [2] * 12, shared=[(5, 48), (4, 32), (3, 32)]))
+    rng = np.random.default_rng(36)
+    c = b.cache(K)
+    for _ in range(8):
+        q = rng.integers(-3, b.total + 30, 13).astype(np.int32)
+        g = rng.integers(-2, 15, 4).astype(np.int32)
+        kw = dict(total_q=b.total, max_q=2, q_heads=b.Hq)
+        got = []
+        for qs, gs in ((q, g), (np.maximum.accumulate(q.clip(0, b.total)), np.maximum.accumulate(g.clip(0, 12)))):
+            for plan in (K.prefix_plan(c, ints(b.slot), ints(qs), ints(gs), ints(b.shared), **kw),
+                         K.window_plan(c, ints(b.slot), ints(qs), 20, 2, **kw)):
+                out, lse = torch.zeros_like(b.q).contiguous(), torch.zeros(b.q.shape[:2], device="cuda")
+                got.append(K.attention(b.q, c, 0, plan, out=out, lse=lse))
+        for i in (0, 1):
+            for x, y in zip(got[i], got[i + 2]):
+                assert torch.equal(x, y)

@@ -239,3 +239,39 @@ def test_refusals(K):
     x = torch.zeros((1, 2, 8), dtype=torch.float16, device="cuda")
     with pytest.raises(K.L.EwsjfError):
         c.append(2, x, x, ints([0]), ints([0, 1]))
+
+
+@pytest.mark.parametrize("pages", [1024, 70000])
+def test_needs_past_32_bits(K, pages):
+    """Requests that together need 2^32 pages and more: what follows the first that does not fit is refused too."""
+    width = 1 << 20
+    c, _ = make(K, pages, 1, 2, width, layers=1, heads=1)
+    n = K.L.MAX_CACHE_BATCH
+    t = np.full(n, width)
+    t[0], t[-1] = 5, 0
+    s = np.zeros(n)
+    s[0] = 1
+    assert c.extend(ints(s), ints(t)).tolist() == [1] + [0] * (n - 1)
+    assert int(c.refs.sum()) == 5 and c.length.tolist() == [0, 5]
+    assert c.table[1, :5].tolist() == [0, 1, 2, 3, 4] and int((c.table >= 0).sum()) == 5
+
+
+@pytest.mark.parametrize("page,order", [(1, "head"), (4, "token")])
+def test_a_large_pool(K, page, order):
+    """Pools that one workgroup does not rank."""
+    c, r = make(K, 70001, page, 9, 20000, layers=1, heads=1, order=order)
+    rng = np.random.default_rng(page)
+    for step in range(6):
+        pick, t = rng.permutation(8), rng.integers(0, 20000, 8)
+        assert c.extend(ints(pick), ints(t)).tolist() == r.extend(pick, t)
+        half = r.length[pick[0]] // 2
+        c.release(ints(pick[4:])), r.release(pick[4:])
+        assert c.fork(ints(pick[:1]), ints(pick[5:6]), ints([half])).tolist() == r.fork(pick[:1], pick[5:6], [half])
+        same(c, r)
+        out = c.compact()
+        table, refs, used = r.compact()
+        assert np.array_equal(out[0].cpu().numpy(), table) and np.array_equal(out[1].cpu().numpy(), refs)
+        c.adopt(*out[:2])
+        r.table, r.refs = table, refs
+        r.data[:] = c.data.cpu().float().numpy()
+        same(c, r)
