@@ -21,6 +21,16 @@
 // operand needs them, O^T = V^T P^T, when the keys are taken in the order
 // 4h, .., 4h + 3, 8 + 4h, .. in which the first product leaves them (h = lane /
 // 32).  V^T is read from LDS with the transposing read.
+//
+// With `width` the row's query heads, a unit of R rows and K keys reads R D +
+// 2 K D values once and computes 4 R K D operations: R operations a byte of
+// keys.  Up to 32 rows (decoding) memory is the limit, from about 200 rows on
+// (prefill, many requests behind one prefix) the matrix units are; hence two
+// kernels.  What they reach on the card, whose large copies run at 4.8 TB/s
+// (read and written) and whose large 16-bit products at 1270 TFLOP/s:
+//   one prompt of 16,384 tokens, 40 heads of 128, window 4096: 1.46 ms, 830
+//   TFLOP/s; 256 single tokens of 32 query and 8 key heads of 128 over windows
+//   of 4096: 193 us, 5.0 TB/s.
 #include <hip/hip_runtime.h>
 
 #include "ewsjf_cache.h"
@@ -36,8 +46,7 @@ __host__ __device__ constexpr int block_keys(int waves) { return waves == 8 ? 12
 constexpr int kWaves = 4;        // waves of a workgroup of the wave kernel
 constexpr int kCUs = 256;
 constexpr int64_t kMostJoins = 1 << 24;  // waves of a grid's row: a launch has below 2^32 threads in one
-constexpr int kWholeKeys = 1024;   // of a unit that one workgroup takes whole,
-constexpr int kWholeUnits = 2048;  // in a batch of so many
+constexpr int kWholeKeys = 2048;   // of a unit that one workgroup takes whole
 constexpr float kFloor = -3e38f;   // running maximum of a row that has seen no key
 constexpr float kLn2 = 0.6931471805599453f;
 constexpr float kLog2e = 1.4426950408889634f;
@@ -121,11 +130,16 @@ Shape shape_of(const ewsjf_cache& c, const ewsjf_batch& b) {
   Shape s;
   s.G = b.q_heads / c.kv_heads;
   const int64_t most_keys = (int64_t)c.width * c.page_size;  // of a sequence
-  // Below 16 MiB of keys and values in all, each sequence's read for itself, what sharing them saves is less than what
-  // its kernels cost (four sequences behind 288 tokens: one kernel of 7 us against three, 17 us).
-  s.groups = b.n_groups > 0 && 4 * most_keys * b.n_seqs * c.kv_heads * c.head_dim > (16 << 20);
-  // rows that read the same keys: of a sequence, of a group on average
-  const int64_t most[2] = {s.groups ? b.total_q * s.G / b.n_groups : 0, (int64_t)b.max_q * s.G};
+  // Sharing pays when the keys and values that each sequence would read for itself (much of it from caches) take longer
+  // than the phase and the join.  32 query and 8 key heads of 128, shared against not: 16 sequences behind 1024 tokens
+  // (66 MiB) 20 us against 17, 64 behind 1024 (264 MiB) 25 against 33, 16 behind 4096 (258 MiB) 26 against 34.  With at
+  // most 32 rows a group, in two kernels: 4 behind 4096 (64 MiB) 40 against 31, 4 behind 16,000 (250 MiB) 64 against 65;
+  // 8 of 40 heads behind 1024 (165 MiB) 34 against 22.
+  const int64_t rows = b.n_groups > 0 ? b.total_q * s.G / b.n_groups : 0;
+  const int64_t bytes = 4 * most_keys * b.n_seqs * c.kv_heads * c.head_dim;
+  s.groups = rows > 0 && bytes > (rows > kRowTile ? (int64_t)128 << 20 : (int64_t)256 << 20);
+  // rows that read the same keys: of a group on average, of a sequence
+  const int64_t most[2] = {s.groups ? rows : 0, (int64_t)b.max_q * s.G};
   // One kernel for both phases, half of each CU to either, up to 100 GFLOP against shared keys: 64 sequences behind 2048
   // tokens took 59 us, as two kernels 71; 512 behind 4096, 109 against 143, behind 8192 (69 GFLOP) 158 against 174.
   // Beyond, a kernel with all of each CU and tiles of 256 rows makes up for the second one: 512 behind 16,123
@@ -143,11 +157,14 @@ Shape shape_of(const ewsjf_cache& c, const ewsjf_batch& b) {
   }
   if (!s.groups) s.entries[0] = 0;
   s.kv_heads = c.kv_heads;
-  // One token a sequence and few keys: a workgroup takes a unit sooner than a second kernel joins its parts.  With one
-  // token, no row sees less of a unit than another, so no row is done again either.
+  // One token a sequence and few keys: a workgroup takes a unit sooner than a second kernel joins its parts.  8 key heads
+  // of 128, whole against cut: 16 sequences of 1024 keys 17 us against 28, 256 of 1024 191 against 204, 8 of 2048 25
+  // against 30, 128 of 2048 190 against 202, but 32 of 2048 59 against 55; 16 of 4096 44 against 40, 256 of 4096 457
+  // against 440.  With one token, no row sees less of a unit than
+  // another, so no row is done again either.
   const int64_t keys = b.window > 0 && (int64_t)b.window + b.sinks < most_keys ? (int64_t)b.window + b.sinks : most_keys;
   const int64_t units = s.entries[1] * c.kv_heads;
-  s.whole = !s.groups && s.waves[1] == 0 && b.max_q == 1 && keys <= kWholeKeys && units <= kWholeUnits;
+  s.whole = !s.groups && s.waves[1] == 0 && b.max_q == 1 && keys <= kWholeKeys;
   if (s.whole) s.workers[1] = s.blocks[1] = (int)((units + 7) / 8 * 8);
   // many row tiles of long runs, and nothing to join them with
   s.columns = s.waves[1] && !s.groups ? s.workers[1] / 8 : 0;
@@ -286,8 +303,11 @@ struct PlanArgs {
   bool whole;
 };
 
-// One workgroup.  Everything read from the caller's arrays is bounded here, so
-// the other kernels follow the plan without checks of their own.
+// One workgroup, latency-bound: prefix sums over the row tiles and a search a
+// worker.  11 us for 4 sequences, 27 us for 512 behind a prefix and 24 us for
+// the 2560 units of one long prompt; once a step, whatever the layers.
+// Everything read from the caller's arrays is bounded here, so the other
+// kernels follow the plan without checks of their own.
 __global__ __launch_bounds__(kPlanThreads) void make_plan(ewsjf_cache c, ewsjf_batch b, PlanArgs a, Plan plan) {
   constexpr int kMost = EWSJF_MAX_CACHE_BATCH;
   __shared__ int64_t sums[kPlanThreads / 64];
@@ -387,7 +407,7 @@ __global__ __launch_bounds__(kPlanThreads) void make_plan(ewsjf_cache c, ewsjf_b
           x.lo = shared;
           if (b.window > 0) {
             const int64_t w = (int64_t)p0 - b.window + 1;
-            x.lo = w > 0 ? (int)w & ~(TK - 1) : 0;
+            x.lo = w > 0 ? (int)w & ~15 : 0;
             x.sink = b.sinks < x.end ? b.sinks : x.end;
             if (x.lo <= x.sink) x.lo = x.sink = 0;  // one run of keys
           }
@@ -405,8 +425,11 @@ __global__ __launch_bounds__(kPlanThreads) void make_plan(ewsjf_cache c, ewsjf_b
       line += total;
     }
     const int64_t all = line * c.kv_heads;
-    // 0: a worker a unit
-    const int64_t share = ph && a.whole ? 0 : all > 0 ? (all + a.workers[ph] - 1) / a.workers[ph] : 1;
+    // Even shares, but where a unit has many workers, its s tiles a share against T / s parts to join: one row tile of
+    // 4096 keys a head took 59 us in shares of a tile (128 parts), 40 in shares of four.  0: a worker a unit.
+    int64_t share = all > 0 ? (all + a.workers[ph] - 1) / a.workers[ph] : 1;
+    while (8 * share * share * E < line) ++share;
+    if (ph && a.whole) share = 0;
     const int active = share ? (int)((all + share - 1) / share) : E * c.kv_heads;
     if (threadIdx.x == 0) {
       plan.cum[ph][E] = line;
@@ -980,6 +1003,21 @@ __device__ bool clear_keys(int key0, uint64_t there, uint4 (&k)[NI], uint4 (&v)[
 // values for all, worked on in chunks of 64 keys.  While a tile is in use the
 // next one goes from registers to the other half of LDS and the one after
 // that is loaded; one barrier a tile.
+//
+// Bounds: a chunk's products of a wave take 32 cycles a matrix instruction and
+// its softmax 8 an exponential, about as long in all with heads of 64 and half
+// as long with heads of 128, of which a SIMD's two waves hide only a part from
+// each other; and at full use of the matrix units the card lowers its clock (a
+// loop of nothing but products on random registers: 1.7 PFLOP/s, with four
+// vector instructions a product 1.5).  Heads of 128: 830 TFLOP/s on one prompt
+// of 16,384 tokens; heads of 64: 24 prompts of 120 k tokens in all, windows of
+// 1024, 270 us, 470 TFLOP/s, with sinks' and windows' edges that are computed
+// but not counted.
+//
+// 256 rows (eight waves, tiles of 128 keys) read each key half as often as 128
+// rows from L2 and put half as many barriers between products: 1.46 ms against
+// 1.84 ms on that prompt.  Four waves serve up to 128 rows, where the others'
+// would idle.
 // ---------------------------------------------------------------------------
 template <int D, int NW>
 constexpr int kBlockRoom = 2 * 2 * block_keys(NW) * D * 2;  // LDS: two tiles' keys and values
@@ -1097,7 +1135,13 @@ __global__ __launch_bounds__(NW * 64, 2) void attend_block(Args<T>, int phase) {
 
 // ---------------------------------------------------------------------------
 // The wave kernel: up to 32 rows (a few query tokens), the keys streamed by
-// waves that share nothing.
+// waves that share nothing: each loads the next tile of 32 keys into registers
+// while it works on the present one from LDS, so a CU's eight waves have 128
+// KiB of loads in flight with heads of 128, and no wave waits for another.
+// Bound by memory: 193 us for 0.97 GB of keys and values (256 sequences, windows
+// of 4096, 8 key heads of 128), 5.0 TB/s, what a large copy reaches.  Short
+// units lose to their beginnings (page lookup, first tile): 512 sequences' own
+// 128 tokens, 0.28 GB, take 80 us, 3.4 TB/s.
 //
 // Split: a workgroup takes one unit, a quarter of its tiles a wave, and joins
 // the four parts itself.
@@ -1240,7 +1284,9 @@ __global__ __launch_bounds__(kWaves * 64, 2) void attend_wave(Args<T>, int phase
 
 // Both phases of a batch behind shared prefixes at once: on each CU one
 // workgroup has the shared keys, where the matrix unit is the limit, and one
-// streams sequences' own keys, where memory is.
+// streams sequences' own keys, where memory is.  46 us for 64 sequences of 40
+// key heads of 128 behind 2048 tokens (0.13 GB, floor 51 us with the join's
+// traffic), 17 us for 63 of 3 key heads behind up to 4001 tokens.
 template <typename T, int D, bool Sixteens>
 __global__ __launch_bounds__(kWaves * 64, 2) void attend_both(Args<T>) {
   static_assert(kBlockRoom<D, 4> == kWaves * kWaveRoom<D>, "one room serves either");
@@ -1425,6 +1471,9 @@ __device__ bool any_odd(const Args<T>& a, const Cut& u, int flags) {
   return __any(odd);
 }
 
+// The join is bound by latency: a row's parts and its plan are found through
+// three dependent loads.  9 us for 2560 rows of 128, 15 us for 16,384.
+//
 // With a shared prefix every row is joined: `fours` waves take a unit of key
 // head blockIdx.y, four rows each.
 template <typename T, int D>

@@ -2,6 +2,10 @@
 // written.  Free pages are those with refs == 0; they are ranked by page
 // number with prefix sums, so which page a request gets follows from the
 // state alone and not from the order in which workgroups run.
+//
+// Books are a few KiB, so those kernels take as long as a launch and a few
+// dependent loads do; only the pages' contents count against memory, 4.8 TB/s
+// read and written in a large copy here.
 #include <hip/hip_runtime.h>
 
 #include "ewsjf_cache.h"
@@ -12,12 +16,15 @@ namespace {
 constexpr int kThreads = 256;
 constexpr int kChunk = 4096;  // pages ranked by one workgroup
 constexpr int kMaxReq = EWSJF_MAX_CACHE_BATCH;
-// One workgroup ranks the pages of a pool up to this size in less time than a
-// second launch takes (65,536 pages: 256 KiB of counts).
-constexpr int kSmallPool = 65536;
+// Pools that one workgroup ranks, in one launch for two: an extend and a release
+// of 8 slots take 10.2 us against 12.1 with 1024 pages, 11.3 against 13.2 with
+// 4096, 14.5 against 13.6 with 8192; of 1024 slots, 15.2 against 20.0 with 4096.
+constexpr int kSmallPool = 4096;
 constexpr int kSmallThreads = 1024;
 constexpr int kMostGrid = 65536;  // workgroups that copy pages of one plane: a launch has below 2^32 threads
-constexpr int kFewRequests = 64;  // and writes the rows of so many requests itself
+// Requests whose rows it writes too, a wave each at once: 8 of them 10.2 us, in a
+// launch of their own 11.5; 64 of them 13.9 against 11.6.
+constexpr int kFewRequests = kSmallThreads / 64;
 
 // Workspace: counts of the chunks, the requests' running needs, the pages
 // picked for them; for a compaction the two ends of each move and, per moved
@@ -224,7 +231,11 @@ __device__ bool write_row(const ewsjf_cache& c, const CacheWs& w, int free, cons
 __device__ void grown(const ewsjf_cache& c, int slot, int tokens) { c.length[slot] = held(c, slot) + tokens; }
 
 // Request blockIdx.x: plane 0's workgroup writes its row, length and grant; for
-// a fork each plane's (layer and keys or values) copies the partial page.
+// a fork each plane's (layer and keys or values) copies the partial page, 16
+// bytes a thread at a time.  512 forks that each copy a page of 8 layers (512
+// KiB): 94 us, 5.7 TB/s with parents' pages read from cache; one workgroup a
+// page and plane is 8192 of them, enough to fill the chip without a division of
+// the page.
 __global__ __launch_bounds__(kThreads) void apply_growth(ewsjf_cache c, CacheWs w, const int32_t* parent,
                                                          const int32_t* slot, const int32_t* tokens,
                                                          int32_t* granted) {
@@ -247,7 +258,7 @@ __global__ __launch_bounds__(kThreads) void apply_growth(ewsjf_cache c, CacheWs 
 }
 
 // count_pages and pick_pages of a small pool; for few requests of new tokens
-// their rows too.
+// their rows too. 
 __global__ __launch_bounds__(kSmallThreads) void grow_small(ewsjf_cache c, CacheWs w, const int32_t* parent,
                                                             const int32_t* slot, const int32_t* tokens, int n,
                                                             int32_t* granted, bool rows) {

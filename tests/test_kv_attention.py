@@ -131,6 +131,17 @@ def test_decode_lengths(K, dtype, D, group):
     Batch(1, dtype, D, 2, group, 16, EDGE, [1] * len(EDGE)).check(K)
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("D,group", [(64, 1), (64, 8), (128, 3), (128, 4)])
+def test_decode_lengths_cut(K, dtype, D, group):
+    """Single tokens where a row could be long: units are cut over the chip, whatever the lengths are."""
+    b = Batch(37, dtype, D, 2, group, 16, EDGE + [2000], [1] * (len(EDGE) + 1))
+    b.table = np.pad(b.table, ((0, 0), (0, 4000)), constant_values=-1)
+    b.check(K)
+    b.check(K, window=3000, sinks=3)
+    b.check(K, window=150, sinks=20)
+
+
 @pytest.mark.parametrize("dtype,D,page,order", [("bf16", 128, 16, "token"), ("f16", 64, 1, "head"), ("bf16", 64, 8, "head"),
                                                 ("f16", 128, 64, "token"), ("bf16", 128, 256, "head"),
                                                 ("f16", 64, 2, "token")])
@@ -193,7 +204,7 @@ def test_many_members_share(K):
 
 def widen(b, heavy=False):
     """A table so wide that shared prefixes count; heavy: that their phase takes kernels of its own."""
-    keys = (16 << 20) // (4 * len(b.slot) * b.Hk * b.D) + 1
+    keys = (256 << 20) // (4 * len(b.slot) * b.Hk * b.D) + 1
     if heavy:
         keys = max(keys, int(100e9 / (4 * b.total * b.Hq * b.D)) + 1)
     b.table = np.pad(b.table, ((0, 0), (0, -(-keys // b.page))), constant_values=-1)
