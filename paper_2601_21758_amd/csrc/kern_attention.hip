@@ -637,7 +637,9 @@ struct Rows {
       for (int j = 0; j < 16; ++j) o[i][j] *= shrink;
   }
 
-  // Weights of the scores s, rounded to 16 bits, their sum added to the row's.
+  // Weights of the scores s, rounded to 16 bits as the second product's matrix
+  // instructions take them (with 32-bit weights it would run at an eighth of the
+  // rate); their sum, of the 32-bit ones, is added to the row's.
   // They are first taken with the maximum as it stands: a sum of at most 2^10
   // says that none is too large, and a maximum that is a few orders too low
   // loses nothing.  Else the maximum is raised and they are taken again.
@@ -1285,8 +1287,8 @@ __global__ __launch_bounds__(kWaves * 64, 2) void attend_wave(Args<T>, int phase
 // Both phases of a batch behind shared prefixes at once: on each CU one
 // workgroup has the shared keys, where the matrix unit is the limit, and one
 // streams sequences' own keys, where memory is.  46 us for 64 sequences of 40
-// key heads of 128 behind 2048 tokens (0.13 GB, floor 51 us with the join's
-// traffic), 17 us for 63 of 3 key heads behind up to 4001 tokens.
+// key heads of 128 with up to 128 tokens each behind 2048 (0.24 GB, 5.3 TB/s),
+// 17 us for 63 of 3 key heads of 64 behind up to 4001 tokens.
 template <typename T, int D, bool Sixteens>
 __global__ __launch_bounds__(kWaves * 64, 2) void attend_both(Args<T>) {
   static_assert(kBlockRoom<D, 4> == kWaves * kWaveRoom<D>, "one room serves either");

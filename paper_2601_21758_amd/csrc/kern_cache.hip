@@ -297,6 +297,8 @@ __global__ __launch_bounds__(kSmallThreads) void grow_small(ewsjf_cache c, Cache
   }
 }
 
+// A workgroup a slot.  Counts are integers, so the order of the atomics does
+// not matter.
 __global__ __launch_bounds__(kThreads) void release_rows(ewsjf_cache c, const int32_t* slot, const int32_t* begin,
                                                          const int32_t* end) {
   const int s = slot[blockIdx.x];
@@ -320,6 +322,7 @@ __global__ __launch_bounds__(kThreads) void release_rows(ewsjf_cache c, const in
   if (begin == nullptr && threadIdx.x == 0) c.length[s] = 0;
 }
 
+// A workgroup a page and plane.
 __global__ __launch_bounds__(kThreads) void copy_pages(ewsjf_cache c, const int32_t* src, const int32_t* dst, int n) {
   const int plane = blockIdx.y;
   uint16_t* data = static_cast<uint16_t*>(c.data) + plane / 2 * c.layer_stride + plane % 2 * c.kv_stride;
@@ -360,6 +363,10 @@ __global__ __launch_bounds__(kThreads) void list_moves(ewsjf_cache c, CacheWs w,
   }
 }
 
+// The first `book` workgroups write rows and counts, the others take the moved
+// pages' planes in turn.  A target lies below U and a source at or above it, so
+// no page is both.  Bound by memory: 983 pages of 512 KiB, read and written, 210
+// us, 4.9 TB/s, what a large copy reaches.
 __global__ __launch_bounds__(kThreads) void move_pages(ewsjf_cache c, CacheWs w, int32_t* out_table,
                                                        int32_t* out_refs, const int32_t* used, int book) {
   const int moves = w.head[1], U = *used;
@@ -393,7 +400,8 @@ __global__ __launch_bounds__(kThreads) void move_pages(ewsjf_cache c, CacheWs w,
   }
 }
 
-// One workgroup a token: its heads' keys and values into the slot's page.
+// One workgroup a token: its heads' keys and values into the slot's page.  3 us
+// for 8 tokens, a launch; the search for the sequence is its longest part.
 __global__ __launch_bounds__(kThreads) void append_tokens(ewsjf_cache c, int layer, const uint16_t* k,
                                                           const uint16_t* v, int64_t k_token, int64_t k_head,
                                                           int64_t v_token, int64_t v_head, const int32_t* slot,
