@@ -723,8 +723,10 @@ __device__ uint64_t seen_keys(uint64_t there, int here, int p, int window, int s
 // lane's first one on.
 __device__ void hide(float16v& s, uint32_t seen) {
 #pragma unroll
-  for (int r = 0; r < 16; ++r)
-    if (!(seen >> (8 * (r / 4) + r % 4) & 1)) s[r] = -INFINITY;
+  for (int r = 0; r < 16; ++r) {
+    const uint32_t keep = __builtin_amdgcn_sbfe(seen, 8 * (r / 4) + r % 4, 1);  // all bits or none
+    s[r] = __uint_as_float((__float_as_uint(s[r]) & keep) | (0xff800000u & ~keep));
+  }
 }
 
 // Loads the queries of the rows of a lane, zeros past the last one.
