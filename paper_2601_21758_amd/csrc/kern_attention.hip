@@ -57,7 +57,7 @@ struct Entry {
   int32_t slot;       // row of the table, -1: no keys
   int32_t q0, row0, rows, pos0;
   int32_t lo, end;    // keys of the main run
-  int32_t sink;       // keys [0, sink) come before it in tiles of their own
+  int32_t sink;       // keys [0, sink) come before it
   int32_t prefix;     // first row tile of the group's phase, -1: no shared keys
   int32_t prefix_row; // row of this tile's row 0 in the group
   int32_t tiles;
@@ -69,13 +69,13 @@ struct Start {
   int32_t place, entry, head, tile;
 };
 
-// The unit at a place of the line.  By heads: the row tiles of a key head, then
-// the next head's.  In columns: each XCD's eighth of that list is dealt out to
-// `columns` workers in turn, a worker's units following one another on the
-// line; so at any time the workers of an XCD have neighbouring row tiles of one
-// head, which read much the same keys.
+// The unit at a place of a line in columns.  Otherwise the line goes by heads:
+// the row tiles of a key head, then the next head's.  In columns, each XCD's
+// eighth of that list is dealt out to `columns` workers in turn, a worker's units
+// following one another on the line; so at any time the workers of an XCD have
+// neighbouring row tiles of one head, which read much the same keys (24 prompts
+// over windows of 1024: 267 us, by heads 379).
 __device__ int64_t unit_at(int64_t place, int64_t units, int columns) {
-  if (columns == 0) return place;
   int64_t base = 0, size = units;
   for (int x = 7; x >= 0; --x)
     if (place >= units * x / 8) {
@@ -110,7 +110,8 @@ struct Plan {
   Start* start[2];   // [workers]
   Entry* entry[2];
   int64_t* cum[2];   // tiles of one key head before a row tile
-  int64_t* line;     // tiles before a place of the line in columns
+  int64_t* line;     // tiles before a place of the line in columns,
+  int32_t* order;    // and its unit
   size_t bytes;
 };
 
@@ -192,6 +193,7 @@ Plan plan_of(const Shape& s, void* base) {
     p.cum[i] = at.take<int64_t>(s.entries[i] + 1);
   }
   p.line = at.take<int64_t>(s.columns ? s.entries[1] * s.kv_heads + 1 : 0);
+  p.order = at.take<int32_t>(s.columns ? s.entries[1] * s.kv_heads + 1 : 0);
   p.bytes = at.at;
   return p;
 }
@@ -415,7 +417,7 @@ __global__ __launch_bounds__(kPlanThreads) void make_plan(ewsjf_cache c, ewsjf_b
           x.prefix_row = shared > 0 ? (int)((q_at(i) - q_at(group_at(g))) * a.G + x.row0) : 0;
         }
         const int span = x.end > x.lo ? x.end - x.lo : 0;
-        x.tiles = (x.sink + TK - 1) / TK + (span + TK - 1) / TK;
+        x.tiles = (((x.sink + 15) & ~15) + span + TK - 1) / TK;
         if (x.tiles == 0) x.tiles = 1;  // a tile without keys, for the rows' zeros
         entry[e] = x;
       }
@@ -441,10 +443,14 @@ __global__ __launch_bounds__(kPlanThreads) void make_plan(ewsjf_cache c, ewsjf_b
       int64_t before = 0;
       for (int64_t k0 = 0; k0 < units; k0 += kPlanThreads) {
         const int64_t k = k0 + threadIdx.x;
-        const int tiles = k < units ? entry[unit_at(k, units, a.columns) % E].tiles : 0;
+        const int64_t unit = k < units ? unit_at(k, units, a.columns) : 0;
+        const int tiles = k < units ? entry[unit % E].tiles : 0;
         int64_t total;
         const int64_t mine = scan(tiles, sums, total);
-        if (k < units) plan.line[k] = before + mine;
+        if (k < units) {
+          plan.line[k] = before + mine;
+          plan.order[k] = (int)unit;
+        }
         before += total;
       }
       __syncthreads();
@@ -463,7 +469,7 @@ __global__ __launch_bounds__(kPlanThreads) void make_plan(ewsjf_cache c, ewsjf_b
         place = head * E + e;
         rest = at % line - plan.cum[ph][e];
       }
-      const int64_t unit = unit_at(place, units, ph ? a.columns : 0);
+      const int64_t unit = ph && a.columns ? plan.order[place] : place;
       plan.start[ph][w] = Start{(int)place, (int)(unit % E), (int)(unit / E), (int)rest};
     }
     __syncthreads();
@@ -548,7 +554,7 @@ __device__ T constant(const T* p) {
 }
 
 // The unit after a worker's present one.
-__device__ void next_unit(const Phase& ph, int units, int& place, int& e, int& head) {
+__device__ void next_unit(const Plan& plan, const Phase& ph, int units, int& place, int& e, int& head) {
   ++place;
   if (ph.columns == 0) {
     if (++e == ph.entries) {
@@ -558,8 +564,8 @@ __device__ void next_unit(const Phase& ph, int units, int& place, int& e, int& h
     return;
   }
   if (place >= units) return;
-  const int64_t u = unit_at(place, units, ph.columns);
-  e = (int)(u % ph.entries), head = (int)(u / ph.entries);
+  const int u = constant(plan.order + place);
+  head = u / ph.entries, e = u - head * ph.entries;
 }
 
 template <typename T>
@@ -711,13 +717,7 @@ __device__ int first_value() {
   return value_place<D>(4 * (lane >> 5) + (t >> 2), 32 * ((lane >> 4) & 1) + 8 * (t & 3));
 }
 
-// Bits of the keys [here, here + 64) that the row at position p sees.
 __device__ uint64_t bits_below(int n) { return n >= 64 ? ~0ull : n <= 0 ? 0ull : (1ull << n) - 1; }
-__device__ uint64_t seen_keys(uint64_t there, int here, int p, int window, int sinks) {
-  uint64_t m = there & bits_below(p - here + 1);
-  if (window > 0) m &= ~bits_below(p - window - here + 1) | bits_below(sinks - here);
-  return m;
-}
 
 // Scores of keys that a row does not see become -inf; seen: its keys from the
 // lane's first one on.
@@ -797,8 +797,10 @@ __device__ uint4 load_uint4(Global<const char> p) {
   return make_uint4(x.x, x.y, x.z, x.w);
 }
 
-// The key tiles of a unit.  Tile t is keys [first(t), first(t) + TK), of which
-// those below end(t) count.
+// The key tiles of a unit, TK places of a list each: the sinks, up to a multiple
+// of 16, then the main run from a multiple of 16 on.  So tiles are full but for
+// the last (sinks in tiles of their own cost 24 prompts over windows of 1024 a
+// sixth of their time).
 //
 // Sixteens: pages have at least 16 tokens.  Tiles begin at multiples of 16, so
 // each 16 keys lie in one page and are loaded from one address of the wave.
@@ -813,9 +815,9 @@ struct Tiles {
   static constexpr int kGroups = TK / 16, kBatch = 64 / kGroups;
   Global<const int32_t> row;
   Global<const char> base;  // the key head's first key
-  int lo, hi, sink, nst, shift, pages;
+  int hi, sink, skip, move, shift, pages;  // places below skip are keys, the others keys from `move` back
   int c0, c1;        // in tiles [c0, c1) every row sees every key
-  int p_first, p_last, window, sinks;
+  int p_first, p_last;
   uint32_t page_bytes, page_bytes_hi, token_bytes;
   int64_t to_values;
   uint32_t step;  // a lane's place in a load, and how far on the next load of 16 keys is
@@ -827,14 +829,14 @@ struct Tiles {
     const bool there_is = x.slot >= 0;
     row = global(a.table + (int64_t)(there_is ? x.slot : 0) * a.width);
     base = global(reinterpret_cast<const char*>(a.data + head * a.head_stride));
-    lo = x.lo, hi = there_is ? x.end : 0, sink = there_is ? x.sink : 0;
-    nst = (x.sink + TK - 1) / TK;
-    shift = a.page_shift, pages = a.n_pages, window = a.window, sinks = a.sinks;
+    hi = there_is ? x.end : 0, sink = there_is ? x.sink : 0;
+    skip = (x.sink + 15) & ~15, move = x.lo - skip;
+    shift = a.page_shift, pages = a.n_pages;
     p_first = x.pos0 + x.row0 / a.G, p_last = x.pos0 + (x.row0 + x.rows - 1) / a.G;
     const int below = p_first + 1 < hi ? p_first + 1 : hi;    // every row sees the keys before it,
-    const int above = window > 0 ? p_last - window + 1 : lo;  // and those from it on
-    c0 = nst + (above > lo ? (above - lo + TK - 1) / TK : 0);
-    c1 = nst + (below > lo ? (below - lo) / TK : 0);
+    const int above = a.window > 0 ? p_last - a.window + 1 - move : 0;  // and those from this place on
+    c0 = ((above > skip ? above : skip) + TK - 1) / TK;
+    c1 = below > move ? (below - move) / TK : 0;
     const uint64_t bytes = 2 * a.page_stride;
     page_bytes = (uint32_t)bytes, page_bytes_hi = (uint32_t)(bytes >> 32);
     token_bytes = 2 * (uint32_t)a.token_stride;
@@ -843,19 +845,15 @@ struct Tiles {
     stride = KPI * token_bytes;
   }
 
-  __device__ int first(int t) const { return t < nst ? t * TK : lo + (t - nst) * TK; }
-  __device__ int end(int t) const { return t < nst ? sink : hi; }
+  __device__ int key_at(int place) const { return place < skip ? place : place + move; }
   __device__ bool held(int page) const { return (unsigned)page < (unsigned)pages; }
-  // The table's entry for a key of tile t (some entry, past the tile's end).
-  __device__ int entry_of(int t, int key) const {
-    const int kend = end(t);
-    return row[(key < kend ? key : kend > 0 ? kend - 1 : 0) >> shift];
+  // The table's entry for a place (some entry, past the last key).
+  __device__ int entry_of(int place) const {
+    const int key = key_at(place);
+    return row[(key < hi ? key : hi > 0 ? hi - 1 : 0) >> shift];
   }
 
-  __device__ int find(int b) const {
-    const int lane = threadIdx.x & 63, t = b * kBatch + lane / kGroups;
-    return entry_of(t, first(t) + 16 * (lane % kGroups));
-  }
+  __device__ int find(int b) const { return entry_of(b * kBatch * TK + 16 * (threadIdx.x & 63)); }
   __device__ void begin(int t) {
     if (!Sixteens) return;
     batch = t / kBatch;
@@ -896,31 +894,50 @@ struct Tiles {
     }
     bool all = true;
 #pragma unroll
-    for (int c = 0; c < TK; c += 64) all = all && __all(held(entry_of(t, first(t) + c + (threadIdx.x & (TK < 64 ? 31 : 63)))));
+    for (int c = 0; c < TK; c += 64) all = all && __all(held(entry_of(t * TK + c + (threadIdx.x & (TK < 64 ? 31 : 63)))));
     return all;
   }
-  // Every row sees every key of the tile that is there.
+  // Every row sees every key of the tile that is there (false for some tiles of which that is true).
   __device__ bool even(int t) const {
-    const int k0 = first(t), k1 = k0 + TK < end(t) ? k0 + TK : end(t);
+    if (t * TK < skip) return false;
+    const int window = arguments<T>().window, sinks = arguments<T>().sinks;
+    const int k0 = t * TK + move, k1 = k0 + TK < hi ? k0 + TK : hi;
     return k1 - 1 <= p_first && (window == 0 || k0 > p_last - window || k1 <= sinks);
   }
 
   // Bits of the keys of chunk c (64 keys) that are there and that some row may
   // see.
   __device__ uint64_t there(int t, int c = 0) const {
-    const int k0 = first(t) + 64 * c;
+    const int v0 = t * TK + 64 * c;
     uint64_t m = 0;
     if (Sixteens) {
 #pragma unroll
       for (int j = 0; j < (TK < 64 ? TK : 64) / 16; ++j)
         if (held(page_at(t, 4 * c + j))) m |= 0xffffull << (16 * j);
     } else {
-      m = __ballot(held(entry_of(t, k0 + (threadIdx.x & 63))));
+      m = __ballot(held(entry_of(v0 + (threadIdx.x & 63))));
       if (TK == 32) m = (uint32_t)m;
     }
-    m &= bits_below(end(t) - k0);
-    if (window > 0) m &= ~bits_below(p_first - window - k0 + 1) | bits_below(sinks - k0);
-    return m;
+    return m & merged(v0, bits_below(hi - v0 - move) & in_window(v0 + move, p_first));
+  }
+  // Bits of the 64 places from v0 on: the sinks, and of the main run those given.
+  __device__ uint64_t merged(int v0, uint64_t main) const {
+    return (main & ~bits_below(skip - v0)) | bits_below(sink - v0);
+  }
+  // Bits of the keys [here, here + 64) that a row at position p has not left behind.
+  __device__ uint64_t in_window(int here, int p) const {
+    const int window = arguments<T>().window, sinks = arguments<T>().sinks;
+    return window > 0 ? ~bits_below(p - window - here + 1) | bits_below(sinks - here) : ~0ull;
+  }
+  // Those of `there` (chunk c of tile t) that the row at position p sees.  Every row is past the sinks.
+  __device__ uint64_t seen(uint64_t there, int t, int c, int p) const {
+    const int v0 = t * TK + 64 * c, here = v0 + move;
+    return there & merged(v0, bits_below(p - here + 1) & in_window(here, p));
+  }
+  // Some row at a position from `from` to `to` may see keys of the chunk.
+  __device__ bool meets(int t, int c, int from, int to) const {
+    const int v0 = t * TK + 64 * c, k0 = v0 + move, window = arguments<T>().window, sinks = arguments<T>().sinks;
+    return v0 < skip || (k0 < hi && k0 <= to && (window == 0 || k0 + 63 > from - window || k0 < sinks));
   }
 
   // Where 16 keys of a tile lie (page 0's where there is no page).
@@ -929,7 +946,7 @@ struct Tiles {
   };
   __device__ At address(int t, int key) const {
     const int at = page_at(t, key / 16);
-    const uint32_t page = held(at) ? at : 0, in = (first(t) + key) & ((1 << shift) - 1);
+    const uint32_t page = held(at) ? at : 0, in = key_at(t * TK + key) & ((1 << shift) - 1);
     const uint64_t off = (uint64_t)page * page_bytes + ((uint64_t)(page * page_bytes_hi) << 32) + in * token_bytes;
     At r;
     r.k = apart(base + off);
@@ -959,7 +976,7 @@ struct Tiles {
     } else {
 #pragma unroll
       for (int i = 0; i < NI; ++i) {
-        const int key = first(t) + key0 + i * KPI + lane / LPR, at = entry_of(t, key);
+        const int place = t * TK + key0 + i * KPI + lane / LPR, key = key_at(place), at = entry_of(place);
         const Global<const char> p = base + (held(at) ? at : 0) * (int64_t)((uint64_t)page_bytes_hi << 32 | page_bytes) +
                                      (key & mask) * token_bytes + lane % LPR * 16;
         k[i] = load_uint4(p);
@@ -1081,8 +1098,7 @@ __device__ __forceinline__ void block_units(char* room, int phase, int block, in
 #pragma unroll
       for (int j = 0; j < Rows<T, D>::kAhead; ++j) v[j] = rows.read_values(vc, vp, j);
       if (!clean) {
-        const uint64_t seen = seen_keys(tiles.there(t, c), tiles.first(t) + 64 * c, p, tiles.window, tiles.sinks) >>
-                              (4 * (lane >> 5));
+        const uint64_t seen = tiles.seen(tiles.there(t, c), t, c, p) >> (4 * (lane >> 5));
         hide(s[0], (uint32_t)seen);
         hide(s[1], (uint32_t)(seen >> 32));
       }
@@ -1104,10 +1120,7 @@ __device__ __forceinline__ void block_units(char* room, int phase, int block, in
       __syncthreads();
 #pragma unroll
       for (int c = 0; c < TK / 64; ++c) {
-        const int k0 = tiles.first(t) + 64 * c;
-        if (busy && (clean || (k0 < tiles.end(t) && k0 <= w_end &&
-                               (tiles.window == 0 || k0 + 63 > w_first - tiles.window || k0 < tiles.sinks))))
-          chunk(buf, c, clean, t);
+        if (busy && (clean || tiles.meets(t, c, w_first, w_end))) chunk(buf, c, clean, t);
         if (c == 0) {
           // no load in a branch: where the ways meet, the registers would be copied, and the copies would wait
           if (!next) clear(t + 1);
@@ -1124,7 +1137,7 @@ __device__ __forceinline__ void block_units(char* room, int phase, int block, in
     left -= n;
     t0 = 0;
     const Phase ph = constant(z.plan.phase + phase);
-    next_unit(ph, ph.entries * z.kv_heads, place, e, head);
+    next_unit(z.plan, ph, ph.entries * z.kv_heads, place, e, head);
   }
   const Global<int32_t> flags = global(arguments<T>().work.odd[phase]);
   if (lane == 0) flags[id * NW + wave] = 0;
@@ -1215,7 +1228,7 @@ __device__ __forceinline__ void wave_units(char* room, int phase, int block, int
       vec8<T> v[Rows<T, D>::kAhead];
 #pragma unroll
       for (int j = 0; j < Rows<T, D>::kAhead; ++j) v[j] = rows.read_values(values, vp, j);
-      if (!clean) hide(s[0], (uint32_t)seen_keys(held, tiles.first(t), p, tiles.window, tiles.sinks) >> (4 * (lane >> 5)));
+      if (!clean) hide(s[0], (uint32_t)tiles.seen(held, t, 0, p) >> (4 * (lane >> 5)));
       vec8<T> w[2];
       rows.template weigh<1>(s, scale2, w);
       rows.template add<1>(values, vp, w, v);
@@ -1229,7 +1242,7 @@ __device__ __forceinline__ void wave_units(char* room, int phase, int block, int
     left -= n;
     t0 = 0;
     const Phase ph = constant(z.plan.phase + phase);
-    next_unit(ph, ph.entries * z.kv_heads, place, e, head);
+    next_unit(z.plan, ph, ph.entries * z.kv_heads, place, e, head);
   }
   if (!Split) {
     const Global<int32_t> flags = global(arguments<T>().work.odd[phase]);
@@ -1524,7 +1537,7 @@ __global__ __launch_bounds__(256) void join_cuts(Args<T> a, int rows1, int flags
     }
     left -= n;
     t = 0;
-    next_unit(own, own.entries * a.kv_heads, place, e, head);
+    next_unit(a.plan, own, own.entries * a.kv_heads, place, e, head);
   }
 }
 
