@@ -28,9 +28,9 @@
 // (prefill, many requests behind one prefix) the matrix units are; hence two
 // kernels.  What they reach on the card, whose large copies run at 4.8 TB/s
 // (read and written) and whose large 16-bit products at 1270 TFLOP/s:
-//   one prompt of 16,384 tokens, 40 heads of 128, window 4096: 1.46 ms, 830
+//   one prompt of 16,384 tokens, 40 heads of 128, window 4096: 1.5 ms, 800
 //   TFLOP/s; 256 single tokens of 32 query and 8 key heads of 128 over windows
-//   of 4096: 193 us, 5.0 TB/s.
+//   of 4096: 194 us, 5.0 TB/s.
 #include <hip/hip_runtime.h>
 
 #include "ewsjf_cache.h"
@@ -799,8 +799,8 @@ __device__ uint4 load_uint4(Global<const char> p) {
 
 // The key tiles of a unit, TK places of a list each: the sinks, up to a multiple
 // of 16, then the main run from a multiple of 16 on.  So tiles are full but for
-// the last (sinks in tiles of their own cost 24 prompts over windows of 1024 a
-// sixth of their time).
+// the last (with sinks in tiles of their own, 24 prompts over windows of 1024 took
+// 260 us, so 247; over windows of 256, 167 and 146).
 //
 // Sixteens: pages have at least 16 tokens.  Tiles begin at multiples of 16, so
 // each 16 keys lie in one page and are loaded from one address of the wave.
@@ -1030,14 +1030,15 @@ __device__ bool clear_keys(int key0, uint64_t there, uint4 (&k)[NI], uint4 (&v)[
 // as long with heads of 128, of which a SIMD's two waves hide only a part from
 // each other; and at full use of the matrix units the card lowers its clock (a
 // loop of nothing but products on random registers: 1.7 PFLOP/s, with four
-// vector instructions a product 1.5).  Heads of 128: 830 TFLOP/s on one prompt
-// of 16,384 tokens; heads of 64: 24 prompts of 120 k tokens in all, windows of
-// 1024, 270 us, 470 TFLOP/s, with sinks' and windows' edges that are computed
-// but not counted.
+// vector instructions a product 1.5).  Heads of 128: 800 TFLOP/s on one prompt
+// of 16,384 tokens, matrix instructions busy 40% of the cycles and vector
+// instructions 39%, at 2.0 GHz.  Heads of 64: 720 TFLOP/s over windows of 4096;
+// over windows of 1024 a unit has nine tiles, and its beginning, end and masks
+// leave 500 (24 prompts, 20 query and 4 key heads, 253 us with the join).
 //
 // 256 rows (eight waves, tiles of 128 keys) read each key half as often as 128
 // rows from L2 and put half as many barriers between products: 1.46 ms against
-// 1.84 ms on that prompt.  Four waves serve up to 128 rows, where the others'
+// 1.65 ms on that prompt.  Four waves serve up to 128 rows, where the others'
 // would idle.
 // ---------------------------------------------------------------------------
 template <int D, int NW>
