@@ -236,7 +236,7 @@ __device__ void grown(const ewsjf_cache& c, int slot, int tokens) { c.length[slo
 // Request blockIdx.x: plane 0's workgroup writes its row, length and grant; for
 // a fork each plane's (layer and keys or values) copies the partial page, 16
 // bytes a thread at a time.  512 forks that each copy a page of 8 layers (512
-// KiB): 94 us, 5.7 TB/s with parents' pages read from cache; one workgroup a
+// KiB): 78 to 94 us, 5.7 to 6.8 TB/s with parents' pages read from cache; one workgroup a
 // page and plane is 8192 of them, enough to fill the chip without a division of
 // the page.
 __global__ __launch_bounds__(kThreads) void apply_growth(ewsjf_cache c, CacheWs w, const int32_t* parent,
