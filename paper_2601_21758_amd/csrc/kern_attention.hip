@@ -717,7 +717,11 @@ __device__ int first_value() {
   return value_place<D>(4 * (lane >> 5) + (t >> 2), 32 * ((lane >> 4) & 1) + 8 * (t & 3));
 }
 
+// The lowest n bits.
 __device__ uint64_t bits_below(int n) { return n >= 64 ? ~0ull : n <= 0 ? 0ull : (1ull << n) - 1; }
+
+// p - window, of a window of any length.
+__device__ int left_by(int p, int window) { return __builtin_elementwise_sub_sat(p, window); }
 
 // Scores of keys that a row does not see become -inf; seen: its keys from the
 // lane's first one on.
@@ -834,7 +838,7 @@ struct Tiles {
     shift = a.page_shift, pages = a.n_pages;
     p_first = x.pos0 + x.row0 / a.G, p_last = x.pos0 + (x.row0 + x.rows - 1) / a.G;
     const int below = p_first + 1 < hi ? p_first + 1 : hi;    // every row sees the keys before it,
-    const int above = a.window > 0 ? p_last - a.window + 1 - move : 0;  // and those from this place on
+    const int above = a.window > 0 ? left_by(p_last + 1 - move, a.window) : 0;  // and those from this place on
     c0 = ((above > skip ? above : skip) + TK - 1) / TK;
     c1 = below > move ? (below - move) / TK : 0;
     const uint64_t bytes = 2 * a.page_stride;
@@ -902,7 +906,7 @@ struct Tiles {
     if (t * TK < skip) return false;
     const int window = arguments<T>().window, sinks = arguments<T>().sinks;
     const int k0 = t * TK + move, k1 = k0 + TK < hi ? k0 + TK : hi;
-    return k1 - 1 <= p_first && (window == 0 || k0 > p_last - window || k1 <= sinks);
+    return k1 - 1 <= p_first && (window == 0 || k0 > left_by(p_last, window) || k1 <= sinks);
   }
 
   // Bits of the keys of chunk c (64 keys) that are there and that some row may
@@ -927,7 +931,7 @@ struct Tiles {
   // Bits of the keys [here, here + 64) that a row at position p has not left behind.
   __device__ uint64_t in_window(int here, int p) const {
     const int window = arguments<T>().window, sinks = arguments<T>().sinks;
-    return window > 0 ? ~bits_below(p - window - here + 1) | bits_below(sinks - here) : ~0ull;
+    return window > 0 ? ~bits_below(left_by(p - here + 1, window)) | bits_below(sinks - here) : ~0ull;
   }
   // Those of `there` (chunk c of tile t) that the row at position p sees.  Every row is past the sinks.
   __device__ uint64_t seen(uint64_t there, int t, int c, int p) const {
@@ -937,7 +941,7 @@ struct Tiles {
   // Some row at a position from `from` to `to` may see keys of the chunk.
   __device__ bool meets(int t, int c, int from, int to) const {
     const int v0 = t * TK + 64 * c, k0 = v0 + move, window = arguments<T>().window, sinks = arguments<T>().sinks;
-    return v0 < skip || (k0 < hi && k0 <= to && (window == 0 || k0 + 63 > from - window || k0 < sinks));
+    return v0 < skip || (k0 < hi && k0 <= to && (window == 0 || k0 + 63 > left_by(from, window) || k0 < sinks));
   }
 
   // Where 16 keys of a tile lie (page 0's where there is no page).
@@ -1416,10 +1420,10 @@ __device__ void redo_row(const Args<T>& a, const Entry& x, int head, int row, fl
   const T* q = a.q + (x.q0 + token) * a.q_token + (head * a.G + member) * a.q_head;
   float o[D / 64] = {}, sum = 0.f;
   for (int k0 = 0; k0 <= p && x.slot >= 0; k0 += 64) {
-    if (a.window > 0 && k0 >= a.sinks && k0 + 63 <= p - a.window) continue;
+    if (a.window > 0 && k0 >= a.sinks && k0 + 63 <= left_by(p, a.window)) continue;
     const int key = k0 + lane;
     int page = -1;
-    if (key <= p && (a.window == 0 || key > p - a.window || key < a.sinks))
+    if (key <= p && (a.window == 0 || key > left_by(p, a.window) || key < a.sinks))
       page = a.table[(int64_t)x.slot * a.width + (key >> a.page_shift)];
     if (page >= a.n_pages) page = -1;
     const int in = key & ((1 << a.page_shift) - 1);

@@ -487,3 +487,47 @@ def test_starts_out_of_order(K):
         for i in (0, 1):
             for x, y in zip(got[i], got[i + 2]):
                 assert torch.equal(x, y)
+
+
+@pytest.mark.parametrize("q", [1, 70])
+def test_offsets_past_32_bits(K, q):
+    """Pages whose keys lie more than 2^32 bytes, and more than 2^31 elements, behind the first one's."""
+    pages, page, heads, D = 2500, 1024, 8, 128
+    data = torch.empty((1, 2, pages, heads, page, D), dtype=torch.bfloat16, device="cuda")
+    used = np.asarray([2499, 3, 2100])
+    rng = np.random.default_rng(38)
+    small = torch.tensor(rng.standard_normal((1, 2, 3, heads, page, D)), dtype=torch.bfloat16)
+    for i, p in enumerate(used):
+        data[:, :, p] = small[:, :, i].cuda()
+    table, length = np.asarray([[0, 1, 2], [2, 0, -1]]), np.asarray([2300, 1500])
+    q_start = np.asarray([0, q, q + 1])
+    x = torch.tensor(rng.standard_normal((q + 1, 2 * heads, D)), dtype=torch.bfloat16)
+    refs = np.zeros(pages, np.int32)
+    refs[used] = [2, 1, 2]
+    cache = K.PagedCache.of(data, ints(refs), ints(np.where(table < 0, -1, used[table])), ints(length))
+    pick = [0, q - 1, q]
+    for window, sinks in ((0, 0), (700, 5)):
+        kw = dict(total_q=q + 1, max_q=q, q_heads=2 * heads)
+        plan = K.window_plan(cache, ints([0, 1]), ints(q_start), window, sinks, **kw) if window else \
+            K.prefix_plan(cache, ints([0, 1]), ints(q_start), None, None, **kw)
+        out, lse = K.attention(x.cuda(), cache, 0, plan)
+        ref = kv_ref.attention(x.double().numpy(), small.double().numpy()[0], table, length, [0, 1], q_start, page,
+                               D ** -0.5, window, sinks)
+        b_out, b_lse = kv_ref.bounds(*ref, UNIT["bf16"], 2300, float(small.float().abs().max()), D)
+        assert np.all(np.abs(out.cpu().double().numpy() - ref[0])[pick] <= b_out[pick])
+        assert np.all(np.abs(lse.cpu().double().numpy() - ref[1])[pick] <= b_lse[pick])
+    # new tokens and a fork's copy there too
+    k, v = (torch.randn((1, heads, D), device="cuda").bfloat16() for _ in range(2))
+    cache.append(0, k, v, ints([1]), ints([0, 1]))
+    assert torch.equal(data[0, 0, used[0], :, 1499 % page], k[0]) and torch.equal(data[0, 1, used[0], :, 1499 % page], v[0])
+    cache.copy(ints([2499]), ints([2400]))
+    assert torch.equal(data[:, :, 2400], data[:, :, 2499])
+
+
+@pytest.mark.parametrize("window", [2 ** 31 - 1, 2 ** 31 - 200, 2 ** 30])
+@pytest.mark.parametrize("sinks", [0, 3])
+def test_windows_longer_than_any_row(K, window, sinks):
+    n = [300, 70, 33, 1]
+    b = Batch(39, "f16", 64, 2, 4, 16, [300, 90, 20, 200], n)
+    b.length = b.length.astype(np.int64)  # the definition's p - window, without a wrap of its own
+    b.check(K, window=window, sinks=sinks)
