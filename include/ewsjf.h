@@ -553,11 +553,25 @@ ewsjf_status ewsjf_cache_compact(const ewsjf_cache* c, int32_t* out_table, int32
  * (slot[s]) has the tokens [q_start[s], q_start[s + 1]) of k and v (device,
  * 16-bit [total][kv_heads][head_dim] with strides in elements, multiples of
  * 8, 16-byte aligned); with m of them, token i goes to position length - m +
- * i.  q_start: device int32 [n_seqs + 1], ascending from 0 to total. */
+ * i.  q_start: device int32 [n_seqs + 1], ascending from 0 to total.
+ *
+ * ewsjf_cache_append_granted writes nothing for a sequence with granted[s] ==
+ * 0 (device int32 [n_seqs], as ewsjf_cache_extend left it for the same
+ * requests), whose length does not count the tokens; a granted request's go
+ * to the places that it was granted.
+ *
+ * ewsjf_cache_append (granted == NULL there) is for requests that were all
+ * granted, written before their slots are forked.  The tokens of a refused
+ * one replace the last that its slot holds; but a whole page that other rows
+ * hold too is not written, so no other slot reads anything else. */
 ewsjf_status ewsjf_cache_append(const ewsjf_cache* c, int32_t layer, const void* k, const void* v,
                                 int64_t k_token_stride, int64_t k_head_stride, int64_t v_token_stride,
                                 int64_t v_head_stride, const int32_t* slot, const int32_t* q_start, int32_t n_seqs,
                                 int64_t total, hipStream_t stream);
+ewsjf_status ewsjf_cache_append_granted(const ewsjf_cache* c, int32_t layer, const void* k, const void* v,
+                                        int64_t k_token_stride, int64_t k_head_stride, int64_t v_token_stride,
+                                        int64_t v_head_stride, const int32_t* slot, const int32_t* q_start,
+                                        const int32_t* granted, int32_t n_seqs, int64_t total, hipStream_t stream);
 
 /* ---------------------------------------------------------------------------
  * Attention over the cache.

@@ -26,8 +26,8 @@ EXPORTED = ("ewsjf_queue_table_bytes", "ewsjf_workspace_bytes", "ewsjf_table_upl
             "ewsjf_partition_hist", "ewsjf_dispatch", "ewsjf_trial_step", "ewsjf_trial_finish",
             "ewsjf_status_string", "ewsjf_version", "ewsjf_step_static",
             "ewsjf_cache_workspace_bytes", "ewsjf_cache_extend", "ewsjf_cache_fork", "ewsjf_cache_release",
-            "ewsjf_cache_copy", "ewsjf_cache_compact", "ewsjf_cache_append", "ewsjf_attention_plan_bytes",
-            "ewsjf_attention_workspace_bytes", "ewsjf_prefix_plan", "ewsjf_window_plan", "ewsjf_attention")
+            "ewsjf_cache_copy", "ewsjf_cache_compact", "ewsjf_cache_append", "ewsjf_cache_append_granted",
+            "ewsjf_attention_plan_bytes", "ewsjf_attention_workspace_bytes", "ewsjf_prefix_plan", "ewsjf_window_plan", "ewsjf_attention")
 STATIC_SCRATCH_BYTES = 4 << 20
 MAX_CACHE_BATCH, MAX_PAGES, MAX_PAGE_SIZE, MAX_HEAD_DIM = 4096, 1 << 24, 1024, 256
 BF16, F16 = 0, 1
@@ -139,6 +139,8 @@ def lib():
         L.ewsjf_cache_compact.restype = C.c_int
         L.ewsjf_cache_append.argtypes = [vp, i32, vp, vp, i64, i64, i64, i64, vp, vp, i32, i64, vp]
         L.ewsjf_cache_append.restype = C.c_int
+        L.ewsjf_cache_append_granted.argtypes = [vp, i32, vp, vp, i64, i64, i64, i64, vp, vp, vp, i32, i64, vp]
+        L.ewsjf_cache_append_granted.restype = C.c_int
         L.ewsjf_attention_plan_bytes.argtypes = [vp, vp]
         L.ewsjf_attention_plan_bytes.restype = sz
         L.ewsjf_attention_workspace_bytes.argtypes = [vp, vp]

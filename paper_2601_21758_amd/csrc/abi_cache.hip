@@ -144,10 +144,10 @@ ewsjf_status ewsjf_cache_compact(const ewsjf_cache* c, int32_t* out_table, int32
   return launched(ewsjf::launch_cache_compact(*c, out_table, out_refs, used, ws, stream));
 }
 
-ewsjf_status ewsjf_cache_append(const ewsjf_cache* c, int32_t layer, const void* k, const void* v,
-                                int64_t k_token_stride, int64_t k_head_stride, int64_t v_token_stride,
-                                int64_t v_head_stride, const int32_t* slot, const int32_t* q_start, int32_t n_seqs,
-                                int64_t total, hipStream_t stream) {
+ewsjf_status ewsjf_cache_append_granted(const ewsjf_cache* c, int32_t layer, const void* k, const void* v,
+                                        int64_t k_token_stride, int64_t k_head_stride, int64_t v_token_stride,
+                                        int64_t v_head_stride, const int32_t* slot, const int32_t* q_start,
+                                        const int32_t* granted, int32_t n_seqs, int64_t total, hipStream_t stream) {
   ewsjf_status st = cache_status(c);
   if (st != EWSJF_OK) return st;
   if (layer < 0 || layer >= c->layers || n_seqs < 0 || n_seqs > EWSJF_MAX_CACHE_BATCH || total < 0 || total >= kMaxQ)
@@ -160,7 +160,15 @@ ewsjf_status ewsjf_cache_append(const ewsjf_cache* c, int32_t layer, const void*
   if (!aligned16(k) || !aligned16(v)) return EWSJF_ERR_ALIGN;
   if ((st = ewsjf::device_ok()) != EWSJF_OK) return st;
   return launched(ewsjf::launch_cache_append(*c, layer, k, v, k_token_stride, k_head_stride, v_token_stride,
-                                             v_head_stride, slot, q_start, n_seqs, total, stream));
+                                             v_head_stride, slot, q_start, granted, n_seqs, total, stream));
+}
+
+ewsjf_status ewsjf_cache_append(const ewsjf_cache* c, int32_t layer, const void* k, const void* v,
+                                int64_t k_token_stride, int64_t k_head_stride, int64_t v_token_stride,
+                                int64_t v_head_stride, const int32_t* slot, const int32_t* q_start, int32_t n_seqs,
+                                int64_t total, hipStream_t stream) {
+  return ewsjf_cache_append_granted(c, layer, k, v, k_token_stride, k_head_stride, v_token_stride, v_head_stride, slot,
+                                    q_start, nullptr, n_seqs, total, stream);
 }
 
 size_t ewsjf_attention_plan_bytes(const ewsjf_cache* c, const ewsjf_batch* b) {

@@ -25,7 +25,8 @@ hipError_t launch_cache_compact(const ewsjf_cache& c, int32_t* out_table, int32_
                                 hipStream_t stream);
 hipError_t launch_cache_append(const ewsjf_cache& c, int32_t layer, const void* k, const void* v, int64_t k_token,
                                int64_t k_head, int64_t v_token, int64_t v_head, const int32_t* slot,
-                               const int32_t* q_start, int32_t n_seqs, int64_t total, hipStream_t stream);
+                               const int32_t* q_start, const int32_t* granted, int32_t n_seqs, int64_t total,
+                               hipStream_t stream);
 
 size_t attention_plan_bytes(const ewsjf_cache& c, const ewsjf_batch& b);
 size_t attention_ws_bytes(const ewsjf_cache& c, const ewsjf_batch& b);

@@ -405,10 +405,15 @@ __global__ __launch_bounds__(kThreads) void move_pages(ewsjf_cache c, CacheWs w,
 
 // One workgroup a token: its heads' keys and values into the slot's page.  3 us
 // for 8 tokens, a launch; the search for the sequence is its longest part.
+// Without grants a request may be one that found no room: its tokens would then
+// land on tokens that it holds already.  A partial page is the slot's own, a
+// whole one may be others' too, and two requests could write it at once; so a
+// whole page is written only if this row alone has it.
 __global__ __launch_bounds__(kThreads) void append_tokens(ewsjf_cache c, int layer, const uint16_t* k,
                                                           const uint16_t* v, int64_t k_token, int64_t k_head,
                                                           int64_t v_token, int64_t v_head, const int32_t* slot,
-                                                          const int32_t* q_start, int n_seqs) {
+                                                          const int32_t* q_start, const int32_t* granted,
+                                                          int n_seqs) {
   const int64_t t = blockIdx.x;
   int lo = 0, hi = n_seqs;  // the last s with q_start[s] <= t
   while (hi - lo > 1) {
@@ -418,11 +423,12 @@ __global__ __launch_bounds__(kThreads) void append_tokens(ewsjf_cache c, int lay
   }
   const int s = slot[lo];
   const int a = q_start[lo], e = q_start[lo + 1];
-  if (s < 0 || s >= c.n_slots || t < a || t >= e) return;
-  const int64_t pos = (int64_t)held(c, s) - (e - t);
+  if (s < 0 || s >= c.n_slots || t < a || t >= e || (granted != nullptr && granted[lo] == 0)) return;
+  const int64_t have = held(c, s), pos = have - (e - t);
   if (pos < 0 || pos >= (int64_t)c.width * c.page_size) return;
   const int page = c.table[(int64_t)s * c.width + pos / c.page_size];
   if (!in_pool(c, page)) return;
+  if (granted == nullptr && pos / c.page_size < have / c.page_size && c.refs[page] > 1) return;
   uint16_t* to = static_cast<uint16_t*>(c.data) + layer * c.layer_stride + page * c.page_stride +
                  (pos % c.page_size) * c.token_stride;
   const int dv = c.head_dim / 8, vecs = c.kv_heads * dv;
@@ -481,11 +487,12 @@ hipError_t launch_cache_compact(const ewsjf_cache& c, int32_t* out_table, int32_
 
 hipError_t launch_cache_append(const ewsjf_cache& c, int32_t layer, const void* k, const void* v, int64_t k_token,
                                int64_t k_head, int64_t v_token, int64_t v_head, const int32_t* slot,
-                               const int32_t* q_start, int32_t n_seqs, int64_t total, hipStream_t stream) {
+                               const int32_t* q_start, const int32_t* granted, int32_t n_seqs, int64_t total,
+                               hipStream_t stream) {
   if (n_seqs == 0 || total == 0) return hipSuccess;
   append_tokens<<<(unsigned)total, kThreads, 0, stream>>>(
       c, layer, static_cast<const uint16_t*>(k), static_cast<const uint16_t*>(v), k_token, k_head, v_token, v_head,
-      slot, q_start, n_seqs);
+      slot, q_start, granted, n_seqs);
   return hipGetLastError();
 }
 

@@ -6,13 +6,15 @@ admits, on the same card and stream.
     cache = kv.PagedCache.new(layers, n_pages, page_size, kv_heads, head_dim, n_slots, width)
     granted = cache.fork(parent, child, tokens)     # a prompt's pages shared, its partial page copied
     granted = cache.extend(slot, tokens)            # pages for new tokens
-    cache.append(layer, k, v, slot, q_start)        # their keys and values
+    cache.append(layer, k, v, slot, q_start, granted=granted)  # their keys and values
     plan = kv.prefix_plan(cache, slot, q_start, group_start, shared, total_q=.., max_q=.., q_heads=..)
     out, lse = kv.attention(q, cache, layer, plan)  # every layer of the step with the same plan
     cache.release(slot)
 
 Nothing here synchronizes the host; a request that does not fit the pool is
-told by granted == 0 on the device.
+told by granted == 0 on the device.  append writes nothing for it, and a slot
+of -1 (torch.where(granted > 0, slot, -1)) leaves it out of a plan: its
+queries get out 0 and lse -inf.
 """
 from __future__ import annotations
 
@@ -165,18 +167,22 @@ class PagedCache:
         self.table, self.refs = table.view_as(self.table), refs
 
     def append(self, layer: int, k: torch.Tensor, v: torch.Tensor, slot: torch.Tensor, q_start: torch.Tensor,
-               stream=None) -> None:
+               stream=None, *, granted: torch.Tensor | None = None) -> None:
         """Write keys and values [total][kv_heads][head_dim] of the slots'
-        newest tokens (ewsjf_cache_append)."""
+        newest tokens.  granted: what extend gave for these requests; nothing
+        is written for a refused one (ewsjf_cache_append_granted).  None: for
+        requests that were all granted; whole pages that other rows hold too
+        are not written (ewsjf_cache_append)."""
         n, want = slot.numel(), (self.c.kv_heads, self.c.head_dim)
         for t, name in ((k, "k"), (v, "v")):
             if not isinstance(t, torch.Tensor) or t.dtype != self.dtype or t.device != self.device \
                     or t.dim() != 3 or tuple(t.shape[1:]) != want or t.stride(2) != 1 or t.shape != k.shape:
                 raise TypeError(f"{name} must be a CUDA tensor [total][kv_heads][head_dim] of the cache's type")
-        L.check(L.lib().ewsjf_cache_append(self._c, int(layer), k.data_ptr(), v.data_ptr(), _stride(k, 0),
-                                           _stride(k, 1), _stride(v, 0), _stride(v, 1), self._ids(slot, "slot"),
-                                           self._ids(q_start, "q_start", n + 1), n, k.shape[0], _stream(stream)),
-                "ewsjf_cache_append")
+        g = None if granted is None else self._ids(granted, "granted", n)
+        L.check(L.lib().ewsjf_cache_append_granted(self._c, int(layer), k.data_ptr(), v.data_ptr(), _stride(k, 0),
+                                                   _stride(k, 1), _stride(v, 0), _stride(v, 1),
+                                                   self._ids(slot, "slot"), self._ids(q_start, "q_start", n + 1), g,
+                                                   n, k.shape[0], _stream(stream)), "ewsjf_cache_append")
 
 
 class AttentionPlan:
