@@ -18,6 +18,7 @@ queries get out 0 and lse -inf.
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes as C
 
 import torch
@@ -38,17 +39,21 @@ def _stride(t: torch.Tensor, dim: int) -> int:
 
 
 def _new(stream, *args, dtype: torch.dtype, device) -> torch.Tensor:
-    """A tensor that a call on `stream` writes: kept from reuse until that stream is done with it."""
-    t = torch.empty(*args, dtype=dtype, device=device)
-    if stream is not None:
-        t.record_stream(stream)
+    """A tensor that a call on `stream` writes: from that stream's memory (the current stream's may still be in use
+    there), and kept from reuse until the current stream, where the caller has it, is done with it."""
+    if stream is None:
+        return torch.empty(*args, dtype=dtype, device=device)
+    with torch.cuda.stream(stream):
+        t = torch.empty(*args, dtype=dtype, device=device)
+    t.record_stream(torch.cuda.current_stream(t.device))
     return t
 
 
 def _scratch(ws: Workspace | None, nbytes: int, device, stream) -> torch.Tensor:
-    if ws is not None:
-        return ws.get(nbytes)
-    return _new(stream, max(256, nbytes), dtype=torch.uint8, device=device)
+    with contextlib.nullcontext() if stream is None else torch.cuda.stream(stream):
+        if ws is not None:
+            return ws.get(nbytes)
+        return torch.empty(max(256, nbytes), dtype=torch.uint8, device=device)
 
 
 class PagedCache:
