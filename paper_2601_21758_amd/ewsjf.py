@@ -75,6 +75,7 @@ class Workspace:
     def __init__(self, device=None):
         self.device = torch.device(device or "cuda")
         self.buf = None
+        self.used_on = None  # the stream of the last call that kept it (kv)
 
     def get(self, nbytes: int) -> torch.Tensor:
         nbytes = max(256, int(nbytes))

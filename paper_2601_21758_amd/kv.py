@@ -26,6 +26,7 @@ import torch
 from . import _lib as L
 from .ewsjf import Workspace, _need, _stream
 
+_HERE = contextlib.nullcontext()
 _DTYPES = {torch.bfloat16: L.BF16, torch.float16: L.F16}
 
 
@@ -49,11 +50,22 @@ def _new(stream, *args, dtype: torch.dtype, device) -> torch.Tensor:
     return t
 
 
-def _scratch(ws: Workspace | None, nbytes: int, device, stream) -> torch.Tensor:
-    with contextlib.nullcontext() if stream is None else torch.cuda.stream(stream):
-        if ws is not None:
-            return ws.get(nbytes)
-        return torch.empty(max(256, nbytes), dtype=torch.uint8, device=device)
+def _keep(owner, raw: int, stream, *tensors: torch.Tensor) -> None:
+    """The owner's tensors, which a call on the stream (raw: its handle) uses, are kept from reuse until the stream is
+    done with them, whenever the owner lets go of them.  Only needed where the stream is not the last call's."""
+    for t in tensors:
+        t.record_stream(torch.cuda.current_stream(t.device) if stream is None else stream)
+    owner.used_on = raw
+
+
+def _scratch(ws: Workspace | None, nbytes: int, device, raw: int, stream) -> torch.Tensor:
+    with _HERE if stream is None else torch.cuda.stream(stream):
+        if ws is None:
+            return torch.empty(max(256, nbytes), dtype=torch.uint8, device=device)
+        before, buf = ws.buf, ws.get(nbytes)
+    if raw != ws.used_on or buf is not before:
+        _keep(ws, raw, stream, buf)
+    return buf
 
 
 class PagedCache:
@@ -81,6 +93,7 @@ class PagedCache:
             raise ValueError("data, refs, table and length are on one device")
         self.data, self.refs, self.table, self.length = data, refs, table, length
         self.page_size, self.device, self.dtype = page_size, data.device, data.dtype
+        self.used_on = None
         self.c = L.Cache(data.data_ptr(), refs.data_ptr(), table.data_ptr(), length.data_ptr(), *[_stride(data, d) for d in range(5)],
                          layers, n_pages, page_size, kv_heads, head_dim, _DTYPES[data.dtype], *table.shape)
         self._c = _addr(self.c)
@@ -103,6 +116,13 @@ class PagedCache:
                    torch.full((n_slots, width), -1, dtype=torch.int32, device=dev),
                    torch.zeros(n_slots, dtype=torch.int32, device=dev))
 
+    def _on(self, stream) -> int:
+        """The handle of the stream that a call uses the cache on."""
+        raw = _stream(stream)
+        if raw != self.used_on:
+            _keep(self, raw, stream, self.data, self.refs, self.table, self.length)
+        return raw
+
     def _ids(self, t: torch.Tensor, name: str, n: int | None = None) -> int:
         if _need(t, torch.int32, name).device != self.device:
             raise ValueError(f"{name} is on another device than the cache")
@@ -116,10 +136,11 @@ class PagedCache:
         refused (ewsjf_cache_extend)."""
         n = slot.numel()
         granted = _new(stream, n, dtype=torch.int32, device=self.device) if granted is None else granted
-        buf = _scratch(ws, self._ws_bytes, self.device, stream)
+        raw = self._on(stream)
+        buf = _scratch(ws, self._ws_bytes, self.device, raw, stream)
         L.check(L.lib().ewsjf_cache_extend(self._c, self._ids(slot, "slot"), self._ids(tokens, "tokens", n), n,
                                            self._ids(granted, "granted", n), buf.data_ptr(), buf.numel(),
-                                           _stream(stream)), "ewsjf_cache_extend")
+                                           raw), "ewsjf_cache_extend")
         return granted
 
     def fork(self, parent: torch.Tensor, child: torch.Tensor, tokens: torch.Tensor,
@@ -128,10 +149,11 @@ class PagedCache:
         granted, 0 refused (ewsjf_cache_fork)."""
         n = child.numel()
         granted = _new(stream, n, dtype=torch.int32, device=self.device) if granted is None else granted
-        buf = _scratch(ws, self._ws_bytes, self.device, stream)
+        raw = self._on(stream)
+        buf = _scratch(ws, self._ws_bytes, self.device, raw, stream)
         L.check(L.lib().ewsjf_cache_fork(self._c, self._ids(parent, "parent", n), self._ids(child, "child"),
                                          self._ids(tokens, "tokens", n), n, self._ids(granted, "granted", n),
-                                         buf.data_ptr(), buf.numel(), _stream(stream)), "ewsjf_cache_fork")
+                                         buf.data_ptr(), buf.numel(), raw), "ewsjf_cache_fork")
         return granted
 
     def release(self, slot: torch.Tensor, begin: torch.Tensor | None = None, end: torch.Tensor | None = None,
@@ -141,14 +163,14 @@ class PagedCache:
         n = slot.numel()
         b = None if begin is None else self._ids(begin, "begin", n)
         e = None if end is None else self._ids(end, "end", n)
-        L.check(L.lib().ewsjf_cache_release(self._c, self._ids(slot, "slot"), b, e, n, _stream(stream)),
+        L.check(L.lib().ewsjf_cache_release(self._c, self._ids(slot, "slot"), b, e, n, self._on(stream)),
                 "ewsjf_cache_release")
 
     def copy(self, src: torch.Tensor, dst: torch.Tensor, stream=None) -> None:
         """Pages src[j] to pages dst[j] in every layer (ewsjf_cache_copy)."""
         n = src.numel()
         L.check(L.lib().ewsjf_cache_copy(self._c, self._ids(src, "src"), self._ids(dst, "dst", n), n,
-                                         _stream(stream)), "ewsjf_cache_copy")
+                                         self._on(stream)), "ewsjf_cache_copy")
 
     def compact(self, out=None, ws: Workspace | None = None, stream=None):
         """Move the used pages to the front: (table, refs, used[1]) of the
@@ -159,17 +181,18 @@ class PagedCache:
             out = tuple(_new(stream, s, dtype=torch.int32, device=self.device)
                         for s in (self.table.shape, self.refs.shape, 1))
         table, refs, used = out
-        buf = _scratch(ws, self._ws_bytes, self.device, stream)
+        raw = self._on(stream)
+        buf = _scratch(ws, self._ws_bytes, self.device, raw, stream)
         L.check(L.lib().ewsjf_cache_compact(self._c, self._ids(table, "table", self.table.numel()),
                                             self._ids(refs, "refs", self.refs.numel()), self._ids(used, "used", 1),
-                                            buf.data_ptr(), buf.numel(), _stream(stream)), "ewsjf_cache_compact")
+                                            buf.data_ptr(), buf.numel(), raw), "ewsjf_cache_compact")
         return out
 
     def adopt(self, table: torch.Tensor, refs: torch.Tensor) -> None:
         """Take compact()'s table and refs as the cache's own."""
         self.c.table = self._ids(table, "table", self.table.numel())
         self.c.refs = self._ids(refs, "refs", self.refs.numel())
-        self.table, self.refs = table.view_as(self.table), refs
+        self.table, self.refs, self.used_on = table.view_as(self.table), refs, None
 
     def append(self, layer: int, k: torch.Tensor, v: torch.Tensor, slot: torch.Tensor, q_start: torch.Tensor,
                stream=None, *, granted: torch.Tensor | None = None) -> None:
@@ -187,7 +210,7 @@ class PagedCache:
         L.check(L.lib().ewsjf_cache_append_granted(self._c, int(layer), k.data_ptr(), v.data_ptr(), _stride(k, 0),
                                                    _stride(k, 1), _stride(v, 0), _stride(v, 1),
                                                    self._ids(slot, "slot"), self._ids(q_start, "q_start", n + 1), g,
-                                                   n, k.shape[0], _stream(stream)), "ewsjf_cache_append")
+                                                   n, k.shape[0], self._on(stream)), "ewsjf_cache_append")
 
 
 class AttentionPlan:
@@ -204,6 +227,7 @@ class AttentionPlan:
             raise ValueError("a batch of these sizes is not supported (see ewsjf_batch)")
         self.ws_bytes = int(lib.ewsjf_attention_workspace_bytes(cache._c, self._b))
         self.buf = _new(stream, nbytes, dtype=torch.uint8, device=cache.device)
+        self.used_on = _stream(stream)
 
 
 def prefix_plan(cache: PagedCache, slot: torch.Tensor, q_start: torch.Tensor, group_start: torch.Tensor | None,
@@ -218,7 +242,7 @@ def prefix_plan(cache: PagedCache, slot: torch.Tensor, q_start: torch.Tensor, gr
     plan = AttentionPlan(cache, L.Batch(n, groups, int(total_q), int(max_q), int(q_heads), 0, 0), stream)
     L.check(L.lib().ewsjf_prefix_plan(cache._c, plan._b, cache._ids(slot, "slot"),
                                       cache._ids(q_start, "q_start", n + 1), gs, sh, plan.buf.data_ptr(),
-                                      plan.buf.numel(), _stream(stream)), "ewsjf_prefix_plan")
+                                      plan.buf.numel(), cache._on(stream)), "ewsjf_prefix_plan")
     return plan
 
 
@@ -254,9 +278,11 @@ def attention(q: torch.Tensor, cache: PagedCache, layer: int, plan: AttentionPla
         lse = _new(stream, shape[:2], dtype=torch.float32, device=q.device)
     elif _need(lse, torch.float32, "lse").shape != q.shape[:2]:
         raise ValueError("lse is [total_q][q_heads]")
-    buf = _scratch(ws, plan.ws_bytes, cache.device, stream)
+    raw = cache._on(stream)
+    if raw != plan.used_on:
+        _keep(plan, raw, stream, plan.buf)
+    buf = _scratch(ws, plan.ws_bytes, cache.device, raw, stream)
     L.check(L.lib().ewsjf_attention(cache._c, plan._b, int(layer), q.data_ptr(), _stride(q, 0), _stride(q, 1),
                                     shape[2] ** -0.5 if scale is None else float(scale), plan.buf.data_ptr(),
-                                    out.data_ptr(), lse.data_ptr(), buf.data_ptr(), buf.numel(), _stream(stream)),
-            "ewsjf_attention")
+                                    out.data_ptr(), lse.data_ptr(), buf.data_ptr(), buf.numel(), raw), "ewsjf_attention")
     return out, lse

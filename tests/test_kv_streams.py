@@ -1,5 +1,6 @@
 """Memory of calls on another stream than the current one: what a call takes
-comes from that stream's memory."""
+comes from that stream's memory, and what it reads is not given away while the
+stream may still be at it."""
 import os
 import sys
 
@@ -39,6 +40,24 @@ class Case:
                              stream=stream)
 
 
+class Busy:
+    """A stream with work of many milliseconds before whatever is asked of it."""
+
+    def __init__(self):
+        self.stream = torch.cuda.Stream()
+        a = torch.randn((8192, 8192), device="cuda")
+        torch.cuda.synchronize()
+        with torch.cuda.stream(self.stream):
+            for _ in range(6):
+                a = a @ a * 1e-4
+            self.done = torch.cuda.Event()
+            self.done.record()
+        self.a = a
+
+    def later(self):
+        assert not self.done.query(), "the stream's work ended before the test's"
+
+
 def taken_again(tensor_bytes, ptr):
     """Whether memory of this size on the current stream is the memory at ptr; nothing is written there."""
     return torch.empty(tensor_bytes, dtype=torch.uint8, device="cuda").data_ptr() == ptr
@@ -62,6 +81,71 @@ def test_results_come_from_the_streams_memory(K):
         torch.cuda.synchronize()
         assert free, name
         del kept
+
+
+def test_a_plan_is_kept_for_the_stream_that_reads_it(K):
+    case = Case(K)
+    plan = case.plan(K)
+    torch.cuda.synchronize()
+    busy = Busy()
+    kept = K.attention(case.q, case.cache, 0, plan, stream=busy.stream)
+    size, ptr = plan.buf.numel(), plan.buf.data_ptr()
+    del plan
+    again = taken_again(size, ptr)
+    busy.later()
+    torch.cuda.synchronize()
+    assert not again
+    del kept
+
+
+def test_a_workspace_that_grows_is_kept_for_the_stream_that_uses_it(K):
+    case, ws = Case(K), K.Workspace()
+    plan = case.plan(K)
+    ws.get(plan.ws_bytes)  # taken on the current stream
+    torch.cuda.synchronize()
+    busy = Busy()
+    kept = K.attention(case.q, case.cache, 0, plan, ws=ws, stream=busy.stream)
+    size, ptr = ws.buf.numel(), ws.buf.data_ptr()
+    ws.get(2 * size)
+    again = taken_again(size, ptr)
+    busy.later()
+    torch.cuda.synchronize()
+    assert not again
+    # and one that grew on the other stream, used on the current one
+    ws = K.Workspace()
+    busy = Busy()
+    kept = K.attention(case.q, case.cache, 0, plan, ws=ws, stream=busy.stream)
+    torch.cuda.synchronize()
+    size, ptr = ws.buf.numel(), ws.buf.data_ptr()
+    work = Busy()
+    torch.cuda.current_stream().wait_event(work.done)
+    kept = K.attention(case.q, case.cache, 0, plan, ws=ws)
+    ws.get(2 * size)
+    with torch.cuda.stream(busy.stream):
+        again = taken_again(size, ptr)
+    work.later()
+    torch.cuda.synchronize()
+    assert not again
+    del kept
+
+
+def test_a_cache_is_kept_for_the_stream_that_reads_it(K):
+    case = Case(K, pages=4000, slots=20000)
+    plan = case.plan(K)
+    torch.cuda.synchronize()
+    busy = Busy()
+    kept = K.attention(case.q, case.cache, 0, plan, stream=busy.stream)
+    size, ptr = case.cache.data.numel() * 2, case.cache.data.data_ptr()
+    t_size, t_ptr = case.cache.table.numel() * 4, case.cache.table.data_ptr()
+    table, refs = case.cache.table.clone(), case.cache.refs.clone()
+    case.cache.adopt(table, refs)
+    t_again = taken_again(t_size, t_ptr)
+    case.cache = None
+    again = taken_again(size, ptr)
+    busy.later()
+    torch.cuda.synchronize()
+    assert not again and not t_again
+    del kept
 
 
 def test_other_streams_give_the_same(K):
