@@ -94,6 +94,7 @@ class PagedCache:
         self.data, self.refs, self.table, self.length = data, refs, table, length
         self.page_size, self.device, self.dtype = page_size, data.device, data.dtype
         self.used_on = None
+        self.sizes = (data.device, kv_heads, head_dim, page_size, *table.shape)  # what a plan's layout and slots follow
         self.c = L.Cache(data.data_ptr(), refs.data_ptr(), table.data_ptr(), length.data_ptr(), *[_stride(data, d) for d in range(5)],
                          layers, n_pages, page_size, kv_heads, head_dim, _DTYPES[data.dtype], *table.shape)
         self._c = _addr(self.c)
@@ -215,10 +216,12 @@ class PagedCache:
 
 class AttentionPlan:
     """What follows from a batch's lengths, on the device; serves every layer
-    of a step (prefix_plan, window_plan)."""
+    of a step (prefix_plan, window_plan), of its cache or of one with the same
+    sizes, slots and lengths."""
 
     def __init__(self, cache: PagedCache, batch: L.Batch, stream=None):
         self.b = batch
+        self.sizes = cache.sizes
         self.q_shape = (batch.total_q, batch.q_heads, cache.c.head_dim)
         self._b = _addr(batch)
         lib = L.lib()
@@ -267,6 +270,8 @@ def attention(q: torch.Tensor, cache: PagedCache, layer: int, plan: AttentionPla
     [total_q][q_heads] the ln of the softmax's sum (ewsjf_attention).  scale
     defaults to head_dim ** -0.5."""
     shape = plan.q_shape
+    if plan.sizes != cache.sizes:
+        raise ValueError("the plan is of a cache with other sizes")
     if not isinstance(q, torch.Tensor) or q.dtype != cache.dtype or q.device != cache.device or q.shape != shape \
             or q.stride(2) != 1:
         raise TypeError(f"q must be a CUDA tensor {shape} of the cache's type with contiguous dims")
