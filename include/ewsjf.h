@@ -592,7 +592,7 @@ ewsjf_status ewsjf_cache_append_granted(const ewsjf_cache* c, int32_t layer, con
 typedef struct {
   int32_t n_seqs;   /* 0 .. EWSJF_MAX_CACHE_BATCH */
   int32_t n_groups; /* shared prefixes, 0 .. n_seqs */
-  int64_t total_q;  /* query tokens of the batch, below 2^24 */
+  int64_t total_q;  /* query tokens of the batch, below 2^24; 0 without sequences */
   int32_t max_q;    /* at least the most query tokens of a sequence, >= 1: chooses the kernels */
   int32_t q_heads;  /* a multiple of kv_heads, at most 64 a key head */
   int32_t window;   /* visible tokens before and with the query; 0: all */

@@ -59,6 +59,7 @@ ewsjf_status cache_status(const ewsjf_cache* c) {
 bool batch_ok(const ewsjf_cache* c, const ewsjf_batch* b) {
   if (b->n_seqs < 0 || b->n_seqs > EWSJF_MAX_CACHE_BATCH || b->n_groups < 0 || b->n_groups > b->n_seqs) return false;
   if (b->total_q < 0 || b->total_q >= kMaxQ || b->max_q < 1) return false;
+  if (b->total_q > 0 && b->n_seqs == 0) return false;  // nobody's queries
   if (b->q_heads < 1 || b->q_heads % c->kv_heads || b->q_heads / c->kv_heads > kMaxGroup) return false;
   if (b->window < 0 || b->sinks < 0 || (b->window == 0 && b->sinks > 0)) return false;
   if (b->window > 0 && b->n_groups > 0) return false;

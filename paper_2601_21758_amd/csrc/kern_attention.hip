@@ -1612,7 +1612,7 @@ hipError_t launch_attention_plan(const ewsjf_cache& c, const ewsjf_batch& b, con
 hipError_t launch_attention(const ewsjf_cache& c, const ewsjf_batch& b, int32_t layer, const void* q, int64_t q_token,
                             int64_t q_head, float scale, const void* plan, void* out, float* lse, void* ws,
                             hipStream_t stream) {
-  if (b.total_q == 0 || b.n_seqs == 0) return hipSuccess;
+  if (b.total_q == 0) return hipSuccess;
   auto go = [&](auto run) { return run(c, b, layer, q, q_token, q_head, scale, plan, out, lse, ws, stream); };
   if (c.dtype == EWSJF_BF16) return c.head_dim == 64 ? go(launch_typed<__bf16, 64>) : go(launch_typed<__bf16, 128>);
   return c.head_dim == 64 ? go(launch_typed<_Float16, 64>) : go(launch_typed<_Float16, 128>);

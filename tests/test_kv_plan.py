@@ -48,3 +48,23 @@ def test_a_plan_of_another_cache(K):
         c.adopt(table, refs)
         for x, y in zip(K.attention(q, c, 0, plan), want):
             assert torch.equal(x, y)
+
+
+def test_queries_without_sequences():
+    """No sequence could answer them: refused before anything is written or left unwritten."""
+    import ctypes as C
+    from paper_2601_21758_amd import _lib as L
+    if not os.path.exists(L.LIB_PATH):
+        pytest.skip("libewsjf.so not built")
+    lib, fake = L.lib(), 0x10000
+    c = L.Cache(fake, fake, fake, fake, 40960, 20480, 2048, 1024, 64, 2, 10, 16, 2, 64, L.BF16, 4, 5)
+    a = C.addressof(c)
+    for total, window, groups in ((1, 0, 0), (7, 5, 0)):
+        b = L.Batch(0, groups, total, 1, 8, window, 0)
+        p = C.addressof(b)
+        assert lib.ewsjf_attention_plan_bytes(a, p) == lib.ewsjf_attention_workspace_bytes(a, p) == 0
+        assert lib.ewsjf_prefix_plan(a, p, fake, fake, fake, fake, fake, 1 << 30, None) == L.ERR_ARG
+        assert lib.ewsjf_window_plan(a, p, fake, fake, fake, 1 << 30, None) == L.ERR_ARG
+        assert lib.ewsjf_attention(a, p, 0, fake, 512, 64, 0.125, fake, fake, fake, fake, 1 << 30, None) == L.ERR_ARG
+    b = L.Batch(0, 0, 0, 1, 8, 0, 0)
+    assert lib.ewsjf_attention_plan_bytes(a, C.addressof(b)) > 0
