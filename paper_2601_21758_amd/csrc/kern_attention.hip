@@ -47,6 +47,8 @@ constexpr int kWaves = 4;        // waves of a workgroup of the wave kernel
 constexpr int kCUs = 256;
 constexpr int64_t kMostJoins = 1 << 24;  // waves of a grid's row: a launch has below 2^32 threads in one
 constexpr int kWholeKeys = 2048;   // of a unit that one workgroup takes whole
+// Position of a shared phase's first query, past every shared key; its other tokens' do not pass 32 bits.
+constexpr int kPast = 0x7fffffff - (1 << 24);
 constexpr float kFloor = -3e38f;   // running maximum of a row that has seen no key
 constexpr float kLn2 = 0.6931471805599453f;
 constexpr float kLog2e = 1.4426950408889634f;
@@ -340,7 +342,7 @@ __global__ __launch_bounds__(kPlanThreads) void make_plan(ewsjf_cache c, ewsjf_b
   };
   for (int g = threadIdx.x; g < groups; g += kPlanThreads) {
     const int v = a.shared[g];
-    common[g] = v < 0 ? 0 : v;
+    common[g] = v < 0 ? 0 : v < kPast ? v : kPast;
     lead[g] = n;
     members[g] = 0;
   }
@@ -393,7 +395,7 @@ __global__ __launch_bounds__(kPlanThreads) void make_plan(ewsjf_cache c, ewsjf_b
         if (ph == 0) {
           x.slot = a.slot[lead[i]];
           x.q0 = (int)q_at(group_at(i));
-          x.pos0 = 1 << 30;
+          x.pos0 = kPast;
           x.end = common[i];
           x.prefix = -1;
         } else {
