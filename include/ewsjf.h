@@ -585,7 +585,8 @@ ewsjf_status ewsjf_cache_append_granted(const ewsjf_cache* c, int32_t layer, con
  * over the visible keys; a query that sees none has out 0 and lse -inf.
  * Products of 16-bit inputs are summed in binary32, so are the softmax's sum
  * and the output, rounded once at the end; the weights are rounded to 16 bits
- * for the product with the values.
+ * for the product with the values (in float16 to 2^-33 of the largest at
+ * least).
  *
  * A plan holds what follows from the batch's lengths: made once a step, it
  * serves every layer, until a length or a batch member changes. */
