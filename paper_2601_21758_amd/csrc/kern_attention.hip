@@ -28,8 +28,8 @@
 // (prefill, many requests behind one prefix) the matrix units are; hence two
 // kernels.  What they reach on the card, whose large copies run at 4.8 TB/s
 // (read and written) and whose large 16-bit products at 1270 TFLOP/s:
-//   one prompt of 16,384 tokens, 40 heads of 128, window 4096: 1.5 ms, 800
-//   TFLOP/s; 256 single tokens of 32 query and 8 key heads of 128 over windows
+//   one prompt of 16,384 tokens, 40 heads of 128, window 4096: 1.5 to 1.6 ms,
+//   770 to 800 TFLOP/s; 256 single tokens of 32 query and 8 key heads of 128 over windows
 //   of 4096: 194 us, 5.0 TB/s.
 #include <hip/hip_runtime.h>
 
@@ -132,7 +132,7 @@ struct Shape {
 Shape shape_of(const ewsjf_cache& c, const ewsjf_batch& b) {
   Shape s;
   s.G = b.q_heads / c.kv_heads;
-  const int64_t most_keys = (int64_t)c.width * c.page_size;  // of a sequence
+  const int64_t most_keys = (int64_t)c.width * c.page_size;  // of a sequence: lengths are on the device
   // Sharing pays when the keys and values that each sequence would read for itself (much of it from caches) take longer
   // than the phase and the join.  32 query and 8 key heads of 128, shared against not: 16 sequences behind 1024 tokens
   // (66 MiB) 20 us against 17, 64 behind 1024 (264 MiB) 25 against 33, 16 behind 4096 (258 MiB) 26 against 34.  With at
@@ -160,11 +160,11 @@ Shape shape_of(const ewsjf_cache& c, const ewsjf_batch& b) {
   }
   if (!s.groups) s.entries[0] = 0;
   s.kv_heads = c.kv_heads;
-  // One token a sequence and few keys: a workgroup takes a unit sooner than a second kernel joins its parts.  8 key heads
-  // of 128, whole against cut: 16 sequences of 1024 keys 17 us against 28, 256 of 1024 191 against 204, 8 of 2048 25
-  // against 30, 128 of 2048 190 against 202, but 32 of 2048 59 against 55; 16 of 4096 44 against 40, 256 of 4096 457
-  // against 440.  With one token, no row sees less of a unit than
-  // another, so no row is done again either.
+  // One token a sequence and few keys: a workgroup takes a unit sooner than a second kernel joins its parts.  32 query and
+  // 8 key heads of 128, whole against cut: 16 sequences of 1024 keys 16 us against 24, 256 of 1024 189 against 187, 8 of
+  // 2048 24 against 29, 128 of 2048 190 against 193, but 32 of 2048 56 against 50; 16 of 4096 45 against 52, 64 of 4096
+  // 205 against 194, 128 of 4096 374 against 371, 256 of 4096 729 against 715.  With one token, no row sees less of a unit
+  // than another, so no row is done again either.
   const int64_t keys = b.window > 0 && (int64_t)b.window + b.sinks < most_keys ? (int64_t)b.window + b.sinks : most_keys;
   const int64_t units = s.entries[1] * c.kv_heads;
   s.whole = !s.groups && s.waves[1] == 0 && b.max_q == 1 && keys <= kWholeKeys;
@@ -308,8 +308,9 @@ struct PlanArgs {
 };
 
 // One workgroup, latency-bound: prefix sums over the row tiles and a search a
-// worker.  11 us for 4 sequences, 27 us for 512 behind a prefix and 24 us for
-// the 2560 units of one long prompt; once a step, whatever the layers.
+// worker.  14 us for 4 sequences, 27 us for 512 behind a prefix and 25 us for
+// the 2560 units of one long prompt, as long as the smallest attention or
+// longer; once a step, whatever the layers.
 // Everything read from the caller's arrays is bounded here, so the other
 // kernels follow the plan without checks of their own.
 __global__ __launch_bounds__(kPlanThreads) void make_plan(ewsjf_cache c, ewsjf_batch b, PlanArgs a, Plan plan) {
@@ -1421,7 +1422,8 @@ __device__ void part_at(const Parts& p, const Cut& u, int i, int tile_rows, int 
 
 // A row's output again, key by key, without the keys that it does not see: the
 // products of whole tiles take a weight of 0 times a value, which is not 0
-// where the value is not finite.  lse2: the row's lse in the exponent's units.
+// where the value is not finite.  Its weights keep 32 bits, so the row's last bits
+// may differ from those of the tiles.  lse2: the row's lse in the exponent's units.
 template <typename T, int D>
 __device__ void redo_row(const Args<T>& a, const Entry& x, int head, int row, float lse2) {
   const int lane = threadIdx.x & 63;

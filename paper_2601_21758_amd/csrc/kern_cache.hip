@@ -261,7 +261,7 @@ __global__ __launch_bounds__(kThreads) void apply_growth(ewsjf_cache c, CacheWs 
 }
 
 // count_pages and pick_pages of a small pool; for few requests of new tokens
-// their rows too. 
+// their rows too.
 __global__ __launch_bounds__(kSmallThreads) void grow_small(ewsjf_cache c, CacheWs w, const int32_t* parent,
                                                             const int32_t* slot, const int32_t* tokens, int n,
                                                             int32_t* granted, bool rows) {
@@ -403,8 +403,8 @@ __global__ __launch_bounds__(kThreads) void move_pages(ewsjf_cache c, CacheWs w,
   }
 }
 
-// One workgroup a token: its heads' keys and values into the slot's page.  3 us
-// for 8 tokens, a launch; the search for the sequence is its longest part.
+// One workgroup a token: its heads' keys and values into the slot's page.  3.8
+// us for 8 tokens, a launch; the search for the sequence is its longest part.
 // Without grants a request may be one that found no room: its tokens would then
 // land on tokens that it holds already.  A partial page is the slot's own, a
 // whole one may be others' too, and two requests could write it at once; so a
