@@ -5,16 +5,17 @@ admits, on the same card and stream.
 
     cache = kv.PagedCache.new(layers, n_pages, page_size, kv_heads, head_dim, n_slots, width)
     granted = cache.fork(parent, child, tokens)     # a prompt's pages shared, its partial page copied
-    granted = cache.extend(slot, tokens)            # pages for new tokens
-    cache.append(layer, k, v, slot, q_start, granted=granted)  # their keys and values
+    slot = torch.where(granted > 0, child, -1)      # a refused request has no slot in what follows
+    granted = cache.extend(slot, new)               # pages for new tokens
+    slot = torch.where(granted > 0, slot, -1)
     plan = kv.prefix_plan(cache, slot, q_start, group_start, shared, total_q=.., max_q=.., q_heads=..)
-    out, lse = kv.attention(q, cache, layer, plan)  # every layer of the step with the same plan
-    cache.release(slot)
+    cache.append(layer, k, v, slot, q_start, granted=granted)  # every layer: the new tokens' keys and values,
+    out, lse = kv.attention(q, cache, layer, plan)             # and their queries, with the same plan
+    cache.release(child)
 
 Nothing here synchronizes the host; a request that does not fit the pool is
-told by granted == 0 on the device.  append writes nothing for it, and a slot
-of -1 (torch.where(granted > 0, slot, -1)) leaves it out of a plan: its
-queries get out 0 and lse -inf.
+told by granted == 0 on the device.  A slot of -1 is refused, written nowhere
+and released as nothing; its queries get out 0 and lse -inf.
 """
 from __future__ import annotations
 

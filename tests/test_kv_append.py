@@ -110,6 +110,44 @@ def test_forked_before_it_is_written(K):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("spare", [0, 3, 7, 11, 40])
+def test_refused_requests_have_no_slot(K, spare):
+    """A step whose pool runs out in the fork or in the extend: refused requests hold, write and see nothing, the others
+    what the definition says."""
+    page, n, new, heads, D = 16, 8, 3, 2, 64
+    c, r = make(K, 3 + spare, page, n + 1, 6, heads=heads, D=D, seed=spare)
+    c.extend(ints([0]), ints([47])), r.extend([0], [47])
+    child, t = list(range(1, n + 1)), [47, 40, 32, 20, 47, 46, 16, 35]
+    granted = c.fork(ints([0] * n), ints(child), ints(t))
+    forked = r.fork([0] * n, child, t)
+    assert granted.tolist() == forked
+    slot = torch.where(granted > 0, ints(child), -1)
+    granted = c.extend(slot, ints([new] * n))
+    held = [s if ok else -1 for s, ok in zip(child, forked)]
+    want = r.extend(held, [new] * n)
+    assert granted.tolist() == want
+    slot, held = torch.where(granted > 0, slot, -1), [s if ok else -1 for s, ok in zip(held, want)]
+    q_start = np.arange(n + 1) * new
+    x = torch.randn((n * new, 4 * heads, D), device="cuda").half()
+    k, v, q = x[:, :heads], x[:, heads:2 * heads], x[:, 2 * heads:]
+    plan = K.prefix_plan(c, slot, ints(q_start), ints([0, n]), ints([16]), total_q=n * new, max_q=new, q_heads=2 * heads)
+    c.append(0, k, v, slot, ints(q_start), granted=granted)
+    host = [y.cpu().float().numpy() for y in (k, v)]
+    append(r, 0, *host, held, [new] * n, want)
+    same(c, r)
+    out, lse = K.attention(q, c, 0, plan)
+    ref = kv_ref.attention(q.cpu().double().numpy(), r.data[0].astype(np.float64), r.table, r.length, held, q_start, page,
+                           D ** -0.5)
+    b_out, b_lse = kv_ref.bounds(*ref, 2.0 ** -11, 50, float(np.abs(r.data).max()), D)
+    fine = np.isfinite(ref[1])
+    assert fine.any() == (sum(want) > 0) and np.array_equal(np.isfinite(lse.cpu().numpy()), fine)
+    assert np.all(np.abs(out.cpu().double().numpy() - ref[0]) <= b_out) and not out[~torch.tensor(fine)].any()
+    assert np.all(np.abs(lse.cpu().double().numpy()[fine] - ref[1][fine]) <= b_lse[fine])
+    c.release(slot), r.release(held)
+    same(c, r)
+
+
+@pytest.mark.gpu
 def test_grants_are_checked(K):
     c, _ = make(K, 10, 4, 6, 10)
     x = torch.zeros((1, 2, 8), dtype=torch.float16, device="cuda")
