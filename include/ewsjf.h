@@ -609,9 +609,10 @@ size_t ewsjf_attention_workspace_bytes(const ewsjf_cache* c, const ewsjf_batch* 
  * their first shared[g] tokens: the rows of their slots name the same pages
  * there (as forks leave them) or pages with the same contents.  Shared keys
  * are read once for the group, from the row of its first member that has
- * queries; a small batch, a group with fewer than two such members, and the
- * tokens after the last multiple of 16 are read member by member.  Of
- * shared[g] counts at most the tokens before every member's first query.
+ * queries and a slot; a small batch, a group with fewer than two such members,
+ * and the tokens after the last multiple of 16 are read member by member.  Of
+ * shared[g] counts at most the tokens before the first query of each of them;
+ * a member without a slot (outside [0, n_slots)) sees nothing.
  * n_groups = 0: nothing is shared.  window and sinks are 0.  slot, q_start,
  * group_start, shared: device int32 [n_seqs], [n_seqs + 1], [n_groups + 1],
  * [n_groups]; starts ascend, to total_q and n_seqs (one that falls back or

@@ -318,7 +318,7 @@ __global__ __launch_bounds__(kPlanThreads) void make_plan(ewsjf_cache c, ewsjf_b
   __shared__ int64_t sums[kPlanThreads / 64];
   __shared__ int first[kMost + 1];  // first row tile of a sequence or group
   __shared__ int common[kMost];     // a group's shared tokens that count
-  __shared__ int lead[kMost];       // its first member with queries
+  __shared__ int lead[kMost];       // its first member with queries and a slot
   __shared__ int members[kMost];
   __shared__ int q_from[kMost + 1];
   __shared__ int g_from[kMost + 1];
@@ -329,10 +329,10 @@ __global__ __launch_bounds__(kPlanThreads) void make_plan(ewsjf_cache c, ewsjf_b
   __syncthreads();
   auto q_at = [&](int i) -> int64_t { return q_from[i]; };
   auto queries = [&](int i) { return q_at(i + 1) - q_at(i); };
+  auto has_slot = [&](int i) { return a.slot[i] >= 0 && a.slot[i] < c.n_slots; };
   auto tokens = [&](int i) -> int64_t {
-    const int s = a.slot[i];
-    if (s < 0 || s >= c.n_slots) return 0;
-    const int64_t v = c.length[s];
+    if (!has_slot(i)) return 0;
+    const int64_t v = c.length[a.slot[i]];
     return v < 0 ? 0 : v > room ? room : v;
   };
   auto group_at = [&](int g) { return g_from[g]; };
@@ -350,7 +350,7 @@ __global__ __launch_bounds__(kPlanThreads) void make_plan(ewsjf_cache c, ewsjf_b
   __syncthreads();
   for (int i = threadIdx.x; i < n; i += kPlanThreads) {
     const int g = group_of(i);
-    if (g < 0 || queries(i) == 0) continue;
+    if (g < 0 || queries(i) == 0 || !has_slot(i)) continue;
     const int64_t before = tokens(i) - queries(i);
     atomicMin(&common[g], (int)(before < 0 ? 0 : before));
     atomicMin(&lead[g], i);
@@ -401,10 +401,9 @@ __global__ __launch_bounds__(kPlanThreads) void make_plan(ewsjf_cache c, ewsjf_b
           x.prefix = -1;
         } else {
           const int g = group_of(i);
-          const int shared = g < 0 ? 0 : common[g];
-          const int s = a.slot[i];
+          const int shared = g < 0 || !has_slot(i) ? 0 : common[g];
           const int64_t len = tokens(i);
-          x.slot = s < 0 || s >= c.n_slots ? -1 : s;
+          x.slot = has_slot(i) ? a.slot[i] : -1;
           x.q0 = (int)q_at(i);
           x.pos0 = (int)(len - queries(i));
           const int p0 = x.pos0 + x.row0 / a.G, p1 = x.pos0 + (x.row0 + x.rows - 1) / a.G;

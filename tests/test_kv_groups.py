@@ -104,6 +104,19 @@ def test_more_queries_than_tokens_and_slots_outside(K, heavy):
 
 
 @HEAVY
+@pytest.mark.parametrize("out", [[0], [2], [0, 1, 5], [0, 1, 2, 3, 4]])
+def test_members_without_slots_leave_the_rest_sharing(K, heavy, out):
+    """Requests that found no room have no slot: they see nothing, and the others share all the same."""
+    b = widen(Batch(59, "bf16", 128, 2, 4, 16, [250, 233, 264, 300, 270, 241], [1, 2, 1, 30, 1, 1],
+                    shared=[(6, 224)]), heavy)
+    b.slot[out] = [-1, b.n_slots, -7, 2 ** 31 - 1, -2 ** 31][:len(out)]
+    check(K, b)
+    _, plan, _ = plans(K, b)
+    tiles = int(plan.buf[:8].view(torch.int64))  # a plan begins with the shared phase's tiles
+    assert (tiles > 0) == (len(out) < 5)
+
+
+@HEAVY
 def test_many_members(K, heavy):
     """More rows than a tile in one group."""
     n = 150
