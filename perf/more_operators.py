@@ -554,7 +554,7 @@ def _plain_reorder(s):
     source = rows[parent].gather(1, last.clamp(max=rows.shape[1] - 1)[:, None])[:, 0].long()
     need = (heir[parent] != me) & ((lens % ps)[parent] > 0) & (source >= 0)
     free = torch.nonzero(refs == 0).flatten()
-    ok = torch.cumsum(need.long(), 0) <= free.numel()
+    ok = ~need | (torch.cumsum(need.long(), 0) <= free.numel())
     row = torch.where(torch.arange(rows.shape[1], device="cuda") < ((lens + ps - 1) // ps)[parent][:, None],
                       rows[parent], -1)
     copied = (need & ok).nonzero().flatten()
