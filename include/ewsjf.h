@@ -483,6 +483,18 @@ ewsjf_status ewsjf_tactical_step(int32_t* len, const float* arrival, int64_t n, 
  * head_dim).  data is 16-byte aligned, the outer strides are multiples of 8
  * and blocks do not overlap.
  *
+ * 8 bits (EWSJF_E4M3_BF16, EWSJF_E4M3_F16): an element is a byte, the e4m3 code
+ * (sign, 4 bits of exponent, 3 of mantissa, largest 448, no infinity, 0x7f NaN)
+ * of a value over a power of two that a token's head_dim elements of a head
+ * have in common; every stride is in bytes.  A page's block holds the codes, as
+ * above, and behind them a byte b for each head and token, at kv_heads *
+ * page_size * head_dim + head * page_size + token: a code c stands for the
+ * value c 2^(b - 127), which the 16-bit type of the name holds.  Blocks are
+ * kv_heads * page_size * (head_dim + 1) bytes up to a multiple of 16
+ * (ewsjf_cache_page_bytes), head_dim and the outer strides multiples of 16.
+ * Keys and values that are written and read, queries and outputs have that
+ * 16-bit type.
+ *
  * Requests of one call name distinct slots, and a child slot of a fork is not
  * a parent in the same call.  Slots outside [0, n_slots) are refused.
  * Requests are served in order: with need_i pages for request i, request i is
@@ -495,7 +507,7 @@ enum {
   EWSJF_MAX_PAGE_SIZE = 1024,      /* tokens per page (a power of two) */
   EWSJF_MAX_HEAD_DIM = 256         /* of a cache; ewsjf_attention has 64 and 128 */
 };
-enum { EWSJF_BF16 = 0, EWSJF_F16 = 1 };
+enum { EWSJF_BF16 = 0, EWSJF_F16 = 1, EWSJF_E4M3_BF16 = 8, EWSJF_E4M3_F16 = 9 };
 
 typedef struct {
   void* data;
@@ -510,6 +522,10 @@ typedef struct {
 /* Workspace of ewsjf_cache_extend, _fork and _compact (0 for a cache that
  * they refuse). */
 size_t ewsjf_cache_workspace_bytes(const ewsjf_cache* c);
+
+/* Bytes of a page's keys, or of its values, in one layer (0 for sizes that are
+ * refused). */
+size_t ewsjf_cache_page_bytes(int32_t page_size, int32_t kv_heads, int32_t head_dim, int32_t dtype);
 
 /* Room for tokens[i] >= 0 more tokens in slot[i]: its row gets ceil((length +
  * tokens) / page_size) - ceil(length / page_size) pages and its length grows.
@@ -563,7 +579,13 @@ ewsjf_status ewsjf_cache_compact(const ewsjf_cache* c, int32_t* out_table, int32
  * ewsjf_cache_append (granted == NULL there) is for requests that were all
  * granted, written before their slots are forked.  The tokens of a refused
  * one replace the last that its slot holds; but a whole page that other rows
- * hold too is not written, so no other slot reads anything else. */
+ * hold too is not written, so no other slot reads anything else.
+ *
+ * An 8-bit cache gets, of a token's head_dim elements x of a head, the codes of
+ * x / 2^e rounded to nearest even, 2^e the smallest power of two, at least
+ * 2^-117, with |x| <= 448 2^e for all of them.  A magnitude above 1.875 2^127
+ * (bfloat16) or 61440 (float16), an infinity among them, counts as that, the
+ * largest whose value the type holds; a NaN stays one and does not count. */
 ewsjf_status ewsjf_cache_append(const ewsjf_cache* c, int32_t layer, const void* k, const void* v,
                                 int64_t k_token_stride, int64_t k_head_stride, int64_t v_token_stride,
                                 int64_t v_head_stride, const int32_t* slot, const int32_t* q_start, int32_t n_seqs,
@@ -572,6 +594,74 @@ ewsjf_status ewsjf_cache_append_granted(const ewsjf_cache* c, int32_t layer, con
                                         int64_t k_token_stride, int64_t k_head_stride, int64_t v_token_stride,
                                         int64_t v_head_stride, const int32_t* slot, const int32_t* q_start,
                                         const int32_t* granted, int32_t n_seqs, int64_t total, hipStream_t stream);
+
+/* Reads keys and values of one layer.  Sequence s (slot[s]) has the rows
+ * [start[s], start[s + 1]) of k and v (device, 16-bit [total][kv_heads]
+ * [head_dim], dense, 16-byte aligned); row i of it gets token begin[s] + i of the
+ * slot (begin NULL: 0), in 16 bits.  Tokens that the slot does not hold or
+ * has no page for, and the rows of a slot outside [0, n_slots), are 0; rows
+ * past the last sequence's stay as they are.  start: device int32 [n_seqs + 1],
+ * ascending from 0 to at most total. */
+ewsjf_status ewsjf_cache_read(const ewsjf_cache* c, int32_t layer, const int32_t* slot, const int32_t* start,
+                              const int32_t* begin, int32_t n_seqs, int64_t total, void* k, void* v,
+                              hipStream_t stream);
+
+/* slot[i] := what slot[parent[i]] held before the call, for all i at once: the
+ * beams of a search after a selection.  parent[i] counts in the call's own list;
+ * with a parent outside [0, n), or one whose slot is outside [0, n_slots), the
+ * slot is emptied.  Of the requests that name a parent one takes over its row as
+ * it is, the parent itself if it is among them, else the first; the others share its
+ * whole pages (refs + 1) and take a copy of its partial last page, in every
+ * layer, on a page of their own.  The pages of slots that nobody names are
+ * given up first.  Copies are granted in order as long as the free pages
+ * last, lowest pages first; a slot whose copy is refused is emptied.
+ * granted[i] (device int32 [n]) = 1 if the slot holds its parent's tokens, else
+ * 0.  0 <= n <= EWSJF_MAX_CACHE_BATCH. */
+size_t ewsjf_cache_reorder_workspace_bytes(const ewsjf_cache* c, int32_t n);
+ewsjf_status ewsjf_cache_reorder(const ewsjf_cache* c, const int32_t* slot, const int32_t* parent, int32_t n,
+                                 int32_t* granted, void* ws, size_t ws_bytes, hipStream_t stream);
+
+/* ---------------------------------------------------------------------------
+ * The next tokens of a beam search.
+ *
+ * Row r = g * beams + b is beam b of group g.  Its candidates are the tokens
+ * v of [0, vocab) with
+ *   score = score_in[r] + x[r][v] - ln sum_u exp x[r][u],
+ * in binary64 from the logits as they are.  A row with done[r] != 0 has one, `end`, with
+ * score_in[r] itself (its logits are not read).  A logit of NaN counts as -inf;
+ * entries of +inf share their row's probability; a score of NaN counts as -inf, and a score of
+ * -inf is no candidate.
+ *
+ * For each group the `picks` best of its rows' candidates: higher scores first,
+ * of equal scores the lower row, in a row the higher logit, of equal logits the lower
+ * token.  parent (the row r), token and score (rounded to binary32): device
+ * [groups][picks], -1, -1 and -inf where there are no more candidates.
+ *
+ * logits: device, of `dtype`, rows row_stride elements apart, aligned to its elements.
+ * score_in: device float [groups * beams].  done: device int32 [groups * beams]
+ * or NULL, with 0 <= end < vocab. */
+enum { EWSJF_F32 = 2 }; /* logits: EWSJF_BF16, EWSJF_F16 or this */
+enum {
+  EWSJF_MAX_BEAMS = 32,     /* beams of a group */
+  EWSJF_MAX_PICKS = 64,     /* picks of a group */
+  EWSJF_MAX_VOCAB = 1 << 22 /* tokens */
+};
+
+typedef struct {
+  int32_t groups;     /* 0 .. EWSJF_MAX_CACHE_BATCH */
+  int32_t beams;      /* groups * beams <= EWSJF_MAX_CACHE_BATCH */
+  int32_t picks;
+  int32_t vocab;
+  int32_t dtype;
+  int32_t end;
+  int64_t row_stride; /* at least vocab */
+} ewsjf_beams;
+
+/* Workspace of ewsjf_beam_select (0 for sizes that are refused). */
+size_t ewsjf_beam_workspace_bytes(const ewsjf_beams* b);
+ewsjf_status ewsjf_beam_select(const ewsjf_beams* b, const void* logits, const float* score_in, const int32_t* done,
+                               int32_t* parent, int32_t* token, float* score, void* ws, size_t ws_bytes,
+                               hipStream_t stream);
 
 /* ---------------------------------------------------------------------------
  * Attention over the cache.

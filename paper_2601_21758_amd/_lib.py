@@ -27,10 +27,13 @@ EXPORTED = ("ewsjf_queue_table_bytes", "ewsjf_workspace_bytes", "ewsjf_table_upl
             "ewsjf_status_string", "ewsjf_version", "ewsjf_step_static",
             "ewsjf_cache_workspace_bytes", "ewsjf_cache_extend", "ewsjf_cache_fork", "ewsjf_cache_release",
             "ewsjf_cache_copy", "ewsjf_cache_compact", "ewsjf_cache_append", "ewsjf_cache_append_granted",
-            "ewsjf_attention_plan_bytes", "ewsjf_attention_workspace_bytes", "ewsjf_prefix_plan", "ewsjf_window_plan", "ewsjf_attention")
+            "ewsjf_attention_plan_bytes", "ewsjf_attention_workspace_bytes", "ewsjf_prefix_plan", "ewsjf_window_plan", "ewsjf_attention",
+            "ewsjf_cache_page_bytes", "ewsjf_cache_read", "ewsjf_cache_reorder_workspace_bytes", "ewsjf_cache_reorder",
+            "ewsjf_beam_workspace_bytes", "ewsjf_beam_select")
 STATIC_SCRATCH_BYTES = 4 << 20
 MAX_CACHE_BATCH, MAX_PAGES, MAX_PAGE_SIZE, MAX_HEAD_DIM = 4096, 1 << 24, 1024, 256
-BF16, F16 = 0, 1
+BF16, F16, F32, E4M3_BF16, E4M3_F16 = 0, 1, 2, 8, 9
+MAX_BEAMS, MAX_PICKS, MAX_VOCAB = 32, 64, 1 << 22
 
 
 class PartitionParams(C.Structure):
@@ -63,6 +66,11 @@ class Cache(C.Structure):
 class Batch(C.Structure):
     _fields_ = [("n_seqs", C.c_int32), ("n_groups", C.c_int32), ("total_q", C.c_int64), ("max_q", C.c_int32),
                 ("q_heads", C.c_int32), ("window", C.c_int32), ("sinks", C.c_int32)]
+
+
+class Beams(C.Structure):
+    _fields_ = [("groups", C.c_int32), ("beams", C.c_int32), ("picks", C.c_int32), ("vocab", C.c_int32),
+                ("dtype", C.c_int32), ("end", C.c_int32), ("row_stride", C.c_int64)]
 
 
 class EwsjfError(RuntimeError):
@@ -141,6 +149,18 @@ def lib():
         L.ewsjf_cache_append.restype = C.c_int
         L.ewsjf_cache_append_granted.argtypes = [vp, i32, vp, vp, i64, i64, i64, i64, vp, vp, vp, i32, i64, vp]
         L.ewsjf_cache_append_granted.restype = C.c_int
+        L.ewsjf_cache_page_bytes.argtypes = [i32, i32, i32, i32]
+        L.ewsjf_cache_page_bytes.restype = sz
+        L.ewsjf_cache_read.argtypes = [vp, i32, vp, vp, vp, i32, i64, vp, vp, vp]
+        L.ewsjf_cache_read.restype = C.c_int
+        L.ewsjf_cache_reorder_workspace_bytes.argtypes = [vp, i32]
+        L.ewsjf_cache_reorder_workspace_bytes.restype = sz
+        L.ewsjf_cache_reorder.argtypes = [vp, vp, vp, i32, vp, vp, sz, vp]
+        L.ewsjf_cache_reorder.restype = C.c_int
+        L.ewsjf_beam_workspace_bytes.argtypes = [vp]
+        L.ewsjf_beam_workspace_bytes.restype = sz
+        L.ewsjf_beam_select.argtypes = [vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
+        L.ewsjf_beam_select.restype = C.c_int
         L.ewsjf_attention_plan_bytes.argtypes = [vp, vp]
         L.ewsjf_attention_plan_bytes.restype = sz
         L.ewsjf_attention_workspace_bytes.argtypes = [vp, vp]

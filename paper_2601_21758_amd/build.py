@@ -21,7 +21,8 @@ BUILD = os.path.join(PKG, "_build")
 LIB_STAMPS = os.path.join(PKG, "libewsjf_stamps.so")
 BUILD_STAMPS = os.path.join(PKG, "_build_stamps")
 SOURCES = ["abi.hip", "kern_policy.hip", "kern_select.hip", "kern_partition.hip", "kern_tactical.hip",
-           "kern_dispatch.hip", "kern_trial.hip", "abi_cache.hip", "kern_cache.hip", "kern_attention.hip"]
+           "kern_dispatch.hip", "kern_trial.hip", "abi_cache.hip", "kern_cache.hip", "kern_codes.hip", "kern_beam.hip",
+           "kern_attention.hip"]
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-ffp-contract=off",

@@ -34,6 +34,7 @@
 #include <hip/hip_runtime.h>
 
 #include "ewsjf_cache.h"
+#include "ewsjf_codes.h"
 
 namespace ewsjf {
 namespace {
@@ -139,7 +140,7 @@ Shape shape_of(const ewsjf_cache& c, const ewsjf_batch& b) {
   // most 32 rows a group, in two kernels: 4 behind 4096 (64 MiB) 40 against 31, 4 behind 16,000 (250 MiB) 64 against 65;
   // 8 of 40 heads behind 1024 (165 MiB) 34 against 22.
   const int64_t rows = b.n_groups > 0 ? b.total_q * s.G / b.n_groups : 0;
-  const int64_t bytes = 4 * most_keys * b.n_seqs * c.kv_heads * c.head_dim;
+  const int64_t bytes = 2 * cache_element_bytes(c) * most_keys * b.n_seqs * c.kv_heads * c.head_dim;
   s.groups = rows > 0 && bytes > (rows > kRowTile ? (int64_t)128 << 20 : (int64_t)256 << 20);
   // rows that read the same keys: of a group on average, of a sequence
   const int64_t most[2] = {s.groups ? rows : 0, (int64_t)b.max_q * s.G};
@@ -487,9 +488,6 @@ template <int N>
 struct Const {
   static constexpr int value = N;
 };
-template <typename T>
-using vec8 = T __attribute__((ext_vector_type(8)));
-
 __device__ float16v mfma(vec8<__bf16> a, vec8<__bf16> b, float16v c) {
   return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0);
 }
@@ -529,6 +527,7 @@ __device__ int fresh(int x) {
   return x;
 }
 
+__device__ uint32_t nan_codes(uint32_t x) { return ((x & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u; }
 __device__ uint32_t not_finite(uint32_t x, __bf16) { return ((x & 0x7f807f80u) + 0x00800080u) & 0x80008000u; }
 __device__ uint32_t not_finite(uint32_t x, _Float16) { return ((x & 0x7c007c00u) + 0x04000400u) & 0x80008000u; }
 
@@ -572,13 +571,14 @@ __device__ void next_unit(const Plan& plan, const Phase& ph, int units, int& pla
 
 template <typename T>
 struct Args {
-  const T* data;  // the layer's keys
+  const char* data;  // the layer's keys
   const T* q;
   int64_t q_token, q_head;
   const int32_t* table;
   T* out;
   float* lse;
-  int64_t kv_stride, page_stride, head_stride, token_stride;
+  int64_t kv_bytes, page_bytes, head_bytes, token_bytes;  // strides
+  int64_t scales;                                         // from a page's codes to their scales
   int n_pages, page_shift, width, kv_heads, G, window, sinks;
   float scale2;  // scale * log2(e)
   bool join;     // a whole unit's rows still have to be joined with the other phase
@@ -811,6 +811,17 @@ __device__ uint4 load_uint4(Global<const char> p) {
   return make_uint4(x.x, x.y, x.z, x.w);
 }
 
+// Lanes that load a key's elements, 16 bytes each.
+__host__ __device__ constexpr int lanes_a_key(int D, bool codes) { return codes ? D / 16 : D / 8; }
+
+// A wave's loads of keys and values on their way to LDS; of codes also each
+// lane's key's scale bytes.
+template <int NI, bool Codes>
+struct Loaded {
+  uint4 k[NI], v[NI];
+  uint32_t ks[Codes ? NI : 1], vs[Codes ? NI : 1];
+};
+
 // The key tiles of a unit, TK places of a list each: the sinks, up to a multiple
 // of 16, then the main run from a multiple of 16 on.  So tiles are full but for
 // the last (with sinks in tiles of their own, 24 prompts over windows of 1024 took
@@ -822,13 +833,14 @@ __device__ uint4 load_uint4(Global<const char> p) {
 // the batch that the present tile is in and of the next one are held, even
 // batches' in one register and odd ones' in the other.
 // Otherwise every lane looks its key's page up before it loads.
-template <typename T, int D, int TK, bool Sixteens>
+template <typename T, int D, int TK, bool Sixteens, bool Codes>
 struct Tiles {
-  static constexpr int LPR = D / 8, KPI = 64 / LPR;  // lanes a key, keys a load
+  static constexpr int LPR = lanes_a_key(D, Codes), KPI = 64 / LPR;  // keys a load
   static constexpr int kLoads = 16 / KPI;            // loads of 16 keys
   static constexpr int kGroups = TK / 16, kBatch = 64 / kGroups;
   Global<const int32_t> row;
   Global<const char> base;  // the key head's first key
+  Global<const char> scales;
   int hi, sink, skip, move, shift, pages;  // places below skip are keys, the others keys from `move` back
   int c0, c1;        // in tiles [c0, c1) every row sees every key
   int p_first, p_last;
@@ -842,7 +854,8 @@ struct Tiles {
     const int lane = threadIdx.x & 63;
     const bool there_is = x.slot >= 0;
     row = global(a.table + (int64_t)(there_is ? x.slot : 0) * a.width);
-    base = global(reinterpret_cast<const char*>(a.data + head * a.head_stride));
+    base = global(a.data + head * a.head_bytes);
+    scales = global(a.data + a.scales + (head << a.page_shift));
     hi = there_is ? x.end : 0, sink = there_is ? x.sink : 0;
     skip = (x.sink + 15) & ~15, move = x.lo - skip;
     shift = a.page_shift, pages = a.n_pages;
@@ -851,10 +864,10 @@ struct Tiles {
     const int above = a.window > 0 ? left_by(p_last + 1 - move, a.window) : 0;  // and those from this place on
     c0 = ((above > skip ? above : skip) + TK - 1) / TK;
     c1 = below > move ? (below - move) / TK : 0;
-    const uint64_t bytes = 2 * a.page_stride;
+    const uint64_t bytes = a.page_bytes;
     page_bytes = (uint32_t)bytes, page_bytes_hi = (uint32_t)(bytes >> 32);
-    token_bytes = 2 * (uint32_t)a.token_stride;
-    to_values = 2 * a.kv_stride;
+    token_bytes = (uint32_t)a.token_bytes;
+    to_values = a.kv_bytes;
     step = lane / LPR * token_bytes + lane % LPR * 16;
     stride = KPI * token_bytes;
   }
@@ -956,15 +969,16 @@ struct Tiles {
 
   // Where 16 keys of a tile lie (page 0's where there is no page).
   struct At {
-    Global<const char> k, v;
+    Global<const char> k, v, s;
   };
   __device__ At address(int t, int key) const {
     const int at = page_at(t, key / 16);
     const uint32_t page = held(at) ? at : 0, in = key_at(t * TK + key) & ((1 << shift) - 1);
-    const uint64_t off = (uint64_t)page * page_bytes + ((uint64_t)(page * page_bytes_hi) << 32) + in * token_bytes;
+    const uint64_t off = (uint64_t)page * page_bytes + ((uint64_t)(page * page_bytes_hi) << 32);
     At r;
-    r.k = apart(base + off);
+    r.k = apart(base + off + in * token_bytes);
     r.v = apart(r.k + to_values);
+    r.s = Codes ? apart(scales + off + in) : r.k;
     return r;
   }
 
@@ -975,7 +989,7 @@ struct Tiles {
   // Loads keys [key0, key0 + NI KPI) of the tile, key0 a multiple of 16: 16
   // bytes a lane.
   template <int NI>
-  __device__ void load(int t, int key0, uint4 (&k)[NI], uint4 (&v)[NI]) const {
+  __device__ void load(int t, int key0, Loaded<NI, Codes>& x) const {
     const int lane = threadIdx.x & 63, mask = (1 << shift) - 1;
     if (Sixteens) {
 #pragma unroll
@@ -983,52 +997,78 @@ struct Tiles {
         const At at = address(t, key0 + 16 * g);
 #pragma unroll
         for (int i = 0; i < kLoads; ++i) {
-          k[g * kLoads + i] = load16(at.k, i);
-          v[g * kLoads + i] = load16(at.v, i);
+          x.k[g * kLoads + i] = load16(at.k, i);
+          x.v[g * kLoads + i] = load16(at.v, i);
+          if constexpr (Codes) {
+            const Global<const char> s = at.s + i * KPI + lane / LPR;
+            x.ks[g * kLoads + i] = *(Global<const uint8_t>)s;
+            x.vs[g * kLoads + i] = *(Global<const uint8_t>)(s + to_values);
+          }
         }
       }
     } else {
 #pragma unroll
       for (int i = 0; i < NI; ++i) {
         const int place = t * TK + key0 + i * KPI + lane / LPR, key = key_at(place), at = entry_of(place);
-        const Global<const char> p = base + (held(at) ? at : 0) * (int64_t)((uint64_t)page_bytes_hi << 32 | page_bytes) +
-                                     (key & mask) * token_bytes + lane % LPR * 16;
-        k[i] = load_uint4(p);
-        v[i] = load_uint4(p + to_values);
+        const int64_t page = (held(at) ? at : 0) * (int64_t)((uint64_t)page_bytes_hi << 32 | page_bytes);
+        const Global<const char> p = base + page + (key & mask) * token_bytes + lane % LPR * 16;
+        x.k[i] = load_uint4(p);
+        x.v[i] = load_uint4(p + to_values);
+        if constexpr (Codes) {
+          const Global<const char> s = scales + page + (key & mask);
+          x.ks[i] = *(Global<const uint8_t>)s;
+          x.vs[i] = *(Global<const uint8_t>)(s + to_values);
+        }
       }
     }
   }
 };
 
-// A tile's share of one wave, from registers to LDS.
-template <typename T, int D, int NI>
-__device__ void put_keys(char* keys, char* values, int key0, const uint4 (&k)[NI], const uint4 (&v)[NI]) {
-  constexpr int LPR = D / 8, KPI = 64 / LPR;
-  const int lane = threadIdx.x & 63, chunk = lane % LPR;
+// A tile's share of one wave, from registers to LDS, codes as the values that
+// they stand for: the products are those of a 16-bit cache.
+template <typename T, int D, int NI, bool Codes>
+__device__ void put_keys(char* keys, char* values, int key0, const Loaded<NI, Codes>& x) {
+  constexpr int LPR = lanes_a_key(D, Codes), KPI = 64 / LPR, kChunks = Codes ? 2 : 1;  // 16-byte chunks of a lane
+  const int lane = threadIdx.x & 63, chunk = lane % LPR * kChunks;
   const int kp = fresh(key_place<D>(key0 + lane / LPR, chunk));
   const int vp = fresh(value_place<D>(key0 + lane / LPR, chunk * 16));
 #pragma unroll
   for (int i = 0; i < NI; ++i) {
     // KPI keys on, a chunk's place in its row moves with the key
     const int step = i * KPI, move = D == 128 ? (step & 15) << 4 : ((step >> 1) & 7) << 4;
-    *reinterpret_cast<uint4*>(keys + (kp ^ move) + step * D * 2) = k[i];
-    *reinterpret_cast<uint4*>(values + vp + step * D * 2) = v[i];
+    if constexpr (Codes) {
+      const float ks = scale_of(x.ks[i]), vs = scale_of(x.vs[i]);
+      *reinterpret_cast<vec8<T>*>(keys + (kp ^ move) + step * D * 2) = values_of(make_uint2(x.k[i].x, x.k[i].y), ks, T());
+      *reinterpret_cast<vec8<T>*>(keys + (kp ^ move ^ 16) + step * D * 2) = values_of(make_uint2(x.k[i].z, x.k[i].w), ks, T());
+      *reinterpret_cast<vec8<T>*>(values + vp + step * D * 2) = values_of(make_uint2(x.v[i].x, x.v[i].y), vs, T());
+      *reinterpret_cast<vec8<T>*>(values + vp + 16 + step * D * 2) = values_of(make_uint2(x.v[i].z, x.v[i].w), vs, T());
+    } else {
+      *reinterpret_cast<uint4*>(keys + (kp ^ move) + step * D * 2) = x.k[i];
+      *reinterpret_cast<uint4*>(values + vp + step * D * 2) = x.v[i];
+    }
   }
 }
 
 // Before that, zeros for the keys that are not there; true if a value is not
-// finite.
-template <typename T, int D, int NI>
-__device__ bool clear_keys(int key0, uint64_t there, uint4 (&k)[NI], uint4 (&v)[NI]) {
-  constexpr int LPR = D / 8, KPI = 64 / LPR;
+// finite (or of a scale larger than any that is written, which may make it so).
+template <typename T, int D, int NI, bool Codes>
+__device__ bool clear_keys(int key0, uint64_t there, Loaded<NI, Codes>& x) {
+  constexpr int LPR = lanes_a_key(D, Codes), KPI = 64 / LPR;
   const int lane = threadIdx.x & 63;
   uint32_t bad = 0;
 #pragma unroll
   for (int i = 0; i < NI; ++i) {
     const uint32_t keep = there >> (key0 + i * KPI + lane / LPR) & 1 ? ~0u : 0u;
-    k[i].x &= keep, k[i].y &= keep, k[i].z &= keep, k[i].w &= keep;
-    v[i].x &= keep, v[i].y &= keep, v[i].z &= keep, v[i].w &= keep;
-    bad |= not_finite(v[i].x, T()) | not_finite(v[i].y, T()) | not_finite(v[i].z, T()) | not_finite(v[i].w, T());
+    uint4 &k = x.k[i], &v = x.v[i];
+    k.x &= keep, k.y &= keep, k.z &= keep, k.w &= keep;
+    v.x &= keep, v.y &= keep, v.z &= keep, v.w &= keep;
+    if constexpr (Codes) {
+      x.ks[i] = keep ? x.ks[i] : 127, x.vs[i] = keep ? x.vs[i] : 127;
+      bad |= nan_codes(v.x) | nan_codes(v.y) | nan_codes(v.z) | nan_codes(v.w);
+      bad |= x.vs[i] > (__is_same(T, _Float16) ? 135 : 247);
+    } else {
+      bad |= not_finite(v.x, T()) | not_finite(v.y, T()) | not_finite(v.z, T()) | not_finite(v.w, T());
+    }
   }
   return bad != 0;
 }
@@ -1058,10 +1098,10 @@ __device__ bool clear_keys(int key0, uint64_t there, uint4 (&k)[NI], uint4 (&v)[
 template <int D, int NW>
 constexpr int kBlockRoom = 2 * 2 * block_keys(NW) * D * 2;  // LDS: two tiles' keys and values
 
-template <typename T, int D, int NW, bool Sixteens>
+template <typename T, int D, int NW, bool Sixteens, bool Codes>
 __device__ __forceinline__ void block_units(char* room, int phase, int block, int blocks) {
   constexpr int TK = block_keys(NW);
-  using Keys = Tiles<T, D, TK, Sixteens>;
+  using Keys = Tiles<T, D, TK, Sixteens, Codes>;
   constexpr int NI = TK / NW / Keys::KPI, kChunk = 64 * D * 2, kTile = TK * D * 2;
   char* const keys = room;
   char* const values = room + 2 * kTile;
@@ -1098,9 +1138,9 @@ __device__ __forceinline__ void block_units(char* room, int phase, int block, in
     const int w_last = wave * 32 + 31 < x.rows ? wave * 32 + 31 : x.rows - 1;
     const int w_first = x.pos0 + (x.row0 + wave * 32) / a.G, w_end = x.pos0 + (x.row0 + w_last) / a.G;
 
-    uint4 kreg[NI], vreg[NI];
+    Loaded<NI, Codes> next_keys;
     auto clear = [&](int t) {
-      const bool bad = clear_keys<T, D, NI>(mine % 64, tiles.there(t, mine / 64), kreg, vreg);
+      const bool bad = clear_keys<T, D, NI>(mine % 64, tiles.there(t, mine / 64), next_keys);
       odd |= bad && !tiles.even(t);
     };
     auto chunk = [&](int buf, int c, bool clean, int t) {
@@ -1122,11 +1162,11 @@ __device__ __forceinline__ void block_units(char* room, int phase, int block, in
     };
 
     bool clean = tiles.clean(t0), next = tiles.clean(t0 + 1);
-    tiles.load(t0, mine, kreg, vreg);
+    tiles.load(t0, mine, next_keys);
     __syncthreads();  // the last unit's tiles are no longer read
     if (!clean) clear(t0);
-    put_keys<T, D, NI>(keys, values, mine, kreg, vreg);
-    tiles.load(t0 + 1, mine, kreg, vreg);
+    put_keys<T, D, NI>(keys, values, mine, next_keys);
+    tiles.load(t0 + 1, mine, next_keys);
     for (int i = 0; i < n; ++i) {
       const int buf = i & 1, t = t0 + i, t2 = i + 2 < n ? t + 2 : t0 + n - 1;  // the last loads are of no use
       // The pages are looked up before the tile's loads: what waits for a lookup then does not wait for them.
@@ -1139,8 +1179,8 @@ __device__ __forceinline__ void block_units(char* room, int phase, int block, in
         if (c == 0) {
           // no load in a branch: where the ways meet, the registers would be copied, and the copies would wait
           if (!next) clear(t + 1);
-          put_keys<T, D, NI>(keys + (buf ^ 1) * kTile, values + (buf ^ 1) * kTile, mine, kreg, vreg);
-          tiles.load(t2, mine, kreg, vreg);
+          put_keys<T, D, NI>(keys + (buf ^ 1) * kTile, values + (buf ^ 1) * kTile, mine, next_keys);
+          tiles.load(t2, mine, next_keys);
         }
       }
       clean = next, next = third;
@@ -1159,10 +1199,10 @@ __device__ __forceinline__ void block_units(char* room, int phase, int block, in
   if (odd) flags[id * NW + wave] = 1;
 }
 
-template <typename T, int D, int NW, bool Sixteens>
+template <typename T, int D, int NW, bool Sixteens, bool Codes>
 __global__ __launch_bounds__(NW * 64, 2) void attend_block(Args<T>, int phase) {
   __shared__ __align__(16) char room[kBlockRoom<D, NW>];
-  block_units<T, D, NW, Sixteens>(room, phase, blockIdx.x, gridDim.x);
+  block_units<T, D, NW, Sixteens, Codes>(room, phase, blockIdx.x, gridDim.x);
 }
 
 // ---------------------------------------------------------------------------
@@ -1181,9 +1221,9 @@ __global__ __launch_bounds__(NW * 64, 2) void attend_block(Args<T>, int phase) {
 template <int D>
 constexpr int kWaveRoom = 2 * kRowKeys * D * 2;  // LDS of a wave: a tile's keys and values
 
-template <typename T, int D, bool Sixteens, bool Split>
+template <typename T, int D, bool Sixteens, bool Split, bool Codes>
 __device__ __forceinline__ void wave_units(char* room, int phase, int block, int blocks) {
-  using Keys = Tiles<T, D, kRowKeys, Sixteens>;
+  using Keys = Tiles<T, D, kRowKeys, Sixteens, Codes>;
   constexpr int TK = kRowKeys, NI = TK / Keys::KPI;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   char* const keys = room + wave * kWaveRoom<D>;
@@ -1221,21 +1261,21 @@ __device__ __forceinline__ void wave_units(char* room, int phase, int block, int
     load_rows<T, D>(a, x, head, row, rows.q);
     rows.clear();
     const int p = x.pos0 + (x.row0 + (row < x.rows ? row : x.rows - 1)) / a.G;
-    uint4 kreg[NI], vreg[NI];
-    tiles.load(t0, 0, kreg, vreg);
+    Loaded<NI, Codes> next_keys;
+    tiles.load(t0, 0, next_keys);
     for (int i = 0; i < n; ++i) {
       const int t = t0 + i;
       const bool clean = tiles.clean(t);
       uint32_t held = ~0u;
       if (!clean) {
         held = (uint32_t)tiles.there(t);
-        const bool bad = clear_keys<T, D, NI>(0, held, kreg, vreg);
+        const bool bad = clear_keys<T, D, NI>(0, held, next_keys);
         // with one position, what is there is seen by all rows
         odd |= bad && tiles.p_first != tiles.p_last && !tiles.even(t);
       }
-      put_keys<T, D, NI>(keys, values, 0, kreg, vreg);
+      put_keys<T, D, NI>(keys, values, 0, next_keys);
       tiles.advance(t + 1);
-      if (i + 1 < n) tiles.load(t + 1, 0, kreg, vreg);
+      if (i + 1 < n) tiles.load(t + 1, 0, next_keys);
       __builtin_amdgcn_wave_barrier();
       const int kp = fresh(first_key<D>()), vp = fresh(first_value<D>());
       float16v s[1];
@@ -1308,10 +1348,10 @@ __device__ __forceinline__ void wave_units(char* room, int phase, int block, int
   }
 }
 
-template <typename T, int D, bool Sixteens, bool Split>
+template <typename T, int D, bool Sixteens, bool Split, bool Codes>
 __global__ __launch_bounds__(kWaves * 64, 2) void attend_wave(Args<T>, int phase) {
   __shared__ __align__(16) char room[kWaves * kWaveRoom<D>];
-  wave_units<T, D, Sixteens, Split>(room, phase, blockIdx.x, gridDim.x);
+  wave_units<T, D, Sixteens, Split, Codes>(room, phase, blockIdx.x, gridDim.x);
 }
 
 // Both phases of a batch behind shared prefixes at once: on each CU one
@@ -1319,15 +1359,15 @@ __global__ __launch_bounds__(kWaves * 64, 2) void attend_wave(Args<T>, int phase
 // streams sequences' own keys, where memory is.  46 us for 64 sequences of 40
 // key heads of 128 with up to 128 tokens each behind 2048 (0.24 GB, 5.3 TB/s),
 // 17 us for 63 of 3 key heads of 64 behind up to 4001 tokens.
-template <typename T, int D, bool Sixteens>
+template <typename T, int D, bool Sixteens, bool Codes>
 __global__ __launch_bounds__(kWaves * 64, 2) void attend_both(Args<T>) {
   static_assert(kBlockRoom<D, 4> == kWaves * kWaveRoom<D>, "one room serves either");
   __shared__ __align__(16) char room[kBlockRoom<D, 4>];
   // Eight by eight, so that each XCD has both, and the other way round from the XCD's 33rd on, which join its first 32
   // on their CUs.
   const int block = blockIdx.x / 16 * 8 + blockIdx.x % 8;
-  if ((blockIdx.x / 8 + blockIdx.x / 256) % 2 == 0) block_units<T, D, 4, Sixteens>(room, 0, block, gridDim.x / 2);
-  else wave_units<T, D, Sixteens, false>(room, 1, block, gridDim.x / 2);
+  if ((blockIdx.x / 8 + blockIdx.x / 256) % 2 == 0) block_units<T, D, 4, Sixteens, Codes>(room, 0, block, gridDim.x / 2);
+  else wave_units<T, D, Sixteens, false, Codes>(room, 1, block, gridDim.x / 2);
 }
 
 // ---------------------------------------------------------------------------
@@ -1419,11 +1459,18 @@ __device__ void part_at(const Parts& p, const Cut& u, int i, int tile_rows, int 
   ml = p.ml + at;
 }
 
+// Element d of a key or value.
+template <typename T, bool Codes>
+__device__ float element(const char* row, int d, float scale) {
+  if (Codes) return (float)(T)(__builtin_amdgcn_cvt_f32_fp8((uint8_t)row[d], 0) * scale);
+  return (float)reinterpret_cast<const T*>(row)[d];
+}
+
 // A row's output again, key by key, without the keys that it does not see: the
 // products of whole tiles take a weight of 0 times a value, which is not 0
 // where the value is not finite.  Its weights keep 32 bits, so the row's last bits
 // may differ from those of the tiles.  lse2: the row's lse in the exponent's units.
-template <typename T, int D>
+template <typename T, int D, bool Codes>
 __device__ void redo_row(const Args<T>& a, const Entry& x, int head, int row, float lse2) {
   const int lane = threadIdx.x & 63;
   const int at = x.row0 + row, token = at / a.G, member = at - token * a.G;
@@ -1438,17 +1485,23 @@ __device__ void redo_row(const Args<T>& a, const Entry& x, int head, int row, fl
       page = a.table[(int64_t)x.slot * a.width + (key >> a.page_shift)];
     if (page >= a.n_pages) page = -1;
     const int in = key & ((1 << a.page_shift) - 1);
-    const T* k = a.data + (page < 0 ? 0 : page) * a.page_stride + head * a.head_stride + in * a.token_stride;
+    const int64_t at_page = (page < 0 ? 0 : page) * a.page_bytes;
+    const char* k = a.data + at_page + head * a.head_bytes + in * a.token_bytes;
+    float ks = 0.f, vs = 0.f;
+    if (Codes) {
+      const char* scale = a.data + at_page + a.scales + (head << a.page_shift) + in;
+      ks = scale_of((uint8_t)*scale), vs = scale_of((uint8_t)scale[a.kv_bytes]);
+    }
     float s = 0.f;
-    for (int d = 0; d < D; ++d) s = fmaf((float)q[d], (float)k[d], s);
+    for (int d = 0; d < D; ++d) s = fmaf((float)q[d], element<T, Codes>(k, d, ks), s);
     const float w = __builtin_amdgcn_exp2f(fmaf(s, a.scale2, -lse2));
-    const uint64_t v_at = reinterpret_cast<uint64_t>(k + a.kv_stride);
+    const uint64_t v_at = reinterpret_cast<uint64_t>(k + a.kv_bytes);
     for (uint64_t seen = __ballot(page >= 0); seen; seen &= seen - 1) {
       const int i = __builtin_ctzll(seen);
-      const T* v = reinterpret_cast<const T*>(__shfl(v_at, i)) + lane * (D / 64);
-      const float wi = __shfl(w, i);
+      const char* v = reinterpret_cast<const char*>(__shfl(v_at, i));
+      const float wi = __shfl(w, i), vi = __shfl(vs, i);
       sum += wi;
-      for (int d = 0; d < D / 64; ++d) o[d] = fmaf(wi, (float)v[d], o[d]);
+      for (int d = 0; d < D / 64; ++d) o[d] = fmaf(wi, element<T, Codes>(v, lane * (D / 64) + d, vi), o[d]);
     }
   }
   const int64_t dense = (int64_t)(x.q0 + token) * (a.kv_heads * a.G) + head * a.G + member;
@@ -1457,7 +1510,7 @@ __device__ void redo_row(const Args<T>& a, const Entry& x, int head, int row, fl
 
 // Joins the rows of a unit of the sequences' own keys that this wave has: four
 // from `row` on, then `step` on.
-template <typename T, int D>
+template <typename T, int D, bool Codes>
 __device__ void join_rows(const Args<T>& a, const Entry& x, const Cut& u, int head, int row, int step, int rows0,
                           int rows1, bool odd) {
   const int lane = threadIdx.x & 63, i16 = lane & 15;
@@ -1492,7 +1545,7 @@ __device__ void join_rows(const Args<T>& a, const Entry& x, const Cut& u, int he
       if (i16 == 0) a.lse[dense] = kLn2 * lse2;
     }
     for (int i = 0; odd && i < 4 && row + i < x.rows; ++i)
-      redo_row<T, D>(a, x, head, row + i, __shfl(lse2, 16 * i));
+      redo_row<T, D, Codes>(a, x, head, row + i, __shfl(lse2, 16 * i));
   }
 }
 
@@ -1509,7 +1562,7 @@ __device__ bool any_odd(const Args<T>& a, const Cut& u, int flags) {
 //
 // With a shared prefix every row is joined: `fours` waves take a unit of key
 // head blockIdx.y, four rows each.
-template <typename T, int D>
+template <typename T, int D, bool Codes>
 __global__ __launch_bounds__(256) void join_units(Args<T> a, int rows0, int rows1, int flags, int fours) {
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), head = blockIdx.y;
   const Phase own = a.plan.phase[1];
@@ -1517,14 +1570,14 @@ __global__ __launch_bounds__(256) void join_units(Args<T> a, int rows0, int rows
     const int e = id / fours;
     const Entry x = a.plan.entry[1][e];
     const Cut u = cut_of(own, a.plan.cum[1], e, head);
-    join_rows<T, D>(a, x, u, head, (id - e * fours) * 4, fours * 4, rows0, rows1, any_odd(a, u, flags));
+    join_rows<T, D, Codes>(a, x, u, head, (id - e * fours) * 4, fours * 4, rows0, rows1, any_odd(a, u, flags));
   }
 }
 
 // Otherwise only the units that are cut: the worker whose share begins inside a
 // unit, as the first one to, joins it.  A worker that met values that are not
 // finite also does its whole units' rows again.
-template <typename T, int D>
+template <typename T, int D, bool Codes>
 __global__ __launch_bounds__(256) void join_cuts(Args<T> a, int rows1, int flags, int fours) {
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), id = blockIdx.x * 4 + wave, w = id / fours;
   const int row = (id - w * fours) * 4, step = fours * 4;
@@ -1538,7 +1591,7 @@ __global__ __launch_bounds__(256) void join_cuts(Args<T> a, int rows1, int flags
     u.c0 = w * own.share - st.tile;
     u.w0 = u.c0 / u.share;
     u.w1 = (u.c0 + x.tiles - 1) / u.share;
-    join_rows<T, D>(a, x, u, st.head, row, step, rows1, rows1, any_odd(a, u, flags));
+    join_rows<T, D, Codes>(a, x, u, st.head, row, step, rows1, rows1, any_odd(a, u, flags));
   }
   if (!any_odd(a, Cut{w, w, 0, 0}, flags)) return;
   const int64_t all = own.total * a.kv_heads, beg = w * own.share;
@@ -1549,7 +1602,7 @@ __global__ __launch_bounds__(256) void join_cuts(Args<T> a, int rows1, int flags
     for (int r = row / 4; n == x.tiles && r < x.rows; r += step / 4) {
       const int at = x.row0 + r, token = at / a.G;
       const int64_t dense = (int64_t)(x.q0 + token) * (a.kv_heads * a.G) + head * a.G + at - token * a.G;
-      redo_row<T, D>(a, x, head, r, a.lse[dense] * kLog2e);
+      redo_row<T, D, Codes>(a, x, head, r, a.lse[dense] * kLog2e);
     }
     left -= n;
     t = 0;
@@ -1557,19 +1610,21 @@ __global__ __launch_bounds__(256) void join_cuts(Args<T> a, int rows1, int flags
   }
 }
 
-template <typename T, int D>
+template <typename T, int D, bool Codes>
 hipError_t launch_typed(const ewsjf_cache& c, const ewsjf_batch& b, int32_t layer, const void* q, int64_t q_token,
                         int64_t q_head, float scale, const void* plan, void* out, float* lse, void* ws,
                         hipStream_t stream) {
   const Shape s = shape_of(c, b);
   Args<T> a;
-  a.data = static_cast<const T*>(c.data) + layer * c.layer_stride;
+  const int64_t bytes = cache_element_bytes(c);
+  a.data = static_cast<const char*>(c.data) + layer * c.layer_stride * bytes;
   a.q = static_cast<const T*>(q);
   a.q_token = q_token, a.q_head = q_head;
   a.table = c.table;
   a.out = static_cast<T*>(out);
-  a.kv_stride = c.kv_stride, a.page_stride = c.page_stride, a.head_stride = c.head_stride;
-  a.token_stride = c.token_stride;
+  a.kv_bytes = c.kv_stride * bytes, a.page_bytes = c.page_stride * bytes, a.head_bytes = c.head_stride * bytes;
+  a.token_bytes = c.token_stride * bytes;
+  a.scales = (int64_t)c.kv_heads * c.page_size * c.head_dim;
   a.n_pages = c.n_pages, a.page_shift = __builtin_ctz(c.page_size), a.width = c.width, a.kv_heads = c.kv_heads;
   a.G = s.G, a.window = b.window, a.sinks = b.sinks;
   a.scale2 = scale * kLog2e;
@@ -1579,14 +1634,14 @@ hipError_t launch_typed(const ewsjf_cache& c, const ewsjf_batch& b, int32_t laye
   a.lse = lse != nullptr ? lse : a.work.lse;
   const bool sixteens = c.page_size >= 16;
   if (s.both) {
-    auto kernel = sixteens ? attend_both<T, D, true> : attend_both<T, D, false>;
+    auto kernel = sixteens ? attend_both<T, D, true, Codes> : attend_both<T, D, false, Codes>;
     kernel<<<s.blocks[0] + s.blocks[1], kWaves * 64, 0, stream>>>(a);
   }
   for (int p = s.groups ? 0 : 1; p < 2 && !s.both; ++p) {
-    auto kernel = s.waves[p] == 8 ? (sixteens ? attend_block<T, D, 8, true> : attend_block<T, D, 8, false>)
-                  : s.waves[p]    ? (sixteens ? attend_block<T, D, 4, true> : attend_block<T, D, 4, false>)
-                  : s.whole && p  ? (sixteens ? attend_wave<T, D, true, true> : attend_wave<T, D, false, true>)
-                                  : (sixteens ? attend_wave<T, D, true, false> : attend_wave<T, D, false, false>);
+    auto kernel = s.waves[p] == 8 ? (sixteens ? attend_block<T, D, 8, true, Codes> : attend_block<T, D, 8, false, Codes>)
+                  : s.waves[p] ? (sixteens ? attend_block<T, D, 4, true, Codes> : attend_block<T, D, 4, false, Codes>)
+                  : s.whole && p ? (sixteens ? attend_wave<T, D, true, true, Codes> : attend_wave<T, D, false, true, Codes>)
+                                 : (sixteens ? attend_wave<T, D, true, false, Codes> : attend_wave<T, D, false, false, Codes>);
     kernel<<<s.blocks[p], 64 * (s.waves[p] ? s.waves[p] : kWaves), 0, stream>>>(a, p);
   }
   if (s.whole) return hipGetLastError();
@@ -1594,8 +1649,8 @@ hipError_t launch_typed(const ewsjf_cache& c, const ewsjf_batch& b, int32_t laye
   const int fours = (int)((most + 3) / 4), flags = s.waves[1] ? s.waves[1] : 1;
   const int64_t waves = (a.join ? s.entries[1] : s.workers[1]) * fours;
   const unsigned grid = (unsigned)(waves < kMostJoins ? (waves + 3) / 4 : kMostJoins / 4);
-  if (a.join) join_units<T, D><<<dim3(grid, c.kv_heads), 256, 0, stream>>>(a, s.rows[0], s.rows[1], flags, fours);
-  else join_cuts<T, D><<<grid, 256, 0, stream>>>(a, s.rows[1], flags, fours);
+  if (a.join) join_units<T, D, Codes><<<dim3(grid, c.kv_heads), 256, 0, stream>>>(a, s.rows[0], s.rows[1], flags, fours);
+  else join_cuts<T, D, Codes><<<grid, 256, 0, stream>>>(a, s.rows[1], flags, fours);
   return hipGetLastError();
 }
 
@@ -1625,8 +1680,13 @@ hipError_t launch_attention(const ewsjf_cache& c, const ewsjf_batch& b, int32_t 
                             hipStream_t stream) {
   if (b.total_q == 0) return hipSuccess;
   auto go = [&](auto run) { return run(c, b, layer, q, q_token, q_head, scale, plan, out, lse, ws, stream); };
-  if (c.dtype == EWSJF_BF16) return c.head_dim == 64 ? go(launch_typed<__bf16, 64>) : go(launch_typed<__bf16, 128>);
-  return c.head_dim == 64 ? go(launch_typed<_Float16, 64>) : go(launch_typed<_Float16, 128>);
+  const bool narrow = c.head_dim == 64;
+  switch (c.dtype) {
+    case EWSJF_BF16: return narrow ? go(launch_typed<__bf16, 64, false>) : go(launch_typed<__bf16, 128, false>);
+    case EWSJF_F16: return narrow ? go(launch_typed<_Float16, 64, false>) : go(launch_typed<_Float16, 128, false>);
+    case EWSJF_E4M3_BF16: return narrow ? go(launch_typed<__bf16, 64, true>) : go(launch_typed<__bf16, 128, true>);
+    default: return narrow ? go(launch_typed<_Float16, 64, true>) : go(launch_typed<_Float16, 128, true>);
+  }
 }
 
 }  // namespace ewsjf

@@ -91,6 +91,14 @@ __device__ N block_scan(int v, N* sums, N& total) {
   return base + inc - v;
 }
 
+// The keys (values) of page `page` in a plane, layer * 2 + (0 keys, 1 values), and their 16-byte pieces: an 8-bit
+// page's scales lie behind its codes, so that they move as one block.
+__device__ char* block_of(const ewsjf_cache& c, int plane, int64_t page) {
+  return static_cast<char*>(c.data) +
+         (plane / 2 * c.layer_stride + plane % 2 * c.kv_stride + page * c.page_stride) * cache_element_bytes(c);
+}
+__device__ int pieces_of(const ewsjf_cache& c) { return (int)(cache_block(c) * cache_element_bytes(c) / 16); }
+
 __device__ bool in_pool(const ewsjf_cache& c, int page) { return page >= 0 && page < c.n_pages; }
 __device__ int pages_of(const ewsjf_cache& c, int64_t tokens) {
   return (int)((tokens + c.page_size - 1) / c.page_size);
@@ -101,7 +109,8 @@ __device__ int held(const ewsjf_cache& c, int slot) {
 }
 
 // Checks the requests and sums what they need, in 64 bits: requests of up to
-// 2^24 pages each pass 32 bits together.
+// 2^24 pages each pass 32 bits together.  slot == nullptr: w.fine holds the needs,
+// as plan_reorder left them.
 template <int N>
 __device__ void sum_needs(const ewsjf_cache& c, const CacheWs& w, int64_t* sums, const int32_t* parent,
                           const int32_t* slot, const int32_t* tokens, int n) {
@@ -109,7 +118,9 @@ __device__ void sum_needs(const ewsjf_cache& c, const CacheWs& w, int64_t* sums,
   for (int i0 = 0; i0 < n; i0 += N) {
     const int i = i0 + threadIdx.x;
     int need = 0, ok = 0;
-    if (i < n) {
+    if (slot == nullptr) {
+      if (i < n) need = ok = w.fine[i];
+    } else if (i < n) {
       const int s = slot[i];
       const int64_t t = tokens[i];
       if (s >= 0 && s < c.n_slots && t >= 0) {
@@ -253,10 +264,9 @@ __global__ __launch_bounds__(kThreads) void apply_growth(ewsjf_cache c, CacheWs 
   if (!w.fine[i] || after > free || after == first) return;
   const int src = c.table[(int64_t)parent[i] * c.width + tokens[i] / c.page_size];
   if (!in_pool(c, src)) return;
-  uint16_t* data = static_cast<uint16_t*>(c.data) + plane / 2 * c.layer_stride + plane % 2 * c.kv_stride;
-  const uint4* a = reinterpret_cast<const uint4*>(data + src * c.page_stride);
-  uint4* b = reinterpret_cast<uint4*>(data + w.picked[first] * c.page_stride);
-  const int vecs = c.kv_heads * c.page_size * c.head_dim / 8;
+  const uint4* a = reinterpret_cast<const uint4*>(block_of(c, plane, src));
+  uint4* b = reinterpret_cast<uint4*>(block_of(c, plane, w.picked[first]));
+  const int vecs = pieces_of(c);
   for (int j = threadIdx.x; j < vecs; j += kThreads) b[j] = a[j];
 }
 
@@ -300,6 +310,122 @@ __global__ __launch_bounds__(kSmallThreads) void grow_small(ewsjf_cache c, Cache
   }
 }
 
+// ---------------------------------------------------------------------------
+// Reordering: beams take over their parents' rows, all at once.
+// ---------------------------------------------------------------------------
+enum Role : int32_t {
+  kNone,   // the slot does not exist
+  kEmpty,  // no parent
+  kStay,   // its own parent
+  kMove,   // takes over the parent's row
+  kCopy    // shares the parent's whole pages and copies its partial one
+};
+
+struct ReorderWs {
+  CacheWs cache;
+  int32_t* role;    // [n]
+  int32_t* length;  // [n]: before the call
+  int32_t* row;     // [n][width]: rows before the call, of slots that somebody takes over
+  size_t bytes;
+};
+
+ReorderWs reorder_ws(const ewsjf_cache& c, int n, void* base) {
+  ReorderWs w;
+  w.cache = cache_ws(c, base);
+  size_t at = w.cache.bytes;
+  auto take = [&](size_t ints) {
+    int32_t* r = reinterpret_cast<int32_t*>(static_cast<char*>(base) + at);
+    at += (ints * 4 + 255) & ~size_t(255);
+    return r;
+  };
+  w.role = take(n);
+  w.length = take(n);
+  w.row = take((size_t)n * c.width);
+  w.bytes = at;
+  return w;
+}
+
+__device__ bool slot_there(const ewsjf_cache& c, int slot) { return slot >= 0 && slot < c.n_slots; }
+
+// A workgroup a request: its role and need; its row put aside if somebody takes
+// it over, else its pages given up.
+__global__ __launch_bounds__(kThreads) void plan_reorder(ewsjf_cache c, ReorderWs w, const int32_t* slot,
+                                                         const int32_t* parent, int n) {
+  __shared__ int first_of_mine, first_of_parent;  // first request that takes over this slot, the parent's
+  const int i = blockIdx.x, s = slot[i], p = parent[i];
+  const bool there = slot_there(c, s), born = there && p >= 0 && p < n && slot_there(c, slot[p]);
+  if (threadIdx.x == 0) first_of_mine = first_of_parent = n;
+  __syncthreads();
+  for (int j = threadIdx.x; j < n; j += kThreads) {
+    const int q = parent[j];
+    if ((q == i || q == p) && slot_there(c, slot[j])) {
+      if (q == i) atomicMin(&first_of_mine, j);
+      if (q == p) atomicMin(&first_of_parent, j);
+    }
+  }
+  __syncthreads();
+  const int64_t room = (int64_t)c.width * c.page_size;
+  if (threadIdx.x == 0) {
+    int role = kNone, need = 0;
+    if (there) role = kEmpty;
+    if (born) {
+      const int heir = parent[p] == p ? p : first_of_parent;
+      role = p == i ? kStay : heir == i ? kMove : kCopy;
+      if (role == kCopy) {
+        const int64_t t = held(c, slot[p]) < room ? held(c, slot[p]) : room;
+        if (t % c.page_size) need = in_pool(c, c.table[(int64_t)slot[p] * c.width + t / c.page_size]);
+      }
+    }
+    w.role[i] = role;
+    w.cache.fine[i] = need;
+    w.length[i] = there ? (int)(held(c, s) < room ? held(c, s) : room) : 0;
+  }
+  if (!there) return;
+  const int32_t* row = c.table + (int64_t)s * c.width;
+  for (int j = threadIdx.x; j < c.width; j += kThreads) {
+    const int page = row[j];
+    if (first_of_mine < n) w.row[(int64_t)i * c.width + j] = page;
+    else if (in_pool(c, page)) atomicSub(&c.refs[page], 1);
+  }
+}
+
+// Request blockIdx.x: plane 0's workgroup writes its row, counts, length and
+// grant; each plane's copies the partial page.  A page that is copied stays with
+// the row that was taken over, and a page that is written was free, so none is
+// both.
+__global__ __launch_bounds__(kThreads) void apply_reorder(ewsjf_cache c, ReorderWs w, const int32_t* slot,
+                                                          const int32_t* parent, int32_t* granted) {
+  const int i = blockIdx.x, plane = blockIdx.y, role = w.role[i];
+  const int p = parent[i], need = w.cache.fine[i], after = w.cache.cum[i];
+  const bool copied = role == kCopy && (need == 0 || after <= w.cache.head[0]);
+  const int t = role == kMove || role == kCopy ? w.length[p] : 0, full = t / c.page_size;
+  const int32_t* from = w.row + (int64_t)(role == kMove || role == kCopy ? p : 0) * c.width;
+  if (plane == 0) {
+    if (threadIdx.x == 0) granted[i] = role == kStay || role == kMove || copied;
+    if (role == kEmpty || role == kMove || role == kCopy) {
+      int32_t* row = c.table + (int64_t)slot[i] * c.width;
+      for (int j = threadIdx.x; j < c.width; j += kThreads) {
+        int page = -1;
+        if (role == kMove) {
+          page = from[j];
+        } else if (copied && j < full) {
+          page = from[j];
+          if (in_pool(c, page)) atomicAdd(&c.refs[page], 1);
+        } else if (copied && need && j == full) {
+          page = w.cache.picked[after - 1];
+        }
+        row[j] = page;
+      }
+      if (threadIdx.x == 0) c.length[slot[i]] = role == kMove || copied ? t : 0;
+    }
+  }
+  if (!copied || !need) return;
+  const uint4* a = reinterpret_cast<const uint4*>(block_of(c, plane, from[full]));
+  uint4* b = reinterpret_cast<uint4*>(block_of(c, plane, w.cache.picked[after - 1]));
+  const int vecs = pieces_of(c);
+  for (int j = threadIdx.x; j < vecs; j += kThreads) b[j] = a[j];
+}
+
 // A workgroup a slot.  Counts are integers, so the order of the atomics does
 // not matter.
 __global__ __launch_bounds__(kThreads) void release_rows(ewsjf_cache c, const int32_t* slot, const int32_t* begin,
@@ -328,13 +454,12 @@ __global__ __launch_bounds__(kThreads) void release_rows(ewsjf_cache c, const in
 // A workgroup a page and plane.
 __global__ __launch_bounds__(kThreads) void copy_pages(ewsjf_cache c, const int32_t* src, const int32_t* dst, int n) {
   const int plane = blockIdx.y;
-  uint16_t* data = static_cast<uint16_t*>(c.data) + plane / 2 * c.layer_stride + plane % 2 * c.kv_stride;
-  const int vecs = c.kv_heads * c.page_size * c.head_dim / 8;
+  const int vecs = pieces_of(c);
   for (int i = blockIdx.x; i < n; i += gridDim.x) {
     const int a = src[i], b = dst[i];
     if (!in_pool(c, a) || !in_pool(c, b)) continue;
-    const uint4* from = reinterpret_cast<const uint4*>(data + a * c.page_stride);
-    uint4* to = reinterpret_cast<uint4*>(data + b * c.page_stride);
+    const uint4* from = reinterpret_cast<const uint4*>(block_of(c, plane, a));
+    uint4* to = reinterpret_cast<uint4*>(block_of(c, plane, b));
     for (int j = threadIdx.x; j < vecs; j += kThreads) to[j] = from[j];
   }
 }
@@ -392,13 +517,12 @@ __global__ __launch_bounds__(kThreads) void move_pages(ewsjf_cache c, CacheWs w,
     }
     return;
   }
-  const int planes = 2 * c.layers, vecs = c.kv_heads * c.page_size * c.head_dim / 8;
+  const int planes = 2 * c.layers, vecs = pieces_of(c);
   const int64_t tasks = (int64_t)moves * planes;
   for (int64_t i = blockIdx.x - book; i < tasks; i += gridDim.x - book) {
     const int j = (int)(i / planes), plane = (int)(i % planes);
-    uint16_t* data = static_cast<uint16_t*>(c.data) + plane / 2 * c.layer_stride + plane % 2 * c.kv_stride;
-    const uint4* a = reinterpret_cast<const uint4*>(data + w.movers[j] * c.page_stride);
-    uint4* b = reinterpret_cast<uint4*>(data + w.picked[j] * c.page_stride);
+    const uint4* a = reinterpret_cast<const uint4*>(block_of(c, plane, w.movers[j]));
+    uint4* b = reinterpret_cast<uint4*>(block_of(c, plane, w.picked[j]));
     for (int v = threadIdx.x; v < vecs; v += kThreads) b[v] = a[v];
   }
 }
@@ -460,6 +584,24 @@ hipError_t launch_cache_grow(const ewsjf_cache& c, const int32_t* parent, const 
     pick_pages<<<chunks, kThreads, 0, stream>>>(c, w, chunks, n);
   }
   apply_growth<<<dim3(n, parent ? 2 * c.layers : 1), kThreads, 0, stream>>>(c, w, parent, slot, tokens, granted);
+  return hipGetLastError();
+}
+
+size_t cache_reorder_ws_bytes(const ewsjf_cache& c, int32_t n) { return reorder_ws(c, n, nullptr).bytes; }
+
+hipError_t launch_cache_reorder(const ewsjf_cache& c, const int32_t* slot, const int32_t* parent, int32_t n,
+                                int32_t* granted, void* ws, hipStream_t stream) {
+  if (n == 0) return hipSuccess;
+  const ReorderWs w = reorder_ws(c, n, ws);
+  const int chunks = (c.n_pages + kChunk - 1) / kChunk;
+  plan_reorder<<<n, kThreads, 0, stream>>>(c, w, slot, parent, n);
+  if (c.n_pages <= kSmallPool) {
+    grow_small<<<1, kSmallThreads, 0, stream>>>(c, w.cache, nullptr, nullptr, nullptr, n, nullptr, false);
+  } else {
+    count_pages<<<chunks + 1, kThreads, 0, stream>>>(c, w.cache, chunks, false, nullptr, nullptr, nullptr, n);
+    pick_pages<<<chunks, kThreads, 0, stream>>>(c, w.cache, chunks, n);
+  }
+  apply_reorder<<<dim3(n, 2 * c.layers), kThreads, 0, stream>>>(c, w, slot, parent, granted);
   return hipGetLastError();
 }
 

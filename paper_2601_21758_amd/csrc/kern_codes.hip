@@ -1,0 +1,217 @@
+// Keys and values of an 8-bit cache: quantised as they are written, read back.
+//
+// A row is a head's elements x of one token.  With top = max |x| and 2^e the
+// smallest power of two with top <= 448 2^e, the codes are x / 2^e rounded to
+// e4m3 and the row's scale byte is e + 127.  A power of two loses nothing against
+// any other scale (codes are floating point: their relative step is the same
+// everywhere, and 448 2^e >= top > 224 2^e leaves 14 binades below), divides
+// exactly, and makes the values exact in 16 bits: four significant bits.
+//
+// Both are bound by memory: a token of H heads of D moves 2 H (3 D + 1) bytes.
+#include <hip/hip_runtime.h>
+
+#include "ewsjf_cache.h"
+#include "ewsjf_codes.h"
+
+namespace ewsjf {
+namespace {
+
+constexpr int kThreads = 256;
+constexpr int kTokens = 16;      // most tokens of a workgroup
+constexpr int kMostGrid = 65536;
+
+// Where a workgroup's tokens lie: element offset of (head 0, token) in the layer's keys, and of its scale byte behind
+// the page's codes; -1: nowhere.
+struct Place {
+  int64_t at, scale;
+  int slot;
+};
+
+__device__ int last_at_most(const int32_t* key, int n, int64_t v) {
+  int lo = 0, hi = n;
+  while (hi - lo > 1) {
+    const int mid = (lo + hi) / 2;
+    if (key[mid] <= v) lo = mid;
+    else hi = mid;
+  }
+  return lo;
+}
+
+__device__ Place place_of(const ewsjf_cache& c, int64_t page, int pos) {
+  const int in = pos & (c.page_size - 1);
+  const int64_t block = page * c.page_stride;
+  return Place{block + in * c.token_stride, block + (int64_t)c.kv_heads * c.page_size * c.head_dim + in, 0};
+}
+
+// Token t's place, as the cache's append finds it: what is not granted, not
+// held or shared with other rows is not written.
+__device__ Place written_place(const ewsjf_cache& c, const int32_t* slot, const int32_t* q_start,
+                               const int32_t* granted, int n_seqs, int64_t t) {
+  const Place nowhere{-1, -1, 0};
+  const int i = last_at_most(q_start, n_seqs, t), s = slot[i], a = q_start[i], e = q_start[i + 1];
+  if (s < 0 || s >= c.n_slots || t < a || t >= e || (granted != nullptr && granted[i] == 0)) return nowhere;
+  const int shift = __builtin_ctz(c.page_size), have = c.length[s] < 0 ? 0 : c.length[s], pos = have - (int)(e - t);
+  if (pos < 0 || pos >> shift >= c.width) return nowhere;
+  const int page = c.table[(int64_t)s * c.width + (pos >> shift)];
+  if (page < 0 || page >= c.n_pages) return nowhere;
+  if (granted == nullptr && pos >> shift < have >> shift && c.refs[page] > 1) return nowhere;
+  return place_of(c, page, pos);
+}
+
+// Row t's place of a read; slot -1: no sequence has the row, which stays as it is.
+__device__ Place read_place(const ewsjf_cache& c, const int32_t* slot, const int32_t* start, const int32_t* begin,
+                            int n_seqs, int64_t t) {
+  Place p{-1, -1, -1};
+  const int i = last_at_most(start, n_seqs, t), s = slot[i];
+  const int64_t a = start[i], e = start[i + 1];
+  if (t < a || t >= e) return p;
+  p.slot = 0;
+  if (s < 0 || s >= c.n_slots) return p;
+  const int64_t pos = (begin != nullptr ? begin[i] : 0) + t - a;
+  const int shift = __builtin_ctz(c.page_size);
+  if (pos < 0 || pos >= c.length[s] || pos >> shift >= c.width) return p;
+  const int page = c.table[(int64_t)s * c.width + (pos >> shift)];
+  if (page < 0 || page >= c.n_pages) return p;
+  return place_of(c, page, (int)pos);
+}
+
+// e + 127 of a row whose largest magnitude is `top`.  448 = 1.75 2^8: with top = f 2^k, e is k - 8, one more if f > 1.75.
+__device__ int scale_byte(float top) {
+  const int up = (int)((__float_as_uint(top) + 0x1fffffu) >> 23) - 8;
+  return up < 127 - 117 ? 127 - 117 : up;
+}
+
+// Lanes of a row, 8 elements each: a power of two, so that a row's lanes are a group of a wave.
+__host__ __device__ int lanes_of(int head_dim) {
+  int g = 1;
+  while (8 * g < head_dim) g *= 2;
+  return g;
+}
+
+template <typename T>
+__global__ __launch_bounds__(kThreads) void append_codes(ewsjf_cache c, int layer, const T* k, const T* v,
+                                                         int64_t k_token, int64_t k_head, int64_t v_token,
+                                                         int64_t v_head, const int32_t* slot, const int32_t* q_start,
+                                                         const int32_t* granted, int n_seqs, int64_t total,
+                                                         int tokens) {
+  __shared__ Place place[kTokens];
+  const int lanes = lanes_of(c.head_dim), each = kThreads / lanes;
+  const int lane = threadIdx.x & (lanes - 1), d = lane * 8;
+  const bool busy = d < c.head_dim;
+  char* data = static_cast<char*>(c.data) + layer * c.layer_stride;
+  const float most = cache_most(c);
+  for (int64_t t0 = (int64_t)blockIdx.x * tokens; t0 < total; t0 += (int64_t)gridDim.x * tokens) {
+    const int n = total - t0 < tokens ? (int)(total - t0) : tokens;
+    __syncthreads();
+    if ((int)threadIdx.x < n) place[threadIdx.x] = written_place(c, slot, q_start, granted, n_seqs, t0 + threadIdx.x);
+    __syncthreads();
+    const int rows = n * 2 * c.kv_heads;
+    for (int r = threadIdx.x / lanes; r < rows; r += each) {
+      const int h = r % c.kv_heads, i = r / c.kv_heads / 2, x = r / c.kv_heads % 2;
+      const Place p = place[i];
+      if (p.at < 0) continue;  // all lanes of the row
+      vec8<T> in = {};
+      const int64_t t = t0 + i;
+      if (busy) in = *reinterpret_cast<const vec8<T>*>(x ? v + t * v_token + h * v_head + d : k + t * k_token + h * k_head + d);
+      float y[8], top = 0.f;
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        y[j] = (float)in[j];
+        y[j] = y[j] > most ? most : y[j] < -most ? -most : y[j];  // a NaN stays
+        top = fabsf(y[j]) > top ? fabsf(y[j]) : top;              // and does not count (a signalling one would, in a maximum)
+      }
+      for (int s = lanes / 2; s; s >>= 1) top = fmaxf(top, __shfl_xor(top, s));
+      const int byte = scale_byte(top);
+      const float inv = scale_of(254 - byte);  // 2^-e
+      uint32_t lo = 0, hi = 0;
+      lo = __builtin_amdgcn_cvt_pk_fp8_f32(y[0] * inv, y[1] * inv, lo, false);
+      lo = __builtin_amdgcn_cvt_pk_fp8_f32(y[2] * inv, y[3] * inv, lo, true);
+      hi = __builtin_amdgcn_cvt_pk_fp8_f32(y[4] * inv, y[5] * inv, hi, false);
+      hi = __builtin_amdgcn_cvt_pk_fp8_f32(y[6] * inv, y[7] * inv, hi, true);
+      char* to = data + x * c.kv_stride;
+      if (busy) *reinterpret_cast<uint2*>(to + p.at + h * c.head_stride + d) = make_uint2(lo, hi);
+      if (lane == 0) to[p.scale + h * c.page_size] = (char)byte;
+    }
+  }
+}
+
+template <typename T, bool Codes>
+__global__ __launch_bounds__(kThreads) void read_tokens(ewsjf_cache c, int layer, const int32_t* slot,
+                                                        const int32_t* start, const int32_t* begin, int n_seqs,
+                                                        int64_t total, T* k, T* v, int tokens) {
+  __shared__ Place place[kTokens];
+  const int lanes = lanes_of(c.head_dim), each = kThreads / lanes;
+  const int d = (threadIdx.x & (lanes - 1)) * 8;
+  const char* data = static_cast<const char*>(c.data) + layer * c.layer_stride * (Codes ? 1 : 2);
+  for (int64_t t0 = (int64_t)blockIdx.x * tokens; t0 < total; t0 += (int64_t)gridDim.x * tokens) {
+    const int n = total - t0 < tokens ? (int)(total - t0) : tokens;
+    __syncthreads();
+    if ((int)threadIdx.x < n) place[threadIdx.x] = read_place(c, slot, start, begin, n_seqs, t0 + threadIdx.x);
+    __syncthreads();
+    const int rows = n * 2 * c.kv_heads;
+    for (int r = threadIdx.x / lanes; r < rows && d < c.head_dim; r += each) {
+      const int h = r % c.kv_heads, i = r / c.kv_heads / 2, x = r / c.kv_heads % 2;
+      const Place p = place[i];
+      if (p.slot < 0) continue;
+      vec8<T> y = {};
+      if (p.at >= 0) {
+        const int64_t at = x * c.kv_stride + p.at + h * c.head_stride + d;
+        if (Codes) {
+          const float scale = scale_of((uint8_t)data[x * c.kv_stride + p.scale + h * c.page_size]);
+          y = values_of(*reinterpret_cast<const uint2*>(data + at), scale, T());
+        } else {
+          y = *reinterpret_cast<const vec8<T>*>(data + 2 * at);
+        }
+      }
+      *reinterpret_cast<vec8<T>*>((x ? v : k) + ((t0 + i) * c.kv_heads + h) * c.head_dim + d) = y;
+    }
+  }
+}
+
+// Tokens of a workgroup: as many as leave the chip four workgroups a CU.
+int tokens_each(int64_t total) {
+  const int64_t n = total / 1024;
+  return n < 1 ? 1 : n > kTokens ? kTokens : (int)n;
+}
+unsigned grid_of(int64_t total, int tokens) {
+  const int64_t n = (total + tokens - 1) / tokens;
+  return (unsigned)(n < kMostGrid ? n : kMostGrid);
+}
+
+}  // namespace
+
+hipError_t launch_cache_append_codes(const ewsjf_cache& c, int32_t layer, const void* k, const void* v,
+                                     int64_t k_token, int64_t k_head, int64_t v_token, int64_t v_head,
+                                     const int32_t* slot, const int32_t* q_start, const int32_t* granted,
+                                     int32_t n_seqs, int64_t total, hipStream_t stream) {
+  if (n_seqs == 0 || total == 0) return hipSuccess;
+  const int tokens = tokens_each(total);
+  auto go = [&](auto type) {
+    using T = decltype(type);
+    append_codes<T><<<grid_of(total, tokens), kThreads, 0, stream>>>(
+        c, layer, static_cast<const T*>(k), static_cast<const T*>(v), k_token, k_head, v_token, v_head, slot, q_start,
+        granted, n_seqs, total, tokens);
+  };
+  if (c.dtype == EWSJF_E4M3_BF16) go(__bf16());
+  else go(_Float16());
+  return hipGetLastError();
+}
+
+hipError_t launch_cache_read(const ewsjf_cache& c, int32_t layer, const int32_t* slot, const int32_t* start,
+                             const int32_t* begin, int32_t n_seqs, int64_t total, void* k, void* v,
+                             hipStream_t stream) {
+  if (n_seqs == 0 || total == 0) return hipSuccess;
+  const int tokens = tokens_each(total);
+  auto go = [&](auto type, auto kernel) {
+    using T = decltype(type);
+    kernel<<<grid_of(total, tokens), kThreads, 0, stream>>>(c, layer, slot, start, begin, n_seqs, total,
+                                                            static_cast<T*>(k), static_cast<T*>(v), tokens);
+  };
+  if (c.dtype == EWSJF_E4M3_BF16) go(__bf16(), read_tokens<__bf16, true>);
+  else if (c.dtype == EWSJF_E4M3_F16) go(_Float16(), read_tokens<_Float16, true>);
+  else if (c.dtype == EWSJF_BF16) go(__bf16(), read_tokens<__bf16, false>);
+  else go(_Float16(), read_tokens<_Float16, false>);
+  return hipGetLastError();
+}
+
+}  // namespace ewsjf

@@ -1,7 +1,7 @@
-"""Thin PyTorch binding of the paged key/value cache and its attention
-(ewsjf_cache_*, ewsjf_prefix_plan, ewsjf_window_plan, ewsjf_attention in
-include/ewsjf.h): what a server runs for the requests a scheduling step
-admits, on the same card and stream.
+"""Thin PyTorch binding of the paged key/value cache, of 16 or 8 bits, and its
+attention (ewsjf_cache_*, ewsjf_prefix_plan, ewsjf_window_plan,
+ewsjf_attention in include/ewsjf.h): what a server runs for the requests a
+scheduling step admits, on the same card and stream.
 
     cache = kv.PagedCache.new(layers, n_pages, page_size, kv_heads, head_dim, n_slots, width)
     granted = cache.fork(parent, child, tokens)     # a prompt's pages shared, its partial page copied
@@ -11,6 +11,8 @@ admits, on the same card and stream.
     plan = kv.prefix_plan(cache, slot, q_start, group_start, shared, total_q=.., max_q=.., q_heads=..)
     cache.append(layer, k, v, slot, q_start, granted=granted)  # every layer: the new tokens' keys and values,
     out, lse = kv.attention(q, cache, layer, plan)             # and their queries, with the same plan
+    granted = cache.reorder(slot, parent)           # beams: each slot takes over its parent's tokens
+    k, v = cache.read(layer, slot, start, total=..) # what the pages stand for, dense
     cache.release(child)
 
 Nothing here synchronizes the host; a request that does not fit the pool is
@@ -29,6 +31,7 @@ from .ewsjf import Workspace, _need, _stream
 
 _HERE = contextlib.nullcontext()
 _DTYPES = {torch.bfloat16: L.BF16, torch.float16: L.F16}
+_CODES = {torch.bfloat16: L.E4M3_BF16, torch.float16: L.E4M3_F16}
 
 
 def _addr(struct) -> int:
@@ -69,6 +72,14 @@ def _scratch(ws: Workspace | None, nbytes: int, device, raw: int, stream) -> tor
     return buf
 
 
+def page_bytes(page_size: int, kv_heads: int, head_dim: int) -> int:
+    """Bytes of a page's keys, or of its values, in an 8-bit cache (ewsjf_cache_page_bytes)."""
+    n = int(L.lib().ewsjf_cache_page_bytes(page_size, kv_heads, head_dim, L.E4M3_BF16))
+    if n == 0:
+        raise ValueError("pages of these sizes are not supported (see ewsjf_cache)")
+    return n
+
+
 class PagedCache:
     """Pages of keys and values, the rows that name them and their counts.
 
@@ -77,7 +88,12 @@ class PagedCache:
     [page_size][kv_heads][head_dim] (give that tensor transposed).  refs: int32
     [n_pages], rows that hold a page, 0 for a free one.  table: int32
     [n_slots][width], a slot's pages, -1 for none.  length: int32 [n_slots],
-    tokens held."""
+    tokens held.
+
+    In 8 bits (`of_bytes`, `new(bits=8)`) data is uint8
+    [layers][2][n_pages][page_bytes], a page's e4m3 codes and behind them the
+    exponents of their scales (`codes`, `scales`), and dtype is the 16-bit type
+    of what is appended, read and attended with."""
 
     def __init__(self, data: torch.Tensor, refs: torch.Tensor, table: torch.Tensor, length: torch.Tensor):
         if not isinstance(data, torch.Tensor) or data.dtype not in _DTYPES or not data.is_cuda or data.dim() != 6 \
@@ -88,16 +104,22 @@ class PagedCache:
         _need(table, torch.int32, "table")
         _need(length, torch.int32, "length")
         layers, _, n_pages, kv_heads, page_size, head_dim = data.shape
+        self._hold(data, refs, table, length, [_stride(data, d) for d in range(5)],
+                   (layers, n_pages, page_size, kv_heads, head_dim), data.dtype, _DTYPES[data.dtype])
+
+    def _hold(self, data, refs, table, length, strides, sizes, dtype, code) -> None:
+        layers, n_pages, page_size, kv_heads, head_dim = sizes
         if table.dim() != 2 or refs.shape != (n_pages,) or length.shape != (table.shape[0],):
             raise ValueError("refs has one entry per page, table and length one row per slot")
         if any(t.device != data.device for t in (refs, table, length)):
             raise ValueError("data, refs, table and length are on one device")
         self.data, self.refs, self.table, self.length = data, refs, table, length
-        self.page_size, self.device, self.dtype = page_size, data.device, data.dtype
+        self.page_size, self.device, self.dtype = page_size, data.device, dtype
         self.used_on = None
-        self.sizes = (data.device, kv_heads, head_dim, page_size, *table.shape)  # what a plan's layout and slots follow
-        self.c = L.Cache(data.data_ptr(), refs.data_ptr(), table.data_ptr(), length.data_ptr(), *[_stride(data, d) for d in range(5)],
-                         layers, n_pages, page_size, kv_heads, head_dim, _DTYPES[data.dtype], *table.shape)
+        # what a plan's layout and slots follow
+        self.sizes = (data.device, kv_heads, head_dim, page_size, *table.shape, code >= L.E4M3_BF16)
+        self.c = L.Cache(data.data_ptr(), refs.data_ptr(), table.data_ptr(), length.data_ptr(), *strides,
+                         layers, n_pages, page_size, kv_heads, head_dim, code, *table.shape)
         self._c = _addr(self.c)
         self._ws_bytes = int(L.lib().ewsjf_cache_workspace_bytes(self._c))
         if self._ws_bytes == 0:
@@ -109,18 +131,72 @@ class PagedCache:
         return cls(data, refs, table, length)
 
     @classmethod
+    def of_bytes(cls, data: torch.Tensor, refs: torch.Tensor, table: torch.Tensor, length: torch.Tensor,
+                 page_size: int, kv_heads: int, head_dim: int, dtype: torch.dtype = torch.bfloat16,
+                 tokens_first: bool = False) -> "PagedCache":
+        """An 8-bit cache over tensors that the caller holds: data uint8
+        [layers][2][n_pages][page_bytes(page_size, kv_heads, head_dim)], the
+        last dim contiguous.  tokens_first: a page's codes lie as
+        [page_size][kv_heads][head_dim]."""
+        if dtype not in _CODES:
+            raise TypeError("dtype is bfloat16 or float16: what the codes stand for")
+        if not isinstance(data, torch.Tensor) or data.dtype != torch.uint8 or not data.is_cuda or data.dim() != 4 \
+                or data.shape[1] != 2 or data.shape[3] != page_bytes(page_size, kv_heads, head_dim) \
+                or data.stride(3) != 1:
+            raise TypeError("data must be a CUDA tensor [layers][2][n_pages][page_bytes] of uint8")
+        _need(refs, torch.int32, "refs")
+        _need(table, torch.int32, "table")
+        _need(length, torch.int32, "length")
+        self = cls.__new__(cls)
+        inner = (head_dim, kv_heads * head_dim) if tokens_first else (page_size * head_dim, head_dim)
+        self._hold(data, refs, table, length, [_stride(data, d) for d in range(3)] + list(inner),
+                   (data.shape[0], data.shape[2], page_size, kv_heads, head_dim), dtype, _CODES[dtype])
+        return self
+
+    @classmethod
     def new(cls, layers: int, n_pages: int, page_size: int, kv_heads: int, head_dim: int, n_slots: int, width: int,
-            dtype: torch.dtype = torch.bfloat16, device=None) -> "PagedCache":
-        """An empty cache: every page free, every slot without tokens."""
+            dtype: torch.dtype = torch.bfloat16, device=None, bits: int = 16) -> "PagedCache":
+        """An empty cache: every page free, every slot without tokens.  bits: 16, or 8 for e4m3 codes."""
+        if bits not in (8, 16):
+            raise ValueError("bits is 16 or 8")
         dev = torch.device(device or "cuda")
-        return cls(torch.zeros((layers, 2, n_pages, kv_heads, page_size, head_dim), dtype=dtype, device=dev),
-                   torch.zeros(n_pages, dtype=torch.int32, device=dev),
-                   torch.full((n_slots, width), -1, dtype=torch.int32, device=dev),
-                   torch.zeros(n_slots, dtype=torch.int32, device=dev))
+        books = (torch.zeros(n_pages, dtype=torch.int32, device=dev),
+                 torch.full((n_slots, width), -1, dtype=torch.int32, device=dev),
+                 torch.zeros(n_slots, dtype=torch.int32, device=dev))
+        if bits == 16:
+            return cls(torch.zeros((layers, 2, n_pages, kv_heads, page_size, head_dim), dtype=dtype, device=dev), *books)
+        data = torch.zeros((layers, 2, n_pages, page_bytes(page_size, kv_heads, head_dim)), dtype=torch.uint8, device=dev)
+        return cls.of_bytes(data, *books, page_size, kv_heads, head_dim, dtype)
+
+    @property
+    def bits(self) -> int:
+        return 8 if self.c.dtype >= L.E4M3_BF16 else 16
+
+    @property
+    def codes(self) -> torch.Tensor:
+        """An 8-bit cache's codes, float8_e4m3fn [layers][2][n_pages][kv_heads][page_size][head_dim], in place."""
+        c, n = self.c, self.c.kv_heads * self.c.page_size * self.c.head_dim
+        if self.bits != 8:
+            raise ValueError("a 16-bit cache has no codes")
+        flat = self.data[..., :n].view(torch.float8_e4m3fn)
+        if c.token_stride == c.head_dim or c.page_size == 1:
+            return flat.unflatten(-1, (c.kv_heads, c.page_size, c.head_dim))
+        return flat.unflatten(-1, (c.page_size, c.kv_heads, c.head_dim)).transpose(3, 4)
+
+    @property
+    def scales(self) -> torch.Tensor:
+        """An 8-bit cache's scales, uint8 [layers][2][n_pages][kv_heads][page_size], in place: b stands for 2^(b - 127)."""
+        c, n = self.c, self.c.kv_heads * self.c.page_size
+        if self.bits != 8:
+            raise ValueError("a 16-bit cache has no scales")
+        return self.data[..., n * c.head_dim:n * (c.head_dim + 1)].unflatten(-1, (c.kv_heads, c.page_size))
 
     def _on(self, stream) -> int:
         """The handle of the stream that a call uses the cache on."""
         raw = _stream(stream)
+        if stream is not None and stream.device != self.device or \
+                stream is None and self.device.index not in (None, torch._C._cuda_getDevice()):
+            raise ValueError("the cache is on another device than the call's stream")
         if raw != self.used_on:
             _keep(self, raw, stream, self.data, self.refs, self.table, self.length)
         return raw
@@ -213,6 +289,48 @@ class PagedCache:
                                                    _stride(k, 1), _stride(v, 0), _stride(v, 1),
                                                    self._ids(slot, "slot"), self._ids(q_start, "q_start", n + 1), g,
                                                    n, k.shape[0], self._on(stream)), "ewsjf_cache_append")
+
+
+    def read(self, layer: int, slot: torch.Tensor, start: torch.Tensor, begin: torch.Tensor | None = None, *,
+             total: int | None = None, out=None, stream=None):
+        """Keys and values (k, v) [total][kv_heads][head_dim] of the slots'
+        tokens, in 16 bits: rows [start[s], start[s + 1]) get the tokens of
+        slot[s] from begin[s] on (None: 0), zeros where there is none
+        (ewsjf_cache_read).  out: (k, v) to write into, whose rows past the
+        last sequence's stay as they are; otherwise `total` rows are made."""
+        n, want = slot.numel(), (self.c.kv_heads, self.c.head_dim)
+        if out is None:
+            if total is None:
+                raise ValueError("total or out is needed")
+            k, v = out = tuple(_new(stream, (int(total), *want), dtype=self.dtype, device=self.device) for _ in range(2))
+        else:
+            k, v = out
+            for t, name in ((k, "k"), (v, "v")):
+                if _need(t, self.dtype, name).dim() != 3 or tuple(t.shape[1:]) != want or t.shape != k.shape \
+                        or t.device != self.device:
+                    raise ValueError(f"{name} is [total][kv_heads][head_dim] on the cache's device")
+            if total is not None and total != k.shape[0]:
+                raise ValueError("out has total rows")
+        b = None if begin is None else self._ids(begin, "begin", n)
+        L.check(L.lib().ewsjf_cache_read(self._c, int(layer), self._ids(slot, "slot"), self._ids(start, "start", n + 1),
+                                         b, n, k.shape[0], k.data_ptr(), v.data_ptr(), self._on(stream)),
+                "ewsjf_cache_read")
+        return out
+
+    def reorder(self, slot: torch.Tensor, parent: torch.Tensor, granted: torch.Tensor | None = None,
+                ws: Workspace | None = None, stream=None) -> torch.Tensor:
+        """slot[i] := what slot[parent[i]] held, for all i at once; a parent of
+        -1 empties the slot.  int32 [n], 1 for a slot that holds its parent's
+        tokens, else 0 (ewsjf_cache_reorder)."""
+        n = slot.numel()
+        granted = _new(stream, n, dtype=torch.int32, device=self.device) if granted is None else granted
+        nbytes = int(L.lib().ewsjf_cache_reorder_workspace_bytes(self._c, n))
+        raw = self._on(stream)
+        buf = _scratch(ws, nbytes, self.device, raw, stream)
+        L.check(L.lib().ewsjf_cache_reorder(self._c, self._ids(slot, "slot"), self._ids(parent, "parent", n), n,
+                                            self._ids(granted, "granted", n), buf.data_ptr(), buf.numel(), raw),
+                "ewsjf_cache_reorder")
+        return granted
 
 
 class AttentionPlan:
