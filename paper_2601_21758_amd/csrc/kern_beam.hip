@@ -5,12 +5,13 @@
 // second, a workgroup a group, joins the sums, scores what is left and ranks it.
 //
 // Scores are compared across rows, so the logarithms of the sums have to be
-// right far beyond the logits' own 8 to 24 bits: with sums in binary32 (errors of
-// 1e-7) about one step of 64 groups of eight beams in a hundred would rank two
-// candidates the wrong way round.  Exponentials are taken in binary64 to 2e-13:
+// right far beyond the logits' own 8 to 24 bits: with sums right to 1e-7, about
+// one call in a hundred with 64 groups of eight beams would rank two candidates the
+// wrong way round.  So exponentials are taken to 5e-10 and summed in binary64:
 //   e^x = 2^(n / 256) e^r, n = round(256 x / ln 2), |r| <= ln 2 / 512,
-// 2^(n / 256) an exponent and one of 256 numbers in LDS, e^r three terms.
-// binary64 adds and fused products run at binary32's rate here.
+// 2^(n / 256) an exponent and one of 256 numbers in LDS, e^r - 1 two terms in
+// binary32 (the third is at most 4e-10, of the sign of r).  binary64 adds and
+// fused products run at binary32's rate here.
 #include <hip/hip_runtime.h>
 
 #include "ewsjf_cache.h"
@@ -19,7 +20,9 @@ namespace ewsjf {
 namespace {
 
 constexpr int kThreads = 256;      // of a segment's workgroup
-constexpr int kJoinThreads = 1024; // of a group's
+constexpr int kWaves = kThreads / 64;
+constexpr int kWavePieces = 128;   // pieces with candidates that a wave keeps
+constexpr int kJoinThreads = 1024; // of a group's workgroup
 constexpr int kMostFound = 2048;   // candidates that a workgroup ranks at once
 constexpr int kWanted = 512;       // workgroups that a launch should have
 constexpr int kVocabBits = 22, kRowBits = 5;
@@ -36,14 +39,16 @@ struct Sizes {
   int segments;  // of a row
 };
 
-Sizes sizes_of(const ewsjf_beams& b) {
-  const int in = b.dtype == EWSJF_F32 ? 4 : 8;                 // elements of a piece
-  const int64_t pieces = (b.vocab + in - 1 + in - 1) / in;     // of a row that begins anywhere in one
-  Sizes s{8, 0};
-  for (;; s.vectors /= 2) {
-    s.segments = (int)((pieces + kThreads * s.vectors - 1) / (kThreads * s.vectors));
-    if (s.vectors == 1 || (int64_t)b.groups * b.beams * s.segments >= kWanted) return s;
-  }
+// skew: elements that a row's first piece has before it, at most (the workspace is sized for any).
+Sizes sizes_of(const ewsjf_beams& b, int skew) {
+  const int in = b.dtype == EWSJF_F32 ? 4 : 8;  // elements of a piece
+  auto segments = [&](int vectors, int skew) {
+    const int64_t pieces = (b.vocab + skew + in - 1) / in;
+    return (int)((pieces + kThreads * vectors - 1) / (kThreads * vectors));
+  };
+  int vectors = 8;
+  while (vectors > 1 && (int64_t)b.groups * b.beams * segments(vectors, in - 1) < kWanted) vectors /= 2;
+  return Sizes{vectors, segments(vectors, skew < 0 ? in - 1 : skew)};
 }
 
 struct Work {
@@ -126,61 +131,143 @@ __device__ void sort_entries(Entry* entry, int n, const Entry& none, Above above
 // ---------------------------------------------------------------------------
 // Segments
 // ---------------------------------------------------------------------------
-// The largest magnitudes, as whole numbers: of a word, of each half of it.
-__device__ uint32_t larger32(uint32_t a, const uint4& v) {
-  const uint32_t m = 0x7fffffffu;
-  return max(max(max(a, v.x & m), max(v.y & m, v.z & m)), v.w & m);
+// 16 bytes of logits.  `order`: a word's logits as whole numbers in their order, with a sign; a NaN without one is above
+// infinity, one with a sign below all.  `clamp`: to at least the negative `low`, a NaN with a sign among them.
+__device__ uint32_t order_of(uint32_t w, float) { return w ^ ((uint32_t)((int32_t)w >> 31) & 0x7fffffffu); }
+typedef __attribute__((ext_vector_type(2))) int16_t i16x2;
+typedef __attribute__((ext_vector_type(2))) uint16_t u16x2;
+__device__ uint32_t order16(uint32_t w) {
+  const i16x2 sign = __builtin_bit_cast(i16x2, w) >> 15;
+  return w ^ (__builtin_bit_cast(uint32_t, sign) & 0x7fff7fffu);
 }
-__device__ uint32_t larger16(uint32_t a, const uint4& v) {
-  typedef __attribute__((ext_vector_type(2))) uint16_t u16x2;
-  auto halves = [](uint32_t x) { return __builtin_bit_cast(u16x2, x & 0x7fff7fffu); };
-  const u16x2 x = __builtin_elementwise_max(halves(v.x), halves(v.y));
-  const u16x2 y = __builtin_elementwise_max(halves(v.z), halves(v.w));
-  return __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(u16x2, a), __builtin_elementwise_max(x, y)));
+__device__ uint32_t max16(uint32_t a, uint32_t b) {
+  return __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(i16x2, a), __builtin_bit_cast(i16x2, b)));
+}
+// Halves that are NaN become those of `none`.
+__device__ uint32_t without_nan16(uint32_t w, uint32_t inf, uint32_t none) {
+  const uint32_t nan = ((w & 0x7fff7fffu) + (0x7fffu - inf) * 0x10001u) & 0x80008000u, mask = (nan >> 15) * 0xffffu;
+  return (w & ~mask) | (none & mask);
+}
+// The larger half of an ordered word, in the upper half.
+__device__ int32_t upper(uint32_t w) { return max((int32_t)w, (int32_t)(w << 16)) & (int32_t)0xffff0000; }
+__device__ uint32_t clamp16(uint32_t w, uint32_t low) {
+  return __builtin_bit_cast(uint32_t, __builtin_elementwise_min(__builtin_bit_cast(u16x2, w), __builtin_bit_cast(u16x2, low)));
 }
 
 template <typename T>
-struct Piece;  // 16 bytes of logits
+struct Piece;
 template <>
 struct Piece<float> {
   static constexpr int N = 4;
-  static __device__ uint32_t larger(uint32_t a, const uint4& v) { return larger32(a, v); }
-  static __device__ bool has_nan(uint32_t a) { return a > 0x7f800000u; }
   static constexpr uint32_t kNone = 0xff800000u;
+  static constexpr int32_t kInf = 0x7f800000;
   static __device__ float at(const uint4& v, int i) { return __uint_as_float((&v.x)[i]); }
+  static __device__ int32_t largest(const uint4& v) {
+    return max(max((int32_t)order_of(v.x, 0.f), (int32_t)order_of(v.y, 0.f)),
+               max((int32_t)order_of(v.z, 0.f), (int32_t)order_of(v.w, 0.f)));
+  }
+  static __device__ float value(int32_t order) { return __uint_as_float(order_of((uint32_t)order, 0.f)); }
+  static __device__ uint32_t low_of(float low) { return __float_as_uint(low); }
+  static __device__ uint32_t clamp(uint32_t w, uint32_t low) { return min(w, low); }
+  static __device__ uint32_t without_nan(uint32_t w) { return (w & 0x7fffffffu) > 0x7f800000u ? kNone : w; }
 };
 template <>
 struct Piece<__bf16> {
   static constexpr int N = 8;
-  static __device__ uint32_t larger(uint32_t a, const uint4& v) { return larger16(a, v); }
-  static __device__ bool has_nan(uint32_t a) { return a >> 16 > 0x7f80u || (a & 0xffffu) > 0x7f80u; }
   static constexpr uint32_t kNone = 0xff80ff80u;
+  static constexpr int32_t kInf = 0x7f800000;
   static __device__ float at(const uint4& v, int i) {
     const uint32_t w = (&v.x)[i / 2];
     return __uint_as_float(i % 2 ? w & 0xffff0000u : w << 16);
   }
+  static __device__ int32_t largest(const uint4& v) {
+    return upper(max16(max16(order16(v.x), order16(v.y)), max16(order16(v.z), order16(v.w))));
+  }
+  static __device__ float value(int32_t order) { return __uint_as_float(order16((uint32_t)order & 0xffff0000u)); }
+  static __device__ uint32_t low_of(float low) { return (__float_as_uint(low) >> 16) * 0x10001u; }
+  static __device__ uint32_t clamp(uint32_t w, uint32_t low) { return clamp16(w, low); }
+  static __device__ uint32_t without_nan(uint32_t w) { return without_nan16(w, 0x7f80u, kNone); }
 };
 template <>
 struct Piece<_Float16> {
   static constexpr int N = 8;
-  static __device__ uint32_t larger(uint32_t a, const uint4& v) { return larger16(a, v); }
-  static __device__ bool has_nan(uint32_t a) { return a >> 16 > 0x7c00u || (a & 0xffffu) > 0x7c00u; }
   static constexpr uint32_t kNone = 0xfc00fc00u;
-  static __device__ float at(const uint4& v, int i) {
-    union {
-      uint16_t bits;
-      _Float16 x;
-    } u;
-    u.bits = (uint16_t)((&v.x)[i / 2] >> (i % 2 * 16));
-    return (float)u.x;
+  static constexpr int32_t kInf = 0x7c000000;
+  static __device__ float half(uint32_t bits) { return (float)__builtin_bit_cast(_Float16, (uint16_t)bits); }
+  static __device__ float at(const uint4& v, int i) { return half((&v.x)[i / 2] >> (i % 2 * 16)); }
+  static __device__ int32_t largest(const uint4& v) {
+    return upper(max16(max16(order16(v.x), order16(v.y)), max16(order16(v.z), order16(v.w))));
+  }
+  static __device__ float value(int32_t order) { return half(order16((uint32_t)order) >> 16); }
+  static __device__ uint32_t low_of(float low) { return __builtin_bit_cast(uint16_t, (_Float16)low) * 0x10001u; }
+  static __device__ uint32_t clamp(uint32_t w, uint32_t low) { return clamp16(w, low); }
+  static __device__ uint32_t without_nan(uint32_t w) { return without_nan16(w, 0x7c00u, kNone); }
+};
+
+// A value in its type's order, as `largest` gives it.
+template <typename T>
+__device__ int32_t order_in(float y) {
+  if constexpr (sizeof(T) == 4) return (int32_t)order_of(__float_as_uint(y), 0.f);
+  else return (int32_t)(order16(__builtin_bit_cast(uint16_t, (T)y)) << 16);
+}
+
+// The exponentials of a wave's logits, relative to 2^from.
+struct PowerTable {
+  double at[256];
+};
+// 2^(i / 256), by its series, less i in the bits that `Powers` adds it to.
+constexpr PowerTable power_table() {
+  PowerTable t{};
+  for (int i = 0; i < 256; ++i) {
+    const double x = i * 0.0027076061740622863;
+    double sum = 0.;
+    for (int k = 24; k >= 1; --k) sum = (sum + 1.) * x / k;
+    t.at[i] = sum + 1.;
+  }
+  return t;
+}
+__device__ const PowerTable kPowers = power_table();
+
+struct Powers {
+  static constexpr double kPerLn2 = 369.3299304675746;  // 256 / ln 2
+  static constexpr float kHigh = (float)kPerLn2, kLow = (float)(kPerLn2 - (double)kHigh);
+  static constexpr double kStep = 0.0027076061740622863;  // ln 2 / 256
+  static constexpr float kOne = (float)kStep, kTwo = (float)(kStep * kStep / 2);
+  // Sums with `round`, 1.5 2^23 less a multiple of 256, are rounded to whole numbers, n - 256 from in their low bits.
+  // Those bits, 12 to the left, add n >> 8 - from to a binary64's exponent and n & 255 below it, which the table's numbers
+  // have less; the others, of 1.5 2^23, leave the word.
+  static __device__ double entry(int i) {
+    const uint64_t b = __double_as_longlong(kPowers.at[i]);
+    return __longlong_as_double(b - ((uint64_t)i << 44));
+  }
+  const double* table;
+  float round;
+  double sum = 0., more = 0.;
+  struct Term {
+    double two;  // the table's number
+    uint32_t bits;
+    float p;     // e^r - 1 with r in steps
+  };
+
+  __device__ Term ask(float y) const {
+    const float t = fmaf(y, kHigh, round);
+    const uint32_t bits = __float_as_uint(t);
+    const double two = table[bits & 255];
+    const float r = fmaf(y, kLow, fmaf(y, kHigh, -(t - round)));  // in [-1/2, 1/2]
+    return Term{two, bits, fmaf(r, kTwo, kOne) * r};
+  }
+  __device__ void add(const Term& x) {
+    const uint64_t e = __double_as_longlong(x.two);
+    const double two = __longlong_as_double((uint64_t)((uint32_t)(e >> 32) + (x.bits << 12)) << 32 | (uint32_t)e);
+    sum += two;
+    more = fma(two, (double)x.p, more);
   }
 };
 
-constexpr double kPerLn2 = 369.3299304675746;  // 256 / ln 2
-constexpr double kLn2Part = 0.0027076061740622863;  // ln 2 / 256
-constexpr double kRound = 6755399441055744.;  // 1.5 2^52: a sum with it is rounded to a whole number, in its low bits
+// Keeps what follows from v from living in registers since it was last used.
+__device__ void fresh(uint4& v) { asm volatile("" : "+v"(v.x), "+v"(v.y), "+v"(v.z), "+v"(v.w)); }
 
-// Workgroup (segment, row).
+// Workgroup (segment, row); its waves share nothing before the end.
 template <typename T, int NV>
 __global__ __launch_bounds__(kThreads) void take_segments(ewsjf_beams b, const T* logits, const float* score_in,
                                                           const int32_t* done, Work w, int segments) {
@@ -188,174 +275,215 @@ __global__ __launch_bounds__(kThreads) void take_segments(ewsjf_beams b, const T
   constexpr int N = P::N;
   __shared__ double power[256];
   __shared__ uint64_t found[kMostFound];
-  __shared__ double sums[kThreads / 64];
-  __shared__ float tops[kThreads / 64];
-  __shared__ uint32_t least[kThreads / 64];
+  __shared__ uint4 pieces[kWaves][kWavePieces];  // that hold a wave's candidates,
+  __shared__ int firsts[kWaves][kWavePieces];    // and their first tokens
+  __shared__ Part parts[kWaves];
+  __shared__ int counts[kWaves], bars[kWaves];
   __shared__ int count;
-  const int row = blockIdx.y, seg = blockIdx.x, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int row = blockIdx.y, seg = blockIdx.x, lane = threadIdx.x & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   // rows without candidates are not read
   if (!(score_in[row] > -INFINITY) || (done != nullptr && done[row] != 0)) return;
   const T* x = logits + row * b.row_stride;
   const int skew = (int)((reinterpret_cast<uintptr_t>(x) & 15) / sizeof(T));  // elements of the first piece before the row
+  const int piece0 = seg * kThreads * NV + wave * 64 * NV + lane;
+  auto token_of = [&](int i) { return (piece0 + i * 64) * N - skew; };  // of piece i's first element
   uint4 v[NV];
-  const int piece0 = seg * kThreads * NV + threadIdx.x;
 #pragma unroll
   for (int i = 0; i < NV; ++i) {
-    const int64_t first = (int64_t)(piece0 + i * kThreads) * N - skew;  // token of the piece's first element
+    const int first = token_of(i);
     v[i] = make_uint4(P::kNone, P::kNone, P::kNone, P::kNone);
-    if (first >= 0 && first + N <= b.vocab) {
-      v[i] = *reinterpret_cast<const uint4*>(x + first);
-    } else {
-      T part[N];
-      *reinterpret_cast<uint4*>(part) = v[i];
+    if (first >= 0 && first + N <= b.vocab) v[i] = *reinterpret_cast<const uint4*>(x + first);
+  }
+  power[threadIdx.x] = Powers::entry(threadIdx.x);
+  if (threadIdx.x == 0) count = 0;
+  __syncthreads();
 #pragma unroll
-      for (int j = 0; j < N; ++j)
-        if (first + j >= 0 && first + j < b.vocab) part[j] = x[first + j];
-      v[i] = *reinterpret_cast<const uint4*>(part);
+  for (int i = 0; i < NV; ++i) {
+    const int first = token_of(i);
+    if (first < b.vocab && first + N > 0 && (first < 0 || first + N > b.vocab)) {  // at an end of the row
+      constexpr int kBits = 8 * sizeof(T), kIn = 32 / kBits;
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        uint32_t word = P::kNone;
+#pragma unroll
+        for (int j = 0; j < kIn; ++j) {
+          const int at = first + k * kIn + j;
+          if (at >= 0 && at < b.vocab) {
+            const uint32_t mask = kBits == 32 ? ~0u : 0xffffu << (j * 16);
+            uint32_t bits;
+            if constexpr (kBits == 32) bits = reinterpret_cast<const uint32_t*>(x)[at];
+            else bits = reinterpret_cast<const uint16_t*>(x)[at];
+            word = (word & ~mask) | bits << (j * (kBits % 32));
+          }
+        }
+        (&v[i].x)[k] = word;
+      }
     }
   }
-  power[threadIdx.x] = exp2(threadIdx.x / 256.);
-  if (threadIdx.x == 0) count = 0;
 
-  // NaN become -inf: the maximum of a signalling NaN and a number is a NaN.
-  uint32_t largest = 0;
-#pragma unroll
-  for (int i = 0; i < NV; ++i) largest = P::larger(largest, v[i]);
-  if (P::has_nan(largest)) {
+  int32_t most[NV], top = INT32_MIN;
+  for (;;) {
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
-      T part[N];
-      *reinterpret_cast<uint4*>(part) = v[i];
-#pragma unroll
-      for (int j = 0; j < N; ++j)
-        if (!(P::at(v[i], j) >= -INFINITY)) part[j] = (T)-INFINITY;
-      v[i] = *reinterpret_cast<const uint4*>(part);
+      fresh(v[i]);
+      most[i] = P::largest(v[i]);
+      top = max(top, most[i]);
     }
+    if (!__any(top > P::kInf)) break;
+    top = INT32_MIN;  // a NaN: once more without any
+#pragma unroll
+    for (int i = 0; i < NV; ++i)
+#pragma unroll
+      for (int k = 0; k < 4; ++k) (&v[i].x)[k] = P::without_nan((&v[i].x)[k]);
   }
-
-  float most[NV], ref;
-  double sum, base;
+  // A value that at least `picks` of the wave's logits reach: over the lanes' largest, for many picks over the pieces'
+  // largest or all logits.
+  constexpr int kBits = 8 * sizeof(T);
+  constexpr uint32_t kSign = 0x80000000u;
   uint32_t bar;
-  float top = -INFINITY;
-#pragma unroll
-  for (int i = 0; i < NV; ++i) {
-    most[i] = -INFINITY;
-#pragma unroll
-    for (int j = 0; j < N; ++j) most[i] = fmaxf(most[i], P::at(v[i], j));
-    top = fmaxf(top, most[i]);
-  }
-  constexpr int kBits = __is_same(T, __bf16) ? 16 : 32;
-  if (b.picks <= 32 || NV == 1) {
-    const uint32_t key[1] = {order32(top)};
+  if (b.picks <= 32) {
+    const uint32_t key[1] = {(uint32_t)top ^ kSign};
     bar = wave_threshold<kBits>(key, b.picks);
+  } else if (NV == 1) {
+    uint32_t key[N];
+#pragma unroll
+    for (int j = 0; j < N; ++j) key[j] = order32(P::at(v[0], j));
+    bar = wave_threshold<32>(key, b.picks);
+    const float y = value32(bar);  // back to the type's own order
+    bar = y >= -3.4028234e38f ? (uint32_t)order_in<T>(y) ^ kSign : 0;
   } else {
     uint32_t key[NV];
 #pragma unroll
-    for (int i = 0; i < NV; ++i) key[i] = order32(most[i]);
+    for (int i = 0; i < NV; ++i) key[i] = (uint32_t)most[i] ^ kSign;
     bar = wave_threshold<kBits>(key, b.picks);
   }
   top = wave_max(top);
-  if (lane == 0) tops[wave] = top, least[wave] = bar;
-  __syncthreads();
-  ref = tops[0];
+  const float ref = P::value(top);
+
+  // The sum.
+  double sum = 0.;
+  if (fabsf(ref) < 500.f) {
+    const int from = (int)rintf(ref * Powers::kHigh) >> 8;
+    const uint32_t low = P::low_of(ref - 600.f);  // e^-600 of the largest: nothing, and within a binary64's exponents
+    Powers powers{power, 12582912.f - 256.f * from};
+    constexpr int kAhead = 4;  // numbers of the table that are on their way
+    typename Powers::Term term[2][kAhead];
+    uint4 held;
 #pragma unroll
-  for (int i = 1; i < kThreads / 64; ++i) ref = fmaxf(ref, tops[i]);
+    for (int k = 0; k <= NV * N / kAhead; ++k) {
+      if (k < NV * N / kAhead) {
+        if (k * kAhead % N == 0) {
+          held = v[k * kAhead / N];
+          fresh(held);
 #pragma unroll
-  for (int i = 0; i < kThreads / 64; ++i) bar = least[i] > bar ? least[i] : bar;
-  sum = 0., base = ref;
-  if (ref == INFINITY) {  // the entries of +inf share the row
+          for (int j = 0; j < 4; ++j) (&held.x)[j] = P::clamp((&held.x)[j], low);
+        }
 #pragma unroll
-    for (int i = 0; i < NV; ++i)
-#pragma unroll
-      for (int j = 0; j < N; ++j) sum += P::at(v[i], j) == INFINITY ? 1. : 0.;
-  } else if (fabsf(ref) < 1e6f) {
-    const int from = (int)rint(ref * kPerLn2) >> 8;
-    base = from * 0.6931471805599453;
-    const float low = ref - 600.f;  // e^-600 of the largest: nothing, and within a binary64's exponents
-    double more = 0.;
-#pragma unroll
-    for (int i = 0; i < NV; ++i)
-#pragma unroll
-      for (int j = 0; j < N; ++j) {
-        const double y = fmaxf(P::at(v[i], j), low);
-        const double t = fma(y, kPerLn2, kRound);
-        const int n = (int)__double_as_longlong(t);
-        const double r = fma(y, kPerLn2, -(t - kRound));  // in [-1/2, 1/2]
-        constexpr double c1 = kLn2Part, c2 = c1 * c1 / 2, c3 = c1 * c1 * c1 / 6;
-        const double p = fma(fma(c3, r, c2), r, c1) * r;
-        const uint64_t bits = __double_as_longlong(power[n & 255]);
-        const uint32_t hi = (uint32_t)(bits >> 32) + ((uint32_t)((n >> 8) - from) << 20);
-        const double e = __longlong_as_double((uint64_t)hi << 32 | (uint32_t)bits);
-        sum += e;
-        more = fma(e, p, more);
+        for (int j = 0; j < kAhead; ++j) term[k % 2][j] = powers.ask(P::at(held, (k * kAhead + j) % N));
       }
-    sum += more;
-  } else if (ref > -INFINITY) {  // logits so far out that their multiples pass 32 bits
+      if (k > 0)
 #pragma unroll
+        for (int j = 0; j < kAhead; ++j) powers.add(term[(k - 1) % 2][j]);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+    Powers largest{power, powers.round};
+    largest.add(largest.ask(ref));
+    // e^ref has the errors of the others: a row's only token has probability 1
+    sum = (powers.sum + powers.more) / (largest.sum + largest.more);
+  } else if (ref > -INFINITY) {  // far logits, or entries of +inf, which share the row: read once more
+#pragma unroll 1
     for (int i = 0; i < NV; ++i)
-#pragma unroll
+#pragma unroll 1
       for (int j = 0; j < N; ++j) {
-        const float y = P::at(v[i], j);
-        if (y > -INFINITY) sum += exp((double)y - ref);
+        const int at = token_of(i) + j;
+        const float y = at >= 0 && at < b.vocab ? (float)x[at] : -INFINITY;
+        if (y > -INFINITY) sum += ref == INFINITY ? (y == INFINITY ? 1. : 0.) : exp((double)y - ref);
       }
   }
   sum = wave_sum(sum);
-  if (lane == 0) sums[wave] = sum;
-  __syncthreads();
-  sum = sums[0];
-#pragma unroll
-  for (int i = 1; i < kThreads / 64; ++i) sum += sums[i];
 
-  // The candidates.
-  const float bound = bar > order32(-INFINITY) ? value32(bar) : -INFINITY;  // numbers below are no values
-  auto token_of = [&](int i, int j) { return (uint32_t)((piece0 + i * kThreads) * N + j - skew); };
-  auto key_of = [&](float y, uint32_t token) { return (uint64_t)order32(y) << 32 | (uint32_t)~token; };
+  // The pieces with candidates.
+  const int32_t own = (int32_t)(bar ^ kSign);
+  int n = 0;
 #pragma unroll
-  for (int i = 0; i < NV; ++i)
-    if (most[i] >= bound && most[i] > -INFINITY)
-#pragma unroll
-      for (int j = 0; j < N; ++j) {
-        const float y = P::at(v[i], j);
-        if (y >= bound && y > -INFINITY) {
-          const int at = atomicAdd(&count, 1);
-          if (at < kMostFound) found[at] = key_of(y, token_of(i, j));
-        }
-      }
-  __syncthreads();
-  const int n = count;
-  const int64_t out = (int64_t)row * segments + seg;
-  if (threadIdx.x == 0) w.part[out] = Part{sum, base};
-  uint64_t* best = w.best + out * b.picks;
-  if (n <= kThreads) {  // the usual case: an entry a thread, ranked against the others
-    const uint64_t mine = (int)threadIdx.x < n ? found[threadIdx.x] : 0;
-    int rank = 0;
-    for (int i = 0; i < n; ++i) rank += found[i] > mine;
-    if ((int)threadIdx.x < n && rank < b.picks) best[rank] = mine;
-  } else if (n <= kMostFound) {
-    sort_entries<kThreads>(found, n, (uint64_t)0, [](uint64_t p, uint64_t q) { return p > q; });
-    if ((int)threadIdx.x < b.picks) best[threadIdx.x] = found[threadIdx.x];
-  } else {  // a plateau of equal logits: one pass over the registers a pick
-    uint64_t last = ~0ull;
-    for (int k = 0; k < b.picks; ++k) {
-      uint64_t mine = 0;
-#pragma unroll
-      for (int i = 0; i < NV; ++i)
-#pragma unroll
-        for (int j = 0; j < N; ++j) {
-          const float y = P::at(v[i], j);
-          const uint64_t key = y > -INFINITY ? key_of(y, token_of(i, j)) : 0;
-          if (key < last && key > mine) mine = key;
-        }
-      mine = wave_max(mine);
-      __syncthreads();
-      if (lane == 0) found[wave] = mine;
-      __syncthreads();
-      for (int i = 0; i < kThreads / 64; ++i) mine = found[i] > mine ? found[i] : mine;
-      if (threadIdx.x == 0) best[k] = mine;
-      last = mine;
+  for (int i = 0; i < NV; ++i) {
+    const uint64_t taken = __ballot(most[i] >= own);
+    if (taken) {
+      const int at = n + __builtin_amdgcn_mbcnt_hi((uint32_t)(taken >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)taken, 0));
+      if (taken >> lane & 1 && at < kWavePieces) pieces[wave][at] = v[i], firsts[wave][at] = token_of(i);
+      n += __popcll(taken);
     }
   }
-  for (int k = n + threadIdx.x; k < b.picks; k += kThreads) best[k] = 0;
+  if (lane == 0) parts[wave] = Part{sum, ref}, counts[wave] = n, bars[wave] = own;
+  __syncthreads();
+
+  // Together.
+  const int64_t out = (int64_t)row * segments + seg;
+  if (wave == 0) {
+    const Part p = parts[lane % kWaves];
+    double most = p.base;
+    for (int d = 1; d < kWaves; d *= 2) most = fmax(most, __shfl_xor(most, d));
+    double all = p.base == most ? p.sum : p.base > -INFINITY ? p.sum * exp(p.base - most) : 0.;
+    for (int d = 1; d < kWaves; d *= 2) all += __shfl_xor(all, d);
+    if (lane == 0) w.part[out] = Part{all, most};
+  }
+  int32_t least = bars[0];
+  bool whole = true;
+#pragma unroll
+  for (int i = 0; i < kWaves; ++i) least = max(least, bars[i]), whole &= counts[i] <= kWavePieces;
+  // none of -inf: numbers below are no values
+  const float lowest = -3.4028234e38f, bound = least > order_in<T>(-INFINITY) ? max(P::value(least), lowest) : lowest;
+  auto key_of = [&](float y, uint32_t token) { return (uint64_t)order32(y) << 32 | (uint32_t)~token; };
+  if (whole) {
+#pragma unroll
+    for (int i = 0; i < kWaves; ++i)
+      for (int k = threadIdx.x; k < counts[i] * N; k += kThreads) {
+        float y;
+        if constexpr (N == 4) y = P::at(make_uint4((&pieces[i][k / N].x)[k % N], 0, 0, 0), 0);
+        else y = P::at(make_uint4((&pieces[i][k / N].x)[k % N / 2] >> (k % 2 * 16), 0, 0, 0), 0);
+        if (y >= bound) {
+          const int at = atomicAdd(&count, 1);
+          if (at < kMostFound) found[at] = key_of(y, (uint32_t)(firsts[i][k / N] + k % N));
+        }
+      }
+  }
+  __syncthreads();
+  const int total = whole ? count : kMostFound + 1;
+  uint64_t* best = w.best + out * b.picks;
+  if (total <= kMostFound / 4) {  // each candidate ranked against the others
+    for (int k = threadIdx.x; k < total; k += kThreads) {
+      const uint64_t key = found[k];
+      int rank = 0;
+#pragma unroll 8
+      for (int j = 0; j < total; ++j) rank += found[j] > key;
+      if (rank < b.picks) best[rank] = key;
+    }
+  } else if (total <= kMostFound) {
+    sort_entries<kThreads>(found, total, (uint64_t)0, [](uint64_t p, uint64_t q) { return p > q; });
+    if ((int)threadIdx.x < b.picks) best[threadIdx.x] = found[threadIdx.x];
+  } else {  // a plateau of equal logits: one pass over the segment a pick
+    uint64_t last = ~0ull;
+#pragma unroll 1
+    for (int k = 0; k < b.picks; ++k) {
+      uint64_t next = 0;
+#pragma unroll 1
+      for (int i = 0; i < NV * N; ++i) {
+        const int at = token_of(i / N) + i % N;
+        const float y = at >= 0 && at < b.vocab ? (float)x[at] : -INFINITY;
+        const uint64_t key = y > -INFINITY ? key_of(y, (uint32_t)at) : 0;
+        if (key < last && key > next) next = key;
+      }
+      next = wave_max(next);
+      __syncthreads();
+      if (lane == 0) found[wave] = next;
+      __syncthreads();
+      for (int i = 0; i < kWaves; ++i) next = found[i] > next ? found[i] : next;
+      if (threadIdx.x == 0) best[k] = next;
+      last = next;
+    }
+  }
+  for (int k = total + threadIdx.x; k < b.picks; k += kThreads) best[k] = 0;
 }
 
 // ---------------------------------------------------------------------------
@@ -373,14 +501,23 @@ __device__ bool above(const Entry& a, const Entry& b) {
 __global__ __launch_bounds__(kJoinThreads) void join_groups(ewsjf_beams b, const float* score_in, const int32_t* done,
                                                             Work w, int segments, int32_t* parent, int32_t* token,
                                                             float* score) {
-  constexpr int kWaves = kJoinThreads / 64;
+  constexpr int kWaves = kJoinThreads / 64, kHeld = 2;  // candidates that a thread holds
   __shared__ Entry found[kMostFound];
   __shared__ double base[EWSJF_MAX_BEAMS];  // score of a logit of 0
   __shared__ int kind[EWSJF_MAX_BEAMS];     // 0: no candidates, 1: logits, 2: entries of +inf alone, 3: at its end
-  __shared__ uint64_t least[kWaves];
+  __shared__ uint32_t least[kWaves];
   __shared__ Entry tops[kWaves];
   __shared__ int count;
-  const int group = blockIdx.x, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int group = blockIdx.x, lane = threadIdx.x & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int each = segments * b.picks, all = b.beams * each;
+  const uint64_t* best = w.best + (int64_t)group * all;
+  uint64_t key[kHeld];  // asked for before anything waits
+#pragma unroll
+  for (int i = 0; i < kHeld; ++i) {
+    const int c = threadIdx.x + i * kJoinThreads;
+    key[i] = c < all ? best[c] : 0;
+  }
   if (threadIdx.x == 0) count = 0;
   for (int r = wave; r < b.beams; r += kWaves) {
     const int row = group * b.beams + r;
@@ -390,16 +527,19 @@ __global__ __launch_bounds__(kJoinThreads) void join_groups(ewsjf_beams b, const
       continue;
     }
     const Part* part = w.part + (int64_t)row * segments;
-    double top = -INFINITY;
-    for (int i = lane; i < segments; i += 64) top = fmax(top, part[i].base);
-    top = wave_max(top);
+    Part p{0., -INFINITY};
+    if (lane < segments) p = part[lane];
+    double top = p.base;
+    for (int i = lane + 64; i < segments; i += 64) top = fmax(top, part[i].base);
+    for (int d = 1; d < 64 && d < segments; d *= 2) top = fmax(top, __shfl_xor(top, d));
     double sum = 0.;
-    for (int i = lane; i < segments; i += 64) {
-      const Part p = part[i];
+    for (int i = lane;;) {
       if (p.base == top) sum += p.sum;
       else if (p.base > -INFINITY) sum += p.sum * exp(p.base - top);
+      if ((i += 64) >= segments) break;
+      p = part[i];
     }
-    sum = wave_sum(sum);
+    for (int d = 1; d < 64 && d < segments; d *= 2) sum += __shfl_xor(sum, d);
     if (lane == 0) {
       base[r] = top == INFINITY ? s - log(sum) : s - (top + log(sum));
       kind[r] = top == INFINITY ? 2 : top > -INFINITY ? 1 : 0;
@@ -407,10 +547,8 @@ __global__ __launch_bounds__(kJoinThreads) void join_groups(ewsjf_beams b, const
   }
   __syncthreads();
 
-  const int each = segments * b.picks, all = b.beams * each;
-  const uint64_t* best = w.best + (int64_t)group * all;
   // Candidate c of the group's; place 0: none.
-  auto entry_of = [&](int c) {
+  auto entry_of = [&](int c, uint64_t key) {
     const int r = c / each, k = kind[r];
     Entry e{0, 0};
     const uint64_t before = (uint64_t)((1 << kRowBits) - 1 - r) << (32 + kVocabBits);
@@ -418,7 +556,6 @@ __global__ __launch_bounds__(kJoinThreads) void join_groups(ewsjf_beams b, const
     if (k == 3) {
       if (c == r * each) e = Entry{order64(base[r]), before | 1ull << (31 + kVocabBits) | (last - b.end)};
     } else if (k != 0) {
-      const uint64_t key = best[c];
       const uint32_t o = (uint32_t)(key >> 32), v = ~(uint32_t)key;
       const float x = value32(o);
       if (key != 0 && (k == 1 || x == INFINITY))
@@ -427,24 +564,34 @@ __global__ __launch_bounds__(kJoinThreads) void join_groups(ewsjf_beams b, const
     return e;
   };
   auto none = [](const Entry& e) { return e.place == 0; };
+  // every candidate: f(entry)
+  auto each_entry = [&](auto f) {
+#pragma unroll
+    for (int i = 0; i < kHeld; ++i) {
+      const int c = threadIdx.x + i * kJoinThreads;
+      if (c < all) f(entry_of(c, key[i]));
+    }
+    for (int c = threadIdx.x + kHeld * kJoinThreads; c < all; c += kJoinThreads) f(entry_of(c, best[c]));
+  };
 
-  uint64_t high[2] = {0, 0};  // a thread's two highest scores
-  for (int c = threadIdx.x; c < all; c += kJoinThreads) {
-    const Entry e = entry_of(c);
-    if (e.score > high[0]) high[1] = high[0], high[0] = e.score;
-    else if (e.score > high[1]) high[1] = e.score;
-  }
-  uint64_t bar = wave_threshold<64>(high, b.picks);
+  // A value that at least `picks` of the wave's candidates reach, in a score's upper half: over the lanes' two highest.
+  uint32_t high[2] = {0, 0};
+  each_entry([&](const Entry& e) {
+    const uint32_t o = (uint32_t)(e.score >> 32);
+    if (o > high[0]) high[1] = high[0], high[0] = o;
+    else if (o > high[1]) high[1] = o;
+  });
+  uint32_t bar = wave_threshold<32>(high, b.picks);
   if (lane == 0) least[wave] = bar;
   __syncthreads();
+#pragma unroll
   for (int i = 0; i < kWaves; ++i) bar = least[i] > bar ? least[i] : bar;
-  for (int c = threadIdx.x; c < all; c += kJoinThreads) {
-    const Entry e = entry_of(c);
-    if (!none(e) && e.score >= bar) {
+  each_entry([&](const Entry& e) {
+    if (!none(e) && (uint32_t)(e.score >> 32) >= bar) {
       const int at = atomicAdd(&count, 1);
       if (at < kMostFound) found[at] = e;
     }
-  }
+  });
   __syncthreads();
   const int n = count;
   auto write = [&](int rank, const Entry& e) {
@@ -455,20 +602,24 @@ __global__ __launch_bounds__(kJoinThreads) void join_groups(ewsjf_beams b, const
     token[at] = there ? (1 << kVocabBits) - 1 - (int)(e.place & ((1u << kVocabBits) - 1)) : -1;
     score[at] = there ? (float)value64(e.score) : -INFINITY;
   };
-  if (n <= kJoinThreads / 4) {
-    const Entry mine = (int)threadIdx.x < n ? found[threadIdx.x] : Entry{0, 0};
-    int rank = 0;
-    for (int i = 0; i < n; ++i) rank += above(found[i], mine);
-    if ((int)threadIdx.x < n && rank < b.picks) write(rank, mine);
+  if (n <= kMostFound / 4) {  // each candidate ranked against the others
+    if ((int)threadIdx.x < n) {
+      const Entry mine = found[threadIdx.x];
+      int rank = 0;
+#pragma unroll 8
+      for (int i = 0; i < n; ++i) rank += above(found[i], mine);
+      if (rank < b.picks) write(rank, mine);
+    }
   } else if (n <= kMostFound) {
     sort_entries<kJoinThreads>(found, n, Entry{0, 0}, above);
     if ((int)threadIdx.x < b.picks) write(threadIdx.x, found[threadIdx.x]);
   } else {  // a plateau of equal scores: one pass over the candidates a pick
     Entry last{~0ull, ~0ull};
+#pragma unroll 1
     for (int k = 0; k < b.picks; ++k) {
       Entry mine{0, 0};
       for (int c = threadIdx.x; c < all; c += kJoinThreads) {
-        const Entry e = entry_of(c);
+        const Entry e = entry_of(c, best[c]);
         if (above(last, e) && above(e, mine)) mine = e;
       }
 #pragma unroll
@@ -501,12 +652,14 @@ void launch_segments(const ewsjf_beams& b, const void* logits, const float* scor
 
 }  // namespace
 
-size_t beam_ws_bytes(const ewsjf_beams& b) { return work_of(b, sizes_of(b), nullptr).bytes; }
+size_t beam_ws_bytes(const ewsjf_beams& b) { return work_of(b, sizes_of(b, -1), nullptr).bytes; }
 
 hipError_t launch_beam_select(const ewsjf_beams& b, const void* logits, const float* score_in, const int32_t* done,
                               int32_t* parent, int32_t* token, float* score, void* ws, hipStream_t stream) {
   if (b.groups == 0) return hipSuccess;
-  const Sizes s = sizes_of(b);
+  const int size = b.dtype == EWSJF_F32 ? 4 : 2;
+  const int skew = (b.row_stride * size) % 16 || reinterpret_cast<uintptr_t>(logits) % 16 ? -1 : 0;
+  const Sizes s = sizes_of(b, skew);
   const Work w = work_of(b, s, ws);
   if (b.dtype == EWSJF_F32) launch_segments<float>(b, logits, score_in, done, w, s, stream);
   else if (b.dtype == EWSJF_BF16) launch_segments<__bf16>(b, logits, score_in, done, w, s, stream);
