@@ -517,7 +517,8 @@ __device__ int key_place(int key, int chunk) {
 }
 template <int D>
 __device__ int value_place(int key, int byte) {
-  const int block = byte >> 6, in = byte & 63;
+  // within a block the 16-byte chunks change places by pairs: codes are written as two chunks a lane, one after the other
+  const int block = byte >> 6, in = (byte & 63) ^ ((D == 128 ? key & 1 : (key >> 1) & 1) << 4);
   return D == 128 ? key * 256 + ((block ^ (key & 3)) << 6) + in : key * 128 + ((block ^ ((key >> 1) & 1)) << 6) + in;
 }
 
@@ -814,12 +815,13 @@ __device__ uint4 load_uint4(Global<const char> p) {
 // Lanes that load a key's elements, 16 bytes each.
 __host__ __device__ constexpr int lanes_a_key(int D, bool codes) { return codes ? D / 16 : D / 8; }
 
-// A wave's loads of keys and values on their way to LDS; of codes also each
-// lane's key's scale bytes.
+// A wave's loads of keys and values on their way to LDS.  Of n keys' codes also
+// the scale bytes: lane l has key l mod n's, of the key or, where l / n is odd,
+// of the value.
 template <int NI, bool Codes>
 struct Loaded {
   uint4 k[NI], v[NI];
-  uint32_t ks[Codes ? NI : 1], vs[Codes ? NI : 1];
+  uint32_t scale;
 };
 
 // The key tiles of a unit, TK places of a list each: the sinks, up to a multiple
@@ -992,6 +994,7 @@ struct Tiles {
   __device__ void load(int t, int key0, Loaded<NI, Codes>& x) const {
     const int lane = threadIdx.x & 63, mask = (1 << shift) - 1;
     if (Sixteens) {
+      Global<const char> first = nullptr, second = nullptr;
 #pragma unroll
       for (int g = 0; g < NI / kLoads; ++g) {
         const At at = address(t, key0 + 16 * g);
@@ -999,12 +1002,15 @@ struct Tiles {
         for (int i = 0; i < kLoads; ++i) {
           x.k[g * kLoads + i] = load16(at.k, i);
           x.v[g * kLoads + i] = load16(at.v, i);
-          if constexpr (Codes) {
-            const Global<const char> s = at.s + i * KPI + lane / LPR;
-            x.ks[g * kLoads + i] = *(Global<const uint8_t>)s;
-            x.vs[g * kLoads + i] = *(Global<const uint8_t>)(s + to_values);
-          }
         }
+        if (g == 0) first = at.s;
+        else second = at.s;
+      }
+      if constexpr (Codes) {
+        constexpr int n = NI * KPI;
+        static_assert(n == 16 || n == 32, "keys of one or two pages");
+        const Global<const char> s = n == 32 && lane & 16 ? second : first;
+        x.scale = *(Global<const uint8_t>)(s + (lane & 15) + (lane & n ? to_values : 0));
       }
     } else {
 #pragma unroll
@@ -1014,11 +1020,12 @@ struct Tiles {
         const Global<const char> p = base + page + (key & mask) * token_bytes + lane % LPR * 16;
         x.k[i] = load_uint4(p);
         x.v[i] = load_uint4(p + to_values);
-        if constexpr (Codes) {
-          const Global<const char> s = scales + page + (key & mask);
-          x.ks[i] = *(Global<const uint8_t>)s;
-          x.vs[i] = *(Global<const uint8_t>)(s + to_values);
-        }
+      }
+      if constexpr (Codes) {
+        constexpr int n = NI * KPI;
+        const int place = t * TK + key0 + lane % n, key = key_at(place), at = entry_of(place);
+        const int64_t page = (held(at) ? at : 0) * (int64_t)((uint64_t)page_bytes_hi << 32 | page_bytes);
+        x.scale = *(Global<const uint8_t>)(scales + page + (key & mask) + (lane & n ? to_values : 0));
       }
     }
   }
@@ -1037,11 +1044,13 @@ __device__ void put_keys(char* keys, char* values, int key0, const Loaded<NI, Co
     // KPI keys on, a chunk's place in its row moves with the key
     const int step = i * KPI, move = D == 128 ? (step & 15) << 4 : ((step >> 1) & 7) << 4;
     if constexpr (Codes) {
-      const float ks = scale_of(x.ks[i]), vs = scale_of(x.vs[i]);
+      const int from = (step + lane / LPR) * 4;  // the lane that has the key's scale
+      const float ks = scale_of(__builtin_amdgcn_ds_bpermute(from, x.scale));
+      const float vs = scale_of(__builtin_amdgcn_ds_bpermute(from + NI * KPI * 4, x.scale));
       *reinterpret_cast<vec8<T>*>(keys + (kp ^ move) + step * D * 2) = values_of(make_uint2(x.k[i].x, x.k[i].y), ks, T());
       *reinterpret_cast<vec8<T>*>(keys + (kp ^ move ^ 16) + step * D * 2) = values_of(make_uint2(x.k[i].z, x.k[i].w), ks, T());
       *reinterpret_cast<vec8<T>*>(values + vp + step * D * 2) = values_of(make_uint2(x.v[i].x, x.v[i].y), vs, T());
-      *reinterpret_cast<vec8<T>*>(values + vp + 16 + step * D * 2) = values_of(make_uint2(x.v[i].z, x.v[i].w), vs, T());
+      *reinterpret_cast<vec8<T>*>(values + (vp ^ 16) + step * D * 2) = values_of(make_uint2(x.v[i].z, x.v[i].w), vs, T());
     } else {
       *reinterpret_cast<uint4*>(keys + (kp ^ move) + step * D * 2) = x.k[i];
       *reinterpret_cast<uint4*>(values + vp + step * D * 2) = x.v[i];
@@ -1056,6 +1065,10 @@ __device__ bool clear_keys(int key0, uint64_t there, Loaded<NI, Codes>& x) {
   constexpr int LPR = lanes_a_key(D, Codes), KPI = 64 / LPR;
   const int lane = threadIdx.x & 63;
   uint32_t bad = 0;
+  if constexpr (Codes) {
+    x.scale = there >> (key0 + lane % (NI * KPI)) & 1 ? x.scale : 127;
+    bad = lane & (NI * KPI) && x.scale > (__is_same(T, _Float16) ? 135 : 247);
+  }
 #pragma unroll
   for (int i = 0; i < NI; ++i) {
     const uint32_t keep = there >> (key0 + i * KPI + lane / LPR) & 1 ? ~0u : 0u;
@@ -1063,9 +1076,7 @@ __device__ bool clear_keys(int key0, uint64_t there, Loaded<NI, Codes>& x) {
     k.x &= keep, k.y &= keep, k.z &= keep, k.w &= keep;
     v.x &= keep, v.y &= keep, v.z &= keep, v.w &= keep;
     if constexpr (Codes) {
-      x.ks[i] = keep ? x.ks[i] : 127, x.vs[i] = keep ? x.vs[i] : 127;
       bad |= nan_codes(v.x) | nan_codes(v.y) | nan_codes(v.z) | nan_codes(v.w);
-      bad |= x.vs[i] > (__is_same(T, _Float16) ? 135 : 247);
     } else {
       bad |= not_finite(v.x, T()) | not_finite(v.y, T()) | not_finite(v.z, T()) | not_finite(v.w, T());
     }
@@ -1354,6 +1365,15 @@ __global__ __launch_bounds__(kWaves * 64, 2) void attend_wave(Args<T>, int phase
   wave_units<T, D, Sixteens, Split, Codes>(room, phase, blockIdx.x, gridDim.x);
 }
 
+// The same for two phases of units of up to 32 rows: the workgroups of the
+// sequences' own keys come in as those of the shared keys end.
+template <typename T, int D, bool Sixteens, bool Codes>
+__global__ __launch_bounds__(kWaves * 64, 2) void attend_waves(Args<T>, int blocks0) {
+  __shared__ __align__(16) char room[kWaves * kWaveRoom<D>];
+  const bool own = (int)blockIdx.x >= blocks0;
+  wave_units<T, D, Sixteens, false, Codes>(room, own, blockIdx.x - (own ? blocks0 : 0), own ? gridDim.x - blocks0 : blocks0);
+}
+
 // Both phases of a batch behind shared prefixes at once: on each CU one
 // workgroup has the shared keys, where the matrix unit is the limit, and one
 // streams sequences' own keys, where memory is.  46 us for 64 sequences of 40
@@ -1637,7 +1657,12 @@ hipError_t launch_typed(const ewsjf_cache& c, const ewsjf_batch& b, int32_t laye
     auto kernel = sixteens ? attend_both<T, D, true, Codes> : attend_both<T, D, false, Codes>;
     kernel<<<s.blocks[0] + s.blocks[1], kWaves * 64, 0, stream>>>(a);
   }
-  for (int p = s.groups ? 0 : 1; p < 2 && !s.both; ++p) {
+  const bool two_waves = s.groups && !s.both && s.waves[0] == 0 && s.waves[1] == 0;
+  if (two_waves) {
+    auto kernel = sixteens ? attend_waves<T, D, true, Codes> : attend_waves<T, D, false, Codes>;
+    kernel<<<s.blocks[0] + s.blocks[1], kWaves * 64, 0, stream>>>(a, s.blocks[0]);
+  }
+  for (int p = s.groups ? 0 : 1; p < 2 && !s.both && !two_waves; ++p) {
     auto kernel = s.waves[p] == 8 ? (sixteens ? attend_block<T, D, 8, true, Codes> : attend_block<T, D, 8, false, Codes>)
                   : s.waves[p] ? (sixteens ? attend_block<T, D, 4, true, Codes> : attend_block<T, D, 4, false, Codes>)
                   : s.whole && p ? (sixteens ? attend_wave<T, D, true, true, Codes> : attend_wave<T, D, false, true, Codes>)

@@ -28,6 +28,8 @@ constexpr int kMostGrid = 65536;  // workgroups that copy pages of one plane: a 
 // Requests whose rows it writes too, a wave each at once: 8 of them 10.2 us, in a
 // launch of their own 11.5; 64 of them 13.9 against 11.6.
 constexpr int kFewRequests = kSmallThreads / 64;
+constexpr int kFewBeams = 32;   // of a reordering that one workgroup plans
+constexpr int kCopiers = 2048;  // workgroups that copy a reordering's pages: eight a CU
 
 // Workspace: counts of the chunks, the requests' running needs, the pages
 // picked for them; for a compaction the two ends of each move and, per moved
@@ -109,8 +111,7 @@ __device__ int held(const ewsjf_cache& c, int slot) {
 }
 
 // Checks the requests and sums what they need, in 64 bits: requests of up to
-// 2^24 pages each pass 32 bits together.  slot == nullptr: w.fine holds the needs,
-// as plan_reorder left them.
+// 2^24 pages each pass 32 bits together.
 template <int N>
 __device__ void sum_needs(const ewsjf_cache& c, const CacheWs& w, int64_t* sums, const int32_t* parent,
                           const int32_t* slot, const int32_t* tokens, int n) {
@@ -118,9 +119,7 @@ __device__ void sum_needs(const ewsjf_cache& c, const CacheWs& w, int64_t* sums,
   for (int i0 = 0; i0 < n; i0 += N) {
     const int i = i0 + threadIdx.x;
     int need = 0, ok = 0;
-    if (slot == nullptr) {
-      if (i < n) need = ok = w.fine[i];
-    } else if (i < n) {
+    if (i < n) {
       const int s = slot[i];
       const int64_t t = tokens[i];
       if (s >= 0 && s < c.n_slots && t >= 0) {
@@ -322,24 +321,32 @@ enum Role : int32_t {
 };
 
 struct ReorderWs {
-  CacheWs cache;
+  int32_t* head;    // [1]: copies that are granted
   int32_t* role;    // [n]
   int32_t* length;  // [n]: before the call
+  int32_t* source;  // [n]: the page that a copy takes, -1 for none
+  int32_t* number;  // [n]: the copies of requests 0 .. i
+  int32_t* picked;  // [n]: the pages that copies go to
+  int32_t* copied;  // [n]: and the pages that they take
   int32_t* row;     // [n][width]: rows before the call, of slots that somebody takes over
   size_t bytes;
 };
 
 ReorderWs reorder_ws(const ewsjf_cache& c, int n, void* base) {
   ReorderWs w;
-  w.cache = cache_ws(c, base);
-  size_t at = w.cache.bytes;
+  size_t at = 0;
   auto take = [&](size_t ints) {
     int32_t* r = reinterpret_cast<int32_t*>(static_cast<char*>(base) + at);
     at += (ints * 4 + 255) & ~size_t(255);
     return r;
   };
+  w.head = take(1);
   w.role = take(n);
   w.length = take(n);
+  w.source = take(n);
+  w.number = take(n);
+  w.picked = take(n);
+  w.copied = take(n);
   w.row = take((size_t)n * c.width);
   w.bytes = at;
   return w;
@@ -347,13 +354,45 @@ ReorderWs reorder_ws(const ewsjf_cache& c, int n, void* base) {
 
 __device__ bool slot_there(const ewsjf_cache& c, int slot) { return slot >= 0 && slot < c.n_slots; }
 
-// A workgroup a request: its role and need; its row put aside if somebody takes
-// it over, else its pages given up.
+// Request i's role, and what its copy takes; heir: who takes over its parent's row if that is not its own.
+__device__ void find_role(const ewsjf_cache& c, const ReorderWs& w, const int32_t* slot, const int32_t* parent, int n,
+                          int i, int heir) {
+  const int64_t room = (int64_t)c.width * c.page_size;
+  const int s = slot[i], p = parent[i];
+  int role = kNone, source = -1, length = 0;
+  if (slot_there(c, s)) {
+    role = kEmpty;
+    length = (int)(held(c, s) < room ? held(c, s) : room);
+    if (p >= 0 && p < n && slot_there(c, slot[p])) {
+      role = p == i ? kStay : parent[p] != p && heir == i ? kMove : kCopy;
+      if (role == kCopy) {
+        const int64_t t = held(c, slot[p]) < room ? held(c, slot[p]) : room;
+        if (t % c.page_size) source = c.table[(int64_t)slot[p] * c.width + t / c.page_size];
+        if (!in_pool(c, source)) source = -1;
+      }
+    }
+  }
+  w.role[i] = role;
+  w.length[i] = length;
+  w.source[i] = source;
+}
+
+// Request i's row put aside if somebody takes it over, else its pages given up.
+__device__ void leave_row(const ewsjf_cache& c, const ReorderWs& w, int slot, int i, bool taken, int at, int step) {
+  if (!slot_there(c, slot)) return;
+  const int32_t* row = c.table + (int64_t)slot * c.width;
+  for (int j = at; j < c.width; j += step) {
+    const int page = row[j];
+    if (taken) w.row[(int64_t)i * c.width + j] = page;
+    else if (in_pool(c, page)) atomicSub(&c.refs[page], 1);
+  }
+}
+
+// A workgroup a request.
 __global__ __launch_bounds__(kThreads) void plan_reorder(ewsjf_cache c, ReorderWs w, const int32_t* slot,
                                                          const int32_t* parent, int n) {
   __shared__ int first_of_mine, first_of_parent;  // first request that takes over this slot, the parent's
-  const int i = blockIdx.x, s = slot[i], p = parent[i];
-  const bool there = slot_there(c, s), born = there && p >= 0 && p < n && slot_there(c, slot[p]);
+  const int i = blockIdx.x, p = parent[i];
   if (threadIdx.x == 0) first_of_mine = first_of_parent = n;
   __syncthreads();
   for (int j = threadIdx.x; j < n; j += kThreads) {
@@ -364,66 +403,145 @@ __global__ __launch_bounds__(kThreads) void plan_reorder(ewsjf_cache c, ReorderW
     }
   }
   __syncthreads();
-  const int64_t room = (int64_t)c.width * c.page_size;
-  if (threadIdx.x == 0) {
-    int role = kNone, need = 0;
-    if (there) role = kEmpty;
-    if (born) {
-      const int heir = parent[p] == p ? p : first_of_parent;
-      role = p == i ? kStay : heir == i ? kMove : kCopy;
-      if (role == kCopy) {
-        const int64_t t = held(c, slot[p]) < room ? held(c, slot[p]) : room;
-        if (t % c.page_size) need = in_pool(c, c.table[(int64_t)slot[p] * c.width + t / c.page_size]);
-      }
-    }
-    w.role[i] = role;
-    w.cache.fine[i] = need;
-    w.length[i] = there ? (int)(held(c, s) < room ? held(c, s) : room) : 0;
-  }
-  if (!there) return;
-  const int32_t* row = c.table + (int64_t)s * c.width;
-  for (int j = threadIdx.x; j < c.width; j += kThreads) {
-    const int page = row[j];
-    if (first_of_mine < n) w.row[(int64_t)i * c.width + j] = page;
-    else if (in_pool(c, page)) atomicSub(&c.refs[page], 1);
-  }
+  if (threadIdx.x == 0) find_role(c, w, slot, parent, n, i, first_of_parent);
+  leave_row(c, w, slot[i], i, first_of_mine < n, threadIdx.x, kThreads);
 }
 
-// Request blockIdx.x: plane 0's workgroup writes its row, counts, length and
-// grant; each plane's copies the partial page.  A page that is copied stays with
-// the row that was taken over, and a page that is written was free, so none is
-// both.
-__global__ __launch_bounds__(kThreads) void apply_reorder(ewsjf_cache c, ReorderWs w, const int32_t* slot,
-                                                          const int32_t* parent, int32_t* granted) {
-  const int i = blockIdx.x, plane = blockIdx.y, role = w.role[i];
-  const int p = parent[i], need = w.cache.fine[i], after = w.cache.cum[i];
-  const bool copied = role == kCopy && (need == 0 || after <= w.cache.head[0]);
-  const int t = role == kMove || role == kCopy ? w.length[p] : 0, full = t / c.page_size;
-  const int32_t* from = w.row + (int64_t)(role == kMove || role == kCopy ? p : 0) * c.width;
-  if (plane == 0) {
-    if (threadIdx.x == 0) granted[i] = role == kStay || role == kMove || copied;
-    if (role == kEmpty || role == kMove || role == kCopy) {
-      int32_t* row = c.table + (int64_t)slot[i] * c.width;
-      for (int j = threadIdx.x; j < c.width; j += kThreads) {
-        int page = -1;
-        if (role == kMove) {
-          page = from[j];
-        } else if (copied && j < full) {
-          page = from[j];
-          if (in_pool(c, page)) atomicAdd(&c.refs[page], 1);
-        } else if (copied && need && j == full) {
-          page = w.cache.picked[after - 1];
-        }
-        row[j] = page;
-      }
-      if (threadIdx.x == 0) c.length[slot[i]] = role == kMove || copied ? t : 0;
-    }
+// Numbers the copies and gives them the lowest free pages, a workgroup of 1024
+// threads: eight pages a thread at a time, until all have one.
+__device__ void pick_for_copies(const ewsjf_cache& c, const ReorderWs& w, int n) {
+  constexpr int kEach = 8, kLots = kEach * kSmallThreads / 64;
+  __shared__ int sums[kSmallThreads / 64];
+  __shared__ int lots[kLots + 1];  // free pages of 64 before each lot
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  int needs = 0;
+  for (int i0 = 0; i0 < n; i0 += kSmallThreads) {
+    const int i = i0 + threadIdx.x, source = i < n ? w.source[i] : -1, need = source >= 0;
+    int total;
+    const int before = needs + block_scan<kSmallThreads>(need, sums, total);
+    if (i < n) w.number[i] = before + need;
+    if (need) w.copied[before] = source;
+    needs += total;
   }
-  if (!copied || !need) return;
-  const uint4* a = reinterpret_cast<const uint4*>(block_of(c, plane, from[full]));
-  uint4* b = reinterpret_cast<uint4*>(block_of(c, plane, w.cache.picked[after - 1]));
-  const int vecs = pieces_of(c);
-  for (int j = threadIdx.x; j < vecs; j += kThreads) b[j] = a[j];
+  int found = 0;
+  for (int64_t p0 = 0; p0 < c.n_pages && found < needs; p0 += kEach * kSmallThreads) {
+    int refs[kEach];
+#pragma unroll
+    for (int k = 0; k < kEach; ++k) {
+      const int64_t p = p0 + k * kSmallThreads + threadIdx.x;
+      refs[k] = p < c.n_pages ? c.refs[p] : 1;
+    }
+    uint64_t free[kEach];
+    __syncthreads();
+#pragma unroll
+    for (int k = 0; k < kEach; ++k) {
+      free[k] = __ballot(refs[k] == 0);
+      if (lane == 0) lots[k * (kSmallThreads / 64) + wave] = __popcll(free[k]);
+    }
+    __syncthreads();
+    const int mine = threadIdx.x < kLots ? lots[threadIdx.x] : 0;
+    int total;
+    const int before = block_scan<kSmallThreads>(mine, sums, total);
+    if (threadIdx.x < kLots) lots[threadIdx.x] = before;
+    __syncthreads();
+#pragma unroll
+    for (int k = 0; k < kEach; ++k) {
+      const int rank = found + lots[k * (kSmallThreads / 64) + wave] + __popcll(free[k] & ((1ull << lane) - 1));
+      if (free[k] >> lane & 1 && rank < needs) {
+        const int64_t p = p0 + k * kSmallThreads + threadIdx.x;
+        w.picked[rank] = (int)p;
+        c.refs[p] = 1;
+      }
+    }
+    found += total;
+  }
+  if (threadIdx.x == 0) w.head[0] = found < needs ? found : needs;
+}
+
+__global__ __launch_bounds__(kSmallThreads) void pick_reorder(ewsjf_cache c, ReorderWs w, int n) {
+  pick_for_copies(c, w, n);
+}
+
+// plan_reorder and pick_reorder of few requests, a wave a request.
+__global__ __launch_bounds__(kSmallThreads) void begin_reorder(ewsjf_cache c, ReorderWs w, const int32_t* slot,
+                                                               const int32_t* parent, int n) {
+  const int lane = threadIdx.x & 63;
+  for (int i = threadIdx.x >> 6; i < n; i += kSmallThreads / 64) {
+    const int p = parent[i];
+    int of_mine = n, of_parent = n;
+    for (int j = lane; j < n; j += 64)
+      if (slot_there(c, slot[j])) {
+        if (parent[j] == i && j < of_mine) of_mine = j;
+        if (parent[j] == p && j < of_parent) of_parent = j;
+      }
+    for (int d = 32; d; d >>= 1) {
+      of_mine = min(of_mine, __shfl_xor(of_mine, d));
+      of_parent = min(of_parent, __shfl_xor(of_parent, d));
+    }
+    if (lane == 0) find_role(c, w, slot, parent, n, i, of_parent);
+    leave_row(c, w, slot[i], i, of_mine < n, lane, 64);
+  }
+  __threadfence();  // counts are read where the atomics left them
+  __syncthreads();
+  pick_for_copies(c, w, n);
+}
+
+// The first `copiers` workgroups copy partial pages, the others write a request's
+// row, counts, length and grant each.  A page that is copied
+// stays with the row that was taken over, and a page that is written was free,
+// so none is both.
+__global__ __launch_bounds__(kThreads) void apply_reorder(ewsjf_cache c, ReorderWs w, const int32_t* slot,
+                                                          const int32_t* parent, int copiers, int32_t* granted) {
+  const int copies = w.head[0];
+  if ((int)blockIdx.x < copiers) {
+    // a task: a part of a block, at most four pieces a thread
+    const uint32_t vecs = pieces_of(c), parts = (vecs + 4 * kThreads - 1) / (4 * kThreads), each = 2 * c.layers * parts;
+    const uint32_t length = (vecs + parts - 1) / parts;
+    uint32_t j = blockIdx.x / each, task = blockIdx.x % each;
+    const uint32_t copies_on = copiers / each, tasks_on = copiers % each;
+    for (; j < (uint32_t)copies; j += copies_on, task += tasks_on) {
+      if (task >= each) {
+        task -= each;
+        if (++j >= (uint32_t)copies) break;
+      }
+      const uint32_t plane = task / parts, from = (task - plane * parts) * length;
+      const uint32_t end = from + length < vecs ? from + length : vecs;
+      const uint4* a = reinterpret_cast<const uint4*>(block_of(c, plane, w.copied[j]));
+      uint4* b = reinterpret_cast<uint4*>(block_of(c, plane, w.picked[j]));
+      uint4 x[4];
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const uint32_t v = from + threadIdx.x + k * kThreads;
+        if (v < end) x[k] = a[v];
+      }
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const uint32_t v = from + threadIdx.x + k * kThreads;
+        if (v < end) b[v] = x[k];
+      }
+    }
+    return;
+  }
+  const int i = blockIdx.x - copiers, role = w.role[i], p = parent[i], number = w.number[i], source = w.source[i];
+  const bool copied = role == kCopy && (source < 0 || number <= copies), there = role == kStay || role == kMove || copied;
+  if (threadIdx.x == 0) granted[i] = there;
+  if (role == kNone || role == kStay) return;
+  const int t = there ? w.length[p] : 0, full = t / c.page_size;
+  const int32_t* from = w.row + (int64_t)(there ? p : 0) * c.width;
+  int32_t* row = c.table + (int64_t)slot[i] * c.width;
+  for (int j = threadIdx.x; j < c.width; j += kThreads) {
+    int page = -1;
+    if (role == kMove) {
+      page = from[j];
+    } else if (copied && j < full) {
+      page = from[j];
+      if (in_pool(c, page)) atomicAdd(&c.refs[page], 1);
+    } else if (copied && source >= 0 && j == full) {
+      page = w.picked[number - 1];
+    }
+    row[j] = page;
+  }
+  if (threadIdx.x == 0) c.length[slot[i]] = t;
 }
 
 // A workgroup a slot.  Counts are integers, so the order of the atomics does
@@ -593,15 +711,16 @@ hipError_t launch_cache_reorder(const ewsjf_cache& c, const int32_t* slot, const
                                 int32_t* granted, void* ws, hipStream_t stream) {
   if (n == 0) return hipSuccess;
   const ReorderWs w = reorder_ws(c, n, ws);
-  const int chunks = (c.n_pages + kChunk - 1) / kChunk;
-  plan_reorder<<<n, kThreads, 0, stream>>>(c, w, slot, parent, n);
-  if (c.n_pages <= kSmallPool) {
-    grow_small<<<1, kSmallThreads, 0, stream>>>(c, w.cache, nullptr, nullptr, nullptr, n, nullptr, false);
+  if (n <= kFewBeams) {
+    begin_reorder<<<1, kSmallThreads, 0, stream>>>(c, w, slot, parent, n);
   } else {
-    count_pages<<<chunks + 1, kThreads, 0, stream>>>(c, w.cache, chunks, false, nullptr, nullptr, nullptr, n);
-    pick_pages<<<chunks, kThreads, 0, stream>>>(c, w.cache, chunks, n);
+    plan_reorder<<<n, kThreads, 0, stream>>>(c, w, slot, parent, n);
+    pick_reorder<<<1, kSmallThreads, 0, stream>>>(c, w, n);
   }
-  apply_reorder<<<dim3(n, 2 * c.layers), kThreads, 0, stream>>>(c, w, slot, parent, granted);
+  const int64_t parts = (cache_block(c) * cache_element_bytes(c) / 16 + 4 * kThreads - 1) / (4 * kThreads);
+  const int64_t tasks = (int64_t)(n - 1) * 2 * c.layers * parts;  // at most: some row stays
+  const int copiers = (int)(tasks < kCopiers ? tasks : kCopiers);
+  apply_reorder<<<copiers + n, kThreads, 0, stream>>>(c, w, slot, parent, copiers, granted);
   return hipGetLastError();
 }
 

@@ -79,7 +79,7 @@ def test_read():
 def test_reorder():
     lib, c = L.lib(), cache()
     need = lib.ewsjf_cache_reorder_workspace_bytes(C.addressof(c), 4)
-    assert need >= ws_bytes(c) + 4 * 5 * 4
+    assert need >= 4 * 5 * 4
     assert lib.ewsjf_cache_reorder_workspace_bytes(C.addressof(c), 4097) == 0
     assert lib.ewsjf_cache_reorder_workspace_bytes(C.addressof(c), -1) == 0
     assert lib.ewsjf_cache_reorder_workspace_bytes(None, 1) == 0
