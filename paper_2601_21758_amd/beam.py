@@ -10,6 +10,8 @@ Nothing here synchronizes the host.
 """
 from __future__ import annotations
 
+import functools
+
 import torch
 
 from . import _lib as L
@@ -17,6 +19,14 @@ from .ewsjf import Workspace, _need, _stream
 from .kv import _addr, _new, _scratch
 
 _DTYPES = {torch.bfloat16: L.BF16, torch.float16: L.F16, torch.float32: L.F32}
+_TYPES = (("parent", torch.int32), ("token", torch.int32), ("score", torch.float32))
+
+
+@functools.lru_cache(maxsize=64)
+def _sizes(*sizes):
+    """The struct of a selection of these sizes, and its workspace's bytes."""
+    b = L.Beams(*sizes)
+    return b, int(L.lib().ewsjf_beam_workspace_bytes(_addr(b)))
 
 
 def beam_select(logits: torch.Tensor, score: torch.Tensor, beams: int, picks: int | None = None, *,
@@ -43,22 +53,23 @@ def beam_select(logits: torch.Tensor, score: torch.Tensor, beams: int, picks: in
         raise ValueError("score has one entry per row, on the logits' device")
     if done is not None and (_need(done, torch.int32, "done").numel() != rows or done.device != logits.device):
         raise ValueError("done has one entry per row, on the logits' device")
-    b = L.Beams(groups, beams, picks, vocab, _DTYPES[logits.dtype], int(end),
-                logits.stride(0) if rows > 1 else vocab)
-    nbytes = int(L.lib().ewsjf_beam_workspace_bytes(_addr(b)))
+    b, nbytes = _sizes(groups, beams, picks, vocab, _DTYPES[logits.dtype], int(end),
+                       logits.stride(0) if rows > 1 else vocab)
     if nbytes == 0:
         raise ValueError("a selection of these sizes or strides is not supported (see ewsjf_beam_select)")
-    types = (torch.int32, torch.int32, torch.float32)
     if out is None:
-        out = tuple(_new(stream, (groups, picks), dtype=t, device=logits.device) for t in types)
-    for t, kind, name in zip(out, types, ("parent", "token", "score")):
-        if _need(t, kind, name).shape != (groups, picks) or t.device != logits.device:
-            raise ValueError(f"{name} is [groups][picks] on the logits' device")
+        parent, token, bits = _new(stream, (3, groups, picks), dtype=torch.int32, device=logits.device).unbind(0)
+        out = parent, token, bits.view(torch.float32)
+    else:
+        for t, (name, kind) in zip(out, _TYPES):
+            if _need(t, kind, name).shape != (groups, picks) or t.device != logits.device:
+                raise ValueError(f"{name} is [groups][picks] on the logits' device")
+    parent, token, best = out
     raw = _stream(stream)
-    if (torch.cuda.current_device() if stream is None else stream.device.index) != logits.device.index:
+    if (torch._C._cuda_getDevice() if stream is None else stream.device.index) != logits.device.index:
         raise ValueError("the logits are on another device than the call's stream")
     buf = _scratch(ws, nbytes, logits.device, raw, stream)
     L.check(L.lib().ewsjf_beam_select(_addr(b), logits.data_ptr(), score.data_ptr(),
-                                      None if done is None else done.data_ptr(), *[t.data_ptr() for t in out],
-                                      buf.data_ptr(), buf.numel(), raw), "ewsjf_beam_select")
+                                      None if done is None else done.data_ptr(), parent.data_ptr(), token.data_ptr(),
+                                      best.data_ptr(), buf.data_ptr(), buf.numel(), raw), "ewsjf_beam_select")
     return out

@@ -105,7 +105,7 @@ struct Phase {
   int32_t entries;
   int32_t workers;
   int32_t columns;  // of unit_at
-  int32_t pad;
+  int32_t before;   // workers of the other phase before this one's
 };
 
 struct Plan {
@@ -122,6 +122,8 @@ struct Shape {
   bool groups;  // a shared prefix is a phase of its own
   bool whole;   // a worker a unit: nothing is cut, nothing joined
   bool both;    // both phases in one kernel
+  bool dealt;   // one kernel's waves are dealt out to both phases by their tiles
+  int split;    // whole: waves of a workgroup
   int G;
   int waves[2];  // of a workgroup that shares a unit's keys; 0: the wave kernel
   int rows[2], keys[2], workers[2], blocks[2];
@@ -170,6 +172,11 @@ Shape shape_of(const ewsjf_cache& c, const ewsjf_batch& b) {
   const int64_t units = s.entries[1] * c.kv_heads;
   s.whole = !s.groups && s.waves[1] == 0 && b.max_q == 1 && keys <= kWholeKeys;
   if (s.whole) s.workers[1] = s.blocks[1] = (int)((units + 7) / 8 * 8);
+  // Few units of codes: eight waves share one's tiles.
+  s.split = cache_in_codes(c) && units <= kCUs ? 2 * kWaves : kWaves;
+  // Two phases of up to 32 rows a unit, of codes: 256 beams of 32 requests behind prompts of 2000 tokens, 24 query and 8
+  // key heads of 128, take 43 us, with all waves for the one phase, then all for the other, 51.
+  s.dealt = cache_in_codes(c) && s.groups && s.waves[0] == 0 && s.waves[1] == 0;
   // many row tiles of long runs, and nothing to join them with
   s.columns = s.waves[1] && !s.groups ? s.workers[1] / 8 : 0;
   return s;
@@ -305,7 +312,7 @@ __device__ void climb(const int32_t* from, int n, int most, int* to, int64_t* su
 struct PlanArgs {
   const int32_t *slot, *q_start, *group_start, *shared;
   int rows[2], keys[2], workers[2], G, columns;
-  bool whole;
+  bool whole, dealt;
 };
 
 // One workgroup, latency-bound: prefix sums over the row tiles and a search a
@@ -362,6 +369,25 @@ __global__ __launch_bounds__(kPlanThreads) void make_plan(ewsjf_cache c, ewsjf_b
     common[g] = members[g] < 2 ? 0 : common[g] & ~15;  // nobody to share with; tiles begin at multiples of 16
   __syncthreads();
 
+  int workers[2] = {a.workers[0], a.workers[1]};
+  if (a.dealt) {  // by the phases' tiles, a unit's beginning counted as one
+    int64_t cost = 0, all[2];
+    for (int g = threadIdx.x; g < groups; g += kPlanThreads)
+      cost += ((q_at(group_at(g + 1)) - q_at(group_at(g))) * a.G + a.rows[0] - 1) / a.rows[0] * (common[g] / a.keys[0]);
+    scan(cost, sums, all[0]);
+    cost = 0;
+    for (int i = threadIdx.x; i < n; i += kPlanThreads) {
+      const int g = group_of(i);
+      const int64_t keys = tokens(i) - (g < 0 || !has_slot(i) ? 0 : common[g]);
+      cost += (queries(i) * a.G + a.rows[1] - 1) / a.rows[1] * (1 + (keys > 0 ? keys : 0) / a.keys[1] + 1);
+    }
+    scan(cost, sums, all[1]);
+    const int64_t total = all[0] + all[1];
+    int64_t first = total > 0 ? workers[0] * all[0] / total : 0;
+    if (all[0] > 0) first = first < 1 ? 1 : first > workers[0] - 1 ? workers[0] - 1 : first;
+    workers[1] -= (int)first;
+    workers[0] = first > 0 ? (int)first : 1;
+  }
   for (int ph = 0; ph < 2; ++ph) {
     const int R = a.rows[ph], TK = a.keys[ph], owners = ph ? n : groups;
     Entry* entry = plan.entry[ph];
@@ -432,13 +458,13 @@ __global__ __launch_bounds__(kPlanThreads) void make_plan(ewsjf_cache c, ewsjf_b
     const int64_t all = line * c.kv_heads;
     // Even shares, but where a unit has many workers, its s tiles a share against T / s parts to join: one row tile of
     // 4096 keys a head took 59 us in shares of a tile (128 parts), 40 in shares of four.  0: a worker a unit.
-    int64_t share = all > 0 ? (all + a.workers[ph] - 1) / a.workers[ph] : 1;
+    int64_t share = all > 0 ? (all + workers[ph] - 1) / workers[ph] : 1;
     while (8 * share * share * E < line) ++share;
     if (ph && a.whole) share = 0;
     const int active = share ? (int)((all + share - 1) / share) : E * c.kv_heads;
     if (threadIdx.x == 0) {
       plan.cum[ph][E] = line;
-      plan.phase[ph] = Phase{line, share, E, active, ph ? a.columns : 0, 0};
+      plan.phase[ph] = Phase{line, share, E, active, ph ? a.columns : 0, ph && a.dealt ? a.workers[1] - workers[1] : 0};
     }
     __syncthreads();  // entries and sums are read back by other threads
     const int64_t units = (int64_t)E * c.kv_heads;
@@ -1226,20 +1252,22 @@ __global__ __launch_bounds__(NW * 64, 2) void attend_block(Args<T>, int phase) {
 // units lose to their beginnings (page lookup, first tile): 512 sequences' own
 // 128 tokens, 0.28 GB, take 80 us, 3.4 TB/s.
 //
-// Split: a workgroup takes one unit, a quarter of its tiles a wave, and joins
-// the four parts itself.
+// Split: a workgroup of so many waves takes one unit, an even part of its tiles a
+// wave, and joins the parts itself.
 // ---------------------------------------------------------------------------
 template <int D>
 constexpr int kWaveRoom = 2 * kRowKeys * D * 2;  // LDS of a wave: a tile's keys and values
 
-template <typename T, int D, bool Sixteens, bool Split, bool Codes>
-__device__ __forceinline__ void wave_units(char* room, int phase, int block, int blocks) {
+// The place in line of a kernel's workgroup: an XCD's follow one another.
+__device__ int in_line(int block, int blocks) { return block % 8 * (blocks / 8) + block / 8; }
+
+template <typename T, int D, bool Sixteens, int Split, bool Codes>
+__device__ __forceinline__ void wave_units(char* room, int phase, int id) {
   using Keys = Tiles<T, D, kRowKeys, Sixteens, Codes>;
   constexpr int TK = kRowKeys, NI = TK / Keys::KPI;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   char* const keys = room + wave * kWaveRoom<D>;
   char* const values = keys + TK * D * 2;
-  const int at_line = block % 8 * (blocks / 8) + block / 8, id = Split ? at_line : at_line * kWaves + wave;
   int place, e, head, t0;
   int64_t left;
   {
@@ -1251,7 +1279,7 @@ __device__ __forceinline__ void wave_units(char* room, int phase, int block, int
     const Start st = constant(a.plan.start[phase] + id);
     place = st.place, e = st.entry, head = st.head, t0 = st.tile;
     if (Split) {
-      const int tiles = constant(a.plan.entry[phase] + e).tiles, part = (tiles + kWaves - 1) / kWaves;
+      const int tiles = constant(a.plan.entry[phase] + e).tiles, part = (tiles + Split - 1) / Split;
       t0 = wave * part;
       left = tiles - t0 < part ? tiles - t0 : part;
       if (left < 0) left = 0;
@@ -1316,7 +1344,7 @@ __device__ __forceinline__ void wave_units(char* room, int phase, int block, int
     if (odd) flags[id] = 1;
     return;
   }
-  __shared__ float2 ml[kWaves][kRowTile];
+  __shared__ float2 ml[Split ? Split : 1][kRowTile];
   const Args<T>& a = arguments<T>();
   const Entry x = constant(a.plan.entry[phase] + e);
   const int row = lane & 31, h = lane >> 5;
@@ -1334,12 +1362,12 @@ __device__ __forceinline__ void wave_units(char* room, int phase, int block, int
   __syncthreads();
   constexpr int W = D / 16;
   const int i16 = threadIdx.x & 15;
-  for (int r = threadIdx.x / 16; r < x.rows; r += kWaves * 4) {
+  for (int r = threadIdx.x / 16; r < x.rows; r += Split * 4) {
     float top = kFloor, all = 0.f, o[W] = {};
 #pragma unroll
-    for (int i = 0; i < kWaves; ++i) top = fmaxf(top, ml[i][r].x);
+    for (int i = 0; i < Split; ++i) top = fmaxf(top, ml[i][r].x);
 #pragma unroll
-    for (int i = 0; i < kWaves; ++i) {
+    for (int i = 0; i < Split; ++i) {
       const float w = __builtin_amdgcn_exp2f(ml[i][r].x - top);
       all = fmaf(ml[i][r].y, w, all);
       const float* from = reinterpret_cast<const float*>(room + i * kWaveRoom<D>) + r * D + i16 * W;
@@ -1359,19 +1387,31 @@ __device__ __forceinline__ void wave_units(char* room, int phase, int block, int
   }
 }
 
-template <typename T, int D, bool Sixteens, bool Split, bool Codes>
-__global__ __launch_bounds__(kWaves * 64, 2) void attend_wave(Args<T>, int phase) {
-  __shared__ __align__(16) char room[kWaves * kWaveRoom<D>];
-  wave_units<T, D, Sixteens, Split, Codes>(room, phase, blockIdx.x, gridDim.x);
+template <typename T, int D, bool Sixteens, int Split, bool Codes>
+__global__ __launch_bounds__((Split ? Split : kWaves) * 64, 2) void attend_wave(Args<T>, int phase) {
+  __shared__ __align__(16) char room[(Split ? Split : kWaves) * kWaveRoom<D>];
+  const int place = in_line(blockIdx.x, gridDim.x), wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  wave_units<T, D, Sixteens, Split, Codes>(room, phase, Split ? place : place * kWaves + wave);
 }
 
-// The same for two phases of units of up to 32 rows: the workgroups of the
-// sequences' own keys come in as those of the shared keys end.
+// The same for two phases of units of up to 32 rows.  Of codes, the waves are dealt out to both
+// by the plan; else the workgroups of the sequences' own keys come in as those of the shared keys end.
 template <typename T, int D, bool Sixteens, bool Codes>
 __global__ __launch_bounds__(kWaves * 64, 2) void attend_waves(Args<T>, int blocks0) {
   __shared__ __align__(16) char room[kWaves * kWaveRoom<D>];
-  const bool own = (int)blockIdx.x >= blocks0;
-  wave_units<T, D, Sixteens, false, Codes>(room, own, blockIdx.x - (own ? blocks0 : 0), own ? gridDim.x - blocks0 : blocks0);
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  int phase, id;
+  if (Codes) {
+    id = in_line(blockIdx.x, gridDim.x) * kWaves + wave;
+    const int before = constant(arguments<T>().plan.phase + 1).before;
+    phase = id >= before;
+    if (phase) id -= before;
+  } else {
+    phase = (int)blockIdx.x >= blocks0;
+    const int first = phase ? blocks0 : 0;
+    id = in_line(blockIdx.x - first, phase ? gridDim.x - blocks0 : blocks0) * kWaves + wave;
+  }
+  wave_units<T, D, Sixteens, 0, Codes>(room, phase, id);
 }
 
 // Both phases of a batch behind shared prefixes at once: on each CU one
@@ -1387,7 +1427,7 @@ __global__ __launch_bounds__(kWaves * 64, 2) void attend_both(Args<T>) {
   // on their CUs.
   const int block = blockIdx.x / 16 * 8 + blockIdx.x % 8;
   if ((blockIdx.x / 8 + blockIdx.x / 256) % 2 == 0) block_units<T, D, 4, Sixteens, Codes>(room, 0, block, gridDim.x / 2);
-  else wave_units<T, D, Sixteens, false, Codes>(room, 1, block, gridDim.x / 2);
+  else wave_units<T, D, Sixteens, 0, Codes>(room, 1, in_line(block, gridDim.x / 2) * kWaves + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6));
 }
 
 // ---------------------------------------------------------------------------
@@ -1630,6 +1670,13 @@ __global__ __launch_bounds__(256) void join_cuts(Args<T> a, int rows1, int flags
   }
 }
 
+template <typename T, int D, bool Sixteens, bool Codes>
+void (*split_kernel(int waves))(Args<T>, int) {
+  if constexpr (Codes)
+    if (waves == 2 * kWaves) return attend_wave<T, D, Sixteens, 2 * kWaves, true>;
+  return attend_wave<T, D, Sixteens, kWaves, Codes>;
+}
+
 template <typename T, int D, bool Codes>
 hipError_t launch_typed(const ewsjf_cache& c, const ewsjf_batch& b, int32_t layer, const void* q, int64_t q_token,
                         int64_t q_head, float scale, const void* plan, void* out, float* lse, void* ws,
@@ -1660,14 +1707,15 @@ hipError_t launch_typed(const ewsjf_cache& c, const ewsjf_batch& b, int32_t laye
   const bool two_waves = s.groups && !s.both && s.waves[0] == 0 && s.waves[1] == 0;
   if (two_waves) {
     auto kernel = sixteens ? attend_waves<T, D, true, Codes> : attend_waves<T, D, false, Codes>;
-    kernel<<<s.blocks[0] + s.blocks[1], kWaves * 64, 0, stream>>>(a, s.blocks[0]);
+    kernel<<<s.dealt ? s.blocks[0] : s.blocks[0] + s.blocks[1], kWaves * 64, 0, stream>>>(a, s.blocks[0]);
   }
   for (int p = s.groups ? 0 : 1; p < 2 && !s.both && !two_waves; ++p) {
     auto kernel = s.waves[p] == 8 ? (sixteens ? attend_block<T, D, 8, true, Codes> : attend_block<T, D, 8, false, Codes>)
                   : s.waves[p] ? (sixteens ? attend_block<T, D, 4, true, Codes> : attend_block<T, D, 4, false, Codes>)
-                  : s.whole && p ? (sixteens ? attend_wave<T, D, true, true, Codes> : attend_wave<T, D, false, true, Codes>)
-                                 : (sixteens ? attend_wave<T, D, true, false, Codes> : attend_wave<T, D, false, false, Codes>);
-    kernel<<<s.blocks[p], 64 * (s.waves[p] ? s.waves[p] : kWaves), 0, stream>>>(a, p);
+                  : s.whole && p ? (sixteens ? split_kernel<T, D, true, Codes>(s.split) : split_kernel<T, D, false, Codes>(s.split))
+                                 : (sixteens ? attend_wave<T, D, true, 0, Codes> : attend_wave<T, D, false, 0, Codes>);
+    const int waves = s.waves[p] ? s.waves[p] : s.whole && p ? s.split : kWaves;
+    kernel<<<s.blocks[p], 64 * waves, 0, stream>>>(a, p);
   }
   if (s.whole) return hipGetLastError();
   const int64_t most = (int64_t)b.max_q * s.G < s.rows[1] ? (int64_t)b.max_q * s.G : s.rows[1];
@@ -1693,7 +1741,7 @@ hipError_t launch_attention_plan(const ewsjf_cache& c, const ewsjf_batch& b, con
                                  void* plan, hipStream_t stream) {
   const Shape s = shape_of(c, b);
   PlanArgs a{slot, q_start, group_start, shared, {s.rows[0], s.rows[1]}, {s.keys[0], s.keys[1]},
-             {s.workers[0], s.workers[1]}, s.G, s.columns, s.whole};
+             {s.workers[0], s.workers[1]}, s.G, s.columns, s.whole, s.dealt};
   ewsjf_batch batch = b;
   if (!s.groups) batch.n_groups = 0;
   make_plan<<<1, kPlanThreads, 0, stream>>>(c, batch, a, plan_of(s, plan));

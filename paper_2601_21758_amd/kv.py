@@ -122,6 +122,7 @@ class PagedCache:
                          layers, n_pages, page_size, kv_heads, head_dim, code, *table.shape)
         self._c = _addr(self.c)
         self._ws_bytes = int(L.lib().ewsjf_cache_workspace_bytes(self._c))
+        self._reorder_bytes = {}  # by the number of slots
         if self._ws_bytes == 0:
             raise ValueError("a cache of these sizes or strides is not supported (see ewsjf_cache)")
 
@@ -324,7 +325,9 @@ class PagedCache:
         tokens, else 0 (ewsjf_cache_reorder)."""
         n = slot.numel()
         granted = _new(stream, n, dtype=torch.int32, device=self.device) if granted is None else granted
-        nbytes = int(L.lib().ewsjf_cache_reorder_workspace_bytes(self._c, n))
+        nbytes = self._reorder_bytes.get(n)
+        if nbytes is None:
+            nbytes = self._reorder_bytes[n] = int(L.lib().ewsjf_cache_reorder_workspace_bytes(self._c, n))
         raw = self._on(stream)
         buf = _scratch(ws, nbytes, self.device, raw, stream)
         L.check(L.lib().ewsjf_cache_reorder(self._c, self._ids(slot, "slot"), self._ids(parent, "parent", n), n,
