@@ -373,7 +373,8 @@ __global__ __launch_bounds__(kPlanThreads) void make_plan(ewsjf_cache c, ewsjf_b
   if (a.dealt) {  // by the phases' tiles, a unit's beginning counted as one
     int64_t cost = 0, all[2];
     for (int g = threadIdx.x; g < groups; g += kPlanThreads)
-      cost += ((q_at(group_at(g + 1)) - q_at(group_at(g))) * a.G + a.rows[0] - 1) / a.rows[0] * (common[g] / a.keys[0]);
+      cost += ((q_at(group_at(g + 1)) - q_at(group_at(g))) * a.G + a.rows[0] - 1) / a.rows[0] *
+              ((common[g] + a.keys[0] - 1) / a.keys[0]);
     scan(cost, sums, all[0]);
     cost = 0;
     for (int i = threadIdx.x; i < n; i += kPlanThreads) {

@@ -82,6 +82,38 @@ def test_nan_codes_some_rows_see(K, D, dtype, window, n, q):
     assert ((out - ref[0]).float().abs()[clean] <= 4 * unit * ref[0].float().abs()[clean] + 4 * unit * 4).all()
 
 
+def widen(b):
+    """A table so wide that prefixes shared by few rows count."""
+    keys = (256 << 20) // (2 * len(b.slot) * b.Hk * b.D) + 1
+    b.table = np.pad(b.table, ((0, 0), (0, -(-keys // b.page))), constant_values=-1)
+    return b
+
+
+@pytest.mark.parametrize("dtype,D,group,page,order", [("bf16", 128, 3, 16, "head"), ("f16", 64, 1, 32, "token"),
+                                                      ("bf16", 64, 4, 8, "head"), ("f16", 128, 2, 1, "token")])
+@pytest.mark.parametrize("shared", [[(8, 2000), (8, 777), (8, 31)], [(24, 640)], [(1, 500)] * 24, [(3, 16)] * 8,
+                                    [(0, 90), (24, 1100)], [(8, 0), (8, 1700), (8, 5)], [(20, 300), (1, 2), (1, 1), (2, 3)]])
+def test_beams_behind_prompts(K, dtype, D, group, page, order, shared):
+    """Few rows a group: the waves are dealt out to shared and own keys, also where one of them is nearly nothing."""
+    own = [1 + (11 * i) % 45 for i in range(24)]
+    prompt = [t for m, t in shared for _ in range(m)]
+    b = widen(Codes(41, dtype, D, 2, group, page, [p + x for p, x in zip(prompt, own)], [1] * 24, shared=shared, order=order))
+    b.check(K)
+
+
+@pytest.mark.parametrize("dtype,D", [("bf16", 128), ("f16", 64)])
+def test_few_queries_behind_prompts(K, dtype, D):
+    """Up to three query tokens a sequence, sequences without any and without a slot, more rows in a group than a tile."""
+    q = [1, 3, 0, 2, 1, 1, 3, 2, 1, 0, 1, 1, 2, 1, 3, 1]
+    own = [max(1, x) + (7 * i) % 40 for i, x in enumerate(q)]
+    prompt = [700] * 3 + [33] * 2 + [1200] * 11
+    b = widen(Codes(42, dtype, D, 2, 2, 16, [p + x for p, x in zip(prompt, own)], q, shared=[(3, 700), (2, 33), (11, 1200)]))
+    b.check(K)
+    b.slot[7] = -1
+    b.slot[12] = b.n_slots
+    b.check(K)
+
+
 @pytest.mark.parametrize("q", [1, 70])
 def test_offsets_past_32_bits(K, q):
     """Pages, layers and scales beyond 2^32 bytes."""
