@@ -39,13 +39,16 @@
 namespace ewsjf {
 namespace {
 
-constexpr int kRowTile = 32;     // rows of a unit of the wave kernel
+constexpr int kRowTile = 32;     // rows of a unit of the wave kernel,
+constexpr int kNarrow = 16;      // of the narrow one
 constexpr int kRowKeys = 32;     // its key tile
 // Key tile of the workgroup kernel with four or eight waves of 32 rows: two
 // tiles fill the LDS that a workgroup can have with all waves resident.
 __host__ __device__ constexpr int block_keys(int waves) { return waves == 8 ? 128 : 64; }
 constexpr int kWaves = 4;        // waves of a workgroup of the wave kernel
 constexpr int kCUs = 256;
+// Waves of the narrow kernel on a SIMD.
+__host__ __device__ constexpr int narrow_waves(int D) { return D == 128 ? 2 : 3; }
 constexpr int64_t kMostJoins = 1 << 24;  // waves of a grid's row: a launch has below 2^32 threads in one
 constexpr int kWholeKeys = 2048;   // of a unit that one workgroup takes whole
 // Position of a shared phase's first query, past every shared key; its other tokens' do not pass 32 bits.
@@ -124,6 +127,7 @@ struct Shape {
   bool both;    // both phases in one kernel
   bool dealt;   // one kernel's waves are dealt out to both phases by their tiles
   int split;    // whole: waves of a workgroup
+  bool narrow;  // units of up to 16 rows, of codes: the narrow kernel
   int G;
   int waves[2];  // of a workgroup that shares a unit's keys; 0: the wave kernel
   int rows[2], keys[2], workers[2], blocks[2];
@@ -152,12 +156,13 @@ Shape shape_of(const ewsjf_cache& c, const ewsjf_batch& b) {
   // (135 GFLOP) took 263 us, in one kernel 270.
   const double flops = 4. * b.total_q * b.q_heads * c.head_dim * most_keys;
   s.both = most[0] > kRowTile && most[1] <= kRowTile && flops < 100e9;
+  s.narrow = cache_in_codes(c) && most[0] <= kNarrow && most[1] <= kNarrow;
   for (int p = 0; p < 2; ++p) {
     s.waves[p] = most[p] <= kRowTile ? 0 : most[p] <= 128 || s.both ? 4 : 8;
-    s.rows[p] = s.waves[p] ? 32 * s.waves[p] : kRowTile;
+    s.rows[p] = s.waves[p] ? 32 * s.waves[p] : s.narrow ? kNarrow : kRowTile;
     s.keys[p] = s.waves[p] ? block_keys(s.waves[p]) : kRowKeys;
     // as many as fit the chip at once: eight waves of 256 registers a CU
-    s.blocks[p] = s.waves[p] == 8 || s.both ? kCUs : 2 * kCUs;
+    s.blocks[p] = s.waves[p] == 8 || s.both ? kCUs : s.narrow ? narrow_waves(c.head_dim) * kCUs : 2 * kCUs;
     s.workers[p] = s.waves[p] ? s.blocks[p] : s.blocks[p] * kWaves;
     s.entries[p] = b.total_q * s.G / s.rows[p] + (p ? b.n_seqs : b.n_groups);
   }
@@ -851,6 +856,14 @@ struct Loaded {
   uint32_t scale;
 };
 
+// A narrow wave's loads of 32 keys' codes: of the keys lane l has key l mod 16 of
+// each 16, 16 codes of every 64 from 16 (l / 16) on; values and scales as above.
+template <int D>
+struct NarrowLoaded {
+  uint4 k[2 * (D / 64)], v[2 * (D / 64)];
+  uint32_t scale;
+};
+
 // The key tiles of a unit, TK places of a list each: the sinks, up to a multiple
 // of 16, then the main run from a multiple of 16 on.  So tiles are full but for
 // the last (with sinks in tiles of their own, 24 prompts over windows of 1024 took
@@ -1013,6 +1026,47 @@ struct Tiles {
 
   __device__ uint4 load16(Global<const char> p, int i) const {  // load i of 16 keys
     return load_uint4(apart(p + i * stride) + step);
+  }
+
+  // Loads a tile of 32 keys for the narrow kernel.
+  __device__ void load(int t, NarrowLoaded<D>& x) const {
+    static_assert(TK == 32 && Codes, "the narrow kernel's tiles");
+    const int lane = threadIdx.x & 63, mask = (1 << shift) - 1;
+    const int place = t * TK + (lane & 31);
+    if (Sixteens) {
+      const uint32_t step_k = (lane & 15) * token_bytes + (lane >> 4) * 16;
+      Global<const char> first = nullptr, second = nullptr;
+#pragma unroll
+      for (int g = 0; g < 2; ++g) {
+        const At at = address(t, 16 * g);
+#pragma unroll
+        for (int j = 0; j < D / 64; ++j) x.k[g * (D / 64) + j] = load_uint4(apart(at.k + 64 * j) + step_k);
+#pragma unroll
+        for (int i = 0; i < kLoads; ++i) x.v[g * kLoads + i] = load16(at.v, i);
+        if (g == 0) first = at.s;
+        else second = at.s;
+      }
+      const Global<const char> s = lane & 16 ? second : first;
+      x.scale = *(Global<const uint8_t>)(s + (lane & 15) + (lane & 32 ? to_values : 0));
+    } else {
+      auto page_of = [&](int place) {
+        const int at = entry_of(place);
+        return (held(at) ? at : 0) * (int64_t)((uint64_t)page_bytes_hi << 32 | page_bytes);
+      };
+#pragma unroll
+      for (int g = 0; g < 2; ++g) {
+        const int mine = t * TK + 16 * g + (lane & 15);
+        const Global<const char> p = base + page_of(mine) + (key_at(mine) & mask) * token_bytes + (lane >> 4) * 16;
+#pragma unroll
+        for (int j = 0; j < D / 64; ++j) x.k[g * (D / 64) + j] = load_uint4(p + 64 * j);
+      }
+#pragma unroll
+      for (int i = 0; i < 2 * kLoads; ++i) {
+        const int mine = t * TK + i * KPI + lane / LPR;
+        x.v[i] = load_uint4(base + page_of(mine) + (key_at(mine) & mask) * token_bytes + lane % LPR * 16 + to_values);
+      }
+      x.scale = *(Global<const uint8_t>)(scales + page_of(place) + (key_at(place) & mask) + (lane & 32 ? to_values : 0));
+    }
   }
 
   // Loads keys [key0, key0 + NI KPI) of the tile, key0 a multiple of 16: 16
@@ -1243,6 +1297,36 @@ __global__ __launch_bounds__(NW * 64, 2) void attend_block(Args<T>, int phase) {
   block_units<T, D, NW, Sixteens, Codes>(room, phase, blockIdx.x, gridDim.x);
 }
 
+// Joins the rows that a workgroup's waves have in LDS, `each` bytes a wave.
+template <typename T, int D, int Split, typename Ml>
+__device__ void join_split(const Args<T>& a, const Entry& x, int head, const char* room, int each, const Ml& ml) {
+  constexpr int W = D / 16;
+  const int i16 = threadIdx.x & 15;
+  for (int r = threadIdx.x / 16; r < x.rows; r += Split * 4) {
+    float top = kFloor, all = 0.f, o[W] = {};
+#pragma unroll
+    for (int i = 0; i < Split; ++i) top = fmaxf(top, ml[i][r].x);
+#pragma unroll
+    for (int i = 0; i < Split; ++i) {
+      const float w = __builtin_amdgcn_exp2f(ml[i][r].x - top);
+      all = fmaf(ml[i][r].y, w, all);
+      const float* from = reinterpret_cast<const float*>(room + i * each) + r * D + i16 * W;
+#pragma unroll
+      for (int d = 0; d < W; ++d) o[d] = fmaf(from[d], w, o[d]);
+    }
+    const int at = x.row0 + r, token = at / a.G;
+    const int64_t dense = (int64_t)(x.q0 + token) * (a.kv_heads * a.G) + head * a.G + at - token * a.G;
+    const float inv = all == 0.f ? 0.f : 1.f / all;
+    vec8<T> v = {};
+#pragma unroll
+    for (int d = 0; d < W; ++d) v[d] = (T)(all == 0.f ? 0.f : o[d] * inv);
+    const Global<T> to = global(a.out) + dense * D + i16 * W;
+    if (W == 8) *(Global<vec8<T>>)to = v;
+    else *(Global<uint64_t>)to = *reinterpret_cast<const uint64_t*>(&v);
+    if (i16 == 0) global(a.lse)[dense] = all == 0.f ? -INFINITY : kLn2 * (top + __builtin_amdgcn_logf(all));
+  }
+}
+
 // ---------------------------------------------------------------------------
 // The wave kernel: up to 32 rows (a few query tokens), the keys streamed by
 // waves that share nothing: each loads the next tile of 32 keys into registers
@@ -1361,31 +1445,7 @@ __device__ __forceinline__ void wave_units(char* room, int phase, int id) {
     if (h == 0) ml[wave][row] = make_float2(rows.top, sum);
   }
   __syncthreads();
-  constexpr int W = D / 16;
-  const int i16 = threadIdx.x & 15;
-  for (int r = threadIdx.x / 16; r < x.rows; r += Split * 4) {
-    float top = kFloor, all = 0.f, o[W] = {};
-#pragma unroll
-    for (int i = 0; i < Split; ++i) top = fmaxf(top, ml[i][r].x);
-#pragma unroll
-    for (int i = 0; i < Split; ++i) {
-      const float w = __builtin_amdgcn_exp2f(ml[i][r].x - top);
-      all = fmaf(ml[i][r].y, w, all);
-      const float* from = reinterpret_cast<const float*>(room + i * kWaveRoom<D>) + r * D + i16 * W;
-#pragma unroll
-      for (int d = 0; d < W; ++d) o[d] = fmaf(from[d], w, o[d]);
-    }
-    const int at = x.row0 + r, token = at / a.G;
-    const int64_t dense = (int64_t)(x.q0 + token) * (a.kv_heads * a.G) + head * a.G + at - token * a.G;
-    const float inv = all == 0.f ? 0.f : 1.f / all;
-    vec8<T> v = {};
-#pragma unroll
-    for (int d = 0; d < W; ++d) v[d] = (T)(all == 0.f ? 0.f : o[d] * inv);
-    const Global<T> to = global(a.out) + dense * D + i16 * W;
-    if (W == 8) *(Global<vec8<T>>)to = v;
-    else *(Global<uint64_t>)to = *reinterpret_cast<const uint64_t*>(&v);
-    if (i16 == 0) global(a.lse)[dense] = all == 0.f ? -INFINITY : kLn2 * (top + __builtin_amdgcn_logf(all));
-  }
+  join_split<T, D, Split>(a, x, head, room, kWaveRoom<D>, ml);
 }
 
 template <typename T, int D, bool Sixteens, int Split, bool Codes>
@@ -1413,6 +1473,273 @@ __global__ __launch_bounds__(kWaves * 64, 2) void attend_waves(Args<T>, int bloc
     id = in_line(blockIdx.x - first, phase ? gridDim.x - blocks0 : blocks0) * kWaves + wave;
   }
   wave_units<T, D, Sixteens, 0, Codes>(room, phase, id);
+}
+
+// ---------------------------------------------------------------------------
+// The narrow kernel: up to 16 rows of codes.  The wave kernel with 16x16x32
+// matrix instructions, which leave half the registers and half the products of
+// 32 rows, and with keys that go to the first product from the registers that
+// they were loaded into: a lane has 16 codes of a key, two of its operands, and
+// takes the queries' dims in the same order.  Only values go through LDS.  So
+// three waves fit a SIMD with heads of 128, four with heads of 64, and more
+// loads are on their way.
+// ---------------------------------------------------------------------------
+typedef __attribute__((ext_vector_type(4))) float float4v;
+__device__ float4v mfma16(vec8<__bf16> a, vec8<__bf16> b, float4v c) {
+  return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
+}
+__device__ float4v mfma16(vec8<_Float16> a, vec8<_Float16> b, float4v c) {
+  return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0);
+}
+
+// Joined over the four lanes of a row, 16 apart.
+__device__ float quad_max(float v) {
+  v = pair_max(v);
+  return fmaxf(v, __shfl_xor(v, 16));
+}
+__device__ float quad_sum(float v) {
+  v = pair_sum(v);
+  return v + __shfl_xor(v, 16);
+}
+
+// The softmax state and output of 16 rows: lane l has row l mod 16, of scores the
+// keys 4 (l / 16) .. + 3 of each 16, of the output the dims 4 (l / 16) .. + 3 of each
+// 16.
+template <typename T, int D>
+struct NarrowRows {
+  vec8<T> q[D / 32];
+  float4v o[D / 16];
+  float top, sum;  // as Rows'
+  static constexpr float kLift = Rows<T, D>::kLift, kMostSum = Rows<T, D>::kMostSum;
+
+  __device__ void clear() {
+    top = kFloor;
+    sum = 0.f;
+#pragma unroll
+    for (int i = 0; i < D / 16; ++i) o[i] = float4v{};
+  }
+
+  __device__ float weights(const float4v (&s)[2], float scale2, vec8<T>& w) const {
+    float add[2] = {0.f, 0.f};
+#pragma unroll
+    for (int r = 0; r < 8; ++r) {
+      const float p = __builtin_amdgcn_exp2f(fmaf(s[r / 4][r % 4], scale2, -top));
+      add[r % 2] += p;
+      w[r] = (T)p;
+    }
+    return add[0] + add[1];
+  }
+  __device__ vec8<T> weigh(const float4v (&s)[2], float scale2) {
+    vec8<T> w;
+    float add = weights(s, scale2, w);
+    if (__any(!(add <= kMostSum))) {
+      float most = s[0][0];
+#pragma unroll
+      for (int r = 1; r < 8; ++r) most = fmaxf(most, s[r / 4][r % 4]);
+      const float now = fmaxf(top, quad_max(most) * scale2 - kLift), shrink = __builtin_amdgcn_exp2f(top - now);
+      top = now;
+      sum *= shrink;
+#pragma unroll
+      for (int i = 0; i < D / 16; ++i) o[i] *= shrink;
+      add = weights(s, scale2, w);
+    }
+    sum += add;
+    return w;
+  }
+
+  // V^T of 16 dims and the 32 keys in the order of the weights; first: value_place of the lane's row and column.
+  static __device__ vec8<T> read_values(const char* values, int first, int i) {
+    union {
+      short4v part[2];
+      vec8<T> all;
+    } v;
+    typedef __attribute__((address_space(3))) short4v* lds4;
+    const char* at = values + (first ^ (i << 5));
+    v.part[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4)at);
+    v.part[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4)(at + 16 * D * 2));
+    return v.all;
+  }
+};
+
+template <int D>
+constexpr int kNarrowRoom = 32 * D * 2;  // LDS of a wave: a tile's values
+
+template <typename T, int D, bool Sixteens, int Split>
+__device__ __forceinline__ void narrow_units(char* room, int phase, int id) {
+  using Keys = Tiles<T, D, 32, Sixteens, true>;
+  constexpr int LPR = Keys::LPR, KPI = Keys::KPI;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  char* const values = room + wave * kNarrowRoom<D>;
+  int place, e, head, t0;
+  int64_t left;
+  {
+    const Args<T>& a = arguments<T>();
+    const Phase ph = constant(a.plan.phase + phase);
+    if (id >= ph.workers) return;
+    const int64_t all = ph.total * a.kv_heads, beg = id * ph.share;
+    left = (beg + ph.share < all ? beg + ph.share : all) - beg;
+    const Start st = constant(a.plan.start[phase] + id);
+    place = st.place, e = st.entry, head = st.head, t0 = st.tile;
+    if (Split) {
+      const int tiles = constant(a.plan.entry[phase] + e).tiles, part = (tiles + Split - 1) / Split;
+      t0 = wave * part;
+      left = tiles - t0 < part ? tiles - t0 : part;
+      if (left < 0) left = 0;
+    }
+  }
+  const float scale2 = arguments<T>().scale2;
+  bool leading = true, odd = false;
+  NarrowRows<T, D> rows;
+  const int row = lane & 15, quad = lane >> 4;
+
+  if (Split) rows.clear();
+  while (left > 0) {
+    const Args<T>& a = arguments<T>();
+    const Entry x = constant(a.plan.entry[phase] + e);
+    const int n = (int)(x.tiles - t0 < left ? x.tiles - t0 : left);
+    Keys tiles(a, x, head);
+    tiles.begin(t0);
+    NarrowLoaded<D> next;
+    {
+      const bool there = row < x.rows;
+      const int at = x.row0 + (there ? row : 0), token = at / a.G;
+      const Global<const T> q =
+          global(a.q) + (x.q0 + token) * a.q_token + (head * a.G + at - token * a.G) * a.q_head + 16 * quad;
+#pragma unroll
+      for (int k = 0; k < D / 32; ++k) {
+        rows.q[k] = *(Global<const vec8<T>>)(q + k / 2 * 64 + k % 2 * 8);
+        if (!there) rows.q[k] = vec8<T>{};
+      }
+    }
+    rows.clear();
+    const int p = x.pos0 + (x.row0 + (row < x.rows ? row : x.rows - 1)) / a.G;
+    tiles.load(t0, next);
+    for (int i = 0; i < n; ++i) {
+      const int t = t0 + i;
+      const bool clean = tiles.clean(t);
+      uint32_t held = ~0u;
+      if (!clean) {
+        held = (uint32_t)tiles.there(t);
+        uint32_t bad = 0;
+        next.scale = held >> (lane & 31) & 1 ? next.scale : 127;
+        bad = lane & 32 && next.scale > (__is_same(T, _Float16) ? 135 : 247);
+#pragma unroll
+        for (int j = 0; j < 2 * (D / 64); ++j) {
+          const uint32_t keep = held >> (j / (D / 64) * 16 + row) & 1 ? ~0u : 0u;
+          next.k[j].x &= keep, next.k[j].y &= keep, next.k[j].z &= keep, next.k[j].w &= keep;
+          const uint32_t kept = held >> (j * KPI + lane / LPR) & 1 ? ~0u : 0u;
+          uint4& v = next.v[j];
+          v.x &= kept, v.y &= kept, v.z &= kept, v.w &= kept;
+          bad |= nan_codes(v.x) | nan_codes(v.y) | nan_codes(v.z) | nan_codes(v.w);
+        }
+        // with one position, what is there is seen by all rows
+        odd |= bad != 0 && tiles.p_first != tiles.p_last && !tiles.even(t);
+      }
+      // values to LDS, keys to the first product
+      const int vp = fresh(value_place<D>(lane / LPR, lane % LPR * 32));
+#pragma unroll
+      for (int j = 0; j < 2 * (D / 64); ++j) {
+        const float vs = scale_of(__builtin_amdgcn_ds_bpermute((32 + j * KPI + lane / LPR) * 4, next.scale));
+        const uint4 v = next.v[j];
+        *reinterpret_cast<vec8<T>*>(values + vp + j * KPI * D * 2) = values_of(make_uint2(v.x, v.y), vs, T());
+        *reinterpret_cast<vec8<T>*>(values + (vp ^ 16) + j * KPI * D * 2) = values_of(make_uint2(v.z, v.w), vs, T());
+      }
+      float4v s[2];
+#pragma unroll
+      for (int g = 0; g < 2; ++g) {
+        const float ks = scale_of(__builtin_amdgcn_ds_bpermute((16 * g + row) * 4, next.scale));
+        s[g] = float4v{};
+#pragma unroll
+        for (int j = 0; j < D / 64; ++j) {
+          const uint4 k = next.k[g * (D / 64) + j];
+          s[g] = mfma16(values_of(make_uint2(k.x, k.y), ks, T()), rows.q[2 * j], s[g]);
+          s[g] = mfma16(values_of(make_uint2(k.z, k.w), ks, T()), rows.q[2 * j + 1], s[g]);
+        }
+      }
+      __builtin_amdgcn_sched_barrier(0);  // before the registers are loaded into again
+      tiles.advance(t + 1);
+      if (i + 1 < n) tiles.load(t + 1, next);
+      __builtin_amdgcn_wave_barrier();
+      if (!clean) {
+        const uint32_t seen = (uint32_t)tiles.seen(held, t, 0, p) >> (4 * quad);
+#pragma unroll
+        for (int r = 0; r < 8; ++r) {
+          const uint32_t keep = __builtin_amdgcn_sbfe(seen, r / 4 * 16 + r % 4, 1);
+          s[r / 4][r % 4] = __uint_as_float((__float_as_uint(s[r / 4][r % 4]) & keep) | (0xff800000u & ~keep));
+        }
+      }
+      const vec8<T> w = rows.weigh(s, scale2);
+      const int rp = fresh(value_place<D>(4 * quad + (row >> 2), 8 * (row & 3)));
+#pragma unroll
+      for (int j = 0; j < D / 16; ++j) rows.o[j] = mfma16(rows.read_values(values, rp, j), w, rows.o[j]);
+      __builtin_amdgcn_wave_barrier();
+    }
+    if (Split) break;
+    const Args<T>& z = arguments<T>();
+    const Entry y = constant(z.plan.entry[phase] + e);
+    const bool whole = t0 == 0 && n == y.tiles;
+    const float sum = quad_sum(rows.sum);
+    if (row < y.rows) {
+      const int at = y.row0 + row, token = at / z.G;
+      const int64_t dense = (int64_t)(y.q0 + token) * (z.kv_heads * z.G) + head * z.G + at - token * z.G;
+      if (whole && !z.join) {
+        const float inv = sum > 0.f || sum != sum ? 1.f / sum : 0.f;
+        const Global<T> to = global(z.out) + dense * D + 4 * quad;
+#pragma unroll
+        for (int j = 0; j < D / 16; ++j) {
+          T v[4];
+#pragma unroll
+          for (int d = 0; d < 4; ++d) v[d] = (T)(sum == 0.f ? 0.f : rows.o[j][d] * inv);
+          *(Global<uint64_t>)(to + 16 * j) = *reinterpret_cast<const uint64_t*>(v);
+        }
+        if (quad == 0) global(z.lse)[dense] = sum == 0.f ? -INFINITY : kLn2 * (rows.top + __builtin_amdgcn_logf(sum));
+      } else {
+        const Parts& w = z.work.part[phase];
+        const int64_t slot = (int64_t)id * 2 + (leading ? 0 : 1), at_row = whole ? dense : slot * kNarrow + row;
+        const Global<float> to = global(whole ? w.whole_o : w.o) + at_row * D + 4 * quad;
+#pragma unroll
+        for (int j = 0; j < D / 16; ++j) *(Global<float4v>)(to + 16 * j) = rows.o[j];
+        typedef __attribute__((ext_vector_type(2))) float f2;
+        if (quad == 0) *((Global<f2>)(whole ? w.whole_ml : w.ml) + at_row) = f2{rows.top, sum};
+      }
+    }
+    leading = false;
+    left -= n;
+    t0 = 0;
+    const Phase ph = constant(z.plan.phase + phase);
+    next_unit(z.plan, ph, ph.entries * z.kv_heads, place, e, head);
+  }
+  if (!Split) {
+    const Global<int32_t> flags = global(arguments<T>().work.odd[phase]);
+    if (lane == 0) flags[id] = 0;
+    if (odd) flags[id] = 1;
+    return;
+  }
+  __shared__ float2 ml[Split ? Split : 1][kNarrow];
+  const Args<T>& a = arguments<T>();
+  const Entry x = constant(a.plan.entry[phase] + e);
+  const float sum = quad_sum(rows.sum);
+  float* mine = reinterpret_cast<float*>(values) + row * D + 4 * quad;  // the tiles have been read
+#pragma unroll
+  for (int j = 0; j < D / 16; ++j) *reinterpret_cast<float4v*>(mine + 16 * j) = rows.o[j];
+  if (quad == 0) ml[wave][row] = make_float2(rows.top, sum);
+  __syncthreads();
+  join_split<T, D, Split>(a, x, head, room, kNarrowRoom<D>, ml);
+}
+
+// phase < 0: both, the waves dealt out to them by the plan.
+template <typename T, int D, bool Sixteens, int Split>
+__global__ __launch_bounds__((Split ? Split : kWaves) * 64, Split ? 2 : narrow_waves(D)) void attend_narrow(Args<T>, int phase) {
+  __shared__ __align__(16) char room[(Split ? Split : kWaves) * kNarrowRoom<D>];
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  int id = in_line(blockIdx.x, gridDim.x);
+  if (!Split) id = id * kWaves + wave;
+  if (phase < 0) {
+    const int before = constant(arguments<T>().plan.phase + 1).before;
+    phase = id >= before;
+    if (phase) id -= before;
+  }
+  narrow_units<T, D, Sixteens, Split>(room, phase, id);
 }
 
 // Both phases of a batch behind shared prefixes at once: on each CU one
@@ -1678,6 +2005,15 @@ void (*split_kernel(int waves))(Args<T>, int) {
   return attend_wave<T, D, Sixteens, kWaves, Codes>;
 }
 
+template <typename T, int D, bool Sixteens, bool Codes>
+void (*narrow_kernel(int split))(Args<T>, int) {
+  if constexpr (Codes)
+    return split == 0        ? attend_narrow<T, D, Sixteens, 0>
+           : split == kWaves ? attend_narrow<T, D, Sixteens, kWaves>
+                             : attend_narrow<T, D, Sixteens, 2 * kWaves>;
+  return nullptr;
+}
+
 template <typename T, int D, bool Codes>
 hipError_t launch_typed(const ewsjf_cache& c, const ewsjf_batch& b, int32_t layer, const void* q, int64_t q_token,
                         int64_t q_head, float scale, const void* plan, void* out, float* lse, void* ws,
@@ -1706,11 +2042,15 @@ hipError_t launch_typed(const ewsjf_cache& c, const ewsjf_batch& b, int32_t laye
     kernel<<<s.blocks[0] + s.blocks[1], kWaves * 64, 0, stream>>>(a);
   }
   const bool two_waves = s.groups && !s.both && s.waves[0] == 0 && s.waves[1] == 0;
-  if (two_waves) {
+  if (s.narrow) {
+    auto kernel = !s.whole ? (sixteens ? narrow_kernel<T, D, true, Codes>(0) : narrow_kernel<T, D, false, Codes>(0))
+                           : (sixteens ? narrow_kernel<T, D, true, Codes>(s.split) : narrow_kernel<T, D, false, Codes>(s.split));
+    kernel<<<s.blocks[1], 64 * (s.whole ? s.split : kWaves), 0, stream>>>(a, s.groups ? -1 : 1);
+  } else if (two_waves) {
     auto kernel = sixteens ? attend_waves<T, D, true, Codes> : attend_waves<T, D, false, Codes>;
     kernel<<<s.dealt ? s.blocks[0] : s.blocks[0] + s.blocks[1], kWaves * 64, 0, stream>>>(a, s.blocks[0]);
   }
-  for (int p = s.groups ? 0 : 1; p < 2 && !s.both && !two_waves; ++p) {
+  for (int p = s.groups ? 0 : 1; p < 2 && !s.both && !two_waves && !s.narrow; ++p) {
     auto kernel = s.waves[p] == 8 ? (sixteens ? attend_block<T, D, 8, true, Codes> : attend_block<T, D, 8, false, Codes>)
                   : s.waves[p] ? (sixteens ? attend_block<T, D, 4, true, Codes> : attend_block<T, D, 4, false, Codes>)
                   : s.whole && p ? (sixteens ? split_kernel<T, D, true, Codes>(s.split) : split_kernel<T, D, false, Codes>(s.split))
