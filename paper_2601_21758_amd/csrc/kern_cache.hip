@@ -512,7 +512,7 @@ __global__ __launch_bounds__(kThreads) void apply_reorder(ewsjf_cache c, Reorder
 #pragma unroll
       for (int k = 0; k < 4; ++k) {
         const uint32_t v = from + threadIdx.x + k * kThreads;
-        if (v < end) x[k] = a[v];
+        x[k] = a[v < end ? v : from];  // no branch, or the pieces take turns
       }
 #pragma unroll
       for (int k = 0; k < 4; ++k) {
