@@ -627,19 +627,21 @@ ewsjf_status ewsjf_cache_reorder(const ewsjf_cache* c, const int32_t* slot, cons
  * Row r = g * beams + b is beam b of group g.  Its candidates are the tokens
  * v of [0, vocab) with
  *   score = score_in[r] + x[r][v] - ln sum_u exp x[r][u],
- * in binary64 from the logits as they are.  A row with done[r] != 0 has one, `end`, with
+ * in binary64; the logarithm is right to 2^-29, and 0 plus the logit where a row
+ * has one token alone.  A row with done[r] != 0 has one candidate, `end`, with
  * score_in[r] itself (its logits are not read).  A logit of NaN counts as -inf;
- * entries of +inf share their row's probability; a score of NaN counts as -inf, and a score of
- * -inf is no candidate.
+ * entries of +inf share their row's probability; a score of NaN counts as -inf,
+ * and a score of -inf is no candidate.
  *
  * For each group the `picks` best of its rows' candidates: higher scores first,
  * of equal scores the lower row, in a row the higher logit, of equal logits the lower
  * token.  parent (the row r), token and score (rounded to binary32): device
  * [groups][picks], -1, -1 and -inf where there are no more candidates.
  *
- * logits: device, of `dtype`, rows row_stride elements apart, aligned to its elements.
- * score_in: device float [groups * beams].  done: device int32 [groups * beams]
- * or NULL, with 0 <= end < vocab. */
+ * logits: device, of `dtype`, rows row_stride elements apart, aligned to its
+ * elements.  score_in: device float [groups * beams].  done: device int32
+ * [groups * beams] or NULL, with 0 <= end < vocab.  Results do not overlap what
+ * is read, but score may be score_in where picks is beams. */
 enum { EWSJF_F32 = 2 }; /* logits: EWSJF_BF16, EWSJF_F16 or this */
 enum {
   EWSJF_MAX_BEAMS = 32,     /* beams of a group */

@@ -22,6 +22,10 @@
 // 4h, .., 4h + 3, 8 + 4h, .. in which the first product leaves them (h = lane /
 // 32).  V^T is read from LDS with the transposing read.
 //
+// Keys and values of 8 bits are codes and a power of two a key and head: they
+// become the 16-bit values that they stand for, exactly, on their way from
+// registers to LDS, and the rest is as it is with 16 bits.
+//
 // With `width` the row's query heads, a unit of R rows and K keys reads R D +
 // 2 K D values once and computes 4 R K D operations: R operations a byte of
 // keys.  Up to 32 rows (decoding) memory is the limit, from about 200 rows on
@@ -47,7 +51,8 @@ constexpr int kRowKeys = 32;     // its key tile
 __host__ __device__ constexpr int block_keys(int waves) { return waves == 8 ? 128 : 64; }
 constexpr int kWaves = 4;        // waves of a workgroup of the wave kernel
 constexpr int kCUs = 256;
-// Waves of the narrow kernel on a SIMD.
+// Waves of the narrow kernel on a SIMD: with one more the attention of 256 tokens (below) takes 113 us, so 105, with
+// heads of 64 and twice as many 107 either way.
 __host__ __device__ constexpr int narrow_waves(int D) { return D == 128 ? 2 : 3; }
 constexpr int64_t kMostJoins = 1 << 24;  // waves of a grid's row: a launch has below 2^32 threads in one
 constexpr int kWholeKeys = 2048;   // of a unit that one workgroup takes whole
@@ -177,10 +182,12 @@ Shape shape_of(const ewsjf_cache& c, const ewsjf_batch& b) {
   const int64_t units = s.entries[1] * c.kv_heads;
   s.whole = !s.groups && s.waves[1] == 0 && b.max_q == 1 && keys <= kWholeKeys;
   if (s.whole) s.workers[1] = s.blocks[1] = (int)((units + 7) / 8 * 8);
-  // Few units of codes: eight waves share one's tiles.
-  s.split = cache_in_codes(c) && units <= kCUs ? 2 * kWaves : kWaves;
+  // Few units of codes: eight waves share one's tiles.  8 key heads of 128, eight waves against four: 32 units of 1000 keys
+  // 15.0 us against 18.2 (cut and joined 19.7), 128 of them 16.7 against 20.7, 256 28.0 against 27.4; 256 of 200 keys 14.6
+  // against 11.5, 2048 63 against 37.
+  s.split = cache_in_codes(c) && units <= kCUs / 2 ? 2 * kWaves : kWaves;
   // Two phases of up to 32 rows a unit, of codes: 256 beams of 32 requests behind prompts of 2000 tokens, 24 query and 8
-  // key heads of 128, take 43 us, with all waves for the one phase, then all for the other, 51.
+  // key heads of 128, take 45 us, with all waves for the one phase, then all for the other, 51, as two kernels 56.
   s.dealt = cache_in_codes(c) && s.groups && s.waves[0] == 0 && s.waves[1] == 0;
   // many row tiles of long runs, and nothing to join them with
   s.columns = s.waves[1] && !s.groups ? s.workers[1] / 8 : 0;
@@ -1480,9 +1487,12 @@ __global__ __launch_bounds__(kWaves * 64, 2) void attend_waves(Args<T>, int bloc
 // matrix instructions, which leave half the registers and half the products of
 // 32 rows, and with keys that go to the first product from the registers that
 // they were loaded into: a lane has 16 codes of a key, two of its operands, and
-// takes the queries' dims in the same order.  Only values go through LDS.  So
-// three waves fit a SIMD with heads of 128, four with heads of 64, and more
-// loads are on their way.
+// takes the queries' dims in the same order.  Only values go through LDS.
+// Bound by memory: 256 single tokens over windows of 4096, 32 query and 8 key
+// heads of 128, 0.49 GB, take 105 us, 4.7 TB/s (the wave kernel 111); 512 of them 209
+// us and 1024 395, 5.2 TB/s each more and 12 us for the beginning and the end.
+// With heads of 64 107 us, the wave kernel 117.  Three tokens of one key head and 1000
+// keys: 10.0 us against 11.5.
 // ---------------------------------------------------------------------------
 typedef __attribute__((ext_vector_type(4))) float float4v;
 __device__ float4v mfma16(vec8<__bf16> a, vec8<__bf16> b, float4v c) {
