@@ -503,7 +503,8 @@ __device__ bool above(const Entry& a, const Entry& b) {
 }
 
 // A workgroup a group.  Bound by latency: 8.5 us for 64 groups of 1,024 candidates, 7 us for one, half of them the loads, the
-// logarithms and the threshold that come one after the other.
+// logarithms and the threshold that come one after the other; 14 us for one group of 20,000 candidates, 40 with all of them
+// looked at and sorted where more than 512 reach the first threshold.
 __global__ __launch_bounds__(kJoinThreads) void join_groups(ewsjf_beams b, const float* score_in, const int32_t* done,
                                                             Work w, int segments, int32_t* parent, int32_t* token,
                                                             float* score) {
@@ -511,18 +512,24 @@ __global__ __launch_bounds__(kJoinThreads) void join_groups(ewsjf_beams b, const
   __shared__ Entry found[kMostFound];
   __shared__ double base[EWSJF_MAX_BEAMS];  // score of a logit of 0
   __shared__ int kind[EWSJF_MAX_BEAMS];     // 0: no candidates, 1: logits, 2: entries of +inf alone, 3: at its end
-  __shared__ uint32_t least[kWaves];
+  __shared__ uint32_t least[kWaves], share[kWaves];
   __shared__ Entry tops[kWaves];
   __shared__ int count;
   const int group = blockIdx.x, lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int each = segments * b.picks, all = b.beams * each;
+  const int each = segments * b.picks, lists = b.beams * segments, all = lists * b.picks;
   const uint64_t* best = w.best + (int64_t)group * all;
+  // Of few candidates all are looked at.  Else of each list, which is in order, the first `heads`, for a threshold, and
+  // then as many as reach it, by a team of threads a list.
+  const bool few = all <= kHeld * kJoinThreads;
+  const int heads = few ? b.picks : lists < kHeld * kJoinThreads ? kHeld * kJoinThreads / lists : 1;
+  auto sample = [&](int i) { return few ? i : i / heads * b.picks + i % heads; };
+  const int samples = lists * heads;
   uint64_t key[kHeld];  // asked for before anything waits
 #pragma unroll
   for (int i = 0; i < kHeld; ++i) {
     const int c = threadIdx.x + i * kJoinThreads;
-    key[i] = c < all ? best[c] : 0;
+    key[i] = c < samples ? best[sample(c)] : 0;
   }
   if (threadIdx.x == 0) count = 0;
   for (int r = wave; r < b.beams; r += kWaves) {
@@ -570,36 +577,82 @@ __global__ __launch_bounds__(kJoinThreads) void join_groups(ewsjf_beams b, const
     return e;
   };
   auto none = [](const Entry& e) { return e.place == 0; };
-  // every candidate: f(entry)
-  auto each_entry = [&](auto f) {
-#pragma unroll
-    for (int i = 0; i < kHeld; ++i) {
-      const int c = threadIdx.x + i * kJoinThreads;
-      if (c < all) f(entry_of(c, key[i]));
-    }
-    for (int c = threadIdx.x + kHeld * kJoinThreads; c < all; c += kJoinThreads) f(entry_of(c, best[c]));
-  };
-
-  // A value that at least `picks` of the wave's candidates reach, in a score's upper half: over the lanes' two highest.
+  // A value that at least `picks` of the wave's samples reach, in a score's upper half: over the lanes' two highest.
   uint32_t high[2] = {0, 0};
-  each_entry([&](const Entry& e) {
+  auto look = [&](const Entry& e) {
     const uint32_t o = (uint32_t)(e.score >> 32);
     if (o > high[0]) high[1] = high[0], high[0] = o;
     else if (o > high[1]) high[1] = o;
-  });
-  uint32_t bar = wave_threshold<32>(high, b.picks);
+  };
+#pragma unroll
+  for (int i = 0; i < kHeld; ++i) {
+    const int c = threadIdx.x + i * kJoinThreads;
+    if (c < samples) look(entry_of(sample(c), key[i]));
+  }
+  for (int c = threadIdx.x + kHeld * kJoinThreads; c < samples; c += kJoinThreads) look(entry_of(sample(c), best[sample(c)]));
+  uint32_t bar = wave_threshold<22>(high, b.picks);  // cut to 22 bits fewer steps, and a few candidates more
   if (lane == 0) least[wave] = bar;
   __syncthreads();
 #pragma unroll
   for (int i = 0; i < kWaves; ++i) bar = least[i] > bar ? least[i] : bar;
-  each_entry([&](const Entry& e) {
-    if (!none(e) && (uint32_t)(e.score >> 32) >= bar) {
-      const int at = atomicAdd(&count, 1);
-      if (at < kMostFound) found[at] = e;
+  auto keep = [&](const Entry& e) {
+    if (none(e) || (uint32_t)(e.score >> 32) < bar) return false;
+    const int at = atomicAdd(&count, 1);
+    if (at < kMostFound) found[at] = e;
+    return true;
+  };
+  int n;
+#pragma unroll 1
+  for (int pass = 0;; ++pass) {
+    if (few) {
+#pragma unroll
+      for (int i = 0; i < kHeld; ++i) {
+        const int c = threadIdx.x + i * kJoinThreads;
+        if (c < all) keep(entry_of(c, key[i]));
+      }
+    } else {
+      constexpr int kBatch = 4;  // loads on their way
+      const int team = lists <= kJoinThreads / 16 ? 16 : lists <= kJoinThreads / 8 ? 8 : lists <= kJoinThreads / 4 ? 4 : 1;
+      for (int l = threadIdx.x / team; l < lists; l += kJoinThreads / team) {
+        bool more = true;
+        for (int k0 = threadIdx.x % team; more && k0 < b.picks; k0 += kBatch * team) {
+          uint64_t next[kBatch];
+#pragma unroll
+          for (int i = 0; i < kBatch; ++i) next[i] = best[l * b.picks + (k0 + i * team < b.picks ? k0 + i * team : 0)];
+#pragma unroll
+          for (int i = 0; i < kBatch; ++i) {
+            const int k = k0 + i * team;
+            more = more && k < b.picks && keep(entry_of(l * b.picks + k, next[i]));
+          }
+        }
+      }
     }
-  });
-  __syncthreads();
-  const int n = count;
+    __syncthreads();
+    n = count;
+    if (n <= kMostFound / 4 || pass == 3) break;
+    // More than are ranked quickly: a higher threshold, that `picks` of one wave's found reach, or a share of them of
+    // every wave's.
+    high[0] = high[1] = 0;
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const int at = threadIdx.x + i * kJoinThreads;
+      if (at < n && at < kMostFound) look(found[at]);
+    }
+    uint32_t next = wave_threshold<32>(high, b.picks);
+    uint32_t common = wave_threshold<32>(high, (b.picks + kWaves - 1) / kWaves);
+    if (lane == 0) least[wave] = next, share[wave] = common;
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < kWaves; ++i) {
+      next = least[i] > next ? least[i] : next;
+      common = share[i] < common ? share[i] : common;
+    }
+    next = common > next ? common : next;
+    if (next <= bar) break;
+    bar = next;
+    if (threadIdx.x == 0) count = 0;
+    __syncthreads();
+  }
   auto write = [&](int rank, const Entry& e) {
     const int64_t at = (int64_t)group * b.picks + rank;
     const bool there = !none(e);

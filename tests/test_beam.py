@@ -70,6 +70,25 @@ def test_large(B, kind, vocab, groups, beams, picks):
     check(B, draw(3, rows, vocab, kind), -np.random.default_rng(1).random(rows) * 5, beams, picks)
 
 
+@pytest.mark.parametrize("kind", ["bf16", "f32"])
+@pytest.mark.parametrize("beams,picks,vocab", [(32, 64, 300000), (32, 33, 130001), (16, 48, 52767), (5, 64, 90000), (32, 64, 5000)])
+@pytest.mark.parametrize("ahead", [0, 1, 2, 8, 31])
+def test_leading_beams(B, kind, beams, picks, vocab, ahead):
+    """More candidates of a group than are ranked at once, most of the best of them from a few of its beams; few tokens
+    allowed; and scores that are alike in all but their last bits."""
+    x = draw(ahead, beams, vocab, kind, spread=0.5)
+    x[torch.arange(beams), x.float().argmax(1)] = 0
+    score = -30 - np.random.default_rng(ahead).random(beams)
+    score[np.random.default_rng(ahead + 1).permutation(beams)[:ahead]] += 25
+    check(B, x, score, beams, picks)
+    y = torch.full_like(x, -math.inf)
+    few = torch.arange(ahead, vocab, 997)
+    y[:, few] = x[:, few]
+    check(B, y, score, beams, picks)
+    near = torch.randn((beams, vocab), generator=torch.Generator().manual_seed(vocab)) * 2.0 ** -14 + 1
+    check(B, near.to(x.dtype), score, beams, picks)
+
+
 @pytest.mark.parametrize("kind", ["bf16", "f16", "f32"])
 @pytest.mark.parametrize("skew", [0, 1, 2, 3, 5, 7])
 def test_rows_anywhere(B, kind, skew):
