@@ -721,8 +721,8 @@ ewsjf_status ewsjf_window_plan(const ewsjf_cache* c, const ewsjf_batch* b, const
  * the cache's type, strides in elements, multiples of 8, 16-byte aligned; out:
  * [total_q][q_heads][head_dim], dense; lse: device float [total_q][q_heads] or
  * NULL.  scale > 0.  head_dim 64 or 128.  The plan is one of this batch and
- * cache, or of a cache with the same sizes, slots and lengths: the kernels
- * follow it, and nothing checks that here. */
+ * cache, or of a cache of as many bits with the same sizes, slots and lengths:
+ * the kernels follow it, and nothing checks that here. */
 ewsjf_status ewsjf_attention(const ewsjf_cache* c, const ewsjf_batch* b, int32_t layer, const void* q,
                              int64_t q_token_stride, int64_t q_head_stride, float scale, const void* plan, void* out,
                              float* lse, void* ws, size_t ws_bytes, hipStream_t stream);

@@ -131,6 +131,9 @@ __device__ void sort_entries(Entry* entry, int n, const Entry& none, Above above
 // ---------------------------------------------------------------------------
 // Segments
 // ---------------------------------------------------------------------------
+typedef __attribute__((ext_vector_type(4))) uint32_t u32x4;
+template <typename F>
+__device__ u32x4 each_word(u32x4 v, F f) { return u32x4{f(v.x), f(v.y), f(v.z), f(v.w)}; }
 // 16 bytes of logits.  `order`: a word's logits as whole numbers in their order, with a sign; a NaN without one is above
 // infinity, one with a sign below all.  `clamp`: to at least the negative `low`, a NaN with a sign among them.
 __device__ uint32_t order_of(uint32_t w, float) { return w ^ ((uint32_t)((int32_t)w >> 31) & 0x7fffffffu); }
@@ -161,8 +164,8 @@ struct Piece<float> {
   static constexpr int N = 4;
   static constexpr uint32_t kNone = 0xff800000u;
   static constexpr int32_t kInf = 0x7f800000;
-  static __device__ float at(const uint4& v, int i) { return __uint_as_float((&v.x)[i]); }
-  static __device__ int32_t largest(const uint4& v) {
+  static __device__ float at(u32x4 v, int i) { return __uint_as_float(v[i]); }
+  static __device__ int32_t largest(u32x4 v) {
     return max(max((int32_t)order_of(v.x, 0.f), (int32_t)order_of(v.y, 0.f)),
                max((int32_t)order_of(v.z, 0.f), (int32_t)order_of(v.w, 0.f)));
   }
@@ -176,11 +179,11 @@ struct Piece<__bf16> {
   static constexpr int N = 8;
   static constexpr uint32_t kNone = 0xff80ff80u;
   static constexpr int32_t kInf = 0x7f800000;
-  static __device__ float at(const uint4& v, int i) {
-    const uint32_t w = (&v.x)[i / 2];
+  static __device__ float at(u32x4 v, int i) {
+    const uint32_t w = v[i / 2];
     return __uint_as_float(i % 2 ? w & 0xffff0000u : w << 16);
   }
-  static __device__ int32_t largest(const uint4& v) {
+  static __device__ int32_t largest(u32x4 v) {
     return upper(max16(max16(order16(v.x), order16(v.y)), max16(order16(v.z), order16(v.w))));
   }
   static __device__ float value(int32_t order) { return __uint_as_float(order16((uint32_t)order & 0xffff0000u)); }
@@ -194,8 +197,8 @@ struct Piece<_Float16> {
   static constexpr uint32_t kNone = 0xfc00fc00u;
   static constexpr int32_t kInf = 0x7c000000;
   static __device__ float half(uint32_t bits) { return (float)__builtin_bit_cast(_Float16, (uint16_t)bits); }
-  static __device__ float at(const uint4& v, int i) { return half((&v.x)[i / 2] >> (i % 2 * 16)); }
-  static __device__ int32_t largest(const uint4& v) {
+  static __device__ float at(u32x4 v, int i) { return half(v[i / 2] >> (i % 2 * 16)); }
+  static __device__ int32_t largest(u32x4 v) {
     return upper(max16(max16(order16(v.x), order16(v.y)), max16(order16(v.z), order16(v.w))));
   }
   static __device__ float value(int32_t order) { return half(order16((uint32_t)order) >> 16); }
@@ -211,8 +214,8 @@ __device__ int32_t order_in(float y) {
   else return (int32_t)(order16(__builtin_bit_cast(uint16_t, (T)y)) << 16);
 }
 
-// The exponentials of a wave's logits, relative to 2^from.
-struct PowerTable {
+// The exponentials of a wave's logits.
+struct alignas(16) PowerTable {
   double at[256];
 };
 // 2^(i / 256), by its series, less i in the bits that `Powers` adds it to.
@@ -233,15 +236,14 @@ struct Powers {
   static constexpr float kHigh = (float)kPerLn2, kLow = (float)(kPerLn2 - (double)kHigh);
   static constexpr double kStep = 0.0027076061740622863;  // ln 2 / 256
   static constexpr float kOne = (float)kStep, kTwo = (float)(kStep * kStep / 2);
-  // Sums with `round`, 1.5 2^23 less a multiple of 256, are rounded to whole numbers, n - 256 from in their low bits.
-  // Those bits, 12 to the left, add n >> 8 - from to a binary64's exponent and n & 255 below it, which the table's numbers
-  // have less; the others, of 1.5 2^23, leave the word.
+  // Sums with `round`, 1.5 2^23, are rounded to whole numbers, n in their low bits.  Those bits, 12 to the left, add n >> 8 to
+  // a binary64's exponent and n & 255 below it, which the table's numbers have less; the others, of 1.5 2^23, leave the word.
   static __device__ double entry(int i) {
     const uint64_t b = __double_as_longlong(kPowers.at[i]);
     return __longlong_as_double(b - ((uint64_t)i << 44));
   }
+  static constexpr float round = 12582912.f;
   const double* table;
-  float round;
   double sum = 0., more = 0.;
   struct Term {
     double two;  // the table's number
@@ -265,7 +267,9 @@ struct Powers {
 };
 
 // Keeps what follows from v from living in registers since it was last used.
-__device__ void fresh(uint4& v) { asm volatile("" : "+v"(v.x), "+v"(v.y), "+v"(v.z), "+v"(v.w)); }
+__device__ void fresh(u32x4& v) { asm volatile("" : "+v"(v)); }
+
+__device__ void fresh(double& v) { asm volatile("" : "+v"(v)); }
 
 // Workgroup (segment, row); its waves share nothing before the end.  Bound by vector instructions: 512 rows of 131,072
 // bfloat16 logits, a fifth of them of beams at their end, take 45 to 48 us, 107 MB at 2.3 TB/s, vector units busy 60% of
@@ -279,7 +283,7 @@ __global__ __launch_bounds__(kThreads) void take_segments(ewsjf_beams b, const T
   constexpr int N = P::N;
   __shared__ double power[256];
   __shared__ uint64_t found[kMostFound];
-  __shared__ uint4 pieces[kWaves][kWavePieces];  // that hold a wave's candidates,
+  __shared__ u32x4 pieces[kWaves][kWavePieces];  // that hold a wave's candidates,
   __shared__ int firsts[kWaves][kWavePieces];    // and their first tokens
   __shared__ Part parts[kWaves];
   __shared__ int counts[kWaves], bars[kWaves];
@@ -290,25 +294,30 @@ __global__ __launch_bounds__(kThreads) void take_segments(ewsjf_beams b, const T
   if (!(score_in[row] > -INFINITY) || (done != nullptr && done[row] != 0)) return;
   const T* x = logits + row * b.row_stride;
   const int skew = (int)((reinterpret_cast<uintptr_t>(x) & 15) / sizeof(T));  // elements of the first piece before the row
-  const int piece0 = seg * kThreads * NV + wave * 64 * NV + lane;
-  auto token_of = [&](int i) { return (piece0 + i * 64) * N - skew; };  // of piece i's first element
-  uint4 v[NV];
-#pragma unroll
-  for (int i = 0; i < NV; ++i) {
-    const int first = token_of(i);
-    v[i] = make_uint4(P::kNone, P::kNone, P::kNone, P::kNone);
-    if (first >= 0 && first + N <= b.vocab) v[i] = *reinterpret_cast<const uint4*>(x + first);
-  }
-  power[threadIdx.x] = Powers::entry(threadIdx.x);
+  power[threadIdx.x] = Powers::entry(threadIdx.x);  // waited for before the logits are on their way
   if (threadIdx.x == 0) count = 0;
   __syncthreads();
+  const int piece0 = seg * kThreads * NV + wave * 64 * NV + lane;
+  auto token_of = [&](int i) { return (piece0 + i * 64) * N - skew; };  // of piece i's first element
+  // Loads without a branch, so that each is waited for alone: pieces that do not lie within the row take what lies here, and
+  // are put together afterwards.
+  auto within = [&](int first) { return first >= 0 && first + N <= b.vocab; };
+  u32x4 v[NV];
+  bool all = true;
 #pragma unroll
   for (int i = 0; i < NV; ++i) {
     const int first = token_of(i);
-    if (first < b.vocab && first + N > 0 && (first < 0 || first + N > b.vocab)) {  // at an end of the row
-      constexpr int kBits = 8 * sizeof(T), kIn = 32 / kBits;
+    const bool in = within(first);
+    v[i] = *(const __attribute__((address_space(1))) u32x4*)(in ? (uintptr_t)(x + first) : (uintptr_t)kPowers.at);
+    all &= in;
+  }
+  if (!__all(all)) {
 #pragma unroll
-      for (int k = 0; k < 4; ++k) {
+    for (int i = 0; i < NV; ++i) {
+      const int first = token_of(i);
+      if (within(first)) continue;
+      constexpr int kBits = 8 * sizeof(T), kIn = 32 / kBits;
+      auto word = [&](int k) {
         uint32_t word = P::kNone;
 #pragma unroll
         for (int j = 0; j < kIn; ++j) {
@@ -321,25 +330,51 @@ __global__ __launch_bounds__(kThreads) void take_segments(ewsjf_beams b, const T
             word = (word & ~mask) | bits << (j * (kBits % 32));
           }
         }
-        (&v[i].x)[k] = word;
-      }
+        return word;
+      };
+      v[i] = u32x4{word(0), word(1), word(2), word(3)};
     }
   }
 
+  // Piece after piece, as they come: its largest, the exponentials.
   int32_t most[NV], top = INT32_MIN;
-  for (;;) {
+  Powers powers{power};
+  {
+    const uint32_t low = P::low_of(-600.f);  // e^-600 of a row whose largest is above -500: nothing
+    constexpr int kAhead = 4;                // numbers of the table that are on their way
+    typename Powers::Term term[2][kAhead];
+    u32x4 held;
+#pragma unroll
+    for (int k = 0; k <= NV * N / kAhead; ++k) {
+      if (k < NV * N / kAhead) {
+        const int i = k * kAhead / N;
+        if (k * kAhead % N == 0) {
+          fresh(v[i]);
+          most[i] = P::largest(v[i]);
+          top = max(top, most[i]);
+          held = v[i];
+          fresh(held);
+          held = each_word(held, [&](uint32_t w) { return P::clamp(w, low); });
+        }
+#pragma unroll
+        for (int j = 0; j < kAhead; ++j) term[k % 2][j] = powers.ask(P::at(held, (k * kAhead + j) % N));
+      }
+      if (k > 0)
+#pragma unroll
+        for (int j = 0; j < kAhead; ++j) powers.add(term[(k - 1) % 2][j]);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+  }
+  fresh(powers.sum), fresh(powers.more);  // not put off until they are used
+  const bool nan = __any(top > P::kInf);
+  if (nan) {
+    top = INT32_MIN;
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
-      fresh(v[i]);
+      v[i] = each_word(v[i], [](uint32_t w) { return P::without_nan(w); });
       most[i] = P::largest(v[i]);
       top = max(top, most[i]);
     }
-    if (!__any(top > P::kInf)) break;
-    top = INT32_MIN;  // a NaN: once more without any
-#pragma unroll
-    for (int i = 0; i < NV; ++i)
-#pragma unroll
-      for (int k = 0; k < 4; ++k) (&v[i].x)[k] = P::without_nan((&v[i].x)[k]);
   }
   // A value that at least `picks` of the wave's logits reach: over the lanes' largest, for many picks over the pieces'
   // largest or all logits.
@@ -367,35 +402,12 @@ __global__ __launch_bounds__(kThreads) void take_segments(ewsjf_beams b, const T
 
   // The sum.
   double sum = 0.;
-  if (fabsf(ref) < 500.f) {
-    const int from = (int)rintf(ref * Powers::kHigh) >> 8;
-    const uint32_t low = P::low_of(ref - 600.f);  // e^-600 of the largest: nothing, and within a binary64's exponents
-    Powers powers{power, 12582912.f - 256.f * from};
-    constexpr int kAhead = 4;  // numbers of the table that are on their way
-    typename Powers::Term term[2][kAhead];
-    uint4 held;
-#pragma unroll
-    for (int k = 0; k <= NV * N / kAhead; ++k) {
-      if (k < NV * N / kAhead) {
-        if (k * kAhead % N == 0) {
-          held = v[k * kAhead / N];
-          fresh(held);
-#pragma unroll
-          for (int j = 0; j < 4; ++j) (&held.x)[j] = P::clamp((&held.x)[j], low);
-        }
-#pragma unroll
-        for (int j = 0; j < kAhead; ++j) term[k % 2][j] = powers.ask(P::at(held, (k * kAhead + j) % N));
-      }
-      if (k > 0)
-#pragma unroll
-        for (int j = 0; j < kAhead; ++j) powers.add(term[(k - 1) % 2][j]);
-      __builtin_amdgcn_sched_barrier(0);
-    }
-    Powers largest{power, powers.round};
+  if (!nan && fabsf(ref) < 500.f) {
+    Powers largest{power};
     largest.add(largest.ask(ref));
     // e^ref has the errors of the others: a row's only token has probability 1
     sum = (powers.sum + powers.more) / (largest.sum + largest.more);
-  } else if (ref > -INFINITY) {  // far logits, or entries of +inf, which share the row: read once more
+  } else if (ref > -INFINITY) {  // a NaN, far logits, or entries of +inf, which share the row: read once more
 #pragma unroll 1
     for (int i = 0; i < NV; ++i)
 #pragma unroll 1
@@ -444,8 +456,8 @@ __global__ __launch_bounds__(kThreads) void take_segments(ewsjf_beams b, const T
     for (int i = 0; i < kWaves; ++i)
       for (int k = threadIdx.x; k < counts[i] * N; k += kThreads) {
         float y;
-        if constexpr (N == 4) y = P::at(make_uint4((&pieces[i][k / N].x)[k % N], 0, 0, 0), 0);
-        else y = P::at(make_uint4((&pieces[i][k / N].x)[k % N / 2] >> (k % 2 * 16), 0, 0, 0), 0);
+        const uint32_t word = pieces[i][k / N][k % N * 4 / N];
+        y = P::at(u32x4{N == 4 ? word : word >> (k % 2 * 16), 0, 0, 0}, 0);
         if (y >= bound) {
           const int at = atomicAdd(&count, 1);
           if (at < kMostFound) found[at] = key_of(y, (uint32_t)(firsts[i][k / N] + k % N));
