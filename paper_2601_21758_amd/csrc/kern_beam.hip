@@ -286,7 +286,7 @@ __global__ __launch_bounds__(kThreads) void take_segments(ewsjf_beams b, const T
   __shared__ u32x4 pieces[kWaves][kWavePieces];  // that hold a wave's candidates,
   __shared__ int firsts[kWaves][kWavePieces];    // and their first tokens
   __shared__ Part parts[kWaves];
-  __shared__ int counts[kWaves], bars[kWaves];
+  __shared__ int counts[kWaves], bars[kWaves], plains[kWaves];
   __shared__ int count;
   const int row = blockIdx.y, seg = blockIdx.x, lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -400,13 +400,11 @@ __global__ __launch_bounds__(kThreads) void take_segments(ewsjf_beams b, const T
   top = wave_max(top);
   const float ref = P::value(top);
 
-  // The sum.
+  // The sum of the exponentials; of others than plain ones relative to e^ref.
+  const bool plain = !nan && fabsf(ref) < 500.f;
   double sum = 0.;
-  if (!nan && fabsf(ref) < 500.f) {
-    Powers largest{power};
-    largest.add(largest.ask(ref));
-    // e^ref has the errors of the others: a row's only token has probability 1
-    sum = (powers.sum + powers.more) / (largest.sum + largest.more);
+  if (plain) {
+    sum = powers.sum + powers.more;
   } else if (ref > -INFINITY) {  // a NaN, far logits, or entries of +inf, which share the row: read once more
 #pragma unroll 1
     for (int i = 0; i < NV; ++i)
@@ -431,7 +429,7 @@ __global__ __launch_bounds__(kThreads) void take_segments(ewsjf_beams b, const T
       n += __popcll(taken);
     }
   }
-  if (lane == 0) parts[wave] = Part{sum, ref}, counts[wave] = n, bars[wave] = own;
+  if (lane == 0) parts[wave] = Part{sum, ref}, plains[wave] = plain, counts[wave] = n, bars[wave] = own;
   __syncthreads();
 
   // Together.
@@ -440,9 +438,18 @@ __global__ __launch_bounds__(kThreads) void take_segments(ewsjf_beams b, const T
     const Part p = parts[lane % kWaves];
     double most = p.base;
     for (int d = 1; d < kWaves; d *= 2) most = fmax(most, __shfl_xor(most, d));
-    double all = p.base == most ? p.sum : p.base > -INFINITY ? p.sum * exp(p.base - most) : 0.;
+    const bool alike = __all(plains[lane % kWaves] || p.base == -INFINITY);
+    // e^ref has the errors of the others: a row's only token has probability 1
+    Powers largest{power};
+    largest.add(largest.ask(alike ? (float)most : (float)p.base));
+    const double unit = largest.sum + largest.more;
+    double all = p.sum;
+    if (!alike) {
+      if (plains[lane % kWaves]) all /= unit;
+      if (p.base != most) all = p.base > -INFINITY ? all * exp(p.base - most) : 0.;
+    }
     for (int d = 1; d < kWaves; d *= 2) all += __shfl_xor(all, d);
-    if (lane == 0) w.part[out] = Part{all, most};
+    if (lane == 0) w.part[out] = Part{alike && most > -INFINITY ? all / unit : all, most};
   }
   int32_t least = bars[0];
   bool whole = true;
@@ -452,17 +459,14 @@ __global__ __launch_bounds__(kThreads) void take_segments(ewsjf_beams b, const T
   const float lowest = -3.4028234e38f, bound = least > order_in<T>(-INFINITY) ? max(P::value(least), lowest) : lowest;
   auto key_of = [&](float y, uint32_t token) { return (uint64_t)order32(y) << 32 | (uint32_t)~token; };
   if (whole) {
-#pragma unroll
-    for (int i = 0; i < kWaves; ++i)
-      for (int k = threadIdx.x; k < counts[i] * N; k += kThreads) {
-        float y;
-        const uint32_t word = pieces[i][k / N][k % N * 4 / N];
-        y = P::at(u32x4{N == 4 ? word : word >> (k % 2 * 16), 0, 0, 0}, 0);
-        if (y >= bound) {
-          const int at = atomicAdd(&count, 1);
-          if (at < kMostFound) found[at] = key_of(y, (uint32_t)(firsts[i][k / N] + k % N));
-        }
+    for (int k = lane; k < n * N; k += 64) {
+      const uint32_t word = pieces[wave][k / N][k % N * 4 / N];
+      const float y = P::at(u32x4{N == 4 ? word : word >> (k % 2 * 16), 0, 0, 0}, 0);
+      if (y >= bound) {
+        const int at = atomicAdd(&count, 1);
+        if (at < kMostFound) found[at] = key_of(y, (uint32_t)(firsts[wave][k / N] + k % N));
       }
+    }
   }
   __syncthreads();
   const int total = whole ? count : kMostFound + 1;
