@@ -83,7 +83,7 @@ __device__ double value64(uint64_t o) { return __longlong_as_double(o >> 63 ? o 
 template <int Bits, int M, typename K>
 __device__ K wave_threshold(const K (&key)[M], int n) {
   K t = 0;
-#pragma unroll 1
+#pragma unroll  // rolled, a call of 4 rows takes 5.7 + 7.1 us for 5.2 + 6.5; two bits a step, three thresholds at once, 5.5 + 7.1
   for (int bit = 8 * sizeof(K) - 1; bit >= (int)(8 * sizeof(K)) - Bits; --bit) {
     const K next = t | (K)1 << bit;
     int count = 0;
