@@ -21,13 +21,15 @@ namespace {
 
 constexpr int kThreads = 256;      // of a segment's workgroup
 constexpr int kWaves = kThreads / 64;
-constexpr int kWavePieces = 128;   // pieces with candidates that a wave keeps
+constexpr int kWavePieces = 128;   // pieces with candidates that a wave keeps: above its threshold less than picks, at it picks
+constexpr int kListed = kWaves * (EWSJF_MAX_PICKS - 1) * 8 + kWaves * EWSJF_MAX_PICKS;  // candidates of a segment, at most
 constexpr int kJoinThreads = 1024; // of a group's workgroup
-constexpr int kMostFound = 2048;   // candidates that a workgroup ranks at once
+constexpr int kMostFound = 2048;   // candidates of a group that are ranked at once
 constexpr int kWanted = 512;       // workgroups that a launch should have: a thread has as many pieces as leave them
 constexpr int kVocabBits = 22, kRowBits = 5;
 static_assert(EWSJF_MAX_VOCAB <= 1 << kVocabBits && EWSJF_MAX_BEAMS <= 1 << kRowBits, "a candidate's place is 59 bits");
 static_assert(EWSJF_MAX_PICKS <= 64, "thresholds are taken over the lanes of a wave");
+static_assert(kWavePieces >= 2 * EWSJF_MAX_PICKS - 1, "a wave keeps all pieces with candidates");
 
 // What a segment leaves: sum exp(x) = sum * exp(base).
 struct Part {
@@ -92,6 +94,11 @@ __device__ K wave_threshold(const K (&key)[M], int n) {
     if (count >= n) t = next;
   }
   return t;
+}
+
+// Lanes below this one whose bit is set.
+__device__ int bits_below(uint64_t bits) {
+  return __builtin_amdgcn_mbcnt_hi((uint32_t)(bits >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)bits, 0));
 }
 
 template <typename K>
@@ -282,11 +289,11 @@ __global__ __launch_bounds__(kThreads) void take_segments(ewsjf_beams b, const T
   using P = Piece<T>;
   constexpr int N = P::N;
   __shared__ double power[256];
-  __shared__ uint64_t found[kMostFound];
+  __shared__ uint64_t found[kListed];
   __shared__ u32x4 pieces[kWaves][kWavePieces];  // that hold a wave's candidates,
   __shared__ int firsts[kWaves][kWavePieces];    // and their first tokens
   __shared__ Part parts[kWaves];
-  __shared__ int counts[kWaves], bars[kWaves], plains[kWaves];
+  __shared__ int bars[kWaves], plains[kWaves];
   __shared__ int count;
   const int row = blockIdx.y, seg = blockIdx.x, lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -336,6 +343,10 @@ __global__ __launch_bounds__(kThreads) void take_segments(ewsjf_beams b, const T
     }
   }
 
+  auto largest = [](u32x4 v) {
+    const int32_t most = P::largest(v);
+    return most == order_in<T>(-0.f) ? 0 : most;  // -0 is 0
+  };
   // Piece after piece, as they come: its largest, the exponentials.
   int32_t most[NV], top = INT32_MIN;
   Powers powers{power};
@@ -350,7 +361,7 @@ __global__ __launch_bounds__(kThreads) void take_segments(ewsjf_beams b, const T
         const int i = k * kAhead / N;
         if (k * kAhead % N == 0) {
           fresh(v[i]);
-          most[i] = P::largest(v[i]);
+          most[i] = largest(v[i]);
           top = max(top, most[i]);
           held = v[i];
           fresh(held);
@@ -372,7 +383,7 @@ __global__ __launch_bounds__(kThreads) void take_segments(ewsjf_beams b, const T
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
       v[i] = each_word(v[i], [](uint32_t w) { return P::without_nan(w); });
-      most[i] = P::largest(v[i]);
+      most[i] = largest(v[i]);
       top = max(top, most[i]);
     }
   }
@@ -417,19 +428,36 @@ __global__ __launch_bounds__(kThreads) void take_segments(ewsjf_beams b, const T
   }
   sum = wave_sum(sum);
 
-  // The pieces with candidates.
-  const int32_t own = (int32_t)(bar ^ kSign);
-  int n = 0;
+  // The pieces with candidates, none of -inf alone.
+  auto own_of = [&](uint32_t bar) { return max((int32_t)(bar ^ kSign), order_in<T>(-INFINITY) + 1); };
+  int32_t own = own_of(bar);
+  int n = 0, reach = 0;
+#pragma unroll
+  for (int i = 0; i < NV; ++i) reach += __popcll(__ballot(most[i] >= own));
+  const bool many = reach > kListed / kWaves / 8;  // lanes with more than one, or a plateau
+  if (many && b.picks <= 32) {
+    uint32_t key[NV];
+#pragma unroll
+    for (int i = 0; i < NV; ++i) key[i] = (uint32_t)most[i] ^ kSign;
+    own = own_of(wave_threshold<kBits>(key, b.picks));
+  }
+  int ties = 0;
 #pragma unroll
   for (int i = 0; i < NV; ++i) {
-    const uint64_t taken = __ballot(most[i] >= own);
+    bool mine = most[i] >= own;
+    if (many) {  // of equal pieces the first `picks`, which have the lowest tokens
+      const uint64_t tied = __ballot(most[i] == own);
+      mine = most[i] > own || (most[i] == own && ties + bits_below(tied) < b.picks);
+      ties += __popcll(tied);
+    }
+    const uint64_t taken = __ballot(mine);
     if (taken) {
-      const int at = n + __builtin_amdgcn_mbcnt_hi((uint32_t)(taken >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)taken, 0));
-      if (taken >> lane & 1 && at < kWavePieces) pieces[wave][at] = v[i], firsts[wave][at] = token_of(i);
+      const int at = n + bits_below(taken);
+      if (mine) pieces[wave][at] = v[i], firsts[wave][at] = token_of(i);
       n += __popcll(taken);
     }
   }
-  if (lane == 0) parts[wave] = Part{sum, ref}, plains[wave] = plain, counts[wave] = n, bars[wave] = own;
+  if (lane == 0) parts[wave] = Part{sum, ref}, plains[wave] = plain, bars[wave] = own;
   __syncthreads();
 
   // Together.
@@ -452,56 +480,29 @@ __global__ __launch_bounds__(kThreads) void take_segments(ewsjf_beams b, const T
     if (lane == 0) w.part[out] = Part{alike && most > -INFINITY ? all / unit : all, most};
   }
   int32_t least = bars[0];
-  bool whole = true;
 #pragma unroll
-  for (int i = 0; i < kWaves; ++i) least = max(least, bars[i]), whole &= counts[i] <= kWavePieces;
+  for (int i = 0; i < kWaves; ++i) least = max(least, bars[i]);
   // none of -inf: numbers below are no values
   const float lowest = -3.4028234e38f, bound = least > order_in<T>(-INFINITY) ? max(P::value(least), lowest) : lowest;
-  auto key_of = [&](float y, uint32_t token) { return (uint64_t)order32(y) << 32 | (uint32_t)~token; };
-  if (whole) {
-    for (int k = lane; k < n * N; k += 64) {
-      const uint32_t word = pieces[wave][k / N][k % N * 4 / N];
-      const float y = P::at(u32x4{N == 4 ? word : word >> (k % 2 * 16), 0, 0, 0}, 0);
-      if (y >= bound) {
-        const int at = atomicAdd(&count, 1);
-        if (at < kMostFound) found[at] = key_of(y, (uint32_t)(firsts[wave][k / N] + k % N));
-      }
-    }
+  ties = 0;
+  for (int k0 = 0; k0 < n * N; k0 += 64) {  // in the tokens' order
+    const int k = k0 + lane < n * N ? k0 + lane : 0;
+    const uint32_t word = pieces[wave][k / N][k % N * 4 / N];
+    const float y = P::at(u32x4{N == 4 ? word : word >> (k % 2 * 16), 0, 0, 0}, 0);
+    const uint64_t tied = __ballot(k0 + lane < n * N && y == bound);
+    if (k0 + lane < n * N && (y > bound || (y == bound && ties + bits_below(tied) < b.picks)))
+      found[atomicAdd(&count, 1)] = (uint64_t)order32(y) << 32 | ~(uint32_t)(firsts[wave][k / N] + k % N);
+    ties += __popcll(tied);
   }
   __syncthreads();
-  const int total = whole ? count : kMostFound + 1;
+  const int total = count;
   uint64_t* best = w.best + out * b.picks;
-  if (total <= kMostFound / 4) {  // each candidate ranked against the others
-    for (int k = threadIdx.x; k < total; k += kThreads) {
-      const uint64_t key = found[k];
-      int rank = 0;
+  for (int k = threadIdx.x; k < total; k += kThreads) {  // each candidate ranked against the others
+    const uint64_t key = found[k];
+    int rank = 0;
 #pragma unroll 8
-      for (int j = 0; j < total; ++j) rank += found[j] > key;
-      if (rank < b.picks) best[rank] = key;
-    }
-  } else if (total <= kMostFound) {
-    sort_entries<kThreads>(found, total, (uint64_t)0, [](uint64_t p, uint64_t q) { return p > q; });
-    if ((int)threadIdx.x < b.picks) best[threadIdx.x] = found[threadIdx.x];
-  } else {  // a plateau of equal logits: one pass over the segment a pick
-    uint64_t last = ~0ull;
-#pragma unroll 1
-    for (int k = 0; k < b.picks; ++k) {
-      uint64_t next = 0;
-#pragma unroll 1
-      for (int i = 0; i < NV * N; ++i) {
-        const int at = token_of(i / N) + i % N;
-        const float y = at >= 0 && at < b.vocab ? (float)x[at] : -INFINITY;
-        const uint64_t key = y > -INFINITY ? key_of(y, (uint32_t)at) : 0;
-        if (key < last && key > next) next = key;
-      }
-      next = wave_max(next);
-      __syncthreads();
-      if (lane == 0) found[wave] = next;
-      __syncthreads();
-      for (int i = 0; i < kWaves; ++i) next = found[i] > next ? found[i] : next;
-      if (threadIdx.x == 0) best[k] = next;
-      last = next;
-    }
+    for (int j = 0; j < total; ++j) rank += found[j] > key;
+    if (rank < b.picks) best[rank] = key;
   }
   for (int k = total + threadIdx.x; k < b.picks; k += kThreads) best[k] = 0;
 }

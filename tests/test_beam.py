@@ -116,6 +116,39 @@ def test_ties(B, kind, vocab, picks):
 
 
 @pytest.mark.parametrize("kind", ["bf16", "f16", "f32"])
+@pytest.mark.parametrize("rows,vocab,picks", [(2, 9000, 4), (600, 20000, 4), (600, 20000, 40)])
+def test_zeros_with_signs(B, kind, rows, vocab, picks):
+    """-0 is 0: of both the lower token."""
+    x = torch.full((rows, vocab), -1.0)
+    x[:, 0:64:8] = -0.0
+    x[:, 256:768:8] = 0.0
+    x[1::2, 8003:] = -0.0
+    check(B, x.to(TYPES[kind]), [-1.0] * rows, 1, picks)
+
+
+@pytest.mark.parametrize("kind", ["bf16", "f16", "f32"])
+@pytest.mark.parametrize("picks", [1, 16, 32, 33, 64])
+def test_plateaus_in_long_rows(B, kind, picks):
+    """Few tokens allowed, by -inf or by the type's lowest value; runs of equal logits above and below the last pick's;
+    logits in order; pieces of 16 bytes that are full of the same number."""
+    rows, vocab = 520, 17000
+    g = torch.Generator().manual_seed(picks)
+    x = draw(picks, rows, vocab, kind)
+    few = torch.rand((rows, vocab), generator=g) < 0.0004
+    low = torch.finfo(x.dtype).min
+    x[0::8] = torch.where(few[0::8], x[0::8], -math.inf)
+    x[1::8] = torch.where(few[1::8], x[1::8], low)
+    x[2::8] = (torch.arange(vocab) % 5 == 0).to(x.dtype)
+    x[3::8] = (torch.arange(vocab) / 4096).to(x.dtype)
+    x[4::8] = (-torch.arange(vocab) / 4096).to(x.dtype)
+    x[5::8] = (torch.arange(vocab) // 8 % 64 < picks - 1).to(x.dtype)
+    x[6::8] = ((torch.arange(vocab) % 4096 < 8 * (picks - 1)) * 2 + (torch.arange(vocab) % 3 == 0)).to(x.dtype)
+    x[7::8] = low
+    check(B, x, [-2.0] * rows, 1, picks)
+    check(B, x, -torch.rand(rows, generator=g) * 0.1, 8, picks)
+
+
+@pytest.mark.parametrize("kind", ["bf16", "f16", "f32"])
 @pytest.mark.parametrize("vocab", [50, 5000, 70000])
 def test_masks(B, kind, vocab):
     """Forbidden tokens, rows without any left, the type's lowest value as a mask, NaN and infinities."""
