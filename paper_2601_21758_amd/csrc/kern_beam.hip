@@ -11,7 +11,8 @@
 //   e^x = 2^(n / 256) e^r, n = round(256 x / ln 2), |r| <= ln 2 / 512,
 // 2^(n / 256) an exponent and one of 256 numbers in LDS, e^r - 1 two terms in
 // binary32 (the third is at most 4e-10, of the sign of r).  binary64 adds and
-// fused products run at binary32's rate here.
+// fused products take 4.7 cycles of a SIMD, as integers and binary32's fused
+// products of three registers do (4.5); binary32 with two registers takes 2.6.
 #include <hip/hip_runtime.h>
 
 #include "ewsjf_cache.h"
@@ -279,10 +280,12 @@ __device__ void fresh(u32x4& v) { asm volatile("" : "+v"(v)); }
 __device__ void fresh(double& v) { asm volatile("" : "+v"(v)); }
 
 // Workgroup (segment, row); its waves share nothing before the end.  Bound by vector instructions: 512 rows of 131,072
-// bfloat16 logits, a fifth of them of beams at their end, take 45 to 48 us, 107 MB at 2.3 TB/s, vector units busy 60% of
-// the cycles: 1,475 instructions a wave of 4,096 logits, 12 for each exponential (with polynomials in binary64 17).
-// Logits are unpacked again at each use: kept unpacked they leave four waves on a SIMD, and it took 63 us.  16 pieces a
-// thread take as long as eight.
+// bfloat16 logits, a fifth of them of beams at their end, take 37 us, 107 MB at 2.9 TB/s, vector units busy 68% of the
+// cycles: 1,363 instructions a wave of 4,096 logits, 12 for each exponential (with polynomials in binary64, 10 in all, 10%
+// slower).  The loads alone take 19 us, with exponentials and maxima 27, thresholds and sums 2, pieces and ranks 8.  A chip holds
+// most of these logits at once: with all of a wave's waited for before the first exponential, 47 us.
+// Logits are unpacked again at each use: kept unpacked they leave four waves on a SIMD, and it took 63 us.  With 16 pieces a
+// thread 53 us, with four 44.
 template <typename T, int NV>
 __global__ __launch_bounds__(kThreads) void take_segments(ewsjf_beams b, const T* logits, const float* score_in,
                                                           const int32_t* done, Work w, int segments) {
