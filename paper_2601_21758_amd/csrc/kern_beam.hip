@@ -692,27 +692,39 @@ __global__ __launch_bounds__(kJoinThreads) void join_groups(ewsjf_beams b, const
   } else if (n <= kMostFound) {
     sort_entries<kJoinThreads>(found, n, Entry{0, 0}, above);
     if ((int)threadIdx.x < b.picks) write(threadIdx.x, found[threadIdx.x]);
-  } else {  // a plateau of equal scores: one pass over the candidates a pick
-    Entry last{~0ull, ~0ull};
+  } else {  // a plateau of equal scores: the lists merged, a pick at a time
+    Entry mine;  // the best of this thread's lists that is not picked yet
+    auto renew = [&](const Entry& last) {
+      mine = Entry{0, 0};
+      for (int l = threadIdx.x; l < lists; l += kJoinThreads) {
+        int at = 0;
+        for (int end = b.picks; at < end;) {
+          const int mid = (at + end) / 2, c = l * b.picks + mid;
+          if (above(last, entry_of(c, best[c]))) end = mid;
+          else at = mid + 1;
+        }
+        if (at == b.picks) continue;
+        const int c = l * b.picks + at;
+        const Entry e = entry_of(c, best[c]);
+        if (above(e, mine)) mine = e;
+      }
+    };
+    renew(Entry{~0ull, ~0ull});
 #pragma unroll 1
     for (int k = 0; k < b.picks; ++k) {
-      Entry mine{0, 0};
-      for (int c = threadIdx.x; c < all; c += kJoinThreads) {
-        const Entry e = entry_of(c, best[c]);
-        if (above(last, e) && above(e, mine)) mine = e;
-      }
+      Entry top = mine;
 #pragma unroll
       for (int d = 32; d; d >>= 1) {
-        const Entry o{(uint64_t)__shfl_xor(mine.score, d), (uint64_t)__shfl_xor(mine.place, d)};
-        if (above(o, mine)) mine = o;
+        const Entry o{(uint64_t)__shfl_xor(top.score, d), (uint64_t)__shfl_xor(top.place, d)};
+        if (above(o, top)) top = o;
       }
       __syncthreads();
-      if (lane == 0) tops[wave] = mine;
+      if (lane == 0) tops[wave] = top;
       __syncthreads();
       for (int i = 0; i < kWaves; ++i)
-        if (above(tops[i], mine)) mine = tops[i];
-      if (threadIdx.x == 0) write(k, mine);
-      last = mine;
+        if (above(tops[i], top)) top = tops[i];
+      if (threadIdx.x == 0) write(k, top);
+      if (!none(top) && mine.place == top.place) renew(top);
     }
   }
   for (int k = n + threadIdx.x; k < b.picks; k += kJoinThreads) write(k, Entry{0, 0});
