@@ -323,3 +323,24 @@ def test_empty_calls(K):
     k, v = c.read(0, none, ints([0]), total=0)
     assert k.shape == v.shape == (0, 2, 64)
     assert c.reorder(none, none).numel() == 0
+
+
+def test_another_stream(K):
+    """Appends and reads on a stream that is given, behind work there, while the current one is busy."""
+    c = K.PagedCache.new(1, 80, 16, 4, 64, 3, 40, bits=8)
+    slot, q = ints([0, 2]), ints([0, 300, 301])
+    c.extend(slot, ints([300, 1]))
+    side = torch.cuda.Stream()
+    x = torch.zeros((301, 4, 64), dtype=torch.bfloat16, device="cuda")
+    want = torch.randn(x.shape, generator=torch.Generator().manual_seed(9)).bfloat16()
+    big = torch.randn((4096, 4096), device="cuda")
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        (big @ big).sum()
+        x.copy_(want.cuda())
+    c.append(0, x, x, slot, q, stream=side)
+    k, v = c.read(0, slot, q, total=301, stream=side)
+    big @ big
+    torch.cuda.current_stream().wait_stream(side)
+    values = codes_ref.quantise(want.double().numpy(), "bf16")[2]
+    assert np.array_equal(k.double().cpu().numpy(), values) and np.array_equal(v.double().cpu().numpy(), values)

@@ -82,3 +82,61 @@ def test_one_beam_is_greedy():
     prefix = rng.integers(0, c.vocab, 21).tolist()
     model = serve.Model(c)
     assert serve.BeamServer(model, prefix, prompts).run() == serve.Server(model, prefix, prompts).run()
+
+
+@pytest.mark.parametrize("bits", [8, 16])
+def test_captured_search(bits):
+    """Whole steps of a search in a graph, selection, reordering, room, appends, plan and attention, replayed among eager work:
+    the same answers, books and outputs as eager steps of a cache of its own."""
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    from paper_2601_21758_amd import beam, kv
+    G, B, H, D, V = 5, 4, 2, 64, 700
+    n = G * B
+    g = torch.Generator("cuda").manual_seed(bits)
+    slot, ones = torch.arange(n, dtype=torch.int32, device="cuda"), torch.ones(n, dtype=torch.int32, device="cuda")
+    q_start = torch.arange(n + 1, dtype=torch.int32, device="cuda")
+    logits, q = torch.zeros((n, V), device="cuda"), torch.zeros((n, 2 * H, D), dtype=torch.bfloat16, device="cuda")
+    k, v = (torch.zeros((n, H, D), dtype=torch.bfloat16, device="cuda") for _ in range(2))
+
+    class Search:
+        def __init__(self):
+            self.cache = kv.PagedCache.new(1, 80, 4, H, D, n, 12, bits=bits)
+            self.score = torch.zeros(n, device="cuda")
+
+        def step(self):
+            parent, token, score = beam.beam_select(logits, self.score, B)
+            c = self.cache
+            kept = c.reorder(slot, parent.flatten())
+            room = c.extend(slot, ones)
+            c.append(0, k, v, slot, q_start, granted=room)
+            plan = kv.prefix_plan(c, slot, q_start, None, None, total_q=n, max_q=1, q_heads=2 * H)
+            out, lse = kv.attention(q, c, 0, plan)
+            self.score.copy_(score.flatten())
+            return parent, token, kept, room, out, lse
+
+        def books(self):
+            return self.cache.refs, self.cache.table, self.cache.length, self.score
+
+    def draw():
+        for t in (logits, q, k, v):
+            t.copy_(torch.randn(t.shape, generator=g, device="cuda") * 3)
+
+    eager, replayed = Search(), Search()
+    draw()
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        replayed.step()
+    torch.cuda.current_stream().wait_stream(side)
+    eager.step()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        got = replayed.step()
+    for _ in range(9):
+        draw()
+        graph.replay()
+        torch.cuda.synchronize()
+        for a, b in zip((*got, *replayed.books()), (*eager.step(), *eager.books())):
+            assert torch.equal(a, b)
+    assert int(eager.cache.length.min()) == 10
