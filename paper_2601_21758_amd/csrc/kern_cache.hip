@@ -29,9 +29,9 @@ constexpr int kMostGrid = 65536;  // workgroups that copy pages of one plane: a 
 // launch of their own 11.5; 64 of them 13.9 against 11.6.
 constexpr int kFewRequests = kSmallThreads / 64;
 constexpr int kFewBeams = 32;   // of a reordering that one workgroup plans: 8 beams 9.8 us, in two kernels 3.7 + 6.8
-// Workgroups that copy a reordering's pages, eight a CU: 192 copies of 16 blocks of 16 KiB 31 us, with half as many 36,
-// with twice as many 32.
-constexpr int kCopiers = 2048;
+// Workgroups that copy a reordering's pages, sixteen a CU: 192 copies of 16 blocks of 16 KiB 20.4 us, with half as many and
+// with a quarter 21.6.
+constexpr int kCopiers = 4096;
 
 // Workspace: counts of the chunks, the requests' running needs, the pages
 // picked for them; for a compaction the two ends of each move and, per moved
@@ -315,8 +315,7 @@ __global__ __launch_bounds__(kSmallThreads) void grow_small(ewsjf_cache c, Cache
 // Reordering: beams take over their parents' rows, all at once.
 //
 // 512 beams, 192 of which take a copy of a page of 8 layers (260 KiB): 4.5 us to
-// see who takes over what, 6.4 to pick pages, 31 to copy, where memory is the
-// limit (each copy more 4.8 TB/s, read and written) and 13 us are beginning and end.
+// see who takes over what, 6.4 to pick pages, 20 to copy: memory, 4.9 TB/s.
 // ---------------------------------------------------------------------------
 enum Role : int32_t {
   kNone,   // the slot does not exist
@@ -512,14 +511,16 @@ __global__ __launch_bounds__(kThreads) void apply_reorder(ewsjf_cache c, Reorder
       }
       const uint32_t plane = task / parts, from = (task - plane * parts) * length;
       const uint32_t end = from + length < vecs ? from + length : vecs;
-      const uint4* a = reinterpret_cast<const uint4*>(block_of(c, plane, w.copied[j]));
-      uint4* b = reinterpret_cast<uint4*>(block_of(c, plane, w.picked[j]));
-      uint4 x[4];
+      typedef __attribute__((ext_vector_type(4))) uint32_t Piece;  // uint4 would go through LDS
+      const Piece* a = reinterpret_cast<const Piece*>(block_of(c, plane, w.copied[j]));
+      Piece* b = reinterpret_cast<Piece*>(block_of(c, plane, w.picked[j]));
+      Piece x[4];
 #pragma unroll
       for (int k = 0; k < 4; ++k) {
         const uint32_t v = from + threadIdx.x + k * kThreads;
         x[k] = a[v < end ? v : from];  // no branch, or the pieces take turns
       }
+      asm volatile("" : "+v"(x[0]), "+v"(x[1]), "+v"(x[2]), "+v"(x[3]));  // nor a load next to its store
 #pragma unroll
       for (int k = 0; k < 4; ++k) {
         const uint32_t v = from + threadIdx.x + k * kThreads;
