@@ -600,11 +600,15 @@ ewsjf_status ewsjf_cache_append_granted(const ewsjf_cache* c, int32_t layer, con
  * [head_dim], dense, 16-byte aligned); row i of it gets token begin[s] + i of the
  * slot (begin NULL: 0), in 16 bits.  Tokens that the slot does not hold or
  * has no page for, and the rows of a slot outside [0, n_slots), are 0; rows
- * past the last sequence's stay as they are.  start: device int32 [n_seqs + 1],
+ * past the last sequence's stay as they are (ewsjf_cache_read_all: are 0 too,
+ * for memory that holds nothing yet).  start: device int32 [n_seqs + 1],
  * ascending from 0 to at most total. */
 ewsjf_status ewsjf_cache_read(const ewsjf_cache* c, int32_t layer, const int32_t* slot, const int32_t* start,
                               const int32_t* begin, int32_t n_seqs, int64_t total, void* k, void* v,
                               hipStream_t stream);
+ewsjf_status ewsjf_cache_read_all(const ewsjf_cache* c, int32_t layer, const int32_t* slot, const int32_t* start,
+                                  const int32_t* begin, int32_t n_seqs, int64_t total, void* k, void* v,
+                                  hipStream_t stream);
 
 /* slot[i] := what slot[parent[i]] held before the call, for all i at once: the
  * beams of a search after a selection.  parent[i] counts in the call's own list;

@@ -28,7 +28,7 @@ EXPORTED = ("ewsjf_queue_table_bytes", "ewsjf_workspace_bytes", "ewsjf_table_upl
             "ewsjf_cache_workspace_bytes", "ewsjf_cache_extend", "ewsjf_cache_fork", "ewsjf_cache_release",
             "ewsjf_cache_copy", "ewsjf_cache_compact", "ewsjf_cache_append", "ewsjf_cache_append_granted",
             "ewsjf_attention_plan_bytes", "ewsjf_attention_workspace_bytes", "ewsjf_prefix_plan", "ewsjf_window_plan", "ewsjf_attention",
-            "ewsjf_cache_page_bytes", "ewsjf_cache_read", "ewsjf_cache_reorder_workspace_bytes", "ewsjf_cache_reorder",
+            "ewsjf_cache_page_bytes", "ewsjf_cache_read", "ewsjf_cache_read_all", "ewsjf_cache_reorder_workspace_bytes", "ewsjf_cache_reorder",
             "ewsjf_beam_workspace_bytes", "ewsjf_beam_select")
 STATIC_SCRATCH_BYTES = 4 << 20
 MAX_CACHE_BATCH, MAX_PAGES, MAX_PAGE_SIZE, MAX_HEAD_DIM = 4096, 1 << 24, 1024, 256
@@ -151,8 +151,9 @@ def lib():
         L.ewsjf_cache_append_granted.restype = C.c_int
         L.ewsjf_cache_page_bytes.argtypes = [i32, i32, i32, i32]
         L.ewsjf_cache_page_bytes.restype = sz
-        L.ewsjf_cache_read.argtypes = [vp, i32, vp, vp, vp, i32, i64, vp, vp, vp]
-        L.ewsjf_cache_read.restype = C.c_int
+        for f in (L.ewsjf_cache_read, L.ewsjf_cache_read_all):
+            f.argtypes = [vp, i32, vp, vp, vp, i32, i64, vp, vp, vp]
+            f.restype = C.c_int
         L.ewsjf_cache_reorder_workspace_bytes.argtypes = [vp, i32]
         L.ewsjf_cache_reorder_workspace_bytes.restype = sz
         L.ewsjf_cache_reorder.argtypes = [vp, vp, vp, i32, vp, vp, sz, vp]

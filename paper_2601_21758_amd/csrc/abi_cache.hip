@@ -83,6 +83,20 @@ bool batch_ok(const ewsjf_cache* c, const ewsjf_batch* b) {
 
 ewsjf_status launched(hipError_t e) { return e == hipSuccess ? EWSJF_OK : EWSJF_ERR_LAUNCH; }
 
+ewsjf_status read_rows(const ewsjf_cache* c, int32_t layer, const int32_t* slot, const int32_t* start,
+                       const int32_t* begin, int32_t n_seqs, int64_t total, bool all, void* k, void* v,
+                       hipStream_t stream) {
+  ewsjf_status st = cache_status(c);
+  if (st != EWSJF_OK) return st;
+  if (layer < 0 || layer >= c->layers || n_seqs < 0 || n_seqs > EWSJF_MAX_CACHE_BATCH || total < 0 || total > kMaxRead)
+    return EWSJF_ERR_ARG;
+  if ((n_seqs > 0 || all) && total > 0 && (k == nullptr || v == nullptr)) return EWSJF_ERR_NULL;
+  if (n_seqs > 0 && total > 0 && (slot == nullptr || start == nullptr)) return EWSJF_ERR_NULL;
+  if (!aligned16(k) || !aligned16(v)) return EWSJF_ERR_ALIGN;
+  if ((st = ewsjf::device_ok()) != EWSJF_OK) return st;
+  return launched(ewsjf::launch_cache_read(*c, layer, slot, start, begin, n_seqs, total, all, k, v, stream));
+}
+
 ewsjf_status plan_status(const ewsjf_cache* c, const ewsjf_batch* b, const int32_t* slot, const int32_t* q_start,
                          const void* plan, size_t plan_bytes) {
   const ewsjf_status cs = cache_status(c);
@@ -198,15 +212,13 @@ ewsjf_status ewsjf_cache_append(const ewsjf_cache* c, int32_t layer, const void*
 ewsjf_status ewsjf_cache_read(const ewsjf_cache* c, int32_t layer, const int32_t* slot, const int32_t* start,
                               const int32_t* begin, int32_t n_seqs, int64_t total, void* k, void* v,
                               hipStream_t stream) {
-  ewsjf_status st = cache_status(c);
-  if (st != EWSJF_OK) return st;
-  if (layer < 0 || layer >= c->layers || n_seqs < 0 || n_seqs > EWSJF_MAX_CACHE_BATCH || total < 0 || total > kMaxRead)
-    return EWSJF_ERR_ARG;
-  if (n_seqs > 0 && total > 0 && (k == nullptr || v == nullptr || slot == nullptr || start == nullptr))
-    return EWSJF_ERR_NULL;
-  if (!aligned16(k) || !aligned16(v)) return EWSJF_ERR_ALIGN;
-  if ((st = ewsjf::device_ok()) != EWSJF_OK) return st;
-  return launched(ewsjf::launch_cache_read(*c, layer, slot, start, begin, n_seqs, total, k, v, stream));
+  return read_rows(c, layer, slot, start, begin, n_seqs, total, false, k, v, stream);
+}
+
+ewsjf_status ewsjf_cache_read_all(const ewsjf_cache* c, int32_t layer, const int32_t* slot, const int32_t* start,
+                                  const int32_t* begin, int32_t n_seqs, int64_t total, void* k, void* v,
+                                  hipStream_t stream) {
+  return read_rows(c, layer, slot, start, begin, n_seqs, total, true, k, v, stream);
 }
 
 size_t ewsjf_cache_reorder_workspace_bytes(const ewsjf_cache* c, int32_t n) {

@@ -47,7 +47,7 @@ hipError_t launch_cache_append_codes(const ewsjf_cache& c, int32_t layer, const 
                                      const int32_t* slot, const int32_t* q_start, const int32_t* granted,
                                      int32_t n_seqs, int64_t total, hipStream_t stream);
 hipError_t launch_cache_read(const ewsjf_cache& c, int32_t layer, const int32_t* slot, const int32_t* start,
-                             const int32_t* begin, int32_t n_seqs, int64_t total, void* k, void* v,
+                             const int32_t* begin, int32_t n_seqs, int64_t total, bool all, void* k, void* v,
                              hipStream_t stream);
 size_t cache_reorder_ws_bytes(const ewsjf_cache& c, int32_t n);
 hipError_t launch_cache_reorder(const ewsjf_cache& c, const int32_t* slot, const int32_t* parent, int32_t n,

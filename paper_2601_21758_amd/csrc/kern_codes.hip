@@ -76,13 +76,14 @@ __device__ Place written_place(const ewsjf_cache& c, const int32_t* slot, const 
   return place_of(c, page, pos);
 }
 
-// Row t's place of a read.
+// Row t's place of a read; all: a row that no sequence has is 0 too.
 __device__ Place read_place(const ewsjf_cache& c, const int32_t* slot, const int32_t* start, const int32_t* begin,
-                            int n_seqs, int64_t t) {
-  const Place nowhere{kNowhere, 0, 0, 0};
+                            int n_seqs, int64_t t, bool all) {
+  const Place nowhere{kNowhere, 0, 0, 0}, no_row{all ? kNowhere : kNoRow, 0, 0, 0};
+  if (n_seqs == 0) return no_row;
   const int i = last_at_most(start, n_seqs, t), s = slot[i];
   const int64_t a = start[i], e = start[i + 1];
-  if (t < a || t >= e) return Place{kNoRow, 0, 0, 0};
+  if (t < a || t >= e) return no_row;
   if (s < 0 || s >= c.n_slots) return nowhere;
   const int64_t pos = (begin != nullptr ? begin[i] : 0) + t - a;
   const int shift = __builtin_ctz(c.page_size);
@@ -230,20 +231,20 @@ __global__ __launch_bounds__(kThreads) void append_codes(ewsjf_cache c, int laye
 template <typename T, bool Codes, int kRows>
 __global__ __launch_bounds__(kThreads) void read_tokens(ewsjf_cache c, int layer, const int32_t* slot,
                                                         const int32_t* start, const int32_t* begin, int n_seqs,
-                                                        int64_t total, T* k, T* v, int tokens) {
+                                                        int64_t total, bool all, T* k, T* v, int tokens) {
   constexpr int kBytes = Codes ? 1 : 2;
   __shared__ Place place[kTokens];
   const int lanes = lanes_of(c.head_dim), each = kThreads / lanes;
   const int d = (threadIdx.x & (lanes - 1)) * 8;
   const char* data = static_cast<const char*>(c.data) + layer * c.layer_stride * kBytes;
   __shared__ Seqs seqs;
-  seqs.take(slot, start, n_seqs);
+  if (n_seqs > 0) seqs.take(slot, start, n_seqs);
   for (int64_t t0 = (int64_t)blockIdx.x * tokens; t0 < total; t0 += (int64_t)gridDim.x * tokens) {
     const int n = total - t0 < tokens ? (int)(total - t0) : tokens;
     __syncthreads();
     if ((int)threadIdx.x < n) {
       const int64_t t = t0 + threadIdx.x;
-      Place p = read_place(c, slot, start, begin, n_seqs, t);
+      Place p = read_place(c, slot, start, begin, n_seqs, t, all);
       p.k = p.v = t * (c.kv_heads * c.head_dim);
       place[threadIdx.x] = p;
     }
@@ -315,14 +316,14 @@ hipError_t launch_cache_append_codes(const ewsjf_cache& c, int32_t layer, const 
 }
 
 hipError_t launch_cache_read(const ewsjf_cache& c, int32_t layer, const int32_t* slot, const int32_t* start,
-                             const int32_t* begin, int32_t n_seqs, int64_t total, void* k, void* v,
+                             const int32_t* begin, int32_t n_seqs, int64_t total, bool all, void* k, void* v,
                              hipStream_t stream) {
-  if (n_seqs == 0 || total == 0) return hipSuccess;
+  if ((n_seqs == 0 && !all) || total == 0) return hipSuccess;
   const int tokens = tokens_each(total);
   auto go = [&](auto type, auto one, auto many) {
     using T = decltype(type);
     (one_pass(c, tokens) ? one : many)<<<grid_of(total, tokens), kThreads, 0, stream>>>(
-        c, layer, slot, start, begin, n_seqs, total, static_cast<T*>(k), static_cast<T*>(v), tokens);
+        c, layer, slot, start, begin, n_seqs, total, all, static_cast<T*>(k), static_cast<T*>(v), tokens);
   };
   if (c.dtype == EWSJF_E4M3_BF16) go(__bf16(), read_tokens<__bf16, true, 1>, read_tokens<__bf16, true, kRows>);
   else if (c.dtype == EWSJF_E4M3_F16) go(_Float16(), read_tokens<_Float16, true, 1>, read_tokens<_Float16, true, kRows>);

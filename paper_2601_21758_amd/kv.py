@@ -298,9 +298,11 @@ class PagedCache:
         tokens, in 16 bits: rows [start[s], start[s + 1]) get the tokens of
         slot[s] from begin[s] on (None: 0), zeros where there is none
         (ewsjf_cache_read).  out: (k, v) to write into, whose rows past the
-        last sequence's stay as they are; otherwise `total` rows are made."""
-        n, want = slot.numel(), (self.c.kv_heads, self.c.head_dim)
+        last sequence's stay as they are; otherwise `total` rows are made,
+        those past the last sequence's zeros (ewsjf_cache_read_all)."""
+        n, want, read = slot.numel(), (self.c.kv_heads, self.c.head_dim), L.lib().ewsjf_cache_read
         if out is None:
+            read = L.lib().ewsjf_cache_read_all
             if total is None:
                 raise ValueError("total or out is needed")
             k, v = out = tuple(_new(stream, (int(total), *want), dtype=self.dtype, device=self.device) for _ in range(2))
@@ -313,9 +315,8 @@ class PagedCache:
             if total is not None and total != k.shape[0]:
                 raise ValueError("out has total rows")
         b = None if begin is None else self._ids(begin, "begin", n)
-        L.check(L.lib().ewsjf_cache_read(self._c, int(layer), self._ids(slot, "slot"), self._ids(start, "start", n + 1),
-                                         b, n, k.shape[0], k.data_ptr(), v.data_ptr(), self._on(stream)),
-                "ewsjf_cache_read")
+        L.check(read(self._c, int(layer), self._ids(slot, "slot"), self._ids(start, "start", n + 1), b, n, k.shape[0],
+                     k.data_ptr(), v.data_ptr(), self._on(stream)), "ewsjf_cache_read")
         return out
 
     def reorder(self, slot: torch.Tensor, parent: torch.Tensor, granted: torch.Tensor | None = None,
