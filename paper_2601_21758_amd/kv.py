@@ -18,6 +18,9 @@ scheduling step admits, on the same card and stream.
 Nothing here synchronizes the host; a request that does not fit the pool is
 told by granted == 0 on the device.  A slot of -1 is refused, written nowhere
 and released as nothing; its queries get out 0 and lse -inf.
+
+Calls run on the current stream or on the one that is given.  With either on
+another device than the cache's a call raises ValueError: nothing is launched.
 """
 from __future__ import annotations
 
@@ -381,7 +384,7 @@ def window_plan(cache: PagedCache, slot: torch.Tensor, q_start: torch.Tensor, wi
     plan = AttentionPlan(cache, L.Batch(n, 0, int(total_q), int(max_q), int(q_heads), int(window), int(sinks)), stream)
     L.check(L.lib().ewsjf_window_plan(cache._c, plan._b, cache._ids(slot, "slot"),
                                       cache._ids(q_start, "q_start", n + 1), plan.buf.data_ptr(), plan.buf.numel(),
-                                      _stream(stream)), "ewsjf_window_plan")
+                                      cache._on(stream)), "ewsjf_window_plan")
     return plan
 
 
