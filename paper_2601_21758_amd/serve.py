@@ -121,8 +121,12 @@ class Request:
 class Server:
     """prefix: the common first tokens; prompts: a list of token lists, never empty."""
 
+    most_beams = 1  # that a request may have: this server keeps a slot for each
+
     def __init__(self, model: Model, prefix, prompts, device="cuda"):
         c = self.c = model.c
+        if not 1 <= c.beams <= self.most_beams:
+            raise ValueError(f"{type(self).__name__} has 1 to {self.most_beams} beams a request, not {c.beams}")
         self.model, self.device = model, torch.device(device)
         self.prefix, self.prompts = list(prefix), [list(p) for p in prompts]
         longest = len(self.prefix) + max(len(p) for p in self.prompts) + c.answer
@@ -241,6 +245,8 @@ class Search:
 
 class BeamServer(Server):
     """Answers are the best of `beams` that are searched together; scores: their sums of log probabilities."""
+
+    most_beams = L.MAX_BEAMS
 
     def __init__(self, model: Model, prefix, prompts, device="cuda"):
         if model.c.slots < model.c.beams:
