@@ -279,7 +279,7 @@ class BeamServer(Server):
             first = self._pick(new, x[n:], 1, [0.0] * len(new), [0] * len(new))
             parent += [p if p < 0 else n + p * c.beams for p in first]
         slots, parents = self._ints([s for r in self.running for s in r.slots], parent)
-        self.cache.reorder(slots, parents, ws=self.ws)
+        self._granted(self.cache.reorder(slots, parents, ws=self.ws) | (parents < 0))
         over = [r for r in self.running if len(r.answers[0]) == c.answer or all(r.done)]
         if over:
             self.cache.release(*self._ints([s for r in over for s in r.slots]))
