@@ -15,7 +15,7 @@
 // are the rows, the shared tokens the keys.
 //
 // Scores are computed transposed, S^T = K Q^T, with 32x32x16 matrix
-// instructions: a lane then holds scores of one row (its column), so the
+// instructions (16x16x32 in the kernel of 16 rows): a lane then holds scores of one row (its column), so the
 // softmax's maximum and sum are taken in the lane and joined once with the lane
 // 32 away, and the weights P^T are in the registers as the second product's
 // operand needs them, O^T = V^T P^T, when the keys are taken in the order
@@ -24,17 +24,22 @@
 //
 // Keys and values of 8 bits are codes and a power of two a key and head: they
 // become the 16-bit values that they stand for, exactly, on their way from
-// registers to LDS, and the rest is as it is with 16 bits.
+// registers to LDS, and the rest is as it is with 16 bits.  Units of up to 16
+// rows of codes, a batch's shared ones among them, have a kernel of their own.
 //
 // With `width` the row's query heads, a unit of R rows and K keys reads R D +
 // 2 K D values once and computes 4 R K D operations: R operations a byte of
 // keys.  Up to 32 rows (decoding) memory is the limit, from about 200 rows on
-// (prefill, many requests behind one prefix) the matrix units are; hence two
-// kernels.  What they reach on the card, whose large copies run at 4.8 TB/s
+// (prefill, many requests behind one prefix) the matrix units are; hence a
+// kernel of waves that take units alone and one of workgroups that share them;
+// the kernel of 16 rows is a wave's too.  What they reach on the card, whose large copies run at 4.8 TB/s
 // (read and written) and whose large 16-bit products at 1270 TFLOP/s:
 //   one prompt of 16,384 tokens, 40 heads of 128, window 4096: 1.5 to 1.6 ms,
 //   770 to 800 TFLOP/s; 256 single tokens of 32 query and 8 key heads of 128 over windows
-//   of 4096: 194 us, 5.0 TB/s.
+//   of 4096: 194 us, 5.0 TB/s.  In 8 bits: one whole prompt of 16,384 tokens, 32 query and
+//   8 key heads of 128, 2.05 to 2.15 ms, 1,070 TFLOP/s; the 256 single tokens 111 to 114 us, up
+//   to five new tokens each instead of one (20 rows, the kernel of 32) 131; 64 tokens behind one
+//   prompt of 2048 26 us.
 #include <hip/hip_runtime.h>
 
 #include "ewsjf_cache.h"
@@ -149,7 +154,10 @@ Shape shape_of(const ewsjf_cache& c, const ewsjf_batch& b) {
   // than the phase and the join.  32 query and 8 key heads of 128, shared against not: 16 sequences behind 1024 tokens
   // (66 MiB) 20 us against 17, 64 behind 1024 (264 MiB) 25 against 33, 16 behind 4096 (258 MiB) 26 against 34.  With at
   // most 32 rows a group, in two kernels: 4 behind 4096 (64 MiB) 40 against 31, 4 behind 16,000 (250 MiB) 64 against 65;
-  // 8 of 40 heads behind 1024 (165 MiB) 34 against 22.
+  // 8 of 40 heads behind 1024 (165 MiB) 34 against 22.  One kernel for both phases of few rows saves 4 to 6 us of that (4
+  // groups of 4 behind 6000 tokens 49 us, before 55; 32 of 8 behind 2000 92, before 98; 4 behind 20,000 63, before 69), so a
+  // lower threshold might pay.  Of codes, 24 query and 8 key heads of 128, 16 behind 8000 (354 MiB) 44 against 52, 64 behind
+  // 2400 (484 MiB) 35 against 44, 256 behind 2000 57 against 167.
   const int64_t rows = b.n_groups > 0 ? b.total_q * s.G / b.n_groups : 0;
   const int64_t bytes = 2 * cache_element_bytes(c) * most_keys * b.n_seqs * c.kv_heads * c.head_dim;
   s.groups = rows > 0 && bytes > (rows > kRowTile ? (int64_t)128 << 20 : (int64_t)256 << 20);
@@ -556,7 +564,8 @@ __device__ int key_place(int key, int chunk) {
 }
 template <int D>
 __device__ int value_place(int key, int byte) {
-  // within a block the 16-byte chunks change places by pairs: codes are written as two chunks a lane, one after the other
+  // Within a block the 16-byte chunks change places by pairs: codes are written as two chunks a lane, one after the other.
+  // Codes still have bank conflicts, 16% of LDS cycles in the workgroup kernel, 30 to 44% in the others; 16 bits have none.
   const int block = byte >> 6, in = (byte & 63) ^ ((D == 128 ? key & 1 : (key >> 1) & 1) << 4);
   return D == 128 ? key * 256 + ((block ^ (key & 3)) << 6) + in : key * 128 + ((block ^ ((key >> 1) & 1)) << 6) + in;
 }
