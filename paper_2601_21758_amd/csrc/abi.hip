@@ -76,7 +76,7 @@ ewsjf_status ewsjf::device_ok() { return check_device(); }
 
 extern "C" {
 
-int32_t ewsjf_version(void) { return 10100; }
+int32_t ewsjf_version(void) { return 10200; }
 
 const char* ewsjf_status_string(ewsjf_status s) {
   switch (s) {
